@@ -1,0 +1,316 @@
+"""The experts' products as programs call them: grouped by expert over the sorted rows that ``moe_dispatch`` leaves, with their
+gradients, and with operands in microscaled 4-bit floating point.
+
+``listed()`` names the cases that stand for each range, ``draw(rng)`` gives further ones of the same ranges.  A case is a dict
+of plain values with a ``kind``; A rows, E experts of n x k weights, ``skew`` the exponent of the experts' loads (0: even):
+
+  product   y = x W^T + b                      (``bias``: with b)
+  dx        gradient of x from dy and W
+  dw        gradients of W and b from dy and x (``grad``: the type they are wanted in; ``bias``: with b's)
+  mx4       y = x W^T + b with W held in 4 bits and x quantised on the way
+  quantise  rows into blocks of 32 4-bit values with a common scale, and back
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+MAX_FLOPS = 5.6e11          # the largest listed product: 16384 rows x 2048 x 8192
+MAX_WEIGHTS = 64 * 16384 * 4096
+MAX_PADDED_FLOPS = 2.4e12   # of groups padded to the largest
+BLOCK = 32                  # elements with a common scale
+SCALE_TILE = 256            # scales are laid out by this many reduction elements
+
+DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _product(kind, A, n, k, E, skew=0.0, dtype="bf16", bias=True, grad=None):
+    c = dict(kind=kind, A=A, n=n, k=k, E=E, skew=skew, dtype=dtype, bias=bias)
+    if kind == "dw":
+        c["grad"] = grad or dtype
+    if kind == "dx":
+        c["bias"] = False
+    return c
+
+
+def listed():
+    return [
+        # decode of the widest layer: 256 tokens, top-2, every one of 64 experts' weights (8.6 GB) is read once
+        dict(name="product_decode_wide", **_product("product", 512, 16384, 4096, 64, bias=False)),
+        # prefill of the 350M-shaped layer, first contraction with its bias
+        dict(name="product_prefill_350m", **_product("product", 8192, 4096, 1024, 8)),
+        # the small fp32 layer used where results are compared in full precision
+        dict(name="product_f32_small", **_product("product", 512, 256, 64, 8, dtype="f32")),
+        # training of the XL-shaped layer on skewed routing: gradient of the rows
+        dict(name="dx_xl_skewed", **_product("dx", 16384, 8192, 2048, 32, skew=0.5)),
+        # gradient of an odd number of rows of an odd-sized fp32 layer
+        dict(name="dx_f32_odd", **_product("dx", 777, 520, 264, 5, dtype="f32")),
+        # ... and of the XL-shaped layer's weights and biases, kept in fp32 for the optimizer
+        dict(name="dw_xl_skewed", **_product("dw", 16384, 8192, 2048, 32, skew=0.5, grad="f32")),
+        # a short batch over many small experts: a few rows each, some none; sizes off the tiles
+        dict(name="dw_short_ragged", **_product("dw", 1531, 1544, 904, 60, skew=0.7, bias=False)),
+        # one token of the 350M-shaped model on its way into 4 bits: latency
+        dict(name="quantise_one_token", kind="quantise", A=1, k=1024, dtype="bf16"),
+        # all experts' weights of an XL-shaped layer, as a program that loads a checkpoint quantises them
+        dict(name="quantise_weights_xl", kind="quantise", A=32 * 8192, k=2048, dtype="bf16"),
+        # the smallest call of a serving loop: one token through one expert of the 350M-shaped model in 4 bits
+        dict(name="mx4_one_token", **_product("mx4", 1, 4096, 1024, 8, bias=False)),
+        # decode of the widest layer in 4 bits: 2.3 GB of weights and scales
+        dict(name="mx4_decode_wide", **_product("mx4", 512, 16384, 4096, 64, bias=False)),
+        # prefill of the XL-shaped layer in 4 bits
+        dict(name="mx4_prefill_xl", **_product("mx4", 16384, 8192, 2048, 32)),
+    ]
+
+
+# ---------------------------------------------------------------------------------------------- drawn cases
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    while True:
+        kind = rng.choice(("product", "product", "dx", "dx", "dw", "dw", "quantise", "mx4", "mx4"))
+        if kind == "quantise":
+            c = dict(kind=kind, A=_log_int(rng, 1, 32 * 8192), k=BLOCK * _log_int(rng, 1, 512), dtype=rng.choice(("bf16", "bf16", "f32")))
+            if c["A"] * c["k"] <= 32 * 8192 * 2048:
+                return c
+            continue
+        dtype = "f32" if kind != "mx4" and rng.random() < 0.25 else "bf16"
+        A = _log_int(rng, 1, 32768 if dtype == "bf16" else 4096)
+        # sizes on the tiles' grid, and off it
+        step = rng.choice((64, 64, 8)) if dtype == "bf16" else rng.choice((64, 4))
+        widest = 16384 if dtype == "bf16" else 2048
+        n = step * _log_int(rng, max(1, 64 // step), widest // step)
+        if kind == "mx4":
+            step = BLOCK
+        k = step * _log_int(rng, max(1, 64 // step), widest // step)
+        E = _log_int(rng, 1, 64)
+        c = _product(kind, A, n, k, E, skew=rng.choice((0.0, 0.0, 0.5)), dtype=dtype, bias=rng.random() < 0.5,
+                     grad=rng.choice((dtype, "f32")))
+        largest = A * (3.0 if c["skew"] else 1.0) + 4 * E  # about what the groups are padded to, times E
+        if 2.0 * A * n * k <= MAX_FLOPS and E * n * k <= MAX_WEIGHTS and 2.0 * largest * n * k <= MAX_PADDED_FLOPS:
+            return c
+
+
+# ---------------------------------------------------------------------------------------------- inputs
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _normal(shape, std, dtype, g):
+    return torch.empty(shape, dtype=dtype, device=DEV).normal_(0.0, std, generator=g)
+
+
+def _group_sizes(c, seed):
+    """Rows of each expert: A assignments drawn from loads that fall with a random rank's power."""
+    g = torch.Generator()
+    g.manual_seed(seed)
+    loads = (1.0 / torch.arange(1, c["E"] + 1, dtype=torch.float64) ** c["skew"])[torch.randperm(c["E"], generator=g)]
+    ids = torch.multinomial(loads, c["A"], replacement=True, generator=g)
+    return torch.bincount(ids, minlength=c["E"])
+
+
+def _held_in_four_bits(rows, k, g):
+    """Weights ~ N(0, 0.02) held in blocks of 32: packed codes [rows, k/2] (low half first) and scale bytes [ceil(k/256), rows, 8].
+    A program has them from a checkpoint."""
+    codes = torch.empty((rows, k // 2), dtype=torch.uint8, device=DEV)
+    tiles = (k + SCALE_TILE - 1) // SCALE_TILE
+    scales = torch.zeros((rows, tiles * (SCALE_TILE // BLOCK)), dtype=torch.uint8, device=DEV)
+    steps = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], device=DEV)
+    most = max(1, (1 << 26) // k)
+    for lo in range(0, rows, most):
+        v = _normal((min(most, rows - lo), k // BLOCK, BLOCK), 0.02, torch.float32, g)
+        exponent = torch.frexp(v.abs().amax(-1)).exponent - 3
+        code = torch.bucketize(torch.ldexp(v.abs(), -exponent[..., None]), steps, out_int32=True).to(torch.uint8) + 8 * (v < 0).to(torch.uint8)
+        code = code.view(-1, k // 2, 2)
+        codes[lo:lo + most] = code[..., 0] + 16 * code[..., 1]
+        scales[lo:lo + most, :k // BLOCK] = (exponent + 127).to(torch.uint8)
+    return codes, scales.view(rows, tiles, SCALE_TILE // BLOCK).transpose(0, 1).contiguous()
+
+
+def prepare(case, seed):
+    c, g, dt = case, _gen(seed), DTYPE[case["dtype"]]
+    s = dict(case=c)
+    if c["kind"] == "quantise":
+        # rows of different magnitude, as tokens and channels have
+        s["x"] = (_normal((c["A"], c["k"]), 1.0, torch.float32, g) * torch.exp2(torch.randint(-6, 3, (c["A"], 1), device=DEV, generator=g))).to(dt)
+        s["q"] = torch.empty((c["A"], c["k"] // 2), dtype=torch.uint8, device=DEV)
+        s["scale"] = torch.empty(((c["k"] + SCALE_TILE - 1) // SCALE_TILE, c["A"], SCALE_TILE // BLOCK), dtype=torch.uint8, device=DEV)
+        s["out"] = torch.empty((c["A"], c["k"]), dtype=dt, device=DEV)
+        return s
+    A, n, k, E = c["A"], c["n"], c["k"], c["E"]
+    sizes = _group_sizes(c, seed)
+    offsets = torch.zeros(E + 1, dtype=torch.int32)
+    offsets[1:] = torch.cumsum(sizes, 0)
+    s["offsets"] = offsets.to(DEV)
+    s["largest"] = int(sizes.max())
+    if c["kind"] != "dx":
+        s["x"] = _normal((A, k), 1.0, dt, g)
+    if c["kind"] in ("dx", "dw"):
+        s["dy"] = _normal((A, n), 1e-2, dt, g)
+    if c["kind"] == "mx4":
+        s["codes"], s["scales"] = _held_in_four_bits(E * n, k, g)
+        s["codes"] = s["codes"].view(E, n, k // 2)
+    elif c["kind"] != "dw":
+        s["w"] = _normal((E, n, k), 0.02, dt, g)
+    if c["kind"] == "dw":
+        s["out"] = torch.empty((E, n, k), dtype=DTYPE[c["grad"]], device=DEV)
+    else:
+        s["out"] = torch.empty((A, k if c["kind"] == "dx" else n), dtype=dt, device=DEV)
+    s["bias"] = _normal((E, n), 0.02, dt, g) if c["bias"] and c["kind"] != "dw" else None
+    return s
+
+
+# ---------------------------------------------------------------------------------------------- plain forms
+def _padded(rows, offsets, largest):
+    """Rows of each expert as one [E, largest, *] array in 32 bits, zeros behind the last one."""
+    at = offsets[:-1, None].long() + torch.arange(largest, device=DEV)
+    there = at < offsets[1:, None]
+    return torch.where(there[..., None], rows[at.clamp(max=rows.shape[0] - 1)].float(), 0.0)
+
+
+def _unpadded(groups, offsets, rows):
+    s = torch.arange(rows, device=DEV)
+    e = torch.searchsorted(offsets[1:], s, right=True, out_int32=True).long()
+    return groups[e, s - offsets[e]]
+
+
+def _to_blocks(v):
+    """The values that rows in 32 bits have once they are held in blocks of 32 4-bit numbers."""
+    b = v.reshape(*v.shape[:-1], v.shape[-1] // BLOCK, BLOCK)
+    most = b.abs().amax(-1, keepdim=True)
+    exponent = ((most.view(torch.int32) >> 23) - 127 - 2).clamp(min=-127)
+    scale = torch.ldexp(torch.ones_like(most), exponent)
+    t = b / scale
+    a = t.abs()
+    step = torch.where(a < 2.0, 0.5, torch.where(a < 4.0, 1.0, 2.0))
+    return (torch.copysign(torch.round(a / step) * step, t).clamp(-6.0, 6.0) * scale).reshape(v.shape)
+
+
+def _from_blocks(codes, scales):
+    """Packed codes [E, n, k/2] and scale bytes [tiles, E n, 8] -> values [E, n, k] in 32 bits."""
+    E, n, half = codes.shape
+    values = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0], device=DEV)
+    pairs = torch.stack((values.repeat(16), values.repeat_interleave(16)), 1)  # both numbers of a byte
+    v = pairs[codes.int()].view(E, n, -1, BLOCK)
+    s = scales.transpose(0, 1).reshape(E, n, -1)[..., :2 * half // BLOCK]
+    return (v * torch.exp2(s.float() - 127.0)[..., None]).view(E, n, 2 * half)
+
+
+def _plain(s):
+    c = s["case"]
+    if c["kind"] == "quantise":
+        return _to_blocks(s["x"].float()).to(s["x"].dtype)
+    off, largest, dt = s["offsets"], s["largest"], DTYPE[c["dtype"]]
+    if c["kind"] == "dx":
+        return _unpadded(torch.bmm(_padded(s["dy"], off, largest), s["w"].float()), off, c["A"]).to(dt)
+    if c["kind"] == "dw":
+        dy = _padded(s["dy"], off, largest)
+        dw = torch.bmm(dy.transpose(1, 2), _padded(s["x"], off, largest))
+        grad = DTYPE[c["grad"]]
+        return (dw.to(grad), dy.sum(1).to(grad)) if c["bias"] else dw.to(grad)
+    if c["kind"] == "mx4":
+        w, x = _from_blocks(s["codes"], s["scales"]), _to_blocks(s["x"].float())
+    else:
+        w, x = s["w"].float(), s["x"]
+    y = torch.bmm(_padded(x, off, largest), w.transpose(1, 2))
+    if s["bias"] is not None:
+        y = y + s["bias"].float()[:, None, :]
+    return _unpadded(y, off, c["A"]).to(dt)
+
+
+def run(state):
+    if not own:
+        return _plain(state)
+    import paper_2401_08383_amd as exf
+
+    s, kind = state, state["case"]["kind"]
+    if kind == "product":
+        return exf.moe_grouped_product(s["x"], s["offsets"], s["w"], s["bias"], out=s["out"])
+    if kind == "dx":
+        return exf.moe_grouped_product_dx(s["dy"], s["offsets"], s["w"], out=s["out"])
+    if kind == "dw":
+        dw, db = exf.moe_grouped_product_dw(s["dy"], s["x"], s["offsets"], want_bias=s["case"]["bias"], out=s["out"])
+        return dw if db is None else (dw, db)
+    if kind == "mx4":
+        return exf.moe_grouped_product_mx4(s["x"], s["offsets"], exf.Mx4(s["codes"], s["scales"]), s["bias"], out=s["out"])
+    held = exf.mx4_quantize(s["x"], out=exf.Mx4(s["q"], s["scale"]))
+    return exf.mx4_dequantize(held, out=s["out"])
+
+
+# ---------------------------------------------------------------------------------------------- work
+def work(case):
+    c = case
+    el = 2 if c["dtype"] == "bf16" else 4
+    if c["kind"] == "quantise":
+        held = c["A"] * c["k"] * (1 / 2 + 1 / BLOCK)
+        return {"bytes": 2 * c["A"] * c["k"] * el + 2 * held, "flops": c["A"] * c["k"]}
+    A, n, k, E = c["A"], c["n"], c["k"], c["E"]
+    busy = E * (1 - (1 - 1 / E) ** A)  # experts that have rows (even loads)
+    flops = 2.0 * A * n * k
+    if c["kind"] == "dw":
+        grad = 2 if c["grad"] == "bf16" else 4
+        return {"bytes": A * (n + k) * el + E * n * k * grad + (E * n * grad if c["bias"] else 0), "flops": flops}
+    weights = busy * n * k * ((1 / 2 + 1 / BLOCK) if c["kind"] == "mx4" else el)
+    return {"bytes": weights + A * (n + k) * el + (busy * n * el if c["bias"] else 0), "flops": flops}
+
+
+# ---------------------------------------------------------------------------------------------- 64 bits
+def _quantised64(x):
+    """Each block's numbers, from the definition: a table of what four bits can say, the nearest entry, halfway to the even code."""
+    b = x.double().reshape(*x.shape[:-1], -1, BLOCK)
+    fraction, exponent = torch.frexp(b.abs().amax(-1, keepdim=True))
+    exponent = torch.where(fraction == 0, -127, exponent - 1 - 2).clamp(min=-127)
+    t = torch.ldexp(b, -exponent)
+    table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device=DEV)
+    halfway = (table[1:] + table[:-1]) / 2
+    below, upto = torch.bucketize(t.abs(), halfway), torch.bucketize(t.abs(), halfway, right=True)
+    code = torch.where(below % 2 == 0, below, upto)
+    return torch.ldexp(torch.copysign(table[code], t), exponent).reshape(x.shape)
+
+
+def _held64(codes, scales, e, n):
+    """Weights of expert e from their bytes."""
+    low, high = codes[e] % 16, codes[e] // 16
+    code = torch.stack((low, high), -1).reshape(n, -1)
+    size, sign = (code % 8).double(), 1.0 - 2.0 * (code // 8).double()
+    size = torch.where(size < 4, size / 2, torch.where(size < 6, size - 2, 2 * size - 8))
+    s = scales[:, e * n:(e + 1) * n].permute(1, 0, 2).reshape(n, -1)[:, :code.shape[1] // BLOCK].double() - 127
+    return sign * size * torch.exp2(s).repeat_interleave(BLOCK, 1)
+
+
+def exact(case, seed):
+    c, s = case, prepare(case, seed)
+    if c["kind"] == "quantise":
+        most = max(1, (1 << 26) // c["k"])
+        return torch.cat([_quantised64(part) for part in s["x"].split(most)])
+    lo = s["offsets"].tolist()
+    ranges = [(e, slice(lo[e], lo[e + 1])) for e in range(c["E"])]
+    if c["kind"] == "dw":
+        dw = torch.zeros((c["E"], c["n"], c["k"]), dtype=torch.float64, device=DEV)
+        db = torch.zeros((c["E"], c["n"]), dtype=torch.float64, device=DEV)
+        for e, r in ranges:
+            dy = s["dy"][r].double()
+            dw[e] = dy.t() @ s["x"][r].double()
+            db[e] = dy.sum(0)
+        return (dw, db) if c["bias"] else dw
+    out = torch.zeros((c["A"], c["k"] if c["kind"] == "dx" else c["n"]), dtype=torch.float64, device=DEV)
+    for e, r in ranges:
+        if r.start == r.stop:
+            continue
+        if c["kind"] == "dx":
+            out[r] = s["dy"][r].double() @ s["w"][e].double()
+            continue
+        if c["kind"] == "mx4":
+            out[r] = _quantised64(s["x"][r]) @ _held64(s["codes"], s["scales"], e, c["n"]).t()
+        else:
+            out[r] = s["x"][r].double() @ s["w"][e].double().t()
+        if s["bias"] is not None:
+            out[r] += s["bias"][e].double()
+    return out
