@@ -127,7 +127,7 @@ def _held_in_four_bits(rows, k, g):
     for lo in range(0, rows, most):
         v = _normal((min(most, rows - lo), k // BLOCK, BLOCK), 0.02, torch.float32, g)
         exponent = torch.frexp(v.abs().amax(-1)).exponent - 3
-        code = torch.bucketize(torch.ldexp(v.abs(), -exponent[..., None]), steps, out_int32=True).to(torch.uint8) + 8 * (v < 0).to(torch.uint8)
+        code = torch.bucketize(v.abs() / _power_of_two(exponent)[..., None], steps, out_int32=True).to(torch.uint8) + 8 * (v < 0).to(torch.uint8)
         code = code.view(-1, k // 2, 2)
         codes[lo:lo + most] = code[..., 0] + 16 * code[..., 1]
         scales[lo:lo + most, :k // BLOCK] = (exponent + 127).to(torch.uint8)
@@ -181,12 +181,18 @@ def _unpadded(groups, offsets, rows):
     return groups[e, s - offsets[e]]
 
 
+def _power_of_two(exponent):
+    """2^exponent in 32 bits, exactly (exponent at least -127)."""
+    bits = ((exponent.clamp(min=-126) + 127) << 23).view(torch.float32)
+    return torch.where(exponent < -126, 0.5 * bits, bits)
+
+
 def _to_blocks(v):
     """The values that rows in 32 bits have once they are held in blocks of 32 4-bit numbers."""
     b = v.reshape(*v.shape[:-1], v.shape[-1] // BLOCK, BLOCK)
     most = b.abs().amax(-1, keepdim=True)
     exponent = ((most.view(torch.int32) >> 23) - 127 - 2).clamp(min=-127)
-    scale = torch.ldexp(torch.ones_like(most), exponent)
+    scale = _power_of_two(exponent)
     t = b / scale
     a = t.abs()
     step = torch.where(a < 2.0, 0.5, torch.where(a < 4.0, 1.0, 2.0))
@@ -200,7 +206,7 @@ def _from_blocks(codes, scales):
     pairs = torch.stack((values.repeat(16), values.repeat_interleave(16)), 1)  # both numbers of a byte
     v = pairs[codes.int()].view(E, n, -1, BLOCK)
     s = scales.transpose(0, 1).reshape(E, n, -1)[..., :2 * half // BLOCK]
-    return (v * torch.exp2(s.float() - 127.0)[..., None]).view(E, n, 2 * half)
+    return (v * _power_of_two(s.int() - 127)[..., None]).view(E, n, 2 * half)
 
 
 def _plain(s):
@@ -262,17 +268,22 @@ def work(case):
 
 
 # ---------------------------------------------------------------------------------------------- 64 bits
+def _double_power(exponent):
+    """2^exponent in 64 bits: the number that has this exponent and no other digit."""
+    return ((exponent.long() + 1023) << 52).view(torch.float64)
+
+
 def _quantised64(x):
     """Each block's numbers, from the definition: a table of what four bits can say, the nearest entry, halfway to the even code."""
     b = x.double().reshape(*x.shape[:-1], -1, BLOCK)
     fraction, exponent = torch.frexp(b.abs().amax(-1, keepdim=True))
     exponent = torch.where(fraction == 0, -127, exponent - 1 - 2).clamp(min=-127)
-    t = torch.ldexp(b, -exponent)
+    t = b * _double_power(-exponent)
     table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device=DEV)
     halfway = (table[1:] + table[:-1]) / 2
     below, upto = torch.bucketize(t.abs(), halfway), torch.bucketize(t.abs(), halfway, right=True)
     code = torch.where(below % 2 == 0, below, upto)
-    return torch.ldexp(torch.copysign(table[code], t), exponent).reshape(x.shape)
+    return (torch.copysign(table[code], t) * _double_power(exponent)).reshape(x.shape)
 
 
 def _held64(codes, scales, e, n):
@@ -281,8 +292,8 @@ def _held64(codes, scales, e, n):
     code = torch.stack((low, high), -1).reshape(n, -1)
     size, sign = (code % 8).double(), 1.0 - 2.0 * (code // 8).double()
     size = torch.where(size < 4, size / 2, torch.where(size < 6, size - 2, 2 * size - 8))
-    s = scales[:, e * n:(e + 1) * n].permute(1, 0, 2).reshape(n, -1)[:, :code.shape[1] // BLOCK].double() - 127
-    return sign * size * torch.exp2(s).repeat_interleave(BLOCK, 1)
+    s = scales[:, e * n:(e + 1) * n].permute(1, 0, 2).reshape(n, -1)[:, :code.shape[1] // BLOCK].int() - 127
+    return sign * size * _double_power(s).repeat_interleave(BLOCK, 1)
 
 
 def exact(case, seed):
