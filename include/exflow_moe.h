@@ -3,9 +3,11 @@
  * context-coherent Mixture-of-Experts inference with inter-layer expert affinity
  * (arXiv 2401.08383).
  *
- * Three groups of calls:
+ * Four groups of calls:
  *   MoE expert layer  : moe_gate_topk -> moe_dispatch -> moe_expert_ffn -> moe_combine, or
  *                       moe_gate_topk -> moe_dispatch (index maps only) -> moe_expert_ffn_fused
+ *   experts' products : moe_grouped_product and its gradients, moe_grouped_product_mx4 (operands in 4 bits:
+ *                       mx4_quantize, mx4_dequantize)
  *   affinity statistic: affinity_histogram, placement_locality (both in one pass: affinity_statistics),
  *                       affinity_multihop, routing_transfers
  *   placement search  : placement_locality_from_counts (GPU scoring), exf_placement_search (host)
@@ -195,6 +197,70 @@ int moe_expert_ffn_fused(const void* x, const int32_t* src_of_sorted, const int3
  * ------------------------------------------------------------------------------------- */
 int moe_combine(const void* y_sorted, const int32_t* sorted_of_src, const float* topk_w, int64_t T,
                 int d, int k, int dt, void* out, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * moe_grouped_product, moe_grouped_product_dx, moe_grouped_product_dw — one linear map of every local expert on the rows
+ * routed to it, and its gradients: what an expert FFN of another shape (another activation, gated, adapters) is built from
+ * and what experts are trained with (Introduction / Challenges: experts are context-free feed-forward networks).
+ *
+ * For rows s of expert e, expert_offsets[e] <= s < expert_offsets[e+1] (as written by moe_dispatch):
+ *   y [s][v]    = sum_u x[s][u] * w[e][v][u] + bias[e][v]           moe_grouped_product
+ *   dx[s][u]    = sum_v dy[s][v] * w[e][v][u]                       moe_grouped_product_dx
+ *   dw[e][v][u] = sum_s dy[s][v] * x[s][u]                          moe_grouped_product_dw
+ *   db[e][v]    = sum_s dy[s][v]
+ * Rows outside all experts' ranges are neither read nor written; dw and db of an expert without rows are zero.  Each row's
+ * result depends on that row and its expert alone, and every sum has an order that depends on the sizes and the
+ * offsets only: the same call gives the same bits.
+ *
+ *   x_sorted, dx_sorted [A,k] dt;  y_sorted, dy_sorted [A,n] dt;  w [E_local,n,k] dt;  bias [E_local,n] dt or NULL;
+ *   dw [E_local,n,k], db [E_local,n] (NULL: not wanted) of type grad_dt, EXF_F32 or dt, overwritten, not accumulated.
+ *   A must be an upper bound on expert_offsets[E_local].  Outputs must not overlap inputs.
+ * All sums are kept in fp32 and rounded once.
+ * Shapes: 0 <= A < 2^31; n, k >= 1, multiples of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
+ * workspace: moe_grouped_product_dw_workspace_bytes(A, n, k, E_local, dt) bytes (partial sums of a long reduction).
+ * ------------------------------------------------------------------------------------- */
+int moe_grouped_product(const void* x_sorted, const int32_t* expert_offsets, const void* w, const void* bias, int64_t A,
+                        int n, int k, int E_local, int dt, void* y_sorted, void* stream);
+int moe_grouped_product_dx(const void* dy_sorted, const int32_t* expert_offsets, const void* w, int64_t A, int n, int k,
+                           int E_local, int dt, void* dx_sorted, void* stream);
+size_t moe_grouped_product_dw_workspace_bytes(int64_t A, int n, int k, int E_local, int dt);
+int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorted, const int32_t* expert_offsets, int64_t A, int n,
+                           int k, int E_local, int dt, int grad_dt, void* dw, void* db, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * mx4_quantize, mx4_dequantize — rows in microscaled 4-bit floating point (the OCP microscaling format MXFP4): blocks of
+ * EXF_MX4_BLOCK consecutive elements of a row share a power of two.
+ *   X    = 2^(floor(log2 max|x|) - 2), at least 2^-127 (a block of zeros: 2^-127)
+ *   code = sign, and the nearest to |x| / X of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; halfway: the even code; beyond 6: 6)
+ *   scale byte = log2 X + 127; 255 where the block holds an infinity or a NaN: all its elements stand for NaN.
+ * mx4_dequantize gives back X * element, exactly (a product outside the range of dt cannot occur for what mx4_quantize
+ * wrote; others round as dt does).
+ *
+ *   x, out [rows,k] dt
+ *   q     [rows,k/2]: elements 2i (low half) and 2i+1 of a row in byte i
+ *   scale [ceil(k/256),rows,8]: byte (t,r,j) belongs to elements 256 t + 32 j .. +31 of row r; bytes past the end of a row
+ *         are zero (the contraction reads them).  mx4_scale_bytes(rows, k) bytes.
+ * Shapes: rows >= 0, k >= 32 and k % 32 == 0.  q and scale must be 16-byte aligned.
+ * ------------------------------------------------------------------------------------- */
+#define EXF_MX4_BLOCK 32
+size_t mx4_scale_bytes(int64_t rows, int k);
+int mx4_quantize(const void* x, int64_t rows, int k, int dt, uint8_t* q, uint8_t* scale, void* stream);
+int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t rows, int k, int dt, void* out, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * moe_grouped_product_mx4 — moe_grouped_product of operands held as mx4_quantize writes them.
+ *   w [E_local,n,k/2], w_scale: E_local*n rows of k.
+ *   x_scale != NULL: x_sorted [A,k/2], x_scale: A rows of k.
+ *   x_scale == NULL: x_sorted [A,k] dt; the call quantises it into the workspace.
+ *   bias [E_local,n] dt or NULL;  y_sorted [A,n] dt.  Sums in fp32, rounded once.
+ * Shapes: 0 <= A < 2^31; k >= 32, k % 32 == 0; n >= 1, a multiple of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
+ * workspace: moe_grouped_product_mx4_workspace_bytes(A, k) bytes with x_scale == NULL, otherwise none (NULL).
+ * ------------------------------------------------------------------------------------- */
+size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k);
+int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_scale, const int32_t* expert_offsets, const uint8_t* w,
+                            const uint8_t* w_scale, const void* bias, int64_t A, int n, int k, int E_local, int dt,
+                            void* y_sorted, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
  * moe_layer_forward — one pass of the whole expert layer (the calls above in sequence) for callers that

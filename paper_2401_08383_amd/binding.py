@@ -26,6 +26,7 @@ EXF_F32 = 0
 EXF_BF16 = 1
 EXF_ACT_GELU_ERF = 0
 EXF_ACT_GELU_TANH = 1
+EXF_MX4_BLOCK = 32
 
 _vp, _i, _i64, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
 
@@ -46,6 +47,15 @@ SIGNATURES = {
     "moe_expert_ffn_fused_workspace_bytes": (_sz, [_i64, _i, _i, _i, _i, _i]),
     "moe_expert_ffn_fused": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i, _i, _i, _vp, _vp, _sz, _vp]),
     "moe_combine": (_i, [_vp, _vp, _vp, _i64, _i, _i, _i, _vp, _vp]),
+    "moe_grouped_product": (_i, [_vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i, _vp, _vp]),
+    "moe_grouped_product_dx": (_i, [_vp, _vp, _vp, _i64, _i, _i, _i, _i, _vp, _vp]),
+    "moe_grouped_product_dw_workspace_bytes": (_sz, [_i64, _i, _i, _i, _i]),
+    "moe_grouped_product_dw": (_i, [_vp, _vp, _vp, _i64, _i, _i, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "mx4_scale_bytes": (_sz, [_i64, _i]),
+    "mx4_quantize": (_i, [_vp, _i64, _i, _i, _vp, _vp, _vp]),
+    "mx4_dequantize": (_i, [_vp, _vp, _i64, _i, _i, _vp, _vp]),
+    "moe_grouped_product_mx4_workspace_bytes": (_sz, [_i64, _i]),
+    "moe_grouped_product_mx4": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i, _vp, _vp, _sz, _vp]),
     "moe_layer_forward": (_i, [_vp, _vp]),
     "affinity_histogram_workspace_bytes": (_sz, [_i, _i64, _i]),
     "affinity_histogram": (_i, [_vp, _i, _i64, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -251,6 +261,167 @@ def moe_combine(y_sorted, sorted_of_src, topk_w, out=None):
         out = torch.empty((T, d), dtype=y_sorted.dtype, device=y_sorted.device)
     _check(lib().moe_combine(_ptr(y_sorted), _ptr(sorted_of_src), _ptr(topk_w), T, d, k, dtype_code(y_sorted), _ptr(out),
                              _stream()))
+    return out
+
+
+def _bad(message: str):
+    raise ExflowError(EXF_ERR_BAD_SHAPE, message)
+
+
+def _expect(name, t, shape, dtype, like):
+    """`t` is a dense tensor of this shape and type on the device of `like`."""
+    if tuple(t.shape) != tuple(shape):
+        _bad(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"{name} is {t.dtype}, expected {dtype}")
+    if not t.is_contiguous() or t.device != like.device:
+        _bad(f"{name} must be contiguous and on {like.device}")
+    return t
+
+
+def _grouped(rows, width, expert_offsets, w_shape):
+    """(A, n, k, E_local) of a product whose sorted rows are `width` (0: k, 1: n) wide."""
+    if rows.dim() != 2 or len(w_shape) != 3:
+        _bad(f"rows are [A,*] and weights [E_local,n,k], got {tuple(rows.shape)} and {tuple(w_shape)}")
+    E, n, k = w_shape
+    _expect("the sorted rows", rows, (rows.shape[0], n if width else k), rows.dtype, rows)
+    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, rows)
+    return rows.shape[0], n, k, E
+
+
+def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
+    """y[s] = x_sorted[s] W_e^T (+ bias[e]) for the rows of every expert; w [E_local,n,k]."""
+    A, n, k, E = _grouped(x_sorted, 0, expert_offsets, w.shape)
+    _expect("w", w, (E, n, k), x_sorted.dtype, x_sorted)
+    if bias is not None:
+        _expect("bias", bias, (E, n), x_sorted.dtype, x_sorted)
+    out = torch.empty((A, n), dtype=x_sorted.dtype, device=x_sorted.device) if out is None else _expect("out", out, (A, n), x_sorted.dtype, x_sorted)
+    rc = lib().moe_grouped_product(x_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), _ptr(bias), A, n, k, E, dtype_code(x_sorted),
+                                   out.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+def moe_grouped_product_dx(dy_sorted, expert_offsets, w, out=None):
+    """Gradient of moe_grouped_product's rows: dx[s] = dy_sorted[s] W_e; w [E_local,n,k]."""
+    A, n, k, E = _grouped(dy_sorted, 1, expert_offsets, w.shape)
+    _expect("w", w, (E, n, k), dy_sorted.dtype, dy_sorted)
+    out = torch.empty((A, k), dtype=dy_sorted.dtype, device=dy_sorted.device) if out is None else _expect("out", out, (A, k), dy_sorted.dtype, dy_sorted)
+    rc = lib().moe_grouped_product_dx(dy_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), A, n, k, E, dtype_code(dy_sorted),
+                                      out.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+def moe_grouped_product_dw(dy_sorted, x_sorted, expert_offsets, want_bias=False, grad_dtype=None, workspace=None, out=None, out_bias=None):
+    """Gradients of moe_grouped_product's weights and bias: (dw [E_local,n,k], db [E_local,n] or None), both of `grad_dtype` (that of
+    ``out``, or the rows')."""
+    if dy_sorted.dim() != 2 or x_sorted.dim() != 2 or expert_offsets.dim() != 1:
+        _bad("rows are [A,n] and [A,k], expert_offsets [E_local+1]")
+    n, k, E = dy_sorted.shape[1], x_sorted.shape[1], expert_offsets.shape[0] - 1
+    A = _grouped(x_sorted, 0, expert_offsets, (E, n, k))[0]
+    dev = x_sorted.device
+    _expect("dy_sorted", dy_sorted, (A, n), x_sorted.dtype, x_sorted)
+    if grad_dtype is None:
+        grad_dtype = x_sorted.dtype if out is None else out.dtype
+    out = torch.empty((E, n, k), dtype=grad_dtype, device=dev) if out is None else _expect("out", out, (E, n, k), grad_dtype, x_sorted)
+    if out_bias is not None:
+        _expect("out_bias", out_bias, (E, n), grad_dtype, x_sorted)
+    elif want_bias:
+        out_bias = torch.empty((E, n), dtype=grad_dtype, device=dev)
+    dt = dtype_code(x_sorted)
+    if workspace is None:
+        workspace = _workspace(lib().moe_grouped_product_dw_workspace_bytes(A, n, k, E, dt), dev)
+    rc = lib().moe_grouped_product_dw(dy_sorted.data_ptr(), x_sorted.data_ptr(), expert_offsets.data_ptr(), A, n, k, E, dt, dtype_code(out),
+                                      out.data_ptr(), _ptr(out_bias), workspace.data_ptr(), workspace.numel(), _stream())
+    if rc:
+        _check(rc)
+    return out, out_bias
+
+
+class Mx4:
+    """Rows in microscaled 4-bit floating point: ``q`` uint8 [..., k/2] and ``scale`` uint8 [ceil(k/256), rows, 8] (see mx4_quantize)."""
+    __slots__ = ("q", "scale")
+
+    def __init__(self, q, scale):
+        self.q, self.scale = q, scale
+
+    @property
+    def shape(self):
+        return (*self.q.shape[:-1], 2 * self.q.shape[-1])
+
+    @property
+    def rows(self):
+        return self.q.numel() // max(self.q.shape[-1], 1)
+
+
+def _mx4_scale_shape(rows, k):
+    return ((k + 255) // 256, rows, 8)
+
+
+def _expect_mx4(name, m, like):
+    if m.q.dtype != torch.uint8 or not m.q.is_contiguous() or m.q.device != like.device:
+        _bad(f"{name}.q must be contiguous uint8 on {like.device}")
+    _expect(f"{name}.scale", m.scale, _mx4_scale_shape(m.rows, m.shape[-1]), torch.uint8, like)
+    return m
+
+
+def mx4_quantize(x, out=None):
+    """Rows x [..., k] (k a multiple of 32) -> Mx4."""
+    if x.dim() < 1 or not x.is_contiguous() or x.shape[-1] < EXF_MX4_BLOCK or x.shape[-1] % EXF_MX4_BLOCK:
+        _bad(f"mx4_quantize: contiguous rows of a multiple of {EXF_MX4_BLOCK} elements expected, got {tuple(x.shape)}")
+    k, rows = x.shape[-1], x.numel() // x.shape[-1]
+    if out is None:
+        out = Mx4(torch.empty((*x.shape[:-1], k // 2), dtype=torch.uint8, device=x.device),
+                  torch.empty(_mx4_scale_shape(rows, k), dtype=torch.uint8, device=x.device))
+    elif _expect_mx4("out", out, x).shape != tuple(x.shape):
+        _bad(f"out holds {out.shape}, expected {tuple(x.shape)}")
+    rc = lib().mx4_quantize(x.data_ptr(), rows, k, dtype_code(x), out.q.data_ptr(), out.scale.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+def mx4_dequantize(m, dtype=torch.bfloat16, out=None):
+    """The values an Mx4 stands for, in `dtype` (that of ``out``)."""
+    _expect_mx4("m", m, m.q)
+    out = torch.empty(m.shape, dtype=dtype, device=m.q.device) if out is None else _expect("out", out, m.shape, out.dtype, m.q)
+    rc = lib().mx4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), m.rows, m.shape[-1], dtype_code(out), out.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, out=None, workspace=None):
+    """moe_grouped_product with weights held in 4 bits: w an Mx4 [E_local,n,k]; x_sorted an Mx4 [A,k], or rows of `dtype` that the call
+    quantises.  The result has the type of the rows, or `dtype` (bf16)."""
+    held = isinstance(x_sorted, Mx4)
+    rows = x_sorted.q if held else x_sorted
+    if len(w.shape) != 3 or rows.dim() != 2 or rows.shape[0] * w.shape[-1] != rows.numel() * (2 if held else 1):
+        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {tuple(w.shape)}")
+    _expect_mx4("w", w, rows)
+    A, (E, n, k) = rows.shape[0], w.shape
+    if held:
+        _expect_mx4("x_sorted", x_sorted, rows)
+    else:
+        _expect("x_sorted", rows, (A, k), rows.dtype, rows)
+    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, rows)
+    if dtype is None:
+        dtype = out.dtype if out is not None else (torch.bfloat16 if held else rows.dtype)
+    if not held and dtype != rows.dtype:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"the result of {rows.dtype} rows is {rows.dtype}, not {dtype}")
+    if bias is not None:
+        _expect("bias", bias, (E, n), dtype, rows)
+    out = torch.empty((A, n), dtype=dtype, device=rows.device) if out is None else _expect("out", out, (A, n), dtype, rows)
+    if workspace is None and not held:
+        workspace = _workspace(lib().moe_grouped_product_mx4_workspace_bytes(A, k), rows.device)
+    rc = lib().moe_grouped_product_mx4(rows.data_ptr(), x_sorted.scale.data_ptr() if held else None, expert_offsets.data_ptr(), w.q.data_ptr(),
+                                       w.scale.data_ptr(), _ptr(bias), A, n, k, E, dtype_code(out), out.data_ptr(), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), _stream())
+    if rc:
+        _check(rc)
     return out
 
 

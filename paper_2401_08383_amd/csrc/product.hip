@@ -1,0 +1,158 @@
+// Entry points of the experts' products: checks, and the choice of kernels.
+#include "product.hpp"
+
+namespace exf {
+
+static int check_sizes(const char* fn, int64_t A, int n, int k, int E_local, int dt)
+{
+    if (dt != EXF_F32 && dt != EXF_BF16) return fail(EXF_ERR_BAD_DTYPE, "%s: dt = %d", fn, dt);
+    if (A < 0 || A >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "%s: A = %lld outside [0,2^31)", fn, static_cast<long long>(A));
+    if (E_local < 1 || E_local > EXF_MAX_EXPERTS) return fail(EXF_ERR_BAD_SHAPE, "%s: E_local = %d outside [1,%d]", fn, E_local, EXF_MAX_EXPERTS);
+    const int gran = dt == EXF_BF16 ? 8 : 4;
+    if (n < gran || n % gran != 0 || k < gran || k % gran != 0)
+        return fail(EXF_ERR_BAD_SHAPE, "%s: n = %d and k = %d must be positive multiples of %d", fn, n, k, gran);
+    return EXF_OK;
+}
+
+static size_t type_bytes(int dt) { return dt == EXF_BF16 ? 2 : 4; }
+
+static int check_rows_product(const char* fn, const void* rows, const int32_t* offsets, const void* w, const void* bias, int64_t A, int n, int k,
+                              int E_local, int dt, bool gradient, const void* out)
+{
+    if (int rc = check_sizes(fn, A, n, k, E_local, dt)) return rc;
+    if (A == 0) return EXF_OK;
+    EXF_CHECK_PTR(fn, rows);
+    EXF_CHECK_PTR(fn, offsets);
+    EXF_CHECK_PTR(fn, w);
+    EXF_CHECK_PTR(fn, out);
+    EXF_CHECK_ALIGNED(fn, rows);
+    EXF_CHECK_ALIGNED(fn, w);
+    EXF_CHECK_ALIGNED(fn, out);
+    if (bias != nullptr) EXF_CHECK_ALIGNED(fn, bias);
+    const size_t el = type_bytes(dt), in = static_cast<size_t>(A) * (gradient ? n : k) * el, o = static_cast<size_t>(A) * (gradient ? k : n) * el;
+    if (overlap(out, o, rows, in) || overlap(out, o, w, static_cast<size_t>(E_local) * n * k * el) || overlap(out, o, bias, static_cast<size_t>(E_local) * n * el) ||
+        overlap(out, o, offsets, static_cast<size_t>(E_local + 1) * 4))
+        return fail(EXF_ERR_BAD_SHAPE, "%s: the result must not overlap an input", fn);
+    return EXF_OK;
+}
+
+}  // namespace exf
+
+extern "C" int moe_grouped_product(const void* x_sorted, const int32_t* expert_offsets, const void* w, const void* bias, int64_t A, int n, int k,
+                                   int E_local, int dt, void* y_sorted, void* stream)
+{
+    using namespace exf;
+    if (int rc = check_rows_product("moe_grouped_product", x_sorted, expert_offsets, w, bias, A, n, k, E_local, dt, false, y_sorted)) return rc;
+    if (A == 0) return EXF_OK;
+    const RowsProduct p{x_sorted, expert_offsets, w, bias, y_sorted, static_cast<int>(A), k, n, E_local};
+    const int rc = launch_exact_rows_product(p, false, dt, static_cast<hipStream_t>(stream));
+    return rc == EXF_OK ? check_launch("moe_grouped_product") : rc;
+}
+
+extern "C" int moe_grouped_product_dx(const void* dy_sorted, const int32_t* expert_offsets, const void* w, int64_t A, int n, int k, int E_local, int dt,
+                                      void* dx_sorted, void* stream)
+{
+    using namespace exf;
+    if (int rc = check_rows_product("moe_grouped_product_dx", dy_sorted, expert_offsets, w, nullptr, A, n, k, E_local, dt, true, dx_sorted)) return rc;
+    if (A == 0) return EXF_OK;
+    const RowsProduct p{dy_sorted, expert_offsets, w, nullptr, dx_sorted, static_cast<int>(A), n, k, E_local};
+    const int rc = launch_exact_rows_product(p, true, dt, static_cast<hipStream_t>(stream));
+    return rc == EXF_OK ? check_launch("moe_grouped_product_dx") : rc;
+}
+
+extern "C" size_t moe_grouped_product_dw_workspace_bytes(int64_t A, int n, int k, int E_local, int dt)
+{
+    (void)A, (void)n, (void)k, (void)E_local, (void)dt;
+    return 0;
+}
+
+extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorted, const int32_t* expert_offsets, int64_t A, int n, int k, int E_local,
+                                      int dt, int grad_dt, void* dw, void* db, void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace exf;
+    const char* fn = "moe_grouped_product_dw";
+    if (int rc = check_sizes(fn, A, n, k, E_local, dt)) return rc;
+    if (grad_dt != EXF_F32 && grad_dt != dt) return fail(EXF_ERR_BAD_DTYPE, "%s: grad_dt = %d with dt = %d", fn, grad_dt, dt);
+    if (A > 0) {
+        EXF_CHECK_PTR(fn, dy_sorted);
+        EXF_CHECK_PTR(fn, x_sorted);
+        EXF_CHECK_ALIGNED(fn, dy_sorted);
+        EXF_CHECK_ALIGNED(fn, x_sorted);
+    }
+    EXF_CHECK_PTR(fn, expert_offsets);
+    EXF_CHECK_PTR(fn, dw);
+    EXF_CHECK_ALIGNED(fn, dw);
+    if (db != nullptr) EXF_CHECK_ALIGNED(fn, db);
+    const size_t need = moe_grouped_product_dw_workspace_bytes(A, n, k, E_local, dt);
+    if (need > 0) {
+        EXF_CHECK_PTR(fn, workspace);
+        EXF_CHECK_ALIGNED(fn, workspace);
+        if (workspace_bytes < need) return fail(EXF_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", fn, workspace_bytes, need);
+    }
+    const size_t el = type_bytes(dt), grad = type_bytes(grad_dt), experts = E_local, rows = A;
+    const struct {
+        const void* at;
+        size_t bytes;
+    } in[] = {{dy_sorted, rows * n * el}, {x_sorted, rows * k * el}, {expert_offsets, (experts + 1) * 4}}, out[] = {{dw, experts * n * k * grad}, {db, experts * n * grad}, {workspace, need}};
+    for (const auto& o : out)
+        for (const auto& i : in)
+            if (overlap(o.at, o.bytes, i.at, i.bytes)) return fail(EXF_ERR_BAD_SHAPE, "%s: results and workspace must not overlap an input", fn);
+    if (overlap(dw, out[0].bytes, db, out[1].bytes) || overlap(workspace, need, dw, out[0].bytes) || overlap(workspace, need, db, out[1].bytes))
+        return fail(EXF_ERR_BAD_SHAPE, "%s: results and workspace must not overlap", fn);
+    const WeightGradient p{dy_sorted, x_sorted, expert_offsets, dw, db, workspace, static_cast<int>(A), n, k, E_local};
+    const int rc = launch_exact_weight_gradient(p, dt, grad_dt, static_cast<hipStream_t>(stream));
+    return rc == EXF_OK ? check_launch(fn) : rc;
+}
+
+extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k)
+{
+    if (A < 0 || k < 1) return 0;
+    return exf::align_up(static_cast<size_t>(A) * k / 2, 256) + exf::align_up(mx4_scale_bytes(A, k), 256);
+}
+
+extern "C" int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_scale, const int32_t* expert_offsets, const uint8_t* w, const uint8_t* w_scale,
+                                       const void* bias, int64_t A, int n, int k, int E_local, int dt, void* y_sorted, void* workspace,
+                                       size_t workspace_bytes, void* stream)
+{
+    using namespace exf;
+    const char* fn = "moe_grouped_product_mx4";
+    if (int rc = check_sizes(fn, A, n, k, E_local, dt)) return rc;
+    if (k % EXF_MX4_BLOCK != 0) return fail(EXF_ERR_BAD_SHAPE, "%s: k = %d must be a multiple of %d", fn, k, EXF_MX4_BLOCK);
+    if (A == 0) return EXF_OK;
+    EXF_CHECK_PTR(fn, x_sorted);
+    EXF_CHECK_PTR(fn, expert_offsets);
+    EXF_CHECK_PTR(fn, w);
+    EXF_CHECK_PTR(fn, w_scale);
+    EXF_CHECK_PTR(fn, y_sorted);
+    EXF_CHECK_ALIGNED(fn, x_sorted);
+    EXF_CHECK_ALIGNED(fn, w);
+    EXF_CHECK_ALIGNED(fn, w_scale);
+    EXF_CHECK_ALIGNED(fn, y_sorted);
+    if (x_scale != nullptr) EXF_CHECK_ALIGNED(fn, x_scale);
+    if (bias != nullptr) EXF_CHECK_ALIGNED(fn, bias);
+    const size_t need = x_scale == nullptr ? moe_grouped_product_mx4_workspace_bytes(A, k) : 0;
+    if (need > 0) {
+        EXF_CHECK_PTR(fn, workspace);
+        EXF_CHECK_ALIGNED(fn, workspace);
+        if (workspace_bytes < need) return fail(EXF_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", fn, workspace_bytes, need);
+    }
+    const size_t el = type_bytes(dt), rows = A, held = rows * k / 2, weights = static_cast<size_t>(E_local) * n, out_bytes = rows * n * el;
+    const struct {
+        const void* at;
+        size_t bytes;
+    } in[] = {{x_sorted, need > 0 ? rows * k * el : held}, {x_scale, mx4_scale_bytes(A, k)}, {expert_offsets, static_cast<size_t>(E_local + 1) * 4},
+              {w, weights * k / 2}, {w_scale, mx4_scale_bytes(static_cast<int64_t>(weights), k)}, {bias, weights * el}};
+    for (const auto& i : in)
+        if (overlap(y_sorted, out_bytes, i.at, i.bytes) || overlap(workspace, need, i.at, i.bytes))
+            return fail(EXF_ERR_BAD_SHAPE, "%s: the result and the workspace must not overlap an input", fn);
+    if (overlap(workspace, need, y_sorted, out_bytes)) return fail(EXF_ERR_BAD_SHAPE, "%s: the result and the workspace must not overlap", fn);
+    Mx4Product p{static_cast<const uint8_t*>(x_sorted), x_scale, expert_offsets, w, w_scale, bias, y_sorted, static_cast<int>(A), k, n, E_local};
+    if (need > 0) {
+        uint8_t* q = static_cast<uint8_t*>(workspace);
+        uint8_t* scale = q + align_up(held, 256);
+        if (int rc = mx4_quantize(x_sorted, A, k, dt, q, scale, stream)) return rc;
+        p.rows = q, p.row_scale = scale;
+    }
+    const int rc = launch_mx4_product(p, dt, static_cast<hipStream_t>(stream));
+    return rc == EXF_OK ? check_launch(fn) : rc;
+}

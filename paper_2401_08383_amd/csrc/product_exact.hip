@@ -1,0 +1,215 @@
+// The experts' products in fp32 arithmetic on the matrix cores: fp32 operands.
+//
+// A workgroup of four wavefronts computes 64 x 64 outputs, a wavefront 32 x 32 in 16x16 accumulators (v_mfma_f32_16x16x4_f32).
+// Operands go through registers into LDS, the next stage of 32 reduction elements on its way while one is multiplied.  An
+// operand whose reduction lies along memory is kept [row][reduction] and fetched four elements at a time (a lane's four
+// elements meet the other operand's in four instructions; which four a step sums does not matter as long as both operands
+// agree); one whose reduction lies across memory is kept as it comes, [reduction][row].
+//   Two sets of accumulators take turns every 16 elements: the sum of a long reduction then has half as many roundings in a row.
+#include "product.hpp"
+
+namespace exf {
+
+constexpr int kExactTile = 64, kExactDepth = 32;
+
+template <typename T>
+__device__ __forceinline__ f32x4_t load4(const T* p);
+template <>
+__device__ __forceinline__ f32x4_t load4<float>(const float* p)
+{
+    return *reinterpret_cast<const f32x4_t*>(p);
+}
+template <>
+__device__ __forceinline__ f32x4_t load4<bf16_t>(const bf16_t* p)
+{
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    return f32x4_t{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+}
+__device__ __forceinline__ void store4(float* p, f32x4_t v) { *reinterpret_cast<f32x4_t*>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t* p, f32x4_t v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
+
+// One operand of a tile: 64 rows (output rows or columns) of the reduction [0, depth).
+//   ACROSS false: element (row, r) at base[row * ld + r];  true: at base[r * ld + row].
+template <typename T, bool ACROSS>
+struct ExactOperand {
+    static constexpr int STRIDE = ACROSS ? kExactTile + 4 : kExactDepth + 4;
+    static constexpr int FLOATS = ACROSS ? kExactDepth * STRIDE : kExactTile * STRIDE;
+    const T* base;
+    int64_t ld;
+    int rows, depth;
+    f32x4_t v[2];
+
+    __device__ __forceinline__ void load(int r0)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int t = threadIdx.x + i * 256;
+            const int row = ACROSS ? t % 16 * 4 : t / 8, r = r0 + (ACROSS ? t / 16 : t % 8 * 4);
+            v[i] = row < rows && r < depth ? load4(base + (ACROSS ? static_cast<int64_t>(r) * ld + row : static_cast<int64_t>(row) * ld + r)) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    __device__ __forceinline__ void store(float* lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int t = threadIdx.x + i * 256;
+            *reinterpret_cast<f32x4_t*>(lds + (ACROSS ? t / 16 * STRIDE + t % 16 * 4 : t / 8 * STRIDE + t % 8 * 4)) = v[i];
+        }
+    }
+    // elements r .. r+3 of a row
+    __device__ __forceinline__ f32x4_t fetch(const float* lds, int row, int r) const
+    {
+        if constexpr (!ACROSS) return *reinterpret_cast<const f32x4_t*>(lds + row * STRIDE + r);
+        return f32x4_t{lds[r * STRIDE + row], lds[(r + 1) * STRIDE + row], lds[(r + 2) * STRIDE + row], lds[(r + 3) * STRIDE + row]};
+    }
+};
+
+// D[row][col] = sum_r a(row, r) w(col, r) + bias[col], written where row < a.rows and col < w.rows.
+template <typename T, typename TO, bool A_ACROSS, bool W_ACROSS>
+__device__ __forceinline__ void exact_tile(ExactOperand<T, A_ACROSS> a, ExactOperand<T, W_ACROSS> w, const T* bias, TO* out, int64_t ldo)
+{
+    typedef ExactOperand<T, A_ACROSS> OA;
+    typedef ExactOperand<T, W_ACROSS> OW;
+    __shared__ __attribute__((aligned(16))) float lds[OA::FLOATS + OW::FLOATS];
+    float *la = lds, *lw = lds + OA::FLOATS;
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int row0 = wave / 2 * 32, col0 = wave % 2 * 32, in16 = lane & 15, quad = lane >> 4;
+    f32x4_t acc[2][2][2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[s][i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    a.load(0);
+    w.load(0);
+    for (int r0 = 0; r0 < a.depth; r0 += kExactDepth) {
+        a.store(la);
+        w.store(lw);
+        __syncthreads();
+        if (r0 + kExactDepth < a.depth) {
+            a.load(r0 + kExactDepth);
+            w.load(r0 + kExactDepth);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            f32x4_t fa[2], fw[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                fa[i] = a.fetch(la, row0 + i * 16 + in16, s * 16 + quad * 4);
+                fw[i] = w.fetch(lw, col0 + i * 16 + in16, s * 16 + quad * 4);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[s][i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[j][q], fa[i][q], acc[s][i][j], 0, 0, 0);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = row0 + i * 16 + in16, col = col0 + j * 16 + quad * 4;
+            if (row >= a.rows || col >= w.rows) continue;
+            f32x4_t v = acc[0][i][j] + acc[1][i][j];
+            if (bias != nullptr) v += load4(bias + col);
+            store4(out + static_cast<int64_t>(row) * ldo + col, v);
+        }
+}
+
+template <typename T, bool GRADIENT>
+__global__ __launch_bounds__(256) void exact_rows_kernel(const RowsProduct p, int col_tiles)
+{
+    const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
+    const int tiles = (range.hi - range.lo + kExactTile - 1) / kExactTile;
+    const int upto = wave_inclusive_scan(tiles);
+    const int row_tile = static_cast<int>(blockIdx.x / static_cast<unsigned>(col_tiles)), col_tile = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles));
+    const unsigned long long owner = __ballot(row_tile < upto);
+    if (owner == 0ull) return;
+    const int e = __builtin_ctzll(owner);
+    const int hi = wave_read_lane(range.hi, e);
+    const int row = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * kExactTile;
+    const int col = col_tile * kExactTile;
+    const int64_t K = p.K, N = p.N;
+    const T* weight = static_cast<const T*>(p.weight) + e * N * K;
+    const ExactOperand<T, false> a{static_cast<const T*>(p.rows) + row * K, K, min(kExactTile, hi - row), p.K, {}};
+    const ExactOperand<T, GRADIENT> w{GRADIENT ? weight + col : weight + col * K, GRADIENT ? N : K, min(kExactTile, p.N - col), p.K, {}};
+    exact_tile<T, T>(a, w, p.bias != nullptr ? static_cast<const T*>(p.bias) + e * N + col : nullptr, static_cast<T*>(p.out) + row * N + col, N);
+}
+
+template <typename T, typename TO>
+__global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient p, int row_tiles, int col_tiles)
+{
+    const unsigned per_expert = static_cast<unsigned>(row_tiles) * static_cast<unsigned>(col_tiles);
+    const int e = static_cast<int>(blockIdx.x / per_expert);
+    const unsigned t = blockIdx.x % per_expert;
+    const int row = static_cast<int>(t / static_cast<unsigned>(col_tiles)) * kExactTile, col = static_cast<int>(t % static_cast<unsigned>(col_tiles)) * kExactTile;
+    const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
+    const int lo = wave_read_lane(range.lo, e), n = wave_read_lane(range.hi, e) - lo;
+    const int64_t N = p.N, K = p.K;
+    const ExactOperand<T, true> a{static_cast<const T*>(p.dy) + lo * N + row, N, min(kExactTile, p.N - row), n, {}};
+    const ExactOperand<T, true> w{static_cast<const T*>(p.x) + lo * K + col, K, min(kExactTile, p.K - col), n, {}};
+    exact_tile<T, TO>(a, w, static_cast<const T*>(nullptr), static_cast<TO*>(p.dw) + (e * N + row) * K + col, K);
+}
+
+// db: a workgroup an expert and 64 columns; four rows of threads a column each, joined in order.
+template <typename T, typename TO>
+__global__ __launch_bounds__(256) void bias_gradient_kernel(const WeightGradient p, int col_tiles)
+{
+    __shared__ float part[4][kWave];
+    const int e = static_cast<int>(blockIdx.x / static_cast<unsigned>(col_tiles)), lane = lane_id(), wave = threadIdx.x / kWave;
+    const int col = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles)) * kWave + lane;
+    const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
+    const int lo = wave_read_lane(range.lo, e), hi = wave_read_lane(range.hi, e);
+    float sum = 0.0f;
+    if (col < p.N)
+        for (int s = lo + wave; s < hi; s += 4) {
+            const T v = static_cast<const T*>(p.dy)[static_cast<int64_t>(s) * p.N + col];
+            if constexpr (sizeof(T) == 4) sum += v;
+            else sum += bf16_to_f32(v);
+        }
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || col >= p.N) return;
+    sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    TO* to = static_cast<TO*>(p.db) + static_cast<int64_t>(e) * p.N + col;
+    if constexpr (sizeof(TO) == 4) *to = sum;
+    else *to = f32_to_bf16(sum);
+}
+
+static int64_t tiles_of(int64_t n) { return (n + kExactTile - 1) / kExactTile; }
+
+template <typename T>
+static int launch_rows_as(const RowsProduct& p, bool gradient, hipStream_t stream)
+{
+    const int64_t cols = tiles_of(p.N), grid = (p.max_rows / kExactTile + (p.max_rows < p.E_local ? p.max_rows : p.E_local)) * cols;
+    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product: too many tiles");
+    if (gradient) hipLaunchKernelGGL((exact_rows_kernel<T, true>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
+    else hipLaunchKernelGGL((exact_rows_kernel<T, false>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
+    return EXF_OK;
+}
+int launch_exact_rows_product(const RowsProduct& p, bool gradient, int dt, hipStream_t stream)
+{
+    return dt == EXF_BF16 ? launch_rows_as<bf16_t>(p, gradient, stream) : launch_rows_as<float>(p, gradient, stream);
+}
+
+template <typename T, typename TO>
+static int launch_weight_as(const WeightGradient& p, hipStream_t stream)
+{
+    const int64_t rows = tiles_of(p.N), cols = tiles_of(p.K), grid = p.E_local * rows * cols;
+    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
+    hipLaunchKernelGGL((exact_weight_kernel<T, TO>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(rows), static_cast<int>(cols));
+    if (p.db != nullptr)
+        hipLaunchKernelGGL((bias_gradient_kernel<T, TO>), dim3(static_cast<unsigned>(p.E_local * rows)), dim3(256), 0, stream, p, static_cast<int>(rows));
+    return EXF_OK;
+}
+int launch_exact_weight_gradient(const WeightGradient& p, int dt, int grad_dt, hipStream_t stream)
+{
+    if (dt == EXF_F32) return launch_weight_as<float, float>(p, stream);
+    return grad_dt == EXF_F32 ? launch_weight_as<bf16_t, float>(p, stream) : launch_weight_as<bf16_t, bf16_t>(p, stream);
+}
+
+}  // namespace exf

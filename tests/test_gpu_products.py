@@ -1,0 +1,413 @@
+"""The experts' products against 64 bits: grouped by expert, their gradients, and operands in 4 bits."""
+import pytest
+import torch
+
+import paper_2401_08383_amd as exf
+import product_reference as R
+from helpers import DEV
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _say(msg):
+    print(f"[case] {msg}", flush=True)
+
+
+def _normal(shape, std, dt, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return torch.empty(shape, dtype=torch.float32, device=DEV).normal_(0.0, std, generator=g).to(dt)
+
+
+def _sizes(A, E, seed, empty=0.2):
+    """A rows over E experts, unevenly, some of them without any."""
+    g = torch.Generator()
+    g.manual_seed(seed)
+    loads = torch.rand(E, generator=g) + 0.05
+    loads[torch.rand(E, generator=g) < empty] = 0.0
+    if float(loads.sum()) == 0.0:
+        loads[0] = 1.0
+    return torch.bincount(torch.multinomial(loads, A, replacement=True, generator=g), minlength=E).tolist() if A else [0] * E
+
+
+def _rows_case(kind, sizes, n, k, dtype, bias=False, before=0, behind=0, seed=1, shift=0):
+    """Forward or gradient of the rows; rows before the first range and behind the last one hold NaN, and their results stay."""
+    dt, gradient = TYPES[dtype], kind == "dx"
+    A, E = before + sum(sizes) + behind, len(sizes)
+    _say(f"{kind} sizes={sizes if E <= 12 else (E, sum(sizes))} n={n} k={k} {dtype} bias={bias} before={before} behind={behind} shift={shift}")
+    K, N = (n, k) if gradient else (k, n)
+    off = R.sizes_to_offsets(sizes, before).to(DEV)
+
+    def place(t):  # a pointer that is 16-byte aligned and no more
+        if not shift:
+            return t
+        buf = torch.empty(t.numel() + 8, dtype=t.dtype, device=DEV)
+        buf[8:].copy_(t.flatten())
+        return buf[8:].view(t.shape)
+
+    rows = place(_normal((A, K), 1.0, dt, seed))
+    rows[:before] = float("nan")
+    rows[before + sum(sizes):] = float("nan")
+    w = place(_normal((E, n, k), 0.1, dt, seed + 1))
+    b = place(_normal((E, n), 1.0, dt, seed + 2)) if bias else None
+    out = place(torch.full((A, N), 7.0, dtype=dt, device=DEV))
+    got = exf.moe_grouped_product_dx(rows, off, w, out=out) if gradient else exf.moe_grouped_product(rows, off, w, b, out=out)
+    assert got is out
+    ref, mag, terms = R.rows_product(rows, off, w, b, gradient)
+    there = slice(before, before + sum(sizes))
+    R.assert_sums_close(out[there], ref[there], mag[there], terms, kind)
+    assert (out[:before] == 7.0).all() and (out[before + sum(sizes):] == 7.0).all()
+    again = torch.zeros_like(out)
+    if gradient:
+        exf.moe_grouped_product_dx(rows, off, w, out=again)
+    else:
+        exf.moe_grouped_product(rows, off, w, b, out=again)
+    assert torch.equal(out[there], again[there]), "the same call, other bits"
+
+
+def _dw_case(sizes, n, k, dtype, grad, bias=True, before=0, behind=0, seed=1):
+    dt = TYPES[dtype]
+    A, E = before + sum(sizes) + behind, len(sizes)
+    _say(f"dw sizes={sizes if E <= 12 else (E, sum(sizes))} n={n} k={k} {dtype} grad={grad} bias={bias} before={before} behind={behind}")
+    off = R.sizes_to_offsets(sizes, before).to(DEV)
+    dy, x = _normal((A, n), 1.0, dt, seed), _normal((A, k), 1.0, dt, seed + 1)
+    for t in (dy, x):  # rows of nobody
+        t[:before] = float("nan")
+        t[before + sum(sizes):] = float("inf")
+    out = torch.full((E, n, k), float("nan"), dtype=TYPES[grad], device=DEV)
+    dw, db = exf.moe_grouped_product_dw(dy, x, off, want_bias=bias, out=out)
+    assert dw is out and (db is not None) == bias
+    ref, mag, ref_b, mag_b, terms = R.weight_gradient(dy, x, off)
+    R.assert_sums_close(dw, ref, mag, terms, "dw")
+    if bias:
+        assert db.dtype == TYPES[grad]
+        R.assert_sums_close(db, ref_b, mag_b, terms, "db")
+    dw2, db2 = exf.moe_grouped_product_dw(dy, x, off, want_bias=bias, grad_dtype=TYPES[grad])
+    assert torch.equal(dw, dw2) and (not bias or torch.equal(db, db2)), "the same call, other bits"
+
+
+# the least there is, sizes off every tile, single rows, many rows
+ROWS = [
+    ([1], 8, 8), ([0, 1, 0], 16, 24), ([3, 0, 5], 72, 40), ([63, 65, 1, 0, 64], 136, 200), ([129, 31, 127], 264, 72), ([257, 0, 320, 300], 520, 136),
+    ([5], 1032, 1544), ([700], 256, 512), ([1, 2, 3, 4], 2048, 264),
+]
+
+
+@pytest.mark.parametrize("kind", ["product", "dx"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes,n,k", ROWS)
+def test_rows(kind, dtype, sizes, n, k):
+    _rows_case(kind, sizes, n, k, dtype, bias=kind == "product")
+
+
+@pytest.mark.parametrize("kind", ["product", "dx"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_nobody_stay(kind, dtype):
+    _rows_case(kind, [40, 0, 90], 200, 136, dtype, before=13, behind=21)
+    _rows_case(kind, [0, 0], 64, 64, dtype, before=5, behind=4)
+    _rows_case(kind, [2, 1], 64, 128, dtype, before=1, behind=1)
+
+
+@pytest.mark.parametrize("kind", ["product", "dx"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_are_aligned_to_16_bytes_and_no_more(kind, dtype):
+    _rows_case(kind, [70, 3], 136, 72, dtype, bias=kind == "product", shift=1)
+    _rows_case(kind, [300], 256, 192, dtype, shift=1)
+
+
+# every height of a tile and of its pieces; reductions of one stage, of as many as are in flight, one more; few column tiles and many
+@pytest.mark.parametrize("kind", ["product", "dx"])
+@pytest.mark.parametrize("sizes,n,k", [
+    ([32, 64, 96, 128, 160, 192, 224, 256], 512, 64), ([288, 320, 300, 33], 256, 128), ([500, 520, 700, 1100], 320, 192), ([2100, 40], 640, 256),
+    ([17, 30, 55, 90, 140, 210], 1024, 448), ([1300], 1536, 384), ([150] * 40, 1024, 512), ([8] * 64, 512, 2048), ([250] * 24 + [0] * 8, 768, 320),
+    ([4000, 10, 900], 512, 1000), ([1] * 64, 256, 264),
+])
+def test_rows_in_tiles(kind, sizes, n, k):
+    _rows_case(kind, sizes, n, k, "bf16", bias=kind == "product")
+    if kind == "dx":
+        _rows_case(kind, sizes, k, n, "bf16")
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_rows_of_random_sizes(seed):
+    g = torch.Generator()
+    g.manual_seed(100 + seed)
+    draw = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=g))  # noqa: E731
+    for kind in ("product", "dx"):
+        dtype = "f32" if seed % 4 == 0 else "bf16"
+        E, A = draw(1, 64), draw(1, 3000)
+        _rows_case(kind, _sizes(A, E, seed), 8 * draw(1, 150), 8 * draw(1, 150), dtype, bias=kind == "product" and seed % 2 == 0, seed=seed)
+
+
+@pytest.mark.parametrize("dtype,grad", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("sizes,n,k", [
+    ([1], 8, 8), ([0, 1, 0], 16, 24), ([3, 0, 5], 72, 40), ([63, 65, 1, 0, 64], 136, 200), ([129, 31, 127], 264, 72), ([257, 0, 320, 300], 520, 136),
+    ([5], 1032, 520), ([700], 256, 512), ([1, 2, 3, 4], 512, 264), ([5000], 64, 64), ([0, 0, 0], 40, 48),
+])
+def test_weight_gradients(dtype, grad, sizes, n, k):
+    _dw_case(sizes, n, k, dtype, grad)
+
+
+@pytest.mark.parametrize("sizes,n,k", [([4000, 0, 7], 256, 256), ([9000], 512, 128), ([640, 64, 63, 65, 1], 1024, 768), ([200] * 32, 256, 384),
+                                       ([2048], 1032, 264), ([3] * 64, 128, 192), ([1500, 1500], 2048, 1024)])
+def test_weight_gradients_in_tiles(sizes, n, k):
+    _dw_case(sizes, n, k, "bf16", "f32")
+    _dw_case(sizes, k, n, "bf16", "bf16", bias=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weight_gradients_see_no_rows_of_nobody(dtype):
+    _dw_case([40, 0, 90], 200, 136, dtype, "f32", before=13, behind=21)
+    _dw_case([0, 0], 64, 64, dtype, "f32", before=3, behind=2)
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_weight_gradients_of_random_sizes(seed):
+    g = torch.Generator()
+    g.manual_seed(200 + seed)
+    draw = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=g))  # noqa: E731
+    dtype, grad = (("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"))[seed % 3]
+    _dw_case(_sizes(draw(1, 4000), draw(1, 24), seed), 8 * draw(1, 90), 8 * draw(1, 90), dtype, grad, bias=seed % 2 == 0, seed=seed)
+
+
+def test_no_rows_at_all():
+    off = torch.zeros(4, dtype=torch.int32, device=DEV)
+    w = _normal((3, 64, 32), 1.0, torch.bfloat16, 1)
+    none = torch.empty((0, 32), dtype=torch.bfloat16, device=DEV)
+    assert exf.moe_grouped_product(none, off, w).shape == (0, 64)
+    assert exf.moe_grouped_product_mx4(none, off, exf.mx4_quantize(w)).shape == (0, 64)
+    dy = torch.empty((0, 64), dtype=torch.bfloat16, device=DEV)
+    assert exf.moe_grouped_product_dx(dy, off, w).shape == (0, 32)
+    out = torch.full((3, 64, 32), 5.0, dtype=torch.float32, device=DEV)
+    dw, db = exf.moe_grouped_product_dw(dy, none, off, want_bias=True, out=out)
+    assert (dw == 0).all() and (db == 0).all() and db.dtype == torch.float32
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_that_lead_out_of_the_rows(dtype):
+    """Offsets past the rows, negative or falling: clamped, so nothing is read or written outside; what is inside is right."""
+    dt = TYPES[dtype]
+    A, n, k = 100, 72, 64
+    off = torch.tensor([-5, 30, 60, 400], dtype=torch.int32, device=DEV)
+    x, dy, w = _normal((A, k), 1.0, dt, 1), _normal((A, n), 1.0, dt, 2), _normal((3, n, k), 0.1, dt, 3)
+    R.assert_sums_close(exf.moe_grouped_product(x, off, w), *R.rows_product(x, off, w)[:2], k, "y")
+    R.assert_sums_close(exf.moe_grouped_product_dx(dy, off, w), *R.rows_product(dy, off, w, None, True)[:2], n, "dx")
+    dw, db = exf.moe_grouped_product_dw(dy, x, off, want_bias=True, grad_dtype=torch.float32)
+    ref, mag, ref_b, mag_b, terms = R.weight_gradient(dy, x, off)
+    R.assert_sums_close(dw, ref, mag, terms, "dw")
+    R.assert_sums_close(db, ref_b, mag_b, terms, "db")
+    w4 = exf.mx4_quantize(w)
+    y4 = exf.moe_grouped_product_mx4(x, off, w4)
+    ref, mag, terms = R.rows_product(R.quantised(x)[0], off, R.held_values(w4.q.view(-1, k // 2), w4.scale).view(3, n, k))
+    R.assert_sums_close(y4, ref, mag, terms, "mx4")
+
+
+def test_infinities_stay_with_their_row_and_expert():
+    """An infinity in one row or one expert's weights reaches what is summed with it and nothing else (partial tiles share stages)."""
+    sizes, n, k = [70, 30, 45], 200, 136
+    off = R.sizes_to_offsets(sizes).to(DEV)
+    x, dy = _normal((145, k), 1.0, torch.bfloat16, 1), _normal((145, n), 1.0, torch.bfloat16, 2)
+    w = _normal((3, n, k), 0.1, torch.bfloat16, 3)
+    x[75, 5], dy[75, 7], w[2, 11, 13] = float("inf"), float("inf"), float("inf")
+    y, dx = exf.moe_grouped_product(x, off, w), exf.moe_grouped_product_dx(dy, off, w)
+    dw, _ = exf.moe_grouped_product_dw(dy, x, off)
+    bad = ~torch.isfinite(y)
+    assert bad[75].all() and bad[100:, 11].all() and int(bad.sum()) == n + 45
+    bad = ~torch.isfinite(dx)
+    assert bad[75].all() and bad[100:, 13].all() and int(bad.sum()) == k + 45
+    bad = ~torch.isfinite(dw)
+    assert bad[1, 7].all() and bad[1, :, 5].all() and int(bad.sum()) == n + k - 1
+
+
+def test_gradients_against_differences():
+    """The directional derivative of L = <c, y(x, w, b)> in fp32.  L is linear in each argument, so a central difference has no
+    truncation error; its rounding is 2 |L| terms u / step."""
+    sizes, n, k = [33, 0, 80, 7], 72, 100
+    off = R.sizes_to_offsets(sizes).to(DEV)
+    A, E = sum(sizes), len(sizes)
+    f = torch.float32
+    x, w, b, c = _normal((A, k), 1.0, f, 1), _normal((E, n, k), 0.3, f, 2), _normal((E, n), 1.0, f, 3), _normal((A, n), 1.0, f, 4)
+    dx = exf.moe_grouped_product_dx(c, off, w)
+    dw, db = exf.moe_grouped_product_dw(c, x, off, want_bias=True)
+    loss = lambda x, w, b: float((exf.moe_grouped_product(x, off, w, b).double() * c.double()).sum())  # noqa: E731
+    size = float((R.rows_product(x, off, w, b)[1] * c.double().abs()).sum())
+    for name, at, grad in (("x", x, dx), ("w", w, dw), ("b", b, db)):
+        d = _normal(at.shape, 1.0, f, 9)
+        args = {"x": x, "w": w, "b": b}
+        h = 1.0
+        up, down = loss(**{**args, name: at + h * d}), loss(**{**args, name: at - h * d})
+        slope = float((grad.double() * d.double()).sum())
+        assert abs((up - down) / (2 * h) - slope) <= 8 * 4 * (k + A) * R.U32 * size, name
+
+
+# ----------------------------------------------------------------------------- 4 bits
+def _block_rows(rows, k, dt, seed):
+    """Rows that hold every hard case of a block: all codes and the halfway points, one large value, zeros, the least and the largest numbers."""
+    x = _normal((rows, k), 1.0, torch.float32, seed)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed + 1)
+    x = x * torch.exp2(torch.randint(-40, 40, (rows, 1), device=DEV, generator=g).float())
+    ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 7.9375, 4.0, 3.0, 0.0, -0.0, 0.2421875, 0.2578125], device=DEV)
+    hard = [torch.cat((ties, -ties)), torch.cat((ties, -ties)) * 2.0 ** -100, torch.zeros(32, device=DEV), torch.full((32,), 2.0 ** -133, device=DEV),
+            torch.cat((ties, -ties)) * 2.0 ** -128, torch.full((32,), 3.0e38, device=DEV), torch.cat((torch.tensor([1e30], device=DEV), torch.ones(31, device=DEV))),
+            -torch.cat((ties, -ties)) * 2.0 ** 100]
+    flat = x.view(-1, 32)
+    for i, h in enumerate(hard):
+        flat[(i * 7) % flat.shape[0]] = h
+    return x.to(dt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,k", [(1, 32), (1, 256), (3, 288), (5, 1024), (64, 96), (33, 544), (1000, 512), (2, 8192), (7, 224)])
+def test_quantise(dtype, rows, k):
+    _say(f"quantise rows={rows} k={k} {dtype}")
+    x = _block_rows(rows, k, TYPES[dtype], rows + k)
+    held = exf.mx4_quantize(x)
+    values, byte = R.quantised(x)
+    assert torch.equal(held.scale, R.scale_tiles(byte)), "scales"
+    got = R.held_values(held.q, held.scale)
+    assert torch.equal(got, values) and torch.equal(torch.signbit(got), torch.signbit(values)), "codes"
+    for dt in (torch.bfloat16, torch.float32):
+        back = exf.mx4_dequantize(held, dt)
+        assert torch.equal(back.double(), values) and torch.equal(torch.signbit(back), torch.signbit(values)), dt
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_blocks_that_hold_infinities_or_nans(dtype):
+    x = _normal((4, 288), 1.0, TYPES[dtype], 3)
+    x[0, 3], x[1, 40], x[2, 287], x[3, 256] = float("inf"), float("nan"), float("-inf"), -float("nan")
+    held = exf.mx4_quantize(x)
+    values, byte = R.quantised(x)
+    assert torch.equal(held.scale, R.scale_tiles(byte))
+    back = exf.mx4_dequantize(held)
+    assert torch.equal(torch.isnan(back), torch.isnan(values)) and int(torch.isnan(back).sum()) == 4 * 32
+    assert torch.equal(torch.nan_to_num(back.double()), torch.nan_to_num(values))
+    # ... and what a product sums them into
+    w = _normal((1, 64, 288), 1.0, torch.bfloat16, 4)
+    off = R.sizes_to_offsets([3]).to(DEV)
+    clean = _normal((3, 288), 1.0, TYPES[dtype], 5)
+    clean[1, 70] = float("nan")
+    y = exf.moe_grouped_product_mx4(clean, off, exf.mx4_quantize(w))
+    assert torch.isnan(y[1]).all() and torch.isfinite(y[0]).all() and torch.isfinite(y[2]).all()
+
+
+def test_quantise_of_weights_with_leading_axes():
+    w = _normal((3, 40, 96), 0.1, torch.bfloat16, 1)
+    held = exf.mx4_quantize(w)
+    assert held.shape == (3, 40, 96) and held.rows == 120 and held.scale.shape == (1, 120, 8)
+    assert torch.equal(exf.mx4_dequantize(held).double(), R.quantised(w)[0])
+    assert exf.mx4_quantize(w[:0]).scale.shape == (1, 0, 8)
+
+
+def _mx4_case(sizes, n, k, dtype, bias=True, held=True, before=0, behind=0, seed=1):
+    dt = TYPES[dtype]
+    A, E = before + sum(sizes) + behind, len(sizes)
+    _say(f"mx4 sizes={sizes if E <= 12 else (E, sum(sizes))} n={n} k={k} {dtype} bias={bias} held={held} before={before} behind={behind}")
+    off = R.sizes_to_offsets(sizes, before).to(DEV)
+    x = _normal((A, k), 1.0, dt, seed)
+    x[:before] = float("nan")
+    x[before + sum(sizes):] = float("inf")
+    w = exf.mx4_quantize(_normal((E, n, k), 0.1, dt, seed + 1))
+    b = _normal((E, n), 1.0, dt, seed + 2) if bias else None
+    out = torch.full((A, n), 7.0, dtype=dt, device=DEV)
+    rows = exf.mx4_quantize(x) if held else x
+    got = exf.moe_grouped_product_mx4(rows, off, w, b, out=out)
+    assert got is out
+    ref, mag, terms = R.rows_product(R.quantised(x)[0], off, R.held_values(w.q.view(-1, k // 2), w.scale).view(E, n, k), b)
+    there = slice(before, before + sum(sizes))
+    R.assert_sums_close(out[there], ref[there], mag[there], terms, "mx4")
+    assert (out[:before] == 7.0).all() and (out[before + sum(sizes):] == 7.0).all()
+    again = torch.zeros_like(out)
+    exf.moe_grouped_product_mx4(rows, off, w, b, out=again)
+    assert torch.equal(out[there], again[there]), "the same call, other bits"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes,n,k", [
+    ([1], 8, 32), ([0, 1, 0], 16, 64), ([3, 0, 5], 72, 96), ([63, 65, 1, 0, 64], 136, 224), ([129, 31, 127], 264, 256), ([257, 0, 320, 300], 520, 288),
+    ([5], 1032, 1536), ([700], 256, 512), ([1, 2, 3, 4], 2048, 1056),
+])
+def test_mx4_product(dtype, sizes, n, k):
+    _mx4_case(sizes, n, k, dtype)
+    _mx4_case(sizes, n, k, dtype, bias=False, held=False)
+
+
+@pytest.mark.parametrize("sizes,n,k", [
+    ([32, 64, 96, 128, 160, 192, 224, 256], 512, 256), ([288, 320, 300, 33], 256, 512), ([500, 520, 700, 1100], 320, 768), ([2100, 40], 640, 1024),
+    ([17, 30, 55, 90, 140, 210], 1024, 1792), ([1300], 1536, 1536), ([150] * 40, 1024, 2048), ([8] * 64, 512, 4096), ([250] * 24 + [0] * 8, 768, 1280),
+    ([4000, 10, 900], 512, 992), ([1] * 64, 256, 1056),
+])
+def test_mx4_product_in_tiles(sizes, n, k):
+    _mx4_case(sizes, n, k, "bf16", held=len(sizes) % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_mx4_rows_of_nobody_stay(dtype):
+    _mx4_case([40, 0, 90], 200, 160, dtype, before=13, behind=21)
+    _mx4_case([2, 0], 64, 320, dtype, before=1, behind=3, held=False)
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_mx4_product_of_random_sizes(seed):
+    g = torch.Generator()
+    g.manual_seed(300 + seed)
+    draw = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=g))  # noqa: E731
+    _mx4_case(_sizes(draw(1, 3000), draw(1, 64), seed), 8 * draw(1, 150), 32 * draw(1, 60), "bf16" if seed % 3 else "f32", bias=seed % 2 == 0,
+              held=seed % 2 == 1, seed=seed)
+
+
+# ----------------------------------------------------------------------------- as programs use them
+def test_on_another_stream_and_in_a_graph():
+    """Calls enqueue on the current stream; captured, they replay, with other values in the same tensors."""
+    sizes, n, k = [70, 0, 131, 9], 264, 288
+    off = R.sizes_to_offsets(sizes).to(DEV)
+    A, E = sum(sizes), len(sizes)
+    x, dy, w = (torch.empty(s, dtype=torch.bfloat16, device=DEV) for s in ((A, k), (A, n), (E, n, k)))
+
+    def fill(seed):
+        x.copy_(_normal((A, k), 1.0, torch.bfloat16, seed))
+        dy.copy_(_normal((A, n), 1.0, torch.bfloat16, seed + 1))
+        w.copy_(_normal((E, n, k), 0.1, torch.bfloat16, seed + 2))
+
+    def calls():
+        return (exf.moe_grouped_product(x, off, w), exf.moe_grouped_product_dx(dy, off, w), *exf.moe_grouped_product_dw(dy, x, off, want_bias=True),
+                exf.moe_grouped_product_mx4(x, off, exf.mx4_quantize(w)))
+
+    fill(1)
+    want = calls()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        got = calls()
+    torch.cuda.current_stream().wait_stream(stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = calls()
+    for seed in (1, 11, 21):
+        fill(seed)
+        want = calls()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, want)), seed
+
+
+def test_rows_of_a_dispatch():
+    """What moe_dispatch leaves is what the products take: a share of the experts resident, the rest's assignments dropped."""
+    T, k, d, f, E, E_local = 300, 2, 128, 256, 16, 5
+    g = torch.Generator()
+    g.manual_seed(5)
+    idx = torch.randint(0, E, (T, k), generator=g, dtype=torch.int32).to(DEV)
+    emap = torch.full((E,), -1, dtype=torch.int32)
+    emap[[1, 4, 5, 9, 14]] = torch.arange(5, dtype=torch.int32)
+    x = _normal((T, d), 1.0, torch.bfloat16, 1)
+    disp = exf.moe_dispatch(x, idx, E, E_local=E_local, expert_map=emap.to(DEV))
+    w = _normal((E_local, f, d), 0.1, torch.bfloat16, 2)
+    kept = int(disp.expert_offsets[-1])
+    assert 0 < kept < T * k
+    y = exf.moe_grouped_product(disp.x_sorted, disp.expert_offsets, w)
+    ref, mag, terms = R.rows_product(disp.x_sorted, disp.expert_offsets, w)
+    R.assert_sums_close(y[:kept], ref[:kept], mag[:kept], terms, "y")
