@@ -1,5 +1,5 @@
 // Entry points of the experts' products: checks, and the choice of kernels.
-#include "product.hpp"
+#include "product_tiles.hpp"
 
 namespace exf {
 
@@ -44,8 +44,13 @@ extern "C" int moe_grouped_product(const void* x_sorted, const int32_t* expert_o
     using namespace exf;
     if (int rc = check_rows_product("moe_grouped_product", x_sorted, expert_offsets, w, bias, A, n, k, E_local, dt, false, y_sorted)) return rc;
     if (A == 0) return EXF_OK;
-    const RowsProduct p{x_sorted, expert_offsets, w, bias, y_sorted, static_cast<int>(A), k, n, E_local};
-    const int rc = launch_exact_rows_product(p, false, dt, static_cast<hipStream_t>(stream));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    int rc;
+    if (dt == EXF_BF16) {
+        rc = launch_forward_tiles({x_sorted, expert_offsets, w, static_cast<const bf16_t*>(bias), static_cast<bf16_t*>(y_sorted), nullptr, nullptr, static_cast<int>(A), k, n, E_local}, s);
+    } else {
+        rc = launch_exact_rows_product({x_sorted, expert_offsets, w, bias, y_sorted, static_cast<int>(A), k, n, E_local}, false, s);
+    }
     return rc == EXF_OK ? check_launch("moe_grouped_product") : rc;
 }
 
@@ -55,15 +60,21 @@ extern "C" int moe_grouped_product_dx(const void* dy_sorted, const int32_t* expe
     using namespace exf;
     if (int rc = check_rows_product("moe_grouped_product_dx", dy_sorted, expert_offsets, w, nullptr, A, n, k, E_local, dt, true, dx_sorted)) return rc;
     if (A == 0) return EXF_OK;
-    const RowsProduct p{dy_sorted, expert_offsets, w, nullptr, dx_sorted, static_cast<int>(A), n, k, E_local};
-    const int rc = launch_exact_rows_product(p, true, dt, static_cast<hipStream_t>(stream));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    int rc;
+    if (dt == EXF_BF16) {
+        rc = launch_rows_gradient_tiles({dy_sorted, expert_offsets, w, nullptr, static_cast<bf16_t*>(dx_sorted), nullptr, nullptr, static_cast<int>(A), n, k, E_local}, s);
+    } else {
+        rc = launch_exact_rows_product({dy_sorted, expert_offsets, w, nullptr, dx_sorted, static_cast<int>(A), n, k, E_local}, true, s);
+    }
     return rc == EXF_OK ? check_launch("moe_grouped_product_dx") : rc;
 }
 
 extern "C" size_t moe_grouped_product_dw_workspace_bytes(int64_t A, int n, int k, int E_local, int dt)
 {
-    (void)A, (void)n, (void)k, (void)E_local, (void)dt;
-    return 0;
+    if (A < 1 || n < 1 || k < 1 || E_local < 1 || dt != EXF_BF16) return 0;
+    const int splits = exf::weight_gradient_splits(A, n, k, E_local);
+    return splits > 1 ? exf::align_up(static_cast<size_t>(splits) * E_local * n * k * 4, 256) : 0;
 }
 
 extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorted, const int32_t* expert_offsets, int64_t A, int n, int k, int E_local,
@@ -100,8 +111,11 @@ extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorte
     if (overlap(dw, out[0].bytes, db, out[1].bytes) || overlap(workspace, need, dw, out[0].bytes) || overlap(workspace, need, db, out[1].bytes))
         return fail(EXF_ERR_BAD_SHAPE, "%s: results and workspace must not overlap", fn);
     const WeightGradient p{dy_sorted, x_sorted, expert_offsets, dw, db, workspace, static_cast<int>(A), n, k, E_local};
-    const int rc = launch_exact_weight_gradient(p, dt, grad_dt, static_cast<hipStream_t>(stream));
-    return rc == EXF_OK ? check_launch(fn) : rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (int rc = dt == EXF_BF16 ? launch_weight_gradient_tiles(p, grad_dt, s) : launch_exact_weight_gradient(p, s)) return rc;
+    if (db != nullptr)
+        if (int rc = launch_bias_gradient(p, dt, grad_dt, s)) return rc;
+    return check_launch(fn);
 }
 
 extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k)
@@ -153,6 +167,12 @@ extern "C" int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_sc
         if (int rc = mx4_quantize(x_sorted, A, k, dt, q, scale, stream)) return rc;
         p.rows = q, p.row_scale = scale;
     }
-    const int rc = launch_mx4_product(p, dt, static_cast<hipStream_t>(stream));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    int rc;
+    if (dt == EXF_BF16) {
+        rc = launch_mx4_tiles({p.rows, expert_offsets, w, static_cast<const bf16_t*>(bias), static_cast<bf16_t*>(y_sorted), p.row_scale, w_scale, static_cast<int>(A), k, n, E_local}, s);
+    } else {
+        rc = launch_mx4_product(p, s);
+    }
     return rc == EXF_OK ? check_launch(fn) : rc;
 }

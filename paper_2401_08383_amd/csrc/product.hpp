@@ -39,10 +39,11 @@ struct Mx4Product {
     int max_rows, K, N, E_local;
 };
 
-// The plain matrix-core kernels in fp32 arithmetic (product_exact.hip).
-int launch_exact_rows_product(const RowsProduct& p, bool gradient, int dt, hipStream_t stream);
-int launch_exact_weight_gradient(const WeightGradient& p, int dt, int grad_dt, hipStream_t stream);
-int launch_mx4_product(const Mx4Product& p, int dt, hipStream_t stream);
+// fp32 (product_exact.hip).
+int launch_exact_rows_product(const RowsProduct& p, bool gradient, hipStream_t stream);
+int launch_exact_weight_gradient(const WeightGradient& p, hipStream_t stream);
+int launch_bias_gradient(const WeightGradient& p, int dt, int grad_dt, hipStream_t stream);
+int launch_mx4_product(const Mx4Product& p, hipStream_t stream);  // result in fp32
 
 // Bytes [a, a + n) and [b, b + m) overlap (nothing overlaps a null pointer).
 inline bool overlap(const void* a, size_t n, const void* b, size_t m)

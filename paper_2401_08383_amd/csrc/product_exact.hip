@@ -12,29 +12,15 @@ namespace exf {
 
 constexpr int kExactTile = 64, kExactDepth = 32;
 
-template <typename T>
-__device__ __forceinline__ f32x4_t load4(const T* p);
-template <>
-__device__ __forceinline__ f32x4_t load4<float>(const float* p)
-{
-    return *reinterpret_cast<const f32x4_t*>(p);
-}
-template <>
-__device__ __forceinline__ f32x4_t load4<bf16_t>(const bf16_t* p)
-{
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    return f32x4_t{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
-}
-__device__ __forceinline__ void store4(float* p, f32x4_t v) { *reinterpret_cast<f32x4_t*>(p) = v; }
-__device__ __forceinline__ void store4(bf16_t* p, f32x4_t v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
+__device__ __forceinline__ f32x4_t load4(const float* p) { return *reinterpret_cast<const f32x4_t*>(p); }
 
 // One operand of a tile: 64 rows (output rows or columns) of the reduction [0, depth).
 //   ACROSS false: element (row, r) at base[row * ld + r];  true: at base[r * ld + row].
-template <typename T, bool ACROSS>
+template <bool ACROSS>
 struct ExactOperand {
     static constexpr int STRIDE = ACROSS ? kExactTile + 4 : kExactDepth + 4;
     static constexpr int FLOATS = ACROSS ? kExactDepth * STRIDE : kExactTile * STRIDE;
-    const T* base;
+    const float* base;
     int64_t ld;
     int rows, depth;
     f32x4_t v[2];
@@ -65,11 +51,11 @@ struct ExactOperand {
 };
 
 // D[row][col] = sum_r a(row, r) w(col, r) + bias[col], written where row < a.rows and col < w.rows.
-template <typename T, typename TO, bool A_ACROSS, bool W_ACROSS>
-__device__ __forceinline__ void exact_tile(ExactOperand<T, A_ACROSS> a, ExactOperand<T, W_ACROSS> w, const T* bias, TO* out, int64_t ldo)
+template <bool A_ACROSS, bool W_ACROSS>
+__device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperand<W_ACROSS> w, const float* bias, float* out, int64_t ldo)
 {
-    typedef ExactOperand<T, A_ACROSS> OA;
-    typedef ExactOperand<T, W_ACROSS> OW;
+    typedef ExactOperand<A_ACROSS> OA;
+    typedef ExactOperand<W_ACROSS> OW;
     __shared__ __attribute__((aligned(16))) float lds[OA::FLOATS + OW::FLOATS];
     float *la = lds, *lw = lds + OA::FLOATS;
     const int lane = lane_id(), wave = threadIdx.x / kWave;
@@ -116,11 +102,11 @@ __device__ __forceinline__ void exact_tile(ExactOperand<T, A_ACROSS> a, ExactOpe
             if (row >= a.rows || col >= w.rows) continue;
             f32x4_t v = acc[0][i][j] + acc[1][i][j];
             if (bias != nullptr) v += load4(bias + col);
-            store4(out + static_cast<int64_t>(row) * ldo + col, v);
+            *reinterpret_cast<f32x4_t*>(out + static_cast<int64_t>(row) * ldo + col) = v;
         }
 }
 
-template <typename T, bool GRADIENT>
+template <bool GRADIENT>
 __global__ __launch_bounds__(256) void exact_rows_kernel(const RowsProduct p, int col_tiles)
 {
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
@@ -134,13 +120,12 @@ __global__ __launch_bounds__(256) void exact_rows_kernel(const RowsProduct p, in
     const int row = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * kExactTile;
     const int col = col_tile * kExactTile;
     const int64_t K = p.K, N = p.N;
-    const T* weight = static_cast<const T*>(p.weight) + e * N * K;
-    const ExactOperand<T, false> a{static_cast<const T*>(p.rows) + row * K, K, min(kExactTile, hi - row), p.K, {}};
-    const ExactOperand<T, GRADIENT> w{GRADIENT ? weight + col : weight + col * K, GRADIENT ? N : K, min(kExactTile, p.N - col), p.K, {}};
-    exact_tile<T, T>(a, w, p.bias != nullptr ? static_cast<const T*>(p.bias) + e * N + col : nullptr, static_cast<T*>(p.out) + row * N + col, N);
+    const float* weight = static_cast<const float*>(p.weight) + e * N * K;
+    const ExactOperand<false> a{static_cast<const float*>(p.rows) + row * K, K, min(kExactTile, hi - row), p.K, {}};
+    const ExactOperand<GRADIENT> w{GRADIENT ? weight + col : weight + col * K, GRADIENT ? N : K, min(kExactTile, p.N - col), p.K, {}};
+    exact_tile(a, w, p.bias != nullptr ? static_cast<const float*>(p.bias) + e * N + col : nullptr, static_cast<float*>(p.out) + row * N + col, N);
 }
 
-template <typename T, typename TO>
 __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient p, int row_tiles, int col_tiles)
 {
     const unsigned per_expert = static_cast<unsigned>(row_tiles) * static_cast<unsigned>(col_tiles);
@@ -150,9 +135,9 @@ __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient 
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
     const int lo = wave_read_lane(range.lo, e), n = wave_read_lane(range.hi, e) - lo;
     const int64_t N = p.N, K = p.K;
-    const ExactOperand<T, true> a{static_cast<const T*>(p.dy) + lo * N + row, N, min(kExactTile, p.N - row), n, {}};
-    const ExactOperand<T, true> w{static_cast<const T*>(p.x) + lo * K + col, K, min(kExactTile, p.K - col), n, {}};
-    exact_tile<T, TO>(a, w, static_cast<const T*>(nullptr), static_cast<TO*>(p.dw) + (e * N + row) * K + col, K);
+    const ExactOperand<true> a{static_cast<const float*>(p.dy) + lo * N + row, N, min(kExactTile, p.N - row), n, {}};
+    const ExactOperand<true> w{static_cast<const float*>(p.x) + lo * K + col, K, min(kExactTile, p.K - col), n, {}};
+    exact_tile(a, w, nullptr, static_cast<float*>(p.dw) + (e * N + row) * K + col, K);
 }
 
 // db: a workgroup an expert and 64 columns; four rows of threads a column each, joined in order.
@@ -182,34 +167,32 @@ __global__ __launch_bounds__(256) void bias_gradient_kernel(const WeightGradient
 
 static int64_t tiles_of(int64_t n) { return (n + kExactTile - 1) / kExactTile; }
 
-template <typename T>
-static int launch_rows_as(const RowsProduct& p, bool gradient, hipStream_t stream)
+int launch_exact_rows_product(const RowsProduct& p, bool gradient, hipStream_t stream)
 {
     const int64_t cols = tiles_of(p.N), grid = (p.max_rows / kExactTile + (p.max_rows < p.E_local ? p.max_rows : p.E_local)) * cols;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product: too many tiles");
-    if (gradient) hipLaunchKernelGGL((exact_rows_kernel<T, true>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
-    else hipLaunchKernelGGL((exact_rows_kernel<T, false>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
+    if (gradient) hipLaunchKernelGGL(exact_rows_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
+    else hipLaunchKernelGGL(exact_rows_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
     return EXF_OK;
 }
-int launch_exact_rows_product(const RowsProduct& p, bool gradient, int dt, hipStream_t stream)
-{
-    return dt == EXF_BF16 ? launch_rows_as<bf16_t>(p, gradient, stream) : launch_rows_as<float>(p, gradient, stream);
-}
-
-template <typename T, typename TO>
-static int launch_weight_as(const WeightGradient& p, hipStream_t stream)
+int launch_exact_weight_gradient(const WeightGradient& p, hipStream_t stream)
 {
     const int64_t rows = tiles_of(p.N), cols = tiles_of(p.K), grid = p.E_local * rows * cols;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
-    hipLaunchKernelGGL((exact_weight_kernel<T, TO>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(rows), static_cast<int>(cols));
-    if (p.db != nullptr)
-        hipLaunchKernelGGL((bias_gradient_kernel<T, TO>), dim3(static_cast<unsigned>(p.E_local * rows)), dim3(256), 0, stream, p, static_cast<int>(rows));
+    hipLaunchKernelGGL(exact_weight_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(rows), static_cast<int>(cols));
     return EXF_OK;
 }
-int launch_exact_weight_gradient(const WeightGradient& p, int dt, int grad_dt, hipStream_t stream)
+template <typename T, typename TO>
+static int launch_bias_as(const WeightGradient& p, hipStream_t stream)
 {
-    if (dt == EXF_F32) return launch_weight_as<float, float>(p, stream);
-    return grad_dt == EXF_F32 ? launch_weight_as<bf16_t, float>(p, stream) : launch_weight_as<bf16_t, bf16_t>(p, stream);
+    const int64_t cols = tiles_of(p.N);
+    hipLaunchKernelGGL((bias_gradient_kernel<T, TO>), dim3(static_cast<unsigned>(p.E_local * cols)), dim3(256), 0, stream, p, static_cast<int>(cols));
+    return EXF_OK;
+}
+int launch_bias_gradient(const WeightGradient& p, int dt, int grad_dt, hipStream_t stream)
+{
+    if (dt == EXF_F32) return launch_bias_as<float, float>(p, stream);
+    return grad_dt == EXF_F32 ? launch_bias_as<bf16_t, float>(p, stream) : launch_bias_as<bf16_t, bf16_t>(p, stream);
 }
 
 }  // namespace exf

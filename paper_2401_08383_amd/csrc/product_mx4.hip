@@ -12,13 +12,12 @@ typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8_t;
 
 constexpr int kMxTile = 64;
 
-__device__ __forceinline__ f32x4_t mfma_mx4(i32x4_t a, i32x4_t b, f32x4_t c, int scale_a, int scale_b)
+__device__ __forceinline__ f32x4_t mfma_mx4_direct(i32x4_t a, i32x4_t b, f32x4_t c, int scale_a, int scale_b)
 {
     const i32x8_t wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};  // (4-bit operands: the lower half)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, 0, scale_a, 0, scale_b);
 }
 
-template <bool BF16>
 __global__ __launch_bounds__(64) void mx4_rows_kernel(const Mx4Product p, int col_tiles)
 {
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
@@ -60,7 +59,7 @@ __global__ __launch_bounds__(64) void mx4_rows_kernel(const Mx4Product p, int co
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = mfma_mx4(fw[j], fa[i], acc[i][j], sw[j], sa[i]);
+            for (int j = 0; j < 4; ++j) acc[i][j] = mfma_mx4_direct(fw[j], fa[i], acc[i][j], sw[j], sa[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -69,24 +68,16 @@ __global__ __launch_bounds__(64) void mx4_rows_kernel(const Mx4Product p, int co
             const int r = row0 + i * 16 + in16, c = col0 + j * 16 + quad * 4;
             if (r >= hi || c >= p.N) continue;
             f32x4_t v = acc[i][j];
-            if constexpr (BF16) {
-                if (p.bias != nullptr)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] += bf16_to_f32(static_cast<const bf16_t*>(p.bias)[e * N + c + q]);
-                *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + r * N + c) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-            } else {
-                if (p.bias != nullptr) v += *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p.bias) + e * N + c);
-                *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + r * N + c) = v;
-            }
+            if (p.bias != nullptr) v += *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p.bias) + e * N + c);
+            *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + r * N + c) = v;
         }
 }
 
-int launch_mx4_product(const Mx4Product& p, int dt, hipStream_t stream)
+int launch_mx4_product(const Mx4Product& p, hipStream_t stream)
 {
     const int64_t cols = (p.N + kMxTile - 1) / kMxTile, grid = (p.max_rows / kMxTile + (p.max_rows < p.E_local ? p.max_rows : p.E_local)) * cols;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_mx4: too many tiles");
-    if (dt == EXF_BF16) hipLaunchKernelGGL(mx4_rows_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(64), 0, stream, p, static_cast<int>(cols));
-    else hipLaunchKernelGGL(mx4_rows_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(64), 0, stream, p, static_cast<int>(cols));
+    hipLaunchKernelGGL(mx4_rows_kernel, dim3(static_cast<unsigned>(grid)), dim3(64), 0, stream, p, static_cast<int>(cols));
     return EXF_OK;
 }
 
