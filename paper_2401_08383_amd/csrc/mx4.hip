@@ -67,14 +67,17 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restric
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint32_t* __restrict__ q, const uint8_t* __restrict__ scale, int64_t rows, int k,
+__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint32_t* __restrict__ q, const uint8_t* __restrict__ scale, int64_t rows, int k, int tiles,
                                                              void* __restrict__ out)
 {
-    const int64_t per_row = k / 8, items = rows * per_row, threads = static_cast<int64_t>(gridDim.x) * blockDim.x;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < items; i += threads) {
-        const int64_t row = i / per_row;
-        const int col = static_cast<int>(i - row * per_row) * 8;
-        const uint32_t byte = scale[(col / kScaleTile * rows + row) * 8 + col % kScaleTile / 32], code = q[i];
+    const int lane = lane_id(), half = lane >> 5, chunk = lane & 31;
+    const int64_t items = (rows + 1) / 2 * tiles, waves = static_cast<int64_t>(gridDim.x) * (blockDim.x / kWave);  // an item: a tile of two rows
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (blockDim.x / kWave) + threadIdx.x / kWave; item < items; item += waves) {
+        const int64_t row = item / tiles * 2 + half;
+        const int tile = static_cast<int>(item % tiles), col = tile * kScaleTile + chunk * 8;
+        if (row >= rows || col >= k) continue;
+        const int64_t i = (row * k + col) / 8;
+        const uint32_t byte = scale[(tile * rows + row) * 8 + chunk / 4], code = q[i];
         const float s = scale_value(byte == 255u ? 127u : byte);
         f32x2_t v[4];
         v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 0);
@@ -140,10 +143,11 @@ extern "C" int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t ro
     using namespace exf;
     if (int rc = check_mx4("mx4_dequantize", out, rows, k, dt, q, scale)) return rc;
     if (rows == 0) return EXF_OK;
-    const int64_t items = rows * (k / 8), blocks = (items + 255) / 256;
-    const unsigned grid = static_cast<unsigned>(blocks < 4 * kStreamWorkgroups ? blocks : 4 * kStreamWorkgroups);
+    const int tiles = (k + kScaleTile - 1) / kScaleTile;
+    const int64_t items = (rows + 1) / 2 * tiles;
+    const unsigned grid = static_cast<unsigned>(items / 4 + 1 < 4 * kStreamWorkgroups ? items / 4 + 1 : 4 * kStreamWorkgroups);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dt == EXF_BF16) hipLaunchKernelGGL(mx4_dequantize_kernel<true>, dim3(grid), dim3(256), 0, s, reinterpret_cast<const uint32_t*>(q), scale, rows, k, out);
-    else hipLaunchKernelGGL(mx4_dequantize_kernel<false>, dim3(grid), dim3(256), 0, s, reinterpret_cast<const uint32_t*>(q), scale, rows, k, out);
+    if (dt == EXF_BF16) hipLaunchKernelGGL(mx4_dequantize_kernel<true>, dim3(grid), dim3(256), 0, s, reinterpret_cast<const uint32_t*>(q), scale, rows, k, tiles, out);
+    else hipLaunchKernelGGL(mx4_dequantize_kernel<false>, dim3(grid), dim3(256), 0, s, reinterpret_cast<const uint32_t*>(q), scale, rows, k, tiles, out);
     return check_launch("mx4_dequantize");
 }

@@ -72,9 +72,9 @@ extern "C" int moe_grouped_product_dx(const void* dy_sorted, const int32_t* expe
 
 extern "C" size_t moe_grouped_product_dw_workspace_bytes(int64_t A, int n, int k, int E_local, int dt)
 {
-    if (A < 1 || n < 1 || k < 1 || E_local < 1 || dt != EXF_BF16) return 0;
-    const int splits = exf::weight_gradient_splits(A, n, k, E_local);
-    return splits > 1 ? exf::align_up(static_cast<size_t>(splits) * E_local * n * k * 4, 256) : 0;
+    if (A < 1 || n < 1 || k < 1 || E_local < 1 || (dt != EXF_BF16 && dt != EXF_F32)) return 0;
+    const int splits = dt == EXF_BF16 ? exf::weight_gradient_splits(A, n, k, E_local) : exf::exact_weight_gradient_splits(A, n, k, E_local);
+    return splits > 1 ? exf::align_up(static_cast<size_t>(splits) * E_local * n * (static_cast<size_t>(k) + 1) * 4, 256) : 0;  // dw's and db's
 }
 
 extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorted, const int32_t* expert_offsets, int64_t A, int n, int k, int E_local,
@@ -112,10 +112,8 @@ extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorte
         return fail(EXF_ERR_BAD_SHAPE, "%s: results and workspace must not overlap", fn);
     const WeightGradient p{dy_sorted, x_sorted, expert_offsets, dw, db, workspace, static_cast<int>(A), n, k, E_local};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (int rc = dt == EXF_BF16 ? launch_weight_gradient_tiles(p, grad_dt, s) : launch_exact_weight_gradient(p, s)) return rc;
-    if (db != nullptr)
-        if (int rc = launch_bias_gradient(p, dt, grad_dt, s)) return rc;
-    return check_launch(fn);
+    const int rc = dt == EXF_BF16 ? launch_weight_gradient_tiles(p, grad_dt, s) : launch_exact_weight_gradient(p, s);
+    return rc == EXF_OK ? check_launch(fn) : rc;
 }
 
 extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k)

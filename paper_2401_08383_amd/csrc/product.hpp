@@ -42,7 +42,9 @@ struct Mx4Product {
 // fp32 (product_exact.hip).
 int launch_exact_rows_product(const RowsProduct& p, bool gradient, hipStream_t stream);
 int launch_exact_weight_gradient(const WeightGradient& p, hipStream_t stream);
-int launch_bias_gradient(const WeightGradient& p, int dt, int grad_dt, hipStream_t stream);
+int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local);
+// The sums of `splits` parts of n (and of m) values each, in order, in the type `dt`.
+int launch_join_parts(const float* parts, int64_t n, void* out, const float* more, int64_t m, void* more_out, int splits, int dt, hipStream_t stream);
 int launch_mx4_product(const Mx4Product& p, hipStream_t stream);  // result in fp32
 
 // Bytes [a, a + n) and [b, b + m) overlap (nothing overlaps a null pointer).

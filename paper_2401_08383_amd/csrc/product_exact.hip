@@ -50,9 +50,10 @@ struct ExactOperand {
     }
 };
 
-// D[row][col] = sum_r a(row, r) w(col, r) + bias[col], written where row < a.rows and col < w.rows.
+// D[row][col] = sum_r a(row, r) w(col, r) + bias[col], written where row < a.rows and col < w.rows; sums[row] = sum_r a(row, r) where wanted
+// (a across).
 template <bool A_ACROSS, bool W_ACROSS>
-__device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperand<W_ACROSS> w, const float* bias, float* out, int64_t ldo)
+__device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperand<W_ACROSS> w, const float* bias, float* out, int64_t ldo, float* sums = nullptr)
 {
     typedef ExactOperand<A_ACROSS> OA;
     typedef ExactOperand<W_ACROSS> OW;
@@ -61,6 +62,7 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     const int row0 = wave / 2 * 32, col0 = wave % 2 * 32, in16 = lane & 15, quad = lane >> 4;
     f32x4_t acc[2][2][2];
+    float sum = 0.0f;  // of row `lane`, a quarter of each stage
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -77,6 +79,9 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
             a.load(r0 + kExactDepth);
             w.load(r0 + kExactDepth);
         }
+        if (A_ACROSS && sums != nullptr)
+#pragma unroll
+            for (int r = 0; r < kExactDepth / 4; ++r) sum += la[(wave * (kExactDepth / 4) + r) * OA::STRIDE + lane];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             f32x4_t fa[2], fw[2];
@@ -93,6 +98,11 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
                     for (int j = 0; j < 2; ++j) acc[s][i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[j][q], fa[i][q], acc[s][i][j], 0, 0, 0);
         }
         __syncthreads();
+    }
+    if (A_ACROSS && sums != nullptr) {
+        lds[threadIdx.x] = sum;
+        __syncthreads();
+        if (wave == 0 && lane < a.rows) sums[lane] = (lds[lane] + lds[kWave + lane]) + (lds[2 * kWave + lane] + lds[3 * kWave + lane]);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -126,6 +136,7 @@ __global__ __launch_bounds__(256) void exact_rows_kernel(const RowsProduct p, in
     exact_tile(a, w, p.bias != nullptr ? static_cast<const float*>(p.bias) + e * N + col : nullptr, static_cast<float*>(p.out) + row * N + col, N);
 }
 
+// Parts of the reduction (blockIdx.y) go to [part][E_local][N,K] and sums to [part][E_local][N].
 __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient p, int row_tiles, int col_tiles)
 {
     const unsigned per_expert = static_cast<unsigned>(row_tiles) * static_cast<unsigned>(col_tiles);
@@ -133,36 +144,38 @@ __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient 
     const unsigned t = blockIdx.x % per_expert;
     const int row = static_cast<int>(t / static_cast<unsigned>(col_tiles)) * kExactTile, col = static_cast<int>(t % static_cast<unsigned>(col_tiles)) * kExactTile;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
-    const int lo = wave_read_lane(range.lo, e), n = wave_read_lane(range.hi, e) - lo;
-    const int64_t N = p.N, K = p.K;
-    const ExactOperand<true> a{static_cast<const float*>(p.dy) + lo * N + row, N, min(kExactTile, p.N - row), n, {}};
-    const ExactOperand<true> w{static_cast<const float*>(p.x) + lo * K + col, K, min(kExactTile, p.K - col), n, {}};
-    exact_tile(a, w, nullptr, static_cast<float*>(p.dw) + (e * N + row) * K + col, K);
+    const int lo = wave_read_lane(range.lo, e), all = wave_read_lane(range.hi, e) - lo;
+    const int stages = (all + kExactDepth - 1) / kExactDepth;
+    const int first = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / gridDim.y) * kExactDepth;
+    const int n = max(min(all, static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / gridDim.y) * kExactDepth) - first, 0);
+    const int64_t N = p.N, K = p.K, begin = lo + first, at = static_cast<int64_t>(blockIdx.y) * p.E_local + e;
+    const ExactOperand<true> a{static_cast<const float*>(p.dy) + begin * N + row, N, min(kExactTile, p.N - row), n, {}};
+    const ExactOperand<true> w{static_cast<const float*>(p.x) + begin * K + col, K, min(kExactTile, p.K - col), n, {}};
+    exact_tile(a, w, nullptr, static_cast<float*>(p.dw) + (at * N + row) * K + col, K, p.db != nullptr && col == 0 ? static_cast<float*>(p.db) + at * N + row : nullptr);
 }
 
-// db: a workgroup an expert and 64 columns; four rows of threads a column each, joined in order.
-template <typename T, typename TO>
-__global__ __launch_bounds__(256) void bias_gradient_kernel(const WeightGradient p, int col_tiles)
+template <typename TO>
+__global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ parts, int64_t quads, TO* __restrict__ out, const float* __restrict__ more,
+                                                         int64_t more_quads, TO* __restrict__ more_out, int splits)
 {
-    __shared__ float part[4][kWave];
-    const int e = static_cast<int>(blockIdx.x / static_cast<unsigned>(col_tiles)), lane = lane_id(), wave = threadIdx.x / kWave;
-    const int col = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles)) * kWave + lane;
-    const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
-    const int lo = wave_read_lane(range.lo, e), hi = wave_read_lane(range.hi, e);
-    float sum = 0.0f;
-    if (col < p.N)
-        for (int s = lo + wave; s < hi; s += 4) {
-            const T v = static_cast<const T*>(p.dy)[static_cast<int64_t>(s) * p.N + col];
-            if constexpr (sizeof(T) == 4) sum += v;
-            else sum += bf16_to_f32(v);
-        }
-    part[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0 || col >= p.N) return;
-    sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-    TO* to = static_cast<TO*>(p.db) + static_cast<int64_t>(e) * p.N + col;
-    if constexpr (sizeof(TO) == 4) *to = sum;
-    else *to = f32_to_bf16(sum);
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < quads + more_quads; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const bool first = i < quads;
+        const int64_t at = first ? i : i - quads, each = first ? quads : more_quads;
+        const f32x4_t* from = reinterpret_cast<const f32x4_t*>(first ? parts : more) + at;
+        f32x4_t sum = from[0];
+        for (int s = 1; s < splits; ++s) sum += from[s * each];
+        TO* to = (first ? out : more_out) + at * 4;
+        if constexpr (sizeof(TO) == 4) *reinterpret_cast<f32x4_t*>(to) = sum;
+        else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3]));
+    }
+}
+int launch_join_parts(const float* parts, int64_t n, void* out, const float* more, int64_t m, void* more_out, int splits, int dt, hipStream_t stream)
+{
+    const int64_t blocks = ((n + m) / 4 + 255) / 256;
+    const dim3 grid(static_cast<unsigned>(blocks < 4 * kStreamWorkgroups ? blocks : 4 * kStreamWorkgroups));
+    if (dt == EXF_F32) hipLaunchKernelGGL(join_parts_kernel<float>, grid, dim3(256), 0, stream, parts, n / 4, static_cast<float*>(out), more, m / 4, static_cast<float*>(more_out), splits);
+    else hipLaunchKernelGGL(join_parts_kernel<bf16_t>, grid, dim3(256), 0, stream, parts, n / 4, static_cast<bf16_t*>(out), more, m / 4, static_cast<bf16_t*>(more_out), splits);
+    return EXF_OK;
 }
 
 static int64_t tiles_of(int64_t n) { return (n + kExactTile - 1) / kExactTile; }
@@ -175,24 +188,27 @@ int launch_exact_rows_product(const RowsProduct& p, bool gradient, hipStream_t s
     else hipLaunchKernelGGL(exact_rows_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
     return EXF_OK;
 }
-int launch_exact_weight_gradient(const WeightGradient& p, hipStream_t stream)
+// Parts of at least 256 rows until two workgroups a compute unit have one.
+int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local)
 {
-    const int64_t rows = tiles_of(p.N), cols = tiles_of(p.K), grid = p.E_local * rows * cols;
+    const int64_t wanted = 512 / (E_local * tiles_of(n) * tiles_of(k)), most = A / (256 * E_local);
+    const int64_t s = wanted < most ? wanted : most;
+    return static_cast<int>(s < 2 ? 1 : (s > 16 ? 16 : s));
+}
+int launch_exact_weight_gradient(const WeightGradient& g, hipStream_t stream)
+{
+    const int64_t rows = tiles_of(g.N), cols = tiles_of(g.K), grid = g.E_local * rows * cols, each = static_cast<int64_t>(g.E_local) * g.N * g.K;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
-    hipLaunchKernelGGL(exact_weight_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(rows), static_cast<int>(cols));
-    return EXF_OK;
-}
-template <typename T, typename TO>
-static int launch_bias_as(const WeightGradient& p, hipStream_t stream)
-{
-    const int64_t cols = tiles_of(p.N);
-    hipLaunchKernelGGL((bias_gradient_kernel<T, TO>), dim3(static_cast<unsigned>(p.E_local * cols)), dim3(256), 0, stream, p, static_cast<int>(cols));
-    return EXF_OK;
-}
-int launch_bias_gradient(const WeightGradient& p, int dt, int grad_dt, hipStream_t stream)
-{
-    if (dt == EXF_F32) return launch_bias_as<float, float>(p, stream);
-    return grad_dt == EXF_F32 ? launch_bias_as<bf16_t, float>(p, stream) : launch_bias_as<bf16_t, bf16_t>(p, stream);
+    const int splits = exact_weight_gradient_splits(g.max_rows, g.N, g.K, g.E_local);
+    float* parts = static_cast<float*>(g.workspace);
+    WeightGradient p = g;
+    if (splits > 1) {
+        p.dw = parts;
+        if (p.db != nullptr) p.db = parts + splits * each;
+    }
+    hipLaunchKernelGGL(exact_weight_kernel, dim3(static_cast<unsigned>(grid), static_cast<unsigned>(splits)), dim3(256), 0, stream, p, static_cast<int>(rows), static_cast<int>(cols));
+    if (splits == 1) return EXF_OK;
+    return launch_join_parts(parts, each, g.dw, parts + splits * each, g.db != nullptr ? static_cast<int64_t>(g.E_local) * g.N : 0, g.db, splits, EXF_F32, stream);
 }
 
 }  // namespace exf

@@ -28,11 +28,15 @@ enum ProductKind {
 constexpr int kProductWaves = 4;
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
 
-// One wavefront-wide direct-to-LDS load of 16 or 4 bytes a lane from buffer `rsrc` (a base and how far it reaches).
+// One wavefront-wide direct-to-LDS load of 16 bytes a lane from buffer `rsrc` (a base and how far it reaches); STREAM: past the caches.
+template <bool STREAM>
 __device__ __forceinline__ void lds_buffer_16B(u32x4_v rsrc, uint32_t voff, uint32_t lds_addr)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds\n" : : "v"(voff), "s"(rsrc), "s"(lds_addr) : "memory");
+    if constexpr (STREAM)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen nt lds\n" : : "v"(voff), "s"(rsrc), "s"(lds_addr) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds\n" : : "v"(voff), "s"(rsrc), "s"(lds_addr) : "memory");
 #else
     (void)rsrc; (void)voff; (void)lds_addr;
 #endif
@@ -55,7 +59,7 @@ __device__ __forceinline__ T lds_fetch(uint32_t addr)
 //   across: reduction element r at base + r * ld, the rows side by side.  One load covers 1024 bytes of [reduction][ROWS]; the
 //           32-byte granules (16 rows) of a reduction element are exchanged so that the eight of them that 32 lanes read
 //           together lie in different banks.
-template <int ROWS, bool ACROSS>
+template <int ROWS, bool ACROSS, bool STREAM = false>
 struct StagedOperand {
     static constexpr int GROUPS = ROWS / 8, LOADS = (GROUPS + kProductWaves - 1) / kProductWaves;  // 1 KiB each; of a wavefront
     static constexpr int UNITS = ACROSS ? 64 : 8;  // of the reduction in a stage: elements, 16-byte pieces
@@ -117,7 +121,7 @@ struct StagedOperand {
         const u32x4_v rsrc = {static_cast<uint32_t>(base), static_cast<uint32_t>(base >> 32), kBufferReach, 0x00020000u};
         // (the sign of what is left behind this lane's unit)
         const int spare = left - 1 - place - (ACROSS ? (group(i, wave) - wave) * (512 / ROWS) : 0);
-        lds_buffer_16B(rsrc, off[i] | (static_cast<uint32_t>(spare) & kBufferReach), lds_addr + group(i, wave) * 1024);
+        lds_buffer_16B<STREAM>(rsrc, off[i] | (static_cast<uint32_t>(spare) & kBufferReach), lds_addr + group(i, wave) * 1024);
     }
 
     // ---- operand fetches: 16 rows from row0 + 16 b on, reduction elements 32 ks + 8 (lane/16) .. +7
@@ -219,7 +223,8 @@ struct NoScales {
     static constexpr int LOADS = 0, BYTES = 0;
 };
 
-template <int H, int NT, ProductKind KIND, int STAGES = 8>
+// ONCE: the weights are loaded with the streaming hint (see rows_tile).
+template <int H, int NT, ProductKind KIND, bool ONCE = false, int STAGES = 8>
 struct ProductTile {
     static constexpr bool MX = KIND == kMx4;
     static constexpr int WAVES = kProductWaves;
@@ -229,7 +234,7 @@ struct ProductTile {
     static constexpr int WTM = H / WM, WTN = NT / WN, TM = WTM / 16, TN = WTN / 16;  // outputs of a wavefront
     static constexpr int SLOTS = TM * TN, HALF = SLOTS / 2;  // matrix instructions of a K step (two a stage); of the last one in front of the hand-over
     typedef StagedOperand<H, KIND == kWeightGradient> OpA;
-    typedef StagedOperand<NT, KIND == kRowsGradient || KIND == kWeightGradient> OpW;
+    typedef StagedOperand<NT, KIND == kRowsGradient || KIND == kWeightGradient, ONCE> OpW;
     typedef typename std::conditional<MX, StagedScales<H>, NoScales>::type ScA;
     typedef typename std::conditional<MX, StagedScales<NT>, NoScales>::type ScW;
     static constexpr int A_BYTES = OpA::BYTES + ScA::BYTES, W_BYTES = OpW::BYTES + ScW::BYTES;
@@ -243,6 +248,8 @@ struct ProductTile {
     f32x4_t acc[TM][TN];
     bf16x8_t fw[2][TN], fa[TM];
     int sw[2][TN], sa[TM];  // scales (4 bits)
+    f32x4_t sum[TM];        // of the rows over the reduction (SUMS: multiplied by ones)
+    bf16x8_t ones;
     OpA a;
     OpW w;
     ScA as;
@@ -316,7 +323,7 @@ struct ProductTile {
     // fetched into the register its last instruction has just read.  At the hand-over (everyone's share of the next stage
     // has landed, everyone is done reading this one) in the middle of the last K step this stage is free: its refill, weights
     // first, is spread up to the middle of the next stage's first K step.
-    template <bool NEXT>
+    template <bool NEXT, bool SUMS>
     __device__ __forceinline__ void stage(const Stages& ra, const Stages& rw)
     {
 #pragma unroll
@@ -334,6 +341,7 @@ struct ProductTile {
                     step_w();
                 }
                 multiply(b, r, ks);
+                if (SUMS && r == TN - 1) mfma_16x16x32<false>(ones, fa[b], sum[b]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (!last) {
                     if (r == TN - 1) fetch_a(ra.cur, b, 1);
@@ -374,10 +382,15 @@ struct ProductTile {
         for (int b = 0; b < TM; ++b)
 #pragma unroll
             for (int r = 0; r < TN; ++r) acc[b][r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int b = 0; b < TM; ++b) sum[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        ones = __builtin_bit_cast(bf16x8_t, u32x4_v{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+        asm volatile("" : "+v"(ones));  // (in its registers from here on: a matrix instruction must not follow its operand's write at once)
         pin_accumulators();
     }
 
     // All of a reduction of nk stages, at least one.  Behind it the accumulators hold the sums.
+    template <bool SUMS = false>
     __device__ __forceinline__ void reduce(int nk)
     {
         const int wm = wave / WN, wn = wave % WN;
@@ -413,11 +426,11 @@ struct ProductTile {
         Stages ra{0u, static_cast<uint32_t>(A_BYTES), static_cast<uint32_t>((SA - 1) * A_BYTES)};
         Stages rw{0u, static_cast<uint32_t>(W_BYTES), static_cast<uint32_t>((SB - 1) * W_BYTES)};
         for (int kt = 1; kt < nk; ++kt) {
-            stage<true>(ra, rw);
+            stage<true, SUMS>(ra, rw);
             ra.advance(A_BYTES, SA * A_BYTES);
             rw.advance(W_BYTES, SB * W_BYTES);
         }
-        stage<false>(ra, rw);
+        stage<false, SUMS>(ra, rw);
         wait_vmcnt<0>();  // (loads into LDS that nobody waited for)
         pin_accumulators();
     }
@@ -435,50 +448,94 @@ struct ProductTile {
                 if (b * TN + r < ACC_HALF) asm volatile("" : "+a"(acc[b][r]));
                 else asm volatile("" : "+v"(acc[b][r]));
             }
+#pragma unroll
+        for (int b = 0; b < TM; ++b) asm volatile("" : "+v"(sum[b]));
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #endif
     }
 
+    // 16-byte pieces of row in16 (of 16) and of unit 0 / unit 1, 64 bytes of a row each: lanes 8 to 15 trade with lanes 0 to 7, and `lo` is rows 0 to 7, `hi`
+    // rows 8 to 15, of unit in16 / 8.  A store then covers 128 bytes of a row, a whole line.
+    static __device__ __forceinline__ void trade(const uint32_t (&u0)[4], const uint32_t (&u1)[4], uint4& lo, uint4& hi)
+    {
+        uint32_t l[4], h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            l[i] = __builtin_amdgcn_update_dpp(u0[i], u1[i], 0x128, 0xf, 0xc, false);  // row_ror:8 into the upper half
+            h[i] = __builtin_amdgcn_update_dpp(u1[i], u0[i], 0x128, 0xf, 0x3, false);  // into the lower half
+        }
+        lo = make_uint4(l[0], l[1], l[2], l[3]);
+        hi = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+
     // out[row][col] (+ bias[col]) of the tile's rows and columns that there are, leading dimension ldo.  A lane holds, of the 16 x 16 block
-    // (b, r), row lane%16 and columns 4 (lane/16) .. +3.  bf16: of two blocks side by side the odd rows of 16 lanes of the
-    // first trade with the even ones of the second, and every lane has eight consecutive columns of one block.
+    // (b, r), row lane%16 and columns 4 (lane/16) .. +3: in fp32 16 bytes, 64 of the row with the other lanes.  bf16: of two
+    // blocks side by side the odd rows of 16 lanes of the first trade with the even ones of the second, and every lane has
+    // eight consecutive columns of one block.
     template <typename TO>
     __device__ __forceinline__ void store(TO* out, int64_t ldo, int rows, int cols, const bf16_t* bias) const
     {
+        constexpr int BLOCKS = sizeof(TO) == 4 ? 1 : 2;                // of a unit
+        constexpr bool PAIRS = TN % (2 * BLOCKS) == 0;
+        constexpr int PER = PAIRS ? 2 : 1;                              // units of a store
         const int quad = lane_id() >> 4, in16 = lane_id() & 15, wm = wave / WN, wn = wave % WN;
+        const int in_unit = BLOCKS == 1 ? quad * 4 : (quad & 1) * 16 + (quad >> 1) * 8;
 #pragma unroll
-        for (int r = 0; r < TN; r += 2) {
-            float bias_v[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-            if (bias != nullptr) {
+        for (int r = 0; r < TN; r += BLOCKS * PER) {
+            float bias_v[BLOCKS * PER][4];
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+            for (int q = 0; q < BLOCKS * PER; ++q)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) bias_v[q][v] = bf16_to_f32(bias[min(wn * WTN + (r + q) * 16 + quad * 4 + v, cols - 1)]);
-            }
+                for (int v = 0; v < 4; ++v)
+                    bias_v[q][v] = bias != nullptr ? bf16_to_f32(bias[min(wn * WTN + (r + q) * 16 + quad * 4 + v, cols - 1)]) : 0.0f;
 #pragma unroll
             for (int b = 0; b < TM; ++b) {
-                const int row = wm * WTM + b * 16 + in16;
-                if constexpr (sizeof(TO) == 4) {
+                uint32_t u[PER][4];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int col = wn * WTN + (r + q) * 16 + quad * 4;
-                        const f32x4_t v = acc[b][r + q];
-                        if (row < rows && col < cols)
-                            store_stream16(reinterpret_cast<uint4*>(out + row * ldo + col),
-                                           make_uint4(__float_as_uint(v[0] + bias_v[q][0]), __float_as_uint(v[1] + bias_v[q][1]), __float_as_uint(v[2] + bias_v[q][2]),
-                                                      __float_as_uint(v[3] + bias_v[q][3])));
+                for (int i = 0; i < PER; ++i) {
+                    if constexpr (BLOCKS == 1) {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) u[i][v] = __float_as_uint(acc[b][r + i][v] + bias_v[i][v]);
+                    } else {
+                        uint32_t p[2][2];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+#pragma unroll
+                            for (int v = 0; v < 2; ++v) {
+                                const int block = 2 * i + q;
+                                p[q][v] = pack_bf16x2(acc[b][r + block][2 * v] + bias_v[block][2 * v], acc[b][r + block][2 * v + 1] + bias_v[block][2 * v + 1]);
+                            }
+                        const auto s0 = __builtin_amdgcn_permlane16_swap(p[0][0], p[1][0], false, false);
+                        const auto s1 = __builtin_amdgcn_permlane16_swap(p[0][1], p[1][1], false, false);
+                        u[i][0] = s0[0], u[i][1] = s1[0], u[i][2] = s0[1], u[i][3] = s1[1];
                     }
-                } else {
-                    uint32_t p[2][2];
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-#pragma unroll
-                        for (int v = 0; v < 2; ++v) p[q][v] = pack_bf16x2(acc[b][r + q][2 * v] + bias_v[q][2 * v], acc[b][r + q][2 * v + 1] + bias_v[q][2 * v + 1]);
-                    const auto s0 = __builtin_amdgcn_permlane16_swap(p[0][0], p[1][0], false, false);
-                    const auto s1 = __builtin_amdgcn_permlane16_swap(p[0][1], p[1][1], false, false);
-                    const int col = wn * WTN + r * 16 + (quad & 1) * 16 + (quad >> 1) * 8;
-                    if (row < rows && col < cols) store_stream16(reinterpret_cast<uint4*>(out + row * ldo + col), make_uint4(s0[0], s1[0], s0[1], s1[1]));
                 }
+                const int row = wm * WTM + b * 16, col = wn * WTN + r * 16 + in_unit;
+                if constexpr (PAIRS) {
+                    uint4 lo, hi;
+                    trade(u[0], u[PER - 1], lo, hi);
+                    const int row_lo = row + (in16 & 7), col_of = col + (in16 >> 3) * BLOCKS * 16;
+                    TO* to = out + row_lo * ldo + col_of;
+                    if (row_lo < rows && col_of < cols) store_stream16(reinterpret_cast<uint4*>(to), lo);
+                    if (row_lo + 8 < rows && col_of < cols) store_stream16(reinterpret_cast<uint4*>(to + 8 * ldo), hi);
+                } else if (row + in16 < rows && col < cols) {
+                    store_stream16(reinterpret_cast<uint4*>(out + (row + in16) * ldo + col), make_uint4(u[0][0], u[0][1], u[0][2], u[0][3]));
+                }
+            }
+        }
+    }
+    // The sums over the reduction of the tile's rows (SUMS).
+    template <typename TO>
+    __device__ __forceinline__ void store_sums(TO* out, int rows) const
+    {
+        const int wm = wave / WN;
+        if (wave % WN != 0 || lane_id() >= 16) return;
+#pragma unroll
+        for (int b = 0; b < TM; ++b) {
+            const int row = wm * WTM + b * 16 + lane_id();
+            if (row < rows) {
+                if constexpr (sizeof(TO) == 4) out[row] = sum[b][0];
+                else out[row] = f32_to_bf16(sum[b][0]);
             }
         }
     }
@@ -502,10 +559,10 @@ struct RowsTiles {
     int max_rows, K, N, E_local;
 };
 
-template <int H, int NT, ProductKind KIND>
+template <int H, int NT, ProductKind KIND, bool ONCE>
 __device__ __forceinline__ void rows_tile(const RowsTiles& p, const Tile2D& tile, unsigned char* smem)
 {
-    typedef ProductTile<H, NT, KIND> T;
+    typedef ProductTile<H, NT, KIND, ONCE> T;
     T t;
     begin_tile(t, smem);
     const int64_t row_bytes = KIND == kMx4 ? p.K / 2 : static_cast<int64_t>(p.K) * 2, K = p.K, N = p.N;
@@ -526,31 +583,42 @@ __device__ __forceinline__ void rows_tile(const RowsTiles& p, const Tile2D& tile
     t.store(p.out + tile.row_begin * N + tile.n0, N, rows, cols, p.bias != nullptr ? p.bias + tile.expert * N + tile.n0 : nullptr);
 }
 
-template <int NT, ProductKind KIND>
+// STREAMS: tiles whose weights nobody else reads load them with the streaming hint, and the column tiles of experts of few rows begin the reduction
+// at different places (see locate_tile and streams_weights).
+template <int NT, ProductKind KIND, bool STREAMS>
 __global__ __launch_bounds__(kProductWaves * kWave, 1) void rows_tiles_kernel(const RowsTiles p)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const RowRange range = row_range(p.offsets, p.E_local, p.max_rows);
     Tile2D tile;
-    if (!locate_tile<false>(range, NT, p.N, static_cast<int>(blockIdx.x), RowMap{}, tile)) return;
-#define EXF_CASE(H, CUT)            \
+    if (!locate_tile<STREAMS>(range, NT, p.N, static_cast<int>(blockIdx.x), RowMap{}, tile)) return;
+#define EXF_CASE(H, CUT, ONCE)            \
     case (CUT) * 16 + (H) / kQuantum: \
-        if constexpr (has_instance(NT, H, CUT)) rows_tile<H, (NT >> CUT), KIND>(p, tile, smem); \
+        if constexpr (has_instance(NT, H, CUT) && (!(ONCE) || H <= kTileRows)) rows_tile<H, (NT >> CUT), KIND, ONCE>(p, tile, smem); \
         break
-#define EXF_CASES(CUT)  \
-    EXF_CASE(64, CUT);  \
-    EXF_CASE(96, CUT);  \
-    EXF_CASE(128, CUT); \
-    EXF_CASE(160, CUT); \
-    EXF_CASE(192, CUT); \
-    EXF_CASE(224, CUT); \
-    EXF_CASE(256, CUT); \
-    EXF_CASE(288, CUT); \
-    EXF_CASE(320, CUT)
-    switch (tile.cut * 16 + tile.height / kQuantum) {
-        EXF_CASES(0);
-        EXF_CASES(1);
-        EXF_CASES(2);
+#define EXF_CASES(CUT, ONCE)  \
+    EXF_CASE(64, CUT, ONCE);  \
+    EXF_CASE(96, CUT, ONCE);  \
+    EXF_CASE(128, CUT, ONCE); \
+    EXF_CASE(160, CUT, ONCE); \
+    EXF_CASE(192, CUT, ONCE); \
+    EXF_CASE(224, CUT, ONCE); \
+    EXF_CASE(256, CUT, ONCE); \
+    EXF_CASE(288, CUT, ONCE); \
+    EXF_CASE(320, CUT, ONCE)
+    const int instance = tile.cut * 16 + tile.height / kQuantum;
+    if (STREAMS && tile.once) {
+        switch (instance) {
+            EXF_CASES(0, STREAMS);
+            EXF_CASES(1, STREAMS);
+            EXF_CASES(2, STREAMS);
+        }
+    } else {
+        switch (instance) {
+            EXF_CASES(0, false);
+            EXF_CASES(1, false);
+            EXF_CASES(2, false);
+        }
     }
 #undef EXF_CASES
 #undef EXF_CASE
@@ -568,17 +636,29 @@ constexpr int rows_tiles_lds()
     return most;
 }
 
-template <int NT, ProductKind KIND>
-static int launch_rows_tiles(const RowsTiles& p, hipStream_t stream, const char* fn)
+template <int NT, ProductKind KIND, bool STREAMS>
+static int launch_rows_tiles_as(const RowsTiles& p, hipStream_t stream, const char* fn)
 {
     constexpr size_t lds = rows_tiles_lds<NT, KIND>();
     const int64_t grid = tile_grid(p.max_rows, p.N, NT, p.E_local);
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "%s: too many tiles", fn);
-    auto kern = rows_tiles_kernel<NT, KIND>;
+    auto kern = rows_tiles_kernel<NT, KIND, STREAMS>;
     static std::atomic<uint64_t> allowed{0};
     if (int rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, fn)) return rc;
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(kProductWaves * kWave), lds, stream, p);
     return EXF_OK;
+}
+
+// Weights too many to stay in the memory-side cache of 256 MB from call to call, and so few rows that many experts have one row tile.
+inline bool streams_weights(const RowsTiles& p, ProductKind kind)
+{
+    const int64_t bytes = static_cast<int64_t>(p.E_local) * p.K * p.N * (kind == kMx4 ? 1 : 4) / 2;
+    return p.max_rows <= 1024ll * p.E_local && bytes >= 128ll << 20;
+}
+template <int NT, ProductKind KIND>
+static int launch_rows_tiles(const RowsTiles& p, hipStream_t stream, const char* fn)
+{
+    return streams_weights(p, KIND) ? launch_rows_tiles_as<NT, KIND, true>(p, stream, fn) : launch_rows_tiles_as<NT, KIND, false>(p, stream, fn);
 }
 
 int launch_forward_tiles(const RowsTiles& p, hipStream_t stream);

@@ -14,6 +14,7 @@ struct WeightTiles {
     const bf16_t *dy, *x;
     const int32_t* offsets;
     void* out;          // [splits][E_local][N,K]
+    void* sums;         // [splits][E_local][N] or null: of dy over the rows (tiles of the first columns multiply by ones as well)
     int max_rows, N, K, E_local, splits;
 };
 
@@ -48,28 +49,19 @@ __global__ __launch_bounds__(kProductWaves * kWave, STAGES == 2 ? 2 : 1) void we
     const int first = static_cast<int>(static_cast<int64_t>(stages) * split / p.splits), last = static_cast<int>(static_cast<int64_t>(stages) * (split + 1) / p.splits);
     const int rows = min(n, last * 64) - first * 64;
     const int64_t begin = lo + first * 64, N = p.N, K = p.K;
-    ProductTile<H, NT, kWeightGradient, STAGES> t;
+    ProductTile<H, NT, kWeightGradient, false, STAGES> t;
     begin_tile(t, smem);
+    const bool sums = p.sums != nullptr && col0 == 0;
     if (rows > 0) {
         t.a.begin(p.dy + begin * N + row0, N * 2, min(H, p.N - row0), rows, 0, t.wave);
         t.w.begin(p.x + begin * K + col0, K * 2, min(NT, p.K - col0), rows, 0, t.wave);
-        t.reduce(last - first);
+        if (sums) t.template reduce<true>(last - first);
+        else t.reduce(last - first);
     } else {
         t.clear();
     }
+    if (sums) t.store_sums(static_cast<TO*>(p.sums) + (static_cast<int64_t>(split) * p.E_local + e) * N + row0, min(H, p.N - row0));
     t.store(static_cast<TO*>(p.out) + ((static_cast<int64_t>(split) * p.E_local + e) * N + row0) * K + col0, K, min(H, p.N - row0), min(NT, p.K - col0), nullptr);
-}
-
-// Sums of the parts, in order.
-template <typename TO>
-__global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ parts, int64_t quads, int splits, TO* __restrict__ out)
-{
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < quads; i += static_cast<int64_t>(gridDim.x) * 256) {
-        f32x4_t sum = reinterpret_cast<const f32x4_t*>(parts)[i];
-        for (int s = 1; s < splits; ++s) sum += reinterpret_cast<const f32x4_t*>(parts)[s * quads + i];
-        if constexpr (sizeof(TO) == 4) reinterpret_cast<f32x4_t*>(out)[i] = sum;
-        else reinterpret_cast<uint2*>(out)[i] = make_uint2(pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3]));
-    }
 }
 
 static int64_t tiles_in(int64_t n, int64_t k, int64_t size) { return ((n + size - 1) / size) * ((k + size - 1) / size); }
@@ -109,14 +101,15 @@ template <typename TO>
 static int launch_weight_tiles(const WeightGradient& g, hipStream_t stream)
 {
     const int splits = weight_gradient_splits(g.max_rows, g.N, g.K, g.E_local);
-    WeightTiles p{static_cast<const bf16_t*>(g.dy), static_cast<const bf16_t*>(g.x), g.offsets, splits > 1 ? g.workspace : g.dw, g.max_rows, g.N, g.K, g.E_local, splits};
+    float* parts = static_cast<float*>(g.workspace);
+    const int64_t each = static_cast<int64_t>(g.E_local) * g.N * g.K, sums = static_cast<int64_t>(g.E_local) * g.N;
+    WeightTiles p{static_cast<const bf16_t*>(g.dy), static_cast<const bf16_t*>(g.x), g.offsets, g.dw, g.db, g.max_rows, g.N, g.K, g.E_local, splits};
     if (large_tiles(g.max_rows, g.N, g.K, g.E_local)) return launch_weight_as<256, 256, 8, TO>(p, stream);
     if (splits == 1) return launch_weight_as<128, 128, 2, TO>(p, stream);
+    p.out = parts;
+    if (p.sums != nullptr) p.sums = parts + splits * each;
     if (int rc = launch_weight_as<128, 128, 2, float>(p, stream)) return rc;
-    const int64_t quads = static_cast<int64_t>(g.E_local) * g.N * g.K / 4, blocks = (quads + 255) / 256;
-    hipLaunchKernelGGL(join_parts_kernel<TO>, dim3(static_cast<unsigned>(blocks < 4 * kStreamWorkgroups ? blocks : 4 * kStreamWorkgroups)), dim3(256), 0, stream,
-                       static_cast<const float*>(g.workspace), quads, splits, static_cast<TO*>(g.dw));
-    return EXF_OK;
+    return launch_join_parts(parts, each, g.dw, parts + splits * each, g.db != nullptr ? sums : 0, g.db, splits, sizeof(TO) == 4 ? EXF_F32 : EXF_BF16, stream);
 }
 
 int launch_weight_gradient_tiles(const WeightGradient& p, int grad_dt, hipStream_t stream)
