@@ -244,6 +244,7 @@ int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorted, const in
  * Shapes: rows >= 0, k >= 32 and k % 32 == 0.  q and scale must be 16-byte aligned.
  * ------------------------------------------------------------------------------------- */
 #define EXF_MX4_BLOCK 32
+#define EXF_MX4_INLINE_ROWS 8  /* up to so many rows moe_grouped_product_mx4 quantises as it goes, without a workspace */
 size_t mx4_scale_bytes(int64_t rows, int k);
 int mx4_quantize(const void* x, int64_t rows, int k, int dt, uint8_t* q, uint8_t* scale, void* stream);
 int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t rows, int k, int dt, void* out, void* stream);
@@ -255,7 +256,8 @@ int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t rows, int k, 
  *   x_scale == NULL: x_sorted [A,k] dt; the call quantises it into the workspace.
  *   bias [E_local,n] dt or NULL;  y_sorted [A,n] dt.  Sums in fp32, rounded once.
  * Shapes: 0 <= A < 2^31; k >= 32, k % 32 == 0; n >= 1, a multiple of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
- * workspace: moe_grouped_product_mx4_workspace_bytes(A, k) bytes with x_scale == NULL, otherwise none (NULL).
+ * workspace: moe_grouped_product_mx4_workspace_bytes(A, k) bytes with x_scale == NULL, 0 for A <= EXF_MX4_INLINE_ROWS; otherwise none
+ * (NULL).
  * ------------------------------------------------------------------------------------- */
 size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k);
 int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_scale, const int32_t* expert_offsets, const uint8_t* w,

@@ -27,6 +27,7 @@ EXF_BF16 = 1
 EXF_ACT_GELU_ERF = 0
 EXF_ACT_GELU_TANH = 1
 EXF_MX4_BLOCK = 32
+EXF_MX4_INLINE_ROWS = 8
 
 _vp, _i, _i64, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
 
@@ -264,40 +265,45 @@ def moe_combine(y_sorted, sorted_of_src, topk_w, out=None):
     return out
 
 
+_CODES = {torch.float32: EXF_F32, torch.bfloat16: EXF_BF16}
+
+
 def _bad(message: str):
     raise ExflowError(EXF_ERR_BAD_SHAPE, message)
 
 
-def _expect(name, t, shape, dtype, like):
-    """`t` is a dense tensor of this shape and type on the device of `like`."""
-    if tuple(t.shape) != tuple(shape):
+def _expect(name, t, shape, dtype, dev):
+    """`t` is a dense tensor of this shape and type on device number `dev` (-1: the host)."""
+    if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
+        return t
+    if t.shape != shape:
         _bad(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"{name} is {t.dtype}, expected {dtype}")
-    if not t.is_contiguous() or t.device != like.device:
-        _bad(f"{name} must be contiguous and on {like.device}")
-    return t
+    _bad(f"{name} must be contiguous and on device {dev}")
 
 
-def _grouped(rows, width, expert_offsets, w_shape):
-    """(A, n, k, E_local) of a product whose sorted rows are `width` (0: k, 1: n) wide."""
-    if rows.dim() != 2 or len(w_shape) != 3:
+def _grouped(rows, w_shape):
+    """(E_local, n, k, A, type, its code, device number) of a product of `rows` [A,*] with weights of this shape."""
+    if len(w_shape) != 3 or len(rows.shape) != 2:
         _bad(f"rows are [A,*] and weights [E_local,n,k], got {tuple(rows.shape)} and {tuple(w_shape)}")
-    E, n, k = w_shape
-    _expect("the sorted rows", rows, (rows.shape[0], n if width else k), rows.dtype, rows)
-    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, rows)
-    return rows.shape[0], n, k, E
+    dt = rows.dtype
+    code = _CODES.get(dt)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
+    return (*w_shape, rows.shape[0], dt, code, rows.get_device())
 
 
 def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
     """y[s] = x_sorted[s] W_e^T (+ bias[e]) for the rows of every expert; w [E_local,n,k]."""
-    A, n, k, E = _grouped(x_sorted, 0, expert_offsets, w.shape)
-    _expect("w", w, (E, n, k), x_sorted.dtype, x_sorted)
+    E, n, k, A, dt, code, dev = _grouped(x_sorted, w.shape)
+    _expect("x_sorted", x_sorted, (A, k), dt, dev)
+    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, dev)
+    _expect("w", w, (E, n, k), dt, dev)
     if bias is not None:
-        _expect("bias", bias, (E, n), x_sorted.dtype, x_sorted)
-    out = torch.empty((A, n), dtype=x_sorted.dtype, device=x_sorted.device) if out is None else _expect("out", out, (A, n), x_sorted.dtype, x_sorted)
-    rc = lib().moe_grouped_product(x_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), _ptr(bias), A, n, k, E, dtype_code(x_sorted),
-                                   out.data_ptr(), _stream())
+        bias = _expect("bias", bias, (E, n), dt, dev).data_ptr()
+    out = torch.empty((A, n), dtype=dt, device=x_sorted.device) if out is None else _expect("out", out, (A, n), dt, dev)
+    rc = lib().moe_grouped_product(x_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), bias, A, n, k, E, code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
     return out
@@ -305,11 +311,12 @@ def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
 
 def moe_grouped_product_dx(dy_sorted, expert_offsets, w, out=None):
     """Gradient of moe_grouped_product's rows: dx[s] = dy_sorted[s] W_e; w [E_local,n,k]."""
-    A, n, k, E = _grouped(dy_sorted, 1, expert_offsets, w.shape)
-    _expect("w", w, (E, n, k), dy_sorted.dtype, dy_sorted)
-    out = torch.empty((A, k), dtype=dy_sorted.dtype, device=dy_sorted.device) if out is None else _expect("out", out, (A, k), dy_sorted.dtype, dy_sorted)
-    rc = lib().moe_grouped_product_dx(dy_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), A, n, k, E, dtype_code(dy_sorted),
-                                      out.data_ptr(), _stream())
+    E, n, k, A, dt, code, dev = _grouped(dy_sorted, w.shape)
+    _expect("dy_sorted", dy_sorted, (A, n), dt, dev)
+    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, dev)
+    _expect("w", w, (E, n, k), dt, dev)
+    out = torch.empty((A, k), dtype=dt, device=dy_sorted.device) if out is None else _expect("out", out, (A, k), dt, dev)
+    rc = lib().moe_grouped_product_dx(dy_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), A, n, k, E, code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
     return out
@@ -318,24 +325,26 @@ def moe_grouped_product_dx(dy_sorted, expert_offsets, w, out=None):
 def moe_grouped_product_dw(dy_sorted, x_sorted, expert_offsets, want_bias=False, grad_dtype=None, workspace=None, out=None, out_bias=None):
     """Gradients of moe_grouped_product's weights and bias: (dw [E_local,n,k], db [E_local,n] or None), both of `grad_dtype` (that of
     ``out``, or the rows')."""
-    if dy_sorted.dim() != 2 or x_sorted.dim() != 2 or expert_offsets.dim() != 1:
+    if len(dy_sorted.shape) != 2 or len(x_sorted.shape) != 2 or len(expert_offsets.shape) != 1:
         _bad("rows are [A,n] and [A,k], expert_offsets [E_local+1]")
-    n, k, E = dy_sorted.shape[1], x_sorted.shape[1], expert_offsets.shape[0] - 1
-    A = _grouped(x_sorted, 0, expert_offsets, (E, n, k))[0]
-    dev = x_sorted.device
-    _expect("dy_sorted", dy_sorted, (A, n), x_sorted.dtype, x_sorted)
+    E, n, k, A, dt, code, dev = _grouped(x_sorted, (expert_offsets.shape[0] - 1, dy_sorted.shape[1], x_sorted.shape[1]))
+    _expect("x_sorted", x_sorted, (A, k), dt, dev)
+    _expect("dy_sorted", dy_sorted, (A, n), dt, dev)
+    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, dev)
     if grad_dtype is None:
-        grad_dtype = x_sorted.dtype if out is None else out.dtype
-    out = torch.empty((E, n, k), dtype=grad_dtype, device=dev) if out is None else _expect("out", out, (E, n, k), grad_dtype, x_sorted)
+        grad_dtype = dt if out is None else out.dtype
+    if grad_dtype not in _CODES:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {grad_dtype}")
+    out = torch.empty((E, n, k), dtype=grad_dtype, device=x_sorted.device) if out is None else _expect("out", out, (E, n, k), grad_dtype, dev)
     if out_bias is not None:
-        _expect("out_bias", out_bias, (E, n), grad_dtype, x_sorted)
+        _expect("out_bias", out_bias, (E, n), grad_dtype, dev)
     elif want_bias:
-        out_bias = torch.empty((E, n), dtype=grad_dtype, device=dev)
-    dt = dtype_code(x_sorted)
+        out_bias = torch.empty((E, n), dtype=grad_dtype, device=x_sorted.device)
     if workspace is None:
-        workspace = _workspace(lib().moe_grouped_product_dw_workspace_bytes(A, n, k, E, dt), dev)
-    rc = lib().moe_grouped_product_dw(dy_sorted.data_ptr(), x_sorted.data_ptr(), expert_offsets.data_ptr(), A, n, k, E, dt, dtype_code(out),
-                                      out.data_ptr(), _ptr(out_bias), workspace.data_ptr(), workspace.numel(), _stream())
+        need = lib().moe_grouped_product_dw_workspace_bytes(A, n, k, E, code)
+        workspace = _workspace(need, x_sorted.device) if need else None
+    rc = lib().moe_grouped_product_dw(dy_sorted.data_ptr(), x_sorted.data_ptr(), expert_offsets.data_ptr(), A, n, k, E, code, _CODES[grad_dtype], out.data_ptr(),
+                                      _ptr(out_bias), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
     if rc:
         _check(rc)
     return out, out_bias
@@ -354,31 +363,35 @@ class Mx4:
 
     @property
     def rows(self):
-        return self.q.numel() // max(self.q.shape[-1], 1)
+        return self.scale.shape[1]
 
 
-def _mx4_scale_shape(rows, k):
-    return ((k + 255) // 256, rows, 8)
-
-
-def _expect_mx4(name, m, like):
-    if m.q.dtype != torch.uint8 or not m.q.is_contiguous() or m.q.device != like.device:
-        _bad(f"{name}.q must be contiguous uint8 on {like.device}")
-    _expect(f"{name}.scale", m.scale, _mx4_scale_shape(m.rows, m.shape[-1]), torch.uint8, like)
-    return m
+def _expect_mx4(name, m, shape, dev):
+    """`m` holds this shape on device number `dev`."""
+    k = shape[-1]
+    rows = 1
+    for length in shape[:-1]:
+        rows *= length
+    _expect(f"{name}.q", m.q, (*shape[:-1], k // 2), torch.uint8, dev)
+    _expect(f"{name}.scale", m.scale, ((k + 255) // 256, rows, 8), torch.uint8, dev)
+    return rows
 
 
 def mx4_quantize(x, out=None):
     """Rows x [..., k] (k a multiple of 32) -> Mx4."""
-    if x.dim() < 1 or not x.is_contiguous() or x.shape[-1] < EXF_MX4_BLOCK or x.shape[-1] % EXF_MX4_BLOCK:
-        _bad(f"mx4_quantize: contiguous rows of a multiple of {EXF_MX4_BLOCK} elements expected, got {tuple(x.shape)}")
-    k, rows = x.shape[-1], x.numel() // x.shape[-1]
+    shape, code = x.shape, _CODES.get(x.dtype)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {x.dtype}")
+    k = shape[-1] if len(shape) else 0
+    if k < EXF_MX4_BLOCK or k % EXF_MX4_BLOCK or not x.is_contiguous():
+        _bad(f"mx4_quantize: contiguous rows of a multiple of {EXF_MX4_BLOCK} elements expected, got {tuple(shape)}")
     if out is None:
-        out = Mx4(torch.empty((*x.shape[:-1], k // 2), dtype=torch.uint8, device=x.device),
-                  torch.empty(_mx4_scale_shape(rows, k), dtype=torch.uint8, device=x.device))
-    elif _expect_mx4("out", out, x).shape != tuple(x.shape):
-        _bad(f"out holds {out.shape}, expected {tuple(x.shape)}")
-    rc = lib().mx4_quantize(x.data_ptr(), rows, k, dtype_code(x), out.q.data_ptr(), out.scale.data_ptr(), _stream())
+        rows = x.numel() // k
+        out = Mx4(torch.empty((*shape[:-1], k // 2), dtype=torch.uint8, device=x.device),
+                  torch.empty(((k + 255) // 256, rows, 8), dtype=torch.uint8, device=x.device))
+    else:
+        rows = _expect_mx4("out", out, shape, x.get_device())
+    rc = lib().mx4_quantize(x.data_ptr(), rows, k, code, out.q.data_ptr(), out.scale.data_ptr(), _stream())
     if rc:
         _check(rc)
     return out
@@ -386,9 +399,13 @@ def mx4_quantize(x, out=None):
 
 def mx4_dequantize(m, dtype=torch.bfloat16, out=None):
     """The values an Mx4 stands for, in `dtype` (that of ``out``)."""
-    _expect_mx4("m", m, m.q)
-    out = torch.empty(m.shape, dtype=dtype, device=m.q.device) if out is None else _expect("out", out, m.shape, out.dtype, m.q)
-    rc = lib().mx4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), m.rows, m.shape[-1], dtype_code(out), out.data_ptr(), _stream())
+    shape, dev = m.shape, m.q.get_device()
+    rows = _expect_mx4("m", m, shape, dev)
+    out = torch.empty(shape, dtype=dtype, device=m.q.device) if out is None else _expect("out", out, shape, out.dtype, dev)
+    code = _CODES.get(out.dtype)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {out.dtype}")
+    rc = lib().mx4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), rows, shape[-1], code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
     return out
@@ -397,29 +414,33 @@ def mx4_dequantize(m, dtype=torch.bfloat16, out=None):
 def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, out=None, workspace=None):
     """moe_grouped_product with weights held in 4 bits: w an Mx4 [E_local,n,k]; x_sorted an Mx4 [A,k], or rows of `dtype` that the call
     quantises.  The result has the type of the rows, or `dtype` (bf16)."""
+    shape = w.shape
     held = isinstance(x_sorted, Mx4)
     rows = x_sorted.q if held else x_sorted
-    if len(w.shape) != 3 or rows.dim() != 2 or rows.shape[0] * w.shape[-1] != rows.numel() * (2 if held else 1):
-        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {tuple(w.shape)}")
-    _expect_mx4("w", w, rows)
-    A, (E, n, k) = rows.shape[0], w.shape
+    if len(shape) != 3 or len(rows.shape) != 2:
+        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {tuple(shape)}")
+    E, n, k = shape
+    A, dev = rows.shape[0], rows.get_device()
+    _expect_mx4("w", w, shape, dev)
     if held:
-        _expect_mx4("x_sorted", x_sorted, rows)
+        _expect_mx4("x_sorted", x_sorted, (A, k), dev)
+        x_scale = x_sorted.scale.data_ptr()
+        if dtype is None:
+            dtype = torch.bfloat16 if out is None else out.dtype
     else:
-        _expect("x_sorted", rows, (A, k), rows.dtype, rows)
-    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, rows)
-    if dtype is None:
-        dtype = out.dtype if out is not None else (torch.bfloat16 if held else rows.dtype)
-    if not held and dtype != rows.dtype:
-        raise ExflowError(EXF_ERR_BAD_DTYPE, f"the result of {rows.dtype} rows is {rows.dtype}, not {dtype}")
+        dtype = _expect("x_sorted", rows, (A, k), rows.dtype if dtype is None else dtype, dev).dtype
+        x_scale = None
+    code = _CODES.get(dtype)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dtype}")
+    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, dev)
     if bias is not None:
-        _expect("bias", bias, (E, n), dtype, rows)
-    out = torch.empty((A, n), dtype=dtype, device=rows.device) if out is None else _expect("out", out, (A, n), dtype, rows)
-    if workspace is None and not held:
+        bias = _expect("bias", bias, (E, n), dtype, dev).data_ptr()
+    out = torch.empty((A, n), dtype=dtype, device=rows.device) if out is None else _expect("out", out, (A, n), dtype, dev)
+    if workspace is None and not held and A > EXF_MX4_INLINE_ROWS:
         workspace = _workspace(lib().moe_grouped_product_mx4_workspace_bytes(A, k), rows.device)
-    rc = lib().moe_grouped_product_mx4(rows.data_ptr(), x_sorted.scale.data_ptr() if held else None, expert_offsets.data_ptr(), w.q.data_ptr(),
-                                       w.scale.data_ptr(), _ptr(bias), A, n, k, E, dtype_code(out), out.data_ptr(), _ptr(workspace),
-                                       0 if workspace is None else workspace.numel(), _stream())
+    rc = lib().moe_grouped_product_mx4(rows.data_ptr(), x_scale, expert_offsets.data_ptr(), w.q.data_ptr(), w.scale.data_ptr(), bias, A, n, k, E, code,
+                                       out.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
     if rc:
         _check(rc)
     return out

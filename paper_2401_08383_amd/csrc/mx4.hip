@@ -12,15 +12,6 @@ typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2_t;
 
 constexpr int kScaleTile = 256;
 
-// log2 X + 127 of a block whose largest magnitude has these bits.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t largest)
-{
-    const uint32_t exponent = largest >> 23;
-    return exponent == 255u ? 255u : max(exponent, 2u) - 2u;
-}
-// 2^(byte - 127)
-__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte == 0u ? 0x00400000u : byte << 23); }
-
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, int64_t rows, int k, int tiles, uint32_t* __restrict__ q,
                                                            uint8_t* __restrict__ scale)
@@ -35,33 +26,14 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restric
         uint32_t v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0u;
-        if (there) {
-            if constexpr (BF16) {
-                const uint4 t = load_stream16(reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(x) + row * k + col));
-                const uint32_t p[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[2 * i] = p[i] << 16, v[2 * i + 1] = p[i] & 0xffff0000u;
-            } else {
-                const uint4* at = reinterpret_cast<const uint4*>(static_cast<const float*>(x) + row * k + col);
-                const uint4 a = load_stream16(at), b = load_stream16(at + 1);
-                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-            }
-        }
+        if (there) load_bits8<BF16>(static_cast<const uint8_t*>(x) + (row * k + col) * (BF16 ? 2 : 4), v);
         uint32_t largest = 0u;
 #pragma unroll
         for (int i = 0; i < 8; ++i) largest = max(largest, v[i] & 0x7fffffffu);
         largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 1, kWave)));
         largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 2, kWave)));
         const uint32_t byte = scale_byte(largest);
-        if (there) {
-            const float s = scale_value(byte == 255u ? 127u : byte);
-            uint32_t code = 0u;
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[0]), __uint_as_float(v[1]), s, 0);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[2]), __uint_as_float(v[3]), s, 1);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[4]), __uint_as_float(v[5]), s, 2);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[6]), __uint_as_float(v[7]), s, 3);
-            q[(row * k + col) / 8] = byte == 255u ? 0u : code;
-        }
+        if (there) q[(row * k + col) / 8] = to_codes(v, byte);
         if (row < rows && (chunk & 3) == 0) scale[(tile * rows + row) * 8 + chunk / 4] = static_cast<uint8_t>(there ? byte : 0u);
     }
 }

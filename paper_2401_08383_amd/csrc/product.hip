@@ -36,6 +36,13 @@ static int check_rows_product(const char* fn, const void* rows, const int32_t* o
     return EXF_OK;
 }
 
+// Few rows an expert: a stream of weights (ffn_stream.hip), in its sizes.
+static bool streams_forward(int64_t A, int n, int k, int E_local)
+{
+    const int64_t widest = n > k ? n : k;
+    return n % 64 == 0 && k % 64 == 0 && A <= 28ll * E_local && A * widest < (1ll << 31) && static_cast<int64_t>(n) * k < (1ll << 31);
+}
+
 }  // namespace exf
 
 extern "C" int moe_grouped_product(const void* x_sorted, const int32_t* expert_offsets, const void* w, const void* bias, int64_t A, int n, int k,
@@ -46,10 +53,13 @@ extern "C" int moe_grouped_product(const void* x_sorted, const int32_t* expert_o
     if (A == 0) return EXF_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     int rc;
-    if (dt == EXF_BF16) {
-        rc = launch_forward_tiles({x_sorted, expert_offsets, w, static_cast<const bf16_t*>(bias), static_cast<bf16_t*>(y_sorted), nullptr, nullptr, static_cast<int>(A), k, n, E_local}, s);
+    if (dt == EXF_F32 || streams_forward(A, n, k, E_local)) {
+        StreamGemm g{};
+        g.act = x_sorted, g.weight = w, g.bias = bias, g.out = y_sorted, g.offsets = expert_offsets;
+        g.max_rows = static_cast<int>(A), g.K = k, g.N = n, g.E_local = E_local, g.epi = kEpiNone;
+        rc = launch_stream_gemm(g, dt, s);
     } else {
-        rc = launch_exact_rows_product({x_sorted, expert_offsets, w, bias, y_sorted, static_cast<int>(A), k, n, E_local}, false, s);
+        rc = launch_forward_tiles({x_sorted, expert_offsets, w, static_cast<const bf16_t*>(bias), static_cast<bf16_t*>(y_sorted), nullptr, nullptr, static_cast<int>(A), k, n, E_local}, s);
     }
     return rc == EXF_OK ? check_launch("moe_grouped_product") : rc;
 }
@@ -65,7 +75,7 @@ extern "C" int moe_grouped_product_dx(const void* dy_sorted, const int32_t* expe
     if (dt == EXF_BF16) {
         rc = launch_rows_gradient_tiles({dy_sorted, expert_offsets, w, nullptr, static_cast<bf16_t*>(dx_sorted), nullptr, nullptr, static_cast<int>(A), n, k, E_local}, s);
     } else {
-        rc = launch_exact_rows_product({dy_sorted, expert_offsets, w, nullptr, dx_sorted, static_cast<int>(A), n, k, E_local}, true, s);
+        rc = launch_exact_rows_gradient({dy_sorted, expert_offsets, w, dx_sorted, static_cast<int>(A), n, k, E_local}, s);
     }
     return rc == EXF_OK ? check_launch("moe_grouped_product_dx") : rc;
 }
@@ -118,7 +128,7 @@ extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorte
 
 extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k)
 {
-    if (A < 0 || k < 1) return 0;
+    if (A <= EXF_MX4_INLINE_ROWS || k < 1) return 0;
     return exf::align_up(static_cast<size_t>(A) * k / 2, 256) + exf::align_up(mx4_scale_bytes(A, k), 256);
 }
 
@@ -152,7 +162,7 @@ extern "C" int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_sc
     const struct {
         const void* at;
         size_t bytes;
-    } in[] = {{x_sorted, need > 0 ? rows * k * el : held}, {x_scale, mx4_scale_bytes(A, k)}, {expert_offsets, static_cast<size_t>(E_local + 1) * 4},
+    } in[] = {{x_sorted, x_scale == nullptr ? rows * k * el : held}, {x_scale, mx4_scale_bytes(A, k)}, {expert_offsets, static_cast<size_t>(E_local + 1) * 4},
               {w, weights * k / 2}, {w_scale, mx4_scale_bytes(static_cast<int64_t>(weights), k)}, {bias, weights * el}};
     for (const auto& i : in)
         if (overlap(y_sorted, out_bytes, i.at, i.bytes) || overlap(workspace, need, i.at, i.bytes))
@@ -167,7 +177,9 @@ extern "C" int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_sc
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     int rc;
-    if (dt == EXF_BF16) {
+    if (A <= EXF_MX4_INLINE_ROWS) {
+        rc = launch_mx4_few_rows(p, dt, s);
+    } else if (dt == EXF_BF16) {
         rc = launch_mx4_tiles({p.rows, expert_offsets, w, static_cast<const bf16_t*>(bias), static_cast<bf16_t*>(y_sorted), p.row_scale, w_scale, static_cast<int>(A), k, n, E_local}, s);
     } else {
         rc = launch_mx4_product(p, s);

@@ -5,14 +5,11 @@
 
 namespace exf {
 
-// out[rows of e, N] = rows[rows of e, K] * W_e (+ bias_e), a sorted row at a time:
-//   forward    W_e [N,K] times the row:          weight [E_local,N,K], K = k, N = n
-//   gradient   the row times W_e [K,N]:          weight [E_local,K,N], K = n, N = k
-struct RowsProduct {
+// out[rows of e, N] = rows[rows of e, K] W_e, a sorted row at a time; weight [E_local,K,N].
+struct RowsGradient {
     const void* rows;         // [A,K]
     const int32_t* offsets;   // [E_local+1]
     const void* weight;
-    const void* bias;         // [E_local,N] or null (forward)
     void* out;                // [A,N]
     int max_rows;             // A
     int K, N, E_local;
@@ -27,9 +24,9 @@ struct WeightGradient {
     void* workspace;
     int max_rows, N, K, E_local;
 };
-// As RowsProduct, forward, of rows held by mx4_quantize; scales: [ceil(K/256), rows, 8].
+// out[rows of e, N] = rows[rows of e, K] W_e^T (+ bias_e) of operands held by mx4_quantize; scales: [ceil(K/256), rows, 8].
 struct Mx4Product {
-    const uint8_t* rows;
+    const uint8_t* rows;      // (few rows: of the result's type where row_scale is null)
     const uint8_t* row_scale;
     const int32_t* offsets;
     const uint8_t* weight;
@@ -40,12 +37,13 @@ struct Mx4Product {
 };
 
 // fp32 (product_exact.hip).
-int launch_exact_rows_product(const RowsProduct& p, bool gradient, hipStream_t stream);
+int launch_exact_rows_gradient(const RowsGradient& p, hipStream_t stream);
 int launch_exact_weight_gradient(const WeightGradient& p, hipStream_t stream);
 int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local);
 // The sums of `splits` parts of n (and of m) values each, in order, in the type `dt`.
 int launch_join_parts(const float* parts, int64_t n, void* out, const float* more, int64_t m, void* more_out, int splits, int dt, hipStream_t stream);
 int launch_mx4_product(const Mx4Product& p, hipStream_t stream);  // result in fp32
+int launch_mx4_few_rows(const Mx4Product& p, int dt, hipStream_t stream);  // at most EXF_MX4_INLINE_ROWS
 
 // Bytes [a, a + n) and [b, b + m) overlap (nothing overlaps a null pointer).
 inline bool overlap(const void* a, size_t n, const void* b, size_t m)
@@ -55,6 +53,39 @@ inline bool overlap(const void* a, size_t n, const void* b, size_t m)
 }
 
 // ---- device side -------------------------------------------------------------------------
+// log2 X + 127 of a block of 4-bit numbers whose largest magnitude has these bits (see mx4.hip), and 2^(byte - 127).
+__device__ __forceinline__ uint32_t scale_byte(uint32_t largest)
+{
+    const uint32_t exponent = largest >> 23;
+    return exponent == 255u ? 255u : max(exponent, 2u) - 2u;
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte == 0u ? 0x00400000u : byte << 23); }
+// Eight numbers, given by their bits, divided by the block's power of two and rounded to four bits each.
+__device__ __forceinline__ uint32_t to_codes(const uint32_t (&v)[8], uint32_t byte)
+{
+    const float s = scale_value(byte == 255u ? 127u : byte);
+    uint32_t code = 0u;
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[0]), __uint_as_float(v[1]), s, 0);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[2]), __uint_as_float(v[3]), s, 1);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[4]), __uint_as_float(v[5]), s, 2);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, __uint_as_float(v[6]), __uint_as_float(v[7]), s, 3);
+    return byte == 255u ? 0u : code;
+}
+// Eight consecutive elements as the bits of fp32 numbers.
+template <bool BF16>
+__device__ __forceinline__ void load_bits8(const void* p, uint32_t (&v)[8])
+{
+    if constexpr (BF16) {
+        const uint4 t = *static_cast<const uint4*>(p);
+        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = w[i] << 16, v[2 * i + 1] = w[i] & 0xffff0000u;
+    } else {
+        const uint4 a = static_cast<const uint4*>(p)[0], b = static_cast<const uint4*>(p)[1];
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+}
+
 struct ExpertRows {  // rows [lo, hi) of expert `lane`
     int lo, hi;
 };

@@ -50,10 +50,10 @@ struct ExactOperand {
     }
 };
 
-// D[row][col] = sum_r a(row, r) w(col, r) + bias[col], written where row < a.rows and col < w.rows; sums[row] = sum_r a(row, r) where wanted
+// D[row][col] = sum_r a(row, r) w(col, r), written where row < a.rows and col < w.rows; sums[row] = sum_r a(row, r) where wanted
 // (a across).
 template <bool A_ACROSS, bool W_ACROSS>
-__device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperand<W_ACROSS> w, const float* bias, float* out, int64_t ldo, float* sums = nullptr)
+__device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperand<W_ACROSS> w, float* out, int64_t ldo, float* sums)
 {
     typedef ExactOperand<A_ACROSS> OA;
     typedef ExactOperand<W_ACROSS> OW;
@@ -110,48 +110,130 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
         for (int j = 0; j < 2; ++j) {
             const int row = row0 + i * 16 + in16, col = col0 + j * 16 + quad * 4;
             if (row >= a.rows || col >= w.rows) continue;
-            f32x4_t v = acc[0][i][j] + acc[1][i][j];
-            if (bias != nullptr) v += load4(bias + col);
-            *reinterpret_cast<f32x4_t*>(out + static_cast<int64_t>(row) * ldo + col) = v;
+            *reinterpret_cast<f32x4_t*>(out + static_cast<int64_t>(row) * ldo + col) = acc[0][i][j] + acc[1][i][j];
         }
 }
 
-template <bool GRADIENT>
-__global__ __launch_bounds__(256) void exact_rows_kernel(const RowsProduct p, int col_tiles)
+// ---- small problems: 32 x 32 outputs a workgroup, whose four wavefronts share the reduction (16 elements each in turn) and join their sums
+// through LDS.  Operands come straight from memory into the registers that the matrix instructions read, kAhead turns early.
+constexpr int kSmallTile = 32, kAhead = 3;
+template <bool ACROSS>
+__device__ __forceinline__ f32x4_t small_operand(const float* base, int64_t ld, int row, int r, int depth)
 {
+    if constexpr (!ACROSS) {  // depth is a multiple of four: all four or none
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(base + row * ld + (r < depth ? r : 0));
+        return r < depth ? v : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    } else {
+        f32x4_t v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float x = base[(r + j < depth ? r + j : 0) * ld + row];
+            v[j] = r + j < depth ? x : 0.0f;
+        }
+        return v;
+    }
+}
+template <bool A_ACROSS, bool W_ACROSS>
+__device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows, const float* w, int64_t ldw, int cols, int depth, float* out, int64_t ldo, float* sums)
+{
+    constexpr int STRIDE = kSmallTile + 4;
+    __shared__ __attribute__((aligned(16))) float part[4][kSmallTile * STRIDE];
+    __shared__ float part_sum[4][kSmallTile];
+    const int lane = lane_id(), wave = threadIdx.x / kWave, in16 = lane & 15, quad = lane >> 4;
+    int row[2], col[2];
+    f32x4_t acc[2][2], fa[kAhead][2], fw[kAhead][2];
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        row[i] = min(i * 16 + in16, rows - 1);
+        col[i] = min(i * 16 + in16, cols - 1);
+        acc[i][0] = acc[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    auto load = [&](int turn, int s) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            fa[s][i] = small_operand<A_ACROSS>(a, lda, row[i], (turn * 4 + wave) * 16 + quad * 4, depth);
+            fw[s][i] = small_operand<W_ACROSS>(w, ldw, col[i], (turn * 4 + wave) * 16 + quad * 4, depth);
+        }
+    };
+    const int turns = depth > wave * 16 ? (depth - wave * 16 + 63) / 64 : 0;
+    if (turns > 0) {
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) load(s, s);
+        for (int t = 0; t < turns; t += kAhead) {
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[s][j][q], fa[s][i][q], acc[i][j], 0, 0, 0);
+                if (sums != nullptr)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) sum[i] += (fa[s][i][0] + fa[s][i][1]) + (fa[s][i][2] + fa[s][i][3]);
+                load(t + s + kAhead, s);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<f32x4_t*>(&part[wave][(i * 16 + in16) * STRIDE + j * 16 + quad * 4]) = acc[i][j];
+        if (sums != nullptr) {
+            sum[i] = butterfly_add<16>(butterfly_add<32>(sum[i]));
+            if (quad == 0) part_sum[wave][i * 16 + in16] = sum[i];
+        }
+    }
+    __syncthreads();
+    const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 4, at = r * STRIDE + c;
+    auto of = [&](int wv) { return *reinterpret_cast<const f32x4_t*>(&part[wv][at]); };
+    if (r < rows && c < cols) *reinterpret_cast<f32x4_t*>(out + r * ldo + c) = (of(0) + of(1)) + (of(2) + of(3));
+    if (sums != nullptr && threadIdx.x < kSmallTile && static_cast<int>(threadIdx.x) < rows)
+        sums[threadIdx.x] = (part_sum[0][threadIdx.x] + part_sum[1][threadIdx.x]) + (part_sum[2][threadIdx.x] + part_sum[3][threadIdx.x]);
+}
+
+template <bool SMALL>
+__global__ __launch_bounds__(256) void exact_rows_gradient_kernel(const RowsGradient p, int col_tiles)
+{
+    constexpr int TILE = SMALL ? kSmallTile : kExactTile;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
-    const int tiles = (range.hi - range.lo + kExactTile - 1) / kExactTile;
+    const int tiles = (range.hi - range.lo + TILE - 1) / TILE;
     const int upto = wave_inclusive_scan(tiles);
     const int row_tile = static_cast<int>(blockIdx.x / static_cast<unsigned>(col_tiles)), col_tile = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles));
     const unsigned long long owner = __ballot(row_tile < upto);
     if (owner == 0ull) return;
     const int e = __builtin_ctzll(owner);
     const int hi = wave_read_lane(range.hi, e);
-    const int row = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * kExactTile;
-    const int col = col_tile * kExactTile;
+    const int row = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * TILE;
+    const int col = col_tile * TILE, rows = min(TILE, hi - row), cols = min(TILE, p.N - col);
     const int64_t K = p.K, N = p.N;
-    const float* weight = static_cast<const float*>(p.weight) + e * N * K;
-    const ExactOperand<false> a{static_cast<const float*>(p.rows) + row * K, K, min(kExactTile, hi - row), p.K, {}};
-    const ExactOperand<GRADIENT> w{GRADIENT ? weight + col : weight + col * K, GRADIENT ? N : K, min(kExactTile, p.N - col), p.K, {}};
-    exact_tile(a, w, p.bias != nullptr ? static_cast<const float*>(p.bias) + e * N + col : nullptr, static_cast<float*>(p.out) + row * N + col, N);
+    const float *a = static_cast<const float*>(p.rows) + row * K, *w = static_cast<const float*>(p.weight) + e * N * K + col;
+    float* out = static_cast<float*>(p.out) + row * N + col;
+    if constexpr (SMALL) small_tile<false, true>(a, K, rows, w, N, cols, p.K, out, N, nullptr);
+    else exact_tile(ExactOperand<false>{a, K, rows, p.K, {}}, ExactOperand<true>{w, N, cols, p.K, {}}, out, N, nullptr);
 }
 
 // Parts of the reduction (blockIdx.y) go to [part][E_local][N,K] and sums to [part][E_local][N].
+template <bool SMALL>
 __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient p, int row_tiles, int col_tiles)
 {
     const unsigned per_expert = static_cast<unsigned>(row_tiles) * static_cast<unsigned>(col_tiles);
     const int e = static_cast<int>(blockIdx.x / per_expert);
     const unsigned t = blockIdx.x % per_expert;
-    const int row = static_cast<int>(t / static_cast<unsigned>(col_tiles)) * kExactTile, col = static_cast<int>(t % static_cast<unsigned>(col_tiles)) * kExactTile;
+    constexpr int TILE = SMALL ? kSmallTile : kExactTile;
+    const int row = static_cast<int>(t / static_cast<unsigned>(col_tiles)) * TILE, col = static_cast<int>(t % static_cast<unsigned>(col_tiles)) * TILE;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
     const int lo = wave_read_lane(range.lo, e), all = wave_read_lane(range.hi, e) - lo;
     const int stages = (all + kExactDepth - 1) / kExactDepth;
     const int first = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / gridDim.y) * kExactDepth;
     const int n = max(min(all, static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / gridDim.y) * kExactDepth) - first, 0);
     const int64_t N = p.N, K = p.K, begin = lo + first, at = static_cast<int64_t>(blockIdx.y) * p.E_local + e;
-    const ExactOperand<true> a{static_cast<const float*>(p.dy) + begin * N + row, N, min(kExactTile, p.N - row), n, {}};
-    const ExactOperand<true> w{static_cast<const float*>(p.x) + begin * K + col, K, min(kExactTile, p.K - col), n, {}};
-    exact_tile(a, w, nullptr, static_cast<float*>(p.dw) + (at * N + row) * K + col, K, p.db != nullptr && col == 0 ? static_cast<float*>(p.db) + at * N + row : nullptr);
+    const int rows = min(TILE, p.N - row), cols = min(TILE, p.K - col);
+    const float *a = static_cast<const float*>(p.dy) + begin * N + row, *w = static_cast<const float*>(p.x) + begin * K + col;
+    float *out = static_cast<float*>(p.dw) + (at * N + row) * K + col, *sums = p.db != nullptr && col == 0 ? static_cast<float*>(p.db) + at * N + row : nullptr;
+    if constexpr (SMALL) small_tile<true, true>(a, N, rows, w, K, cols, n, out, K, sums);
+    else exact_tile(ExactOperand<true>{a, N, rows, n, {}}, ExactOperand<true>{w, K, cols, n, {}}, out, K, sums);
 }
 
 template <typename TO>
@@ -178,26 +260,36 @@ int launch_join_parts(const float* parts, int64_t n, void* out, const float* mor
     return EXF_OK;
 }
 
-static int64_t tiles_of(int64_t n) { return (n + kExactTile - 1) / kExactTile; }
 
-int launch_exact_rows_product(const RowsProduct& p, bool gradient, hipStream_t stream)
+// Small tiles where larger ones would leave compute units without one.
+static bool small_tiles(int64_t large) { return large < 2 * 256; }
+
+int launch_exact_rows_gradient(const RowsGradient& p, hipStream_t stream)
 {
-    const int64_t cols = tiles_of(p.N), grid = (p.max_rows / kExactTile + (p.max_rows < p.E_local ? p.max_rows : p.E_local)) * cols;
-    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product: too many tiles");
-    if (gradient) hipLaunchKernelGGL(exact_rows_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
-    else hipLaunchKernelGGL(exact_rows_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, static_cast<int>(cols));
+    const int64_t most_experts = p.max_rows < p.E_local ? p.max_rows : p.E_local;
+    auto tiles = [&](int64_t size) { return (p.max_rows / size + most_experts) * ((p.N + size - 1) / size); };
+    const bool small = small_tiles(tiles(kExactTile));
+    const int64_t grid = tiles(small ? kSmallTile : kExactTile);
+    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dx: too many tiles");
+    if (small) hipLaunchKernelGGL(exact_rows_gradient_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kSmallTile - 1) / kSmallTile);
+    else hipLaunchKernelGGL(exact_rows_gradient_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kExactTile - 1) / kExactTile);
     return EXF_OK;
 }
+
 // Parts of at least 256 rows until two workgroups a compute unit have one.
+static int64_t weight_tiles(int n, int k, int E_local, int size) { return static_cast<int64_t>(E_local) * ((n + size - 1) / size) * ((k + size - 1) / size); }
 int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local)
 {
-    const int64_t wanted = 512 / (E_local * tiles_of(n) * tiles_of(k)), most = A / (256 * E_local);
+    const bool small = small_tiles(weight_tiles(n, k, E_local, kExactTile));
+    const int64_t wanted = 512 / weight_tiles(n, k, E_local, small ? kSmallTile : kExactTile), most = A / (256 * E_local);
     const int64_t s = wanted < most ? wanted : most;
     return static_cast<int>(s < 2 ? 1 : (s > 16 ? 16 : s));
 }
 int launch_exact_weight_gradient(const WeightGradient& g, hipStream_t stream)
 {
-    const int64_t rows = tiles_of(g.N), cols = tiles_of(g.K), grid = g.E_local * rows * cols, each = static_cast<int64_t>(g.E_local) * g.N * g.K;
+    const bool small = small_tiles(weight_tiles(g.N, g.K, g.E_local, kExactTile));
+    const int size = small ? kSmallTile : kExactTile;
+    const int64_t grid = weight_tiles(g.N, g.K, g.E_local, size), each = static_cast<int64_t>(g.E_local) * g.N * g.K;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
     const int splits = exact_weight_gradient_splits(g.max_rows, g.N, g.K, g.E_local);
     float* parts = static_cast<float*>(g.workspace);
@@ -206,7 +298,10 @@ int launch_exact_weight_gradient(const WeightGradient& g, hipStream_t stream)
         p.dw = parts;
         if (p.db != nullptr) p.db = parts + splits * each;
     }
-    hipLaunchKernelGGL(exact_weight_kernel, dim3(static_cast<unsigned>(grid), static_cast<unsigned>(splits)), dim3(256), 0, stream, p, static_cast<int>(rows), static_cast<int>(cols));
+    const dim3 blocks(static_cast<unsigned>(grid), static_cast<unsigned>(splits));
+    const int rows = (g.N + size - 1) / size, cols = (g.K + size - 1) / size;
+    if (small) hipLaunchKernelGGL(exact_weight_kernel<true>, blocks, dim3(256), 0, stream, p, rows, cols);
+    else hipLaunchKernelGGL(exact_weight_kernel<false>, blocks, dim3(256), 0, stream, p, rows, cols);
     if (splits == 1) return EXF_OK;
     return launch_join_parts(parts, each, g.dw, parts + splits * each, g.db != nullptr ? static_cast<int64_t>(g.E_local) * g.N : 0, g.db, splits, EXF_F32, stream);
 }

@@ -3,6 +3,8 @@
 // bytes, and that block's scale byte.
 //
 // A wavefront computes 64 x 64 outputs; operands come straight from memory.
+#include <type_traits>
+
 #include "product.hpp"
 
 namespace exf {
@@ -71,6 +73,102 @@ __global__ __launch_bounds__(64) void mx4_rows_kernel(const Mx4Product p, int co
             if (p.bias != nullptr) v += *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p.bias) + e * N + c);
             *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + r * N + c) = v;
         }
+}
+
+// ---------------------------------------------------------------------------- few rows
+// At most EXF_MX4_INLINE_ROWS rows in all: a workgroup has 16 columns of one expert, its four wavefronts share the reduction and join their sums through
+// LDS.  A lane's operand is one block of one row, so rows that are not held in 4 bits are quantised where they are needed, by
+// the lane that needs them, without a word to any other lane: one launch instead of two, and no workspace.
+constexpr int kFewWaves = 4, kFewAhead = 2;
+template <bool BF16, bool HELD>
+__global__ __launch_bounds__(kFewWaves* kWave) void mx4_few_rows_kernel(const Mx4Product p, int col_tiles)
+{
+    __shared__ f32x4_t part[kFewWaves][kWave];
+    const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
+    unsigned long long busy = __ballot(range.hi > range.lo);
+    for (unsigned skip = blockIdx.x / static_cast<unsigned>(col_tiles); skip > 0; --skip) busy &= busy - 1;
+    if (busy == 0ull) return;
+    const int e = __builtin_ctzll(busy), col0 = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles)) * 16;
+    const int lo = wave_read_lane(range.lo, e), rows = wave_read_lane(range.hi, e) - lo;
+    const int lane = lane_id(), in16 = lane & 15, quad = lane >> 4, wave = threadIdx.x / kWave;
+    const int64_t N = p.N, weight_rows = p.E_local * N, half = p.K / 2;
+    const int64_t col = e * N + min(col0 + in16, p.N - 1), row = lo + min(in16, rows - 1);
+    const int blocks = p.K / 32, steps = (blocks + 3) / 4;
+    struct Operands {
+        i32x4_t w, x;
+        int sw, sx;
+        uint32_t v[HELD ? 1 : 4][8];
+    };
+    auto load = [&](int step, Operands& o) {
+        const int b = min(step * 4 + quad, blocks - 1);
+        o.w = *reinterpret_cast<const i32x4_t*>(p.weight + col * half + b * 16);
+        o.sw = p.weight_scale[(b / 8 * weight_rows + col) * 8 + b % 8];
+        if constexpr (HELD) {
+            o.x = *reinterpret_cast<const i32x4_t*>(p.rows + row * half + b * 16);
+            o.sx = p.row_scale[(static_cast<int64_t>(b / 8) * p.max_rows + row) * 8 + b % 8];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_bits8<BF16>(p.rows + ((row * p.K + b * 32 + i * 8) * (BF16 ? 2 : 4)), o.v[i]);
+        }
+    };
+    auto multiply = [&](int step, Operands& o, f32x4_t acc) {
+        if constexpr (!HELD) {
+            uint32_t largest = 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) largest = max(largest, o.v[i][j] & 0x7fffffffu);
+            const uint32_t byte = scale_byte(largest);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o.x[i] = static_cast<int>(to_codes(o.v[i], byte));
+            o.sx = static_cast<int>(byte);
+        }
+        if (step * 4 + quad >= blocks) {  // past the end: the last block again, without a value
+            o.w = o.x = i32x4_t{0, 0, 0, 0};
+            o.sw = o.sx = 0;
+        }
+        return mfma_mx4_direct(o.w, o.x, acc, o.sw, o.sx);
+    };
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    Operands o[kFewAhead];
+#pragma unroll
+    for (int i = 0; i < kFewAhead; ++i) load(wave + i * kFewWaves, o[i]);
+    for (int step = wave; step < steps; step += kFewAhead * kFewWaves) {
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i) {
+            acc = multiply(step + i * kFewWaves, o[i], acc);
+            load(step + (i + kFewAhead) * kFewWaves, o[i]);
+        }
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    const int c = col0 + quad * 4;
+    if (wave != 0 || in16 >= rows || c >= p.N) return;
+    acc = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    if constexpr (BF16) {
+        if (p.bias != nullptr)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[q] += bf16_to_f32(static_cast<const bf16_t*>(p.bias)[e * N + c + q]);
+        *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + row * N + c) = make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+    } else {
+        if (p.bias != nullptr) acc += *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p.bias) + e * N + c);
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + row * N + c) = acc;
+    }
+}
+
+int launch_mx4_few_rows(const Mx4Product& p, int dt, hipStream_t stream)
+{
+    const int64_t cols = (p.N + 15) / 16, grid = (p.max_rows < p.E_local ? p.max_rows : p.E_local) * cols;
+    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_mx4: too many tiles");
+    auto run = [&](auto bf16, auto held) {
+        hipLaunchKernelGGL((mx4_few_rows_kernel<decltype(bf16)::value, decltype(held)::value>), dim3(static_cast<unsigned>(grid)), dim3(kFewWaves * kWave), 0, stream, p,
+                           static_cast<int>(cols));
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if (dt == EXF_BF16) p.row_scale != nullptr ? run(yes, yes) : run(yes, no);
+    else p.row_scale != nullptr ? run(no, yes) : run(no, no);
+    return EXF_OK;
 }
 
 int launch_mx4_product(const Mx4Product& p, hipStream_t stream)

@@ -98,8 +98,8 @@ def test_workspaces():
     for dt in (B.EXF_F32, B.EXF_BF16):
         need = lib.moe_grouped_product_dw_workspace_bytes(1 << 20, 64, 64, 1, dt)
         if need:
-            assert _dw(A=1 << 20, E=1, dt=dt, size=need - 1) == B.EXF_ERR_WORKSPACE_TOO_SMALL
-            assert _dw(A=1 << 20, E=1, dt=dt, ws=None) == B.EXF_ERR_NULL_PTR
+            assert _dw(A=1 << 20, k=64, E=1, dt=dt, size=need - 1) == B.EXF_ERR_WORKSPACE_TOO_SMALL
+            assert _dw(A=1 << 20, k=64, E=1, dt=dt, ws=None) == B.EXF_ERR_NULL_PTR
     assert lib.mx4_scale_bytes(10, 257) == 2 * 10 * 8 and lib.mx4_scale_bytes(-1, 32) == 0
 
 
