@@ -108,6 +108,7 @@ struct StagedOperand {
         back = -step * (todo - 1);
         base = reinterpret_cast<uint64_t>(uniform_ptr(static_cast<const unsigned char*>(at))) + static_cast<uint64_t>(k0 * step);
     }
+    __device__ __forceinline__ void nothing() { todo = left = total = 0; }  // from here on all loads deliver zeros
     __device__ __forceinline__ void advance()  // to the next stage; behind the end of the reduction follows its begin
     {
         const bool wrap = left <= UNITS;
@@ -241,6 +242,8 @@ struct ProductTile {
     static constexpr int LA = OpA::LOADS + ScA::LOADS, LW = OpW::LOADS + ScW::LOADS, LPW = LA + LW;  // loads of a wavefront a stage
     static constexpr int IN_FLIGHT = (SA > SB ? LA : 0) + (SB - 2) * LPW;  // behind the next stage at a hand-over
     static constexpr int ACC_HALF = 256 / WAVES;
+    template <typename TO>
+    static constexpr int stores() { return TM * TN / (sizeof(TO) == 4 ? 1 : 2); }  // of a lane, by store()
     static_assert(TN % 2 == 0 && TM * 16 * WM == H && TN * 16 * WN == NT, "outputs of a wavefront");
     static_assert(SA >= SB && SA - SB <= 1 && SB >= 2 && IN_FLIGHT < 64, "ring");
     static_assert(product_ring_bytes(H, NT, ROW, STAGES) <= kLdsBytes, "LDS of a compute unit");
@@ -248,7 +251,7 @@ struct ProductTile {
     f32x4_t acc[TM][TN];
     bf16x8_t fw[2][TN], fa[TM];
     int sw[2][TN], sa[TM];  // scales (4 bits)
-    f32x4_t sum[TM];        // of the rows over the reduction (SUMS: multiplied by ones)
+    f32x4_t sum[TM];        // of the rows over the reduction, where asked for: multiplied by ones
     bf16x8_t ones;
     OpA a;
     OpW w;
@@ -310,21 +313,44 @@ struct ProductTile {
             nxt = nxt + bytes == ring ? 0 : nxt + bytes;
         }
     };
-    static constexpr int slot_of(int i) { return i * SLOTS / LPW; }  // of load i of a refill, behind the hand-over
-    // ... of which so many come before the next stage begins
-    static constexpr int early_loads()
+    Stages ra, rw;
+
+    // Slot of load i of a refill, behind the hand-over; STREAM: all in front of the next stage.
+    template <bool STREAM>
+    static constexpr int slot_of(int i)
+    {
+        return i * (STREAM ? SLOTS - HALF : SLOTS) / LPW;
+    }
+    template <bool STREAM>
+    static constexpr int early_loads()  // loads of a refill in front of the next stage
     {
         int n = 0;
-        while (n < LPW && slot_of(n) < SLOTS - HALF) ++n;
+        while (n < LPW && slot_of<STREAM>(n) < SLOTS - HALF) ++n;
         return n;
+    }
+
+    // At a hand-over the next stage has landed when only what was asked for later is in flight: refills, and the stores of those of the last SB - 1
+    // stages that `ends` (a bit each) names as a whole tile's last (loads and stores are counted in the order of their issue).
+    template <int STORES>
+    __device__ __forceinline__ void wait_for_next(unsigned ends)
+    {
+        constexpr int most = 63;  // the counter has six bits
+        constexpr int one = IN_FLIGHT + STORES < most ? IN_FLIGHT + STORES : most, two = IN_FLIGHT + 2 * STORES < most ? IN_FLIGHT + 2 * STORES : most;
+        const int n = STORES > 0 ? __builtin_popcount(ends & ((1u << (SB - 1)) - 1u)) : 0;
+        if (n == 0) wait_vmcnt<IN_FLIGHT>();
+        else if (n == 1) wait_vmcnt<one>();
+        else wait_vmcnt<two>();
     }
 
     // Matrix instructions of one stage.  Operand fetches run one K step ahead: the weights' registers are double, a row fragment is
     // fetched into the register its last instruction has just read.  At the hand-over (everyone's share of the next stage
     // has landed, everyone is done reading this one) in the middle of the last K step this stage is free: its refill, weights
     // first, is spread up to the middle of the next stage's first K step.
-    template <bool NEXT, bool SUMS>
-    __device__ __forceinline__ void stage(const Stages& ra, const Stages& rw)
+    //   feed: steps both operands on to the stage that is loaded next.
+    //   STREAM: tiles in one stream, STORES of a lane behind each.  A refill is complete in front of the next stage, because behind the last
+    //   stage of a tile come its stores, which a load behind them would have to wait for.
+    template <bool NEXT, bool STREAM, int STORES, typename Feed>
+    __device__ __forceinline__ void stage(unsigned ends, bool sums, Feed&& feed)
     {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
@@ -333,15 +359,14 @@ struct ProductTile {
             for (int m = 0; m < SLOTS; ++m) {
                 const int r = m % TN, b = m / TN;
                 if (NEXT && last && m == HALF) {
-                    wait_vmcnt<IN_FLIGHT>();
+                    wait_for_next<STORES>(ends);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // my operand fetches from this stage are complete
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
-                    step_a();
-                    step_w();
+                    feed(*this);
                 }
                 multiply(b, r, ks);
-                if (SUMS && r == TN - 1) mfma_16x16x32<false>(ones, fa[b], sum[b]);
+                if (KIND == kWeightGradient && sums && r == TN - 1) mfma_16x16x32<false>(ones, fa[b], sum[b]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (!last) {
                     if (r == TN - 1) fetch_a(ra.cur, b, 1);
@@ -366,7 +391,7 @@ struct ProductTile {
                 if (NEXT) {
 #pragma unroll
                     for (int i = 0; i < LPW; ++i)
-                        if (slot_of(i) == (begun ? m - HALF : SLOTS - HALF + ks * SLOTS + m)) {
+                        if (slot_of<STREAM>(i) == (begun ? m - HALF : SLOTS - HALF + ks * SLOTS + m)) {
                             if (i < LW) issue_w(begun ? rw.cur : rw.prev, i < LW ? i : 0);
                             else issue_a(begun ? ra.cur : ra.prev, i >= LW ? i - LW : 0);
                         }
@@ -389,9 +414,15 @@ struct ProductTile {
         pin_accumulators();
     }
 
-    // All of a reduction of nk stages, at least one.  Behind it the accumulators hold the sums.
-    template <bool SUMS = false>
-    __device__ __forceinline__ void reduce(int nk)
+    __device__ __forceinline__ void next_stage()
+    {
+        ra.advance(A_BYTES, SA * A_BYTES);
+        rw.advance(W_BYTES, SB * W_BYTES);
+    }
+    // The ring is filled as if the stage before the first one had handed over (all but the late loads of its last stage), and the first operands
+    // are fetched.
+    template <bool STREAM, typename FeedA, typename FeedW>
+    __device__ __forceinline__ void begin_ring(FeedA&& feed_a, FeedW&& feed_w)
     {
         const int wm = wave / WN, wn = wave % WN;
 #pragma unroll
@@ -403,12 +434,11 @@ struct ProductTile {
             from_as = ScA::fetch_base(wm * WTM);
             from_ws = ScW::fetch_base(wn * WTN);
         }
-        // as if the stage before the first one had handed over: the ring full but for the late loads of its last stage
-        constexpr int EARLY = early_loads();
+        constexpr int EARLY = early_loads<STREAM>();
 #pragma unroll
         for (int s = 0; s < SA; ++s) {
-            if (s > 0 && s < SB) step_w();
-            if (s > 0) step_a();
+            if (s > 0 && s < SB) feed_w(*this);
+            if (s > 0) feed_a(*this);
 #pragma unroll
             for (int i = 0; i < LPW; ++i) {
                 if (i < LW && s < SB && (s < SB - 1 || i < EARLY)) issue_w(static_cast<uint32_t>(s * W_BYTES), i < LW ? i : 0);
@@ -422,15 +452,24 @@ struct ProductTile {
         for (int r = 0; r < TN; ++r) fetch_w(0u, r, 0);
 #pragma unroll
         for (int b = 0; b < TM; ++b) fetch_a(0u, b, 0);
+        ra = Stages{0u, static_cast<uint32_t>(A_BYTES), static_cast<uint32_t>((SA - 1) * A_BYTES)};
+        rw = Stages{0u, static_cast<uint32_t>(W_BYTES), static_cast<uint32_t>((SB - 1) * W_BYTES)};
+    }
+
+    // All of a reduction of nk stages, at least one.  Behind it the accumulators hold the sums.
+    __device__ __forceinline__ void reduce(int nk, bool sums = false)
+    {
+        begin_ring<false>([](ProductTile& t) { t.step_a(); }, [](ProductTile& t) { t.step_w(); });
         clear();
-        Stages ra{0u, static_cast<uint32_t>(A_BYTES), static_cast<uint32_t>((SA - 1) * A_BYTES)};
-        Stages rw{0u, static_cast<uint32_t>(W_BYTES), static_cast<uint32_t>((SB - 1) * W_BYTES)};
+        auto on = [](ProductTile& t) {
+            t.step_a();
+            t.step_w();
+        };
         for (int kt = 1; kt < nk; ++kt) {
-            stage<true, SUMS>(ra, rw);
-            ra.advance(A_BYTES, SA * A_BYTES);
-            rw.advance(W_BYTES, SB * W_BYTES);
+            stage<true, false, 0>(0u, sums, on);
+            next_stage();
         }
-        stage<false, SUMS>(ra, rw);
+        stage<false, false, 0>(0u, sums, on);
         wait_vmcnt<0>();  // (loads into LDS that nobody waited for)
         pin_accumulators();
     }
@@ -480,30 +519,30 @@ struct ProductTile {
         constexpr int PER = PAIRS ? 2 : 1;                              // units of a store
         const int quad = lane_id() >> 4, in16 = lane_id() & 15, wm = wave / WN, wn = wave % WN;
         const int in_unit = BLOCKS == 1 ? quad * 4 : (quad & 1) * 16 + (quad >> 1) * 8;
+        float bias_v[TN][4];
 #pragma unroll
-        for (int r = 0; r < TN; r += BLOCKS * PER) {
-            float bias_v[BLOCKS * PER][4];
+        for (int r = 0; r < TN; ++r)
 #pragma unroll
-            for (int q = 0; q < BLOCKS * PER; ++q)
+            for (int v = 0; v < 4; ++v) bias_v[r][v] = bias != nullptr ? bf16_to_f32(bias[min(wn * WTN + r * 16 + quad * 4 + v, cols - 1)]) : 0.0f;
+        // (row by row: rows are often a power of two bytes apart, and column by column all compute units would write to few memory channels at a time)
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    bias_v[q][v] = bias != nullptr ? bf16_to_f32(bias[min(wn * WTN + (r + q) * 16 + quad * 4 + v, cols - 1)]) : 0.0f;
+        for (int b = 0; b < TM; ++b) {
 #pragma unroll
-            for (int b = 0; b < TM; ++b) {
+            for (int r = 0; r < TN; r += BLOCKS * PER) {
                 uint32_t u[PER][4];
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
                     if constexpr (BLOCKS == 1) {
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) u[i][v] = __float_as_uint(acc[b][r + i][v] + bias_v[i][v]);
+                        for (int v = 0; v < 4; ++v) u[i][v] = __float_as_uint(acc[b][r + i][v] + bias_v[r + i][v]);
                     } else {
                         uint32_t p[2][2];
 #pragma unroll
                         for (int q = 0; q < 2; ++q)
 #pragma unroll
                             for (int v = 0; v < 2; ++v) {
-                                const int block = 2 * i + q;
-                                p[q][v] = pack_bf16x2(acc[b][r + block][2 * v] + bias_v[block][2 * v], acc[b][r + block][2 * v + 1] + bias_v[block][2 * v + 1]);
+                                const int c = r + 2 * i + q;
+                                p[q][v] = pack_bf16x2(acc[b][c][2 * v] + bias_v[c][2 * v], acc[b][c][2 * v + 1] + bias_v[c][2 * v + 1]);
                             }
                         const auto s0 = __builtin_amdgcn_permlane16_swap(p[0][0], p[1][0], false, false);
                         const auto s1 = __builtin_amdgcn_permlane16_swap(p[0][1], p[1][1], false, false);
@@ -524,7 +563,7 @@ struct ProductTile {
             }
         }
     }
-    // The sums over the reduction of the tile's rows (SUMS).
+    // The sums over the reduction of the tile's rows.
     template <typename TO>
     __device__ __forceinline__ void store_sums(TO* out, int rows) const
     {

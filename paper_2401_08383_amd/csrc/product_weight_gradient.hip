@@ -1,9 +1,11 @@
 // Weight gradient of the experts' products in tiles, bf16 (see product_tiles.hpp): dw[e][N,K] = dy[rows of e, N]^T x[rows of e, K].
 //
-// The reduction is an expert's rows, so its length differs from expert to expert and all tiles of an expert take equally long:
-// the longest experts come first.  Tiles go out in groups of 32, as many as an XCD has compute units: four rows of tiles by eight
-// columns, which share their operands in that XCD's L2.
-//   Few tiles: the reduction is split, the parts' sums go to the workspace in fp32, and a second launch adds them up in order.
+// The reduction is an expert's rows, so all tiles of an expert take equally long; the longest experts come first.  An XCD takes 32
+// consecutive tiles at a time, one for each compute unit: four rows of tiles by eight columns, which share their operands in its L2.
+//   Long reductions: a workgroup a tile.  Few tiles: the reduction is split, the parts' sums go to the workspace in fp32, and a
+//   second launch adds them up in order.
+//   Short ones, a stage or a few with as many outputs as weights: a workgroup is there for good and its tiles are one stream
+//   of stages; while a tile is multiplied and its results stored, the stages of the next ones are on their way.
 #include "product_tiles.hpp"
 
 namespace exf {
@@ -18,50 +20,157 @@ struct WeightTiles {
     int max_rows, N, K, E_local, splits;
 };
 
-template <int H, int NT, int STAGES, typename TO>
-__global__ __launch_bounds__(kProductWaves * kWave, STAGES == 2 ? 2 : 1) void weight_tiles_kernel(const WeightTiles p)
+// Quotient of wavefront-uniform numbers below 2^24 through the divisor's reciprocal, with a correction.
+__device__ __forceinline__ unsigned quotient(unsigned n, unsigned d, float reciprocal)
+{
+    int q = static_cast<int>(static_cast<float>(n) * reciprocal);
+    const int r = static_cast<int>(n) - q * static_cast<int>(d);
+    q += r < 0 ? -1 : (r >= static_cast<int>(d) ? 1 : 0);
+    return static_cast<unsigned>(__builtin_amdgcn_readfirstlane(q));
+}
+
+// The experts in the order of their rows, most first, and the places of a tile's outputs.
+template <int H, int NT>
+struct WeightOrder {
+    ExpertRows range;
+    int place;                            // lane e: experts in front of expert e
+    unsigned row_tiles, col_tiles, tiles; // of an expert: rows, columns, in all
+    float per_band;                       // 1 / tiles of four rows
+
+    __device__ __forceinline__ void begin(const WeightTiles& p)
+    {
+        range = expert_rows(p.offsets, p.E_local, p.max_rows);
+        row_tiles = static_cast<unsigned>((p.N + H - 1) / H), col_tiles = static_cast<unsigned>((p.K + NT - 1) / NT);
+        tiles = row_tiles * col_tiles;
+        per_band = 1.0f / static_cast<float>(kGroupRows * col_tiles);
+        const int lane = lane_id(), count = range.hi - range.lo;
+        place = lane < p.E_local ? 0 : kWave;
+        for (int j = 0; j < p.E_local; ++j) {
+            const int other = wave_read_lane(count, j);
+            place += other > count || (other == count && j < lane) ? 1 : 0;
+        }
+    }
+    __device__ __forceinline__ int expert(unsigned rank) const { return __builtin_ctzll(__ballot(place == static_cast<int>(rank))); }
+    // Four rows of tiles, column by column.
+    __device__ __forceinline__ void outputs(unsigned tile, int& row0, int& col0) const
+    {
+        const unsigned band = quotient(tile, kGroupRows * col_tiles, per_band), in_band = tile - band * kGroupRows * col_tiles;
+        const unsigned band_rows = min(static_cast<unsigned>(kGroupRows), row_tiles - band * kGroupRows);
+        const unsigned col = band_rows == 3u ? in_band / 3u : in_band >> (band_rows >> 1);
+        row0 = __builtin_amdgcn_readfirstlane(static_cast<int>(band * kGroupRows + in_band - col * band_rows) * H);
+        col0 = __builtin_amdgcn_readfirstlane(static_cast<int>(col) * NT);
+    }
+};
+constexpr unsigned kMostTiles = 1u << 24;
+
+// A workgroup a tile.
+template <int H, int NT, typename TO>
+__global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_tiles_kernel(const WeightTiles p)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    const RowRange range = row_range(p.offsets, p.E_local, p.max_rows);
-    const int lane = lane_id(), count = range.hi - range.lo;
-    const unsigned row_tiles = static_cast<unsigned>((p.N + H - 1) / H), col_tiles = static_cast<unsigned>((p.K + NT - 1) / NT), tiles = row_tiles * col_tiles;
-    const unsigned groups = (tiles + kGroupTiles - 1) / kGroupTiles;  // of an expert's part
-    const unsigned xcd = blockIdx.x % kXcdCount, pos = blockIdx.x / kXcdCount;
-    const unsigned group = pos / kGroupTiles * kXcdCount + xcd;
-    const unsigned part = uniform_udiv(group, groups), tile = (group - part * groups) * kGroupTiles + pos % kGroupTiles;
-    const unsigned rank = uniform_udiv(part, static_cast<unsigned>(p.splits)), split = part - rank * static_cast<unsigned>(p.splits);
-    if (rank >= static_cast<unsigned>(p.E_local) || tile >= tiles) return;
-    int longer = 0;  // experts in front of expert `lane`
-    for (int j = 0; j < p.E_local; ++j) {
-        const int other = wave_read_lane(count, j);
-        longer += other > count || (other == count && j < lane) ? 1 : 0;
-    }
-    const int e = __builtin_ctzll(__ballot(lane < p.E_local && longer == static_cast<int>(rank)));
-    const int lo = wave_read_lane(range.lo, e), n = wave_read_lane(count, e);
-    // four rows of tiles, column by column
-    const unsigned band = uniform_udiv(tile, kGroupRows * col_tiles), in_band = tile - band * kGroupRows * col_tiles;
-    const unsigned band_rows = min(static_cast<unsigned>(kGroupRows), row_tiles - band * kGroupRows);
-    const unsigned col_tile = uniform_udiv(in_band, band_rows);
-    const int row0 = __builtin_amdgcn_readfirstlane(static_cast<int>(band * kGroupRows + in_band - col_tile * band_rows)) * H;
-    const int col0 = __builtin_amdgcn_readfirstlane(static_cast<int>(col_tile)) * NT;
-
-    const int stages = (n + 63) / 64;
-    const int first = static_cast<int>(static_cast<int64_t>(stages) * split / p.splits), last = static_cast<int>(static_cast<int64_t>(stages) * (split + 1) / p.splits);
-    const int rows = min(n, last * 64) - first * 64;
-    const int64_t begin = lo + first * 64, N = p.N, K = p.K;
-    ProductTile<H, NT, kWeightGradient, false, STAGES> t;
-    begin_tile(t, smem);
+    WeightOrder<H, NT> order;
+    order.begin(p);
+    const unsigned index = (blockIdx.x / kXcdCount / kGroupTiles * kXcdCount + blockIdx.x % kXcdCount) * kGroupTiles + blockIdx.x / kXcdCount % kGroupTiles;
+    const unsigned splits = static_cast<unsigned>(p.splits), part = uniform_udiv(index, order.tiles), rank = uniform_udiv(part, splits), split = part - rank * splits;
+    if (rank >= static_cast<unsigned>(p.E_local)) return;
+    const int e = order.expert(rank), lo = wave_read_lane(order.range.lo, e), n = wave_read_lane(order.range.hi, e) - lo, stages = (n + 63) / 64;
+    int row0, col0;
+    order.outputs(index - part * order.tiles, row0, col0);
+    const int first = static_cast<int>(static_cast<int64_t>(stages) * split / splits), last = static_cast<int>(static_cast<int64_t>(stages) * (split + 1) / splits);
+    const int rows = min(H, p.N - row0), cols = min(NT, p.K - col0);
+    const int64_t N = p.N, K = p.K, begin = lo + first * 64, result = (static_cast<int64_t>(split) * p.E_local + e) * N + row0;
     const bool sums = p.sums != nullptr && col0 == 0;
-    if (rows > 0) {
-        t.a.begin(p.dy + begin * N + row0, N * 2, min(H, p.N - row0), rows, 0, t.wave);
-        t.w.begin(p.x + begin * K + col0, K * 2, min(NT, p.K - col0), rows, 0, t.wave);
-        if (sums) t.template reduce<true>(last - first);
-        else t.reduce(last - first);
+    ProductTile<H, NT, kWeightGradient> t;
+    begin_tile(t, smem);
+    if (last > first) {
+        const int depth = min(n, last * 64) - first * 64;
+        t.a.begin(p.dy + begin * N + row0, N * 2, rows, depth, 0, t.wave);
+        t.w.begin(p.x + begin * K + col0, K * 2, cols, depth, 0, t.wave);
+        t.reduce(last - first, sums);
     } else {
         t.clear();
     }
-    if (sums) t.store_sums(static_cast<TO*>(p.sums) + (static_cast<int64_t>(split) * p.E_local + e) * N + row0, min(H, p.N - row0));
-    t.store(static_cast<TO*>(p.out) + ((static_cast<int64_t>(split) * p.E_local + e) * N + row0) * K + col0, K, min(H, p.N - row0), min(NT, p.K - col0), nullptr);
+    if (sums) t.store_sums(static_cast<TO*>(p.sums) + result, rows);
+    t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols, nullptr);
+}
+
+// A stream of tiles, not split.  What the loads know of a tile goes to the multiplication through a queue in the lanes of a few registers.
+template <int H, int NT, int STAGES, typename TO>
+__global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_stream_kernel(const WeightTiles p)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    typedef ProductTile<H, NT, kWeightGradient, false, STAGES> T;
+    constexpr int STORES = T::template stores<TO>();
+    static_assert(T::SA == T::SB, "both operands are loaded of the same stage");
+    const int64_t N = p.N, K = p.K;
+    WeightOrder<H, NT> order;
+    order.begin(p);
+    const unsigned step_rank = uniform_udiv(gridDim.x, order.tiles), step_tile = gridDim.x - step_rank * order.tiles;
+    const unsigned index = blockIdx.x % kXcdCount * kGroupTiles + blockIdx.x / kXcdCount, experts = static_cast<unsigned>(p.E_local);
+    unsigned rank = uniform_udiv(index, order.tiles), tile = index - rank * order.tiles;
+    int queue_stages = 0, queue_expert = 0, queue_row = 0, queue_col = 0;
+    unsigned in = 0u, out = 0u;  // tiles that have entered it and left
+    T t;
+    begin_tile(t, smem);
+    // The next tile with rows is loaded from here on (those without are behind all others); false: there is none.
+    auto enter = [&]() {
+        if (rank >= experts) return false;
+        const int e = order.expert(rank), lo = wave_read_lane(order.range.lo, e), n = wave_read_lane(order.range.hi, e) - lo;
+        if (n == 0) return false;
+        int row0, col0;
+        order.outputs(tile, row0, col0);
+        const int64_t begin = lo;
+        t.a.begin(p.dy + begin * N + row0, N * 2, min(H, p.N - row0), n, 0, t.wave);
+        t.w.begin(p.x + begin * K + col0, K * 2, min(NT, p.K - col0), n, 0, t.wave);
+        const bool mine = lane_id() == static_cast<int>(in % kWave);
+        queue_stages = mine ? (n + 63) / 64 : queue_stages;
+        queue_expert = mine ? e : queue_expert;
+        queue_row = mine ? row0 : queue_row;
+        queue_col = mine ? col0 : queue_col;
+        ++in;
+        rank += step_rank, tile += step_tile;
+        if (tile >= order.tiles) tile -= order.tiles, rank += 1u;
+        return true;
+    };
+    auto feed = [&](T&) {
+        if (t.a.todo > 1) {
+            t.a.advance();
+            t.w.advance();
+        } else if (!enter()) {
+            t.a.nothing();
+            t.w.nothing();
+        }
+    };
+    auto store = [&](int e, int row0, int col0) {
+        const int rows = min(H, p.N - row0), cols = min(NT, p.K - col0);
+        const int64_t result = e * N + row0;
+        if (p.sums != nullptr && col0 == 0) t.store_sums(static_cast<TO*>(p.sums) + result, rows);
+        t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols, nullptr);
+        return rows == H && cols == NT ? 1u : 0u;
+    };
+    if (enter()) t.template begin_ring<true>(feed, [](T&) {});
+    unsigned ends = 0u;
+    for (; out != in; ++out) {
+        const int stages = wave_read_lane(queue_stages, out % kWave), e = wave_read_lane(queue_expert, out % kWave);
+        const int row0 = wave_read_lane(queue_row, out % kWave), col0 = wave_read_lane(queue_col, out % kWave);
+        t.clear();
+        for (int kt = 0; kt < stages; ++kt) {
+            t.template stage<true, true, STORES>(ends, p.sums != nullptr && col0 == 0, feed);
+            t.next_stage();
+            ends <<= 1;
+        }
+        t.pin_accumulators();
+        ends |= store(e, row0, col0);  // (fewer outputs are fewer stores: those are not counted on)
+    }
+    wait_vmcnt<0>();  // (loads into LDS that nobody waited for)
+    t.clear();
+    while (rank < experts) {
+        int row0, col0;
+        order.outputs(tile, row0, col0);
+        store(order.expert(rank), row0, col0);
+        rank += step_rank, tile += step_tile;
+        if (tile >= order.tiles) tile -= order.tiles, rank += 1u;
+    }
 }
 
 static int64_t tiles_in(int64_t n, int64_t k, int64_t size) { return ((n + size - 1) / size) * ((k + size - 1) / size); }
@@ -82,15 +191,17 @@ int weight_gradient_splits(int64_t A, int n, int k, int E_local)
     return static_cast<int>(s < 2 ? 1 : (s > kMostSplits ? kMostSplits : s));
 }
 
+// STAGES: of a stream's ring (0: a workgroup a tile).
 template <int H, int NT, int STAGES, typename TO>
 static int launch_weight_as(const WeightTiles& p, hipStream_t stream)
 {
-    constexpr size_t lds = product_ring_bytes(H, NT, 128, STAGES);
-    const int64_t tiles = static_cast<int64_t>((p.N + H - 1) / H) * ((p.K + NT - 1) / NT);
-    const int64_t groups = (tiles + kGroupTiles - 1) / kGroupTiles * p.E_local * p.splits;
-    const int64_t grid = (groups + kXcdCount - 1) / kXcdCount * kXcdCount * kGroupTiles;
-    if (tiles >= (1ll << 31) || grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
-    auto kern = weight_tiles_kernel<H, NT, STAGES, TO>;
+    constexpr size_t lds = product_ring_bytes(H, NT, 128, STAGES > 0 ? STAGES : 8);
+    const int64_t tiles = static_cast<int64_t>((p.N + H - 1) / H) * ((p.K + NT - 1) / NT), groups = (tiles * p.E_local * p.splits + kGroupTiles - 1) / kGroupTiles;
+    const int64_t grid = STAGES > 0 ? kComputeUnits : (groups + kXcdCount - 1) / kXcdCount * kXcdCount * kGroupTiles;
+    if (tiles >= kMostTiles || grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
+    void (*kern)(WeightTiles);
+    if constexpr (STAGES > 0) kern = weight_stream_kernel<H, NT, STAGES, TO>;
+    else kern = weight_tiles_kernel<H, NT, TO>;
     static std::atomic<uint64_t> allowed{0};
     if (int rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, "moe_grouped_product_dw")) return rc;
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(kProductWaves * kWave), lds, stream, p);
@@ -104,11 +215,11 @@ static int launch_weight_tiles(const WeightGradient& g, hipStream_t stream)
     float* parts = static_cast<float*>(g.workspace);
     const int64_t each = static_cast<int64_t>(g.E_local) * g.N * g.K, sums = static_cast<int64_t>(g.E_local) * g.N;
     WeightTiles p{static_cast<const bf16_t*>(g.dy), static_cast<const bf16_t*>(g.x), g.offsets, g.dw, g.db, g.max_rows, g.N, g.K, g.E_local, splits};
-    if (large_tiles(g.max_rows, g.N, g.K, g.E_local)) return launch_weight_as<256, 256, 8, TO>(p, stream);
-    if (splits == 1) return launch_weight_as<128, 128, 2, TO>(p, stream);
+    if (large_tiles(g.max_rows, g.N, g.K, g.E_local)) return launch_weight_as<256, 256, 0, TO>(p, stream);
+    if (splits == 1) return launch_weight_as<128, 128, 4, TO>(p, stream);
     p.out = parts;
     if (p.sums != nullptr) p.sums = parts + splits * each;
-    if (int rc = launch_weight_as<128, 128, 2, float>(p, stream)) return rc;
+    if (int rc = launch_weight_as<128, 128, 0, float>(p, stream)) return rc;
     return launch_join_parts(parts, each, g.dw, parts + splits * each, g.db != nullptr ? sums : 0, g.db, splits, sizeof(TO) == 4 ? EXF_F32 : EXF_BF16, stream);
 }
 
