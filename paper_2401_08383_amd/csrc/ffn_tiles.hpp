@@ -275,6 +275,8 @@ __device__ __forceinline__ void collect_rows(int expert, int lo, int row_begin, 
     __syncthreads();
 }
 
+// MOST: quanta a tile can take (1: the kernel has no tiles of 320 rows).
+template <int MOST = 2>
 __device__ __forceinline__ TilePlan plan_tiles(const RowRange& range, int n_tiles, const RowMap& probe)
 {
     TilePlan p;
@@ -286,12 +288,12 @@ __device__ __forceinline__ TilePlan plan_tiles(const RowRange& range, int n_tile
     }
     // one quantum per tile, unless two make the launch a round of tiles shorter
     const bool small = cnt <= kSmallRows;
-    const int lean = cnt > 0 ? cut_rows(cnt, 1).tiles : 0, tall = cnt > 0 ? cut_rows(cnt, 2).tiles : 0;
+    const int lean = cnt > 0 ? cut_rows(cnt, 1).tiles : 0, tall = cnt > 0 ? cut_rows(cnt, MOST).tiles : 0;
     const int lean_incl = wave_inclusive_scan(small ? 0 : lean * n_tiles), tall_incl = wave_inclusive_scan(small ? 0 : tall * n_tiles);
     p.small_incl = wave_inclusive_scan(small ? lean * n_tiles : 0);
     const int lean_total = wave_read_lane(lean_incl, kWave - 1), tall_total = wave_read_lane(tall_incl, kWave - 1);
     const bool use_tall = (tall_total + kComputeUnits - 1) / kComputeUnits < (lean_total + kComputeUnits - 1) / kComputeUnits;
-    p.most = use_tall ? 2 : 1;
+    p.most = use_tall ? MOST : 1;
     p.tiles = use_tall ? tall : lean;
     p.big_incl = use_tall ? tall_incl : lean_incl;
     p.total_big = use_tall ? tall_total : lean_total;
@@ -322,11 +324,11 @@ __device__ __forceinline__ int xcd_share(int n, int xcd, int& rot, int& begin)
 // 63.7 -> 47.8 us; one of 2048 x 8192, 130 rows 75.4 -> 60.0; eight of 1024 x 4096, 2000 rows 92.3 -> 81.5; 16 of them, 3062
 // rows (the second contraction alone is cut: 256 x 64 -> 128 x 128) 101.9 -> 96.4.
 constexpr int kUnitsPerXcd = kComputeUnits / kXcdCount;
-template <bool STREAMS>
+template <bool STREAMS, int MOST = 2>
 __device__ __forceinline__ bool locate_tile(const RowRange& range, int NT, int N, int wg, const RowMap& probe, Tile2D& out)
 {
     const int n_tiles = (N + NT - 1) / NT;
-    const TilePlan p = plan_tiles(range, n_tiles, probe);
+    const TilePlan p = plan_tiles<MOST>(range, n_tiles, probe);
     const int xcd = static_cast<int>(static_cast<unsigned>(wg) % kXcdCount);
     int pos = static_cast<int>(static_cast<unsigned>(wg) / kXcdCount);
     int rot = 0, begin = 0, begin_small = 0;

@@ -193,10 +193,10 @@ template <bool ACC_HALF>
 __device__ __forceinline__ void mfma_mx4(bf16x8_t a, bf16x8_t b, f32x4_t& c, int scale_a, int scale_b)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    if constexpr (ACC_HALF)
-        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
-    else
+    if constexpr (!ACC_HALF)
         asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+v"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
+    else
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
 #else
     (void)a; (void)b; (void)c; (void)scale_a; (void)scale_b;
 #endif
@@ -407,10 +407,12 @@ struct ProductTile {
         for (int b = 0; b < TM; ++b)
 #pragma unroll
             for (int r = 0; r < TN; ++r) acc[b][r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if constexpr (KIND == kWeightGradient) {
 #pragma unroll
-        for (int b = 0; b < TM; ++b) sum[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        ones = __builtin_bit_cast(bf16x8_t, u32x4_v{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-        asm volatile("" : "+v"(ones));  // (in its registers from here on: a matrix instruction must not follow its operand's write at once)
+            for (int b = 0; b < TM; ++b) sum[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            ones = __builtin_bit_cast(bf16x8_t, u32x4_v{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+            asm volatile("" : "+v"(ones));  // (in its registers from here on: a matrix instruction must not follow its operand's write at once)
+        }
         pin_accumulators();
     }
 
@@ -487,8 +489,10 @@ struct ProductTile {
                 if (b * TN + r < ACC_HALF) asm volatile("" : "+a"(acc[b][r]));
                 else asm volatile("" : "+v"(acc[b][r]));
             }
+        if constexpr (KIND == kWeightGradient) {
 #pragma unroll
-        for (int b = 0; b < TM; ++b) asm volatile("" : "+v"(sum[b]));
+            for (int b = 0; b < TM; ++b) asm volatile("" : "+v"(sum[b]));
+        }
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #endif
     }
@@ -511,8 +515,18 @@ struct ProductTile {
     // (b, r), row lane%16 and columns 4 (lane/16) .. +3: in fp32 16 bytes, 64 of the row with the other lanes.  bf16: of two
     // blocks side by side the odd rows of 16 lanes of the first trade with the even ones of the second, and every lane has
     // eight consecutive columns of one block.
+    //   A whole tile's stores have no condition, and without a bias nothing is added: where a wavefront is alone on its SIMD every
+    //   instruction here is time.
     template <typename TO>
     __device__ __forceinline__ void store(TO* out, int64_t ldo, int rows, int cols, const bf16_t* bias) const
+    {
+        const bool whole = rows == H && cols == NT;
+        if (bias != nullptr) store_as<TO, true, false>(out, ldo, rows, cols, bias);
+        else if (whole) store_as<TO, false, true>(out, ldo, rows, cols, nullptr);
+        else store_as<TO, false, false>(out, ldo, rows, cols, nullptr);
+    }
+    template <typename TO, bool BIAS, bool WHOLE>
+    __device__ __forceinline__ void store_as(TO* out, int64_t ldo, int rows, int cols, const bf16_t* bias) const
     {
         constexpr int BLOCKS = sizeof(TO) == 4 ? 1 : 2;                // of a unit
         constexpr bool PAIRS = TN % (2 * BLOCKS) == 0;
@@ -523,7 +537,8 @@ struct ProductTile {
 #pragma unroll
         for (int r = 0; r < TN; ++r)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) bias_v[r][v] = bias != nullptr ? bf16_to_f32(bias[min(wn * WTN + r * 16 + quad * 4 + v, cols - 1)]) : 0.0f;
+            for (int v = 0; v < 4; ++v) bias_v[r][v] = BIAS ? bf16_to_f32(bias[min(wn * WTN + r * 16 + quad * 4 + v, cols - 1)]) : 0.0f;
+        auto value = [&](int b, int r, int v) { return BIAS ? acc[b][r][v] + bias_v[r][v] : acc[b][r][v]; };
         // (row by row: rows are often a power of two bytes apart, and column by column all compute units would write to few memory channels at a time)
 #pragma unroll
         for (int b = 0; b < TM; ++b) {
@@ -534,7 +549,7 @@ struct ProductTile {
                 for (int i = 0; i < PER; ++i) {
                     if constexpr (BLOCKS == 1) {
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) u[i][v] = __float_as_uint(acc[b][r + i][v] + bias_v[r + i][v]);
+                        for (int v = 0; v < 4; ++v) u[i][v] = __float_as_uint(value(b, r + i, v));
                     } else {
                         uint32_t p[2][2];
 #pragma unroll
@@ -542,7 +557,7 @@ struct ProductTile {
 #pragma unroll
                             for (int v = 0; v < 2; ++v) {
                                 const int c = r + 2 * i + q;
-                                p[q][v] = pack_bf16x2(acc[b][c][2 * v] + bias_v[c][2 * v], acc[b][c][2 * v + 1] + bias_v[c][2 * v + 1]);
+                                p[q][v] = pack_bf16x2(value(b, c, 2 * v), value(b, c, 2 * v + 1));
                             }
                         const auto s0 = __builtin_amdgcn_permlane16_swap(p[0][0], p[1][0], false, false);
                         const auto s1 = __builtin_amdgcn_permlane16_swap(p[0][1], p[1][1], false, false);
@@ -555,9 +570,9 @@ struct ProductTile {
                     trade(u[0], u[PER - 1], lo, hi);
                     const int row_lo = row + (in16 & 7), col_of = col + (in16 >> 3) * BLOCKS * 16;
                     TO* to = out + row_lo * ldo + col_of;
-                    if (row_lo < rows && col_of < cols) store_stream16(reinterpret_cast<uint4*>(to), lo);
-                    if (row_lo + 8 < rows && col_of < cols) store_stream16(reinterpret_cast<uint4*>(to + 8 * ldo), hi);
-                } else if (row + in16 < rows && col < cols) {
+                    if (WHOLE || (row_lo < rows && col_of < cols)) store_stream16(reinterpret_cast<uint4*>(to), lo);
+                    if (WHOLE || (row_lo + 8 < rows && col_of < cols)) store_stream16(reinterpret_cast<uint4*>(to + 8 * ldo), hi);
+                } else if (WHOLE || (row + in16 < rows && col < cols)) {
                     store_stream16(reinterpret_cast<uint4*>(out + (row + in16) * ldo + col), make_uint4(u[0][0], u[0][1], u[0][2], u[0][3]));
                 }
             }
@@ -622,6 +637,14 @@ __device__ __forceinline__ void rows_tile(const RowsTiles& p, const Tile2D& tile
     t.store(p.out + tile.row_begin * N + tile.n0, N, rows, cols, p.bias != nullptr ? p.bias + tile.expert * N + tile.n0 : nullptr);
 }
 
+// A whole tile of 320 rows and 256 columns in 4 bits has no registers left for the scales (it would spill 44 of them): there tiles take one
+// quantum at most.
+constexpr int most_quanta(ProductKind kind) { return kind == kMx4 ? 1 : 2; }
+constexpr bool has_product_instance(ProductKind kind, int NT, int height, int cut)
+{
+    return has_instance(NT, height, cut) && !(cut == 0 && height > kTileRows + most_quanta(kind) * kQuantum);
+}
+
 // STREAMS: tiles whose weights nobody else reads load them with the streaming hint, and the column tiles of experts of few rows begin the reduction
 // at different places (see locate_tile and streams_weights).
 template <int NT, ProductKind KIND, bool STREAMS>
@@ -630,10 +653,10 @@ __global__ __launch_bounds__(kProductWaves * kWave, 1) void rows_tiles_kernel(co
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const RowRange range = row_range(p.offsets, p.E_local, p.max_rows);
     Tile2D tile;
-    if (!locate_tile<STREAMS>(range, NT, p.N, static_cast<int>(blockIdx.x), RowMap{}, tile)) return;
+    if (!locate_tile<STREAMS, most_quanta(KIND)>(range, NT, p.N, static_cast<int>(blockIdx.x), RowMap{}, tile)) return;
 #define EXF_CASE(H, CUT, ONCE)            \
     case (CUT) * 16 + (H) / kQuantum: \
-        if constexpr (has_instance(NT, H, CUT) && (!(ONCE) || H <= kTileRows)) rows_tile<H, (NT >> CUT), KIND, ONCE>(p, tile, smem); \
+        if constexpr (has_product_instance(KIND, NT, H, CUT) && (!(ONCE) || H <= kTileRows)) rows_tile<H, (NT >> CUT), KIND, ONCE>(p, tile, smem); \
         break
 #define EXF_CASES(CUT, ONCE)  \
     EXF_CASE(64, CUT, ONCE);  \
@@ -671,7 +694,7 @@ constexpr int rows_tiles_lds()
     const int heights[] = {64, 96, 128, 160, 192, 224, 256, 288, 320};
     for (int h : heights)
         for (int cut = 0; cut <= 2; ++cut)
-            if (has_instance(NT, h, cut) && product_ring_bytes(h, NT >> cut, row) > most) most = product_ring_bytes(h, NT >> cut, row);
+            if (has_product_instance(KIND, NT, h, cut) && product_ring_bytes(h, NT >> cut, row) > most) most = product_ring_bytes(h, NT >> cut, row);
     return most;
 }
 
