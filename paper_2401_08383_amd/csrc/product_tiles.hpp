@@ -59,11 +59,13 @@ __device__ __forceinline__ T lds_fetch(uint32_t addr)
 //   across: reduction element r at base + r * ld, the rows side by side.  One load covers 1024 bytes of [reduction][ROWS]; the
 //           32-byte granules (16 rows) of a reduction element are exchanged so that the eight of them that 32 lanes read
 //           together lie in different banks.
-template <int ROWS, bool ACROSS, bool STREAM = false>
+//   STEPS: K steps of 32 bf16 a stage.
+template <int ROWS, bool ACROSS, bool STREAM = false, int STEPS = 2>
 struct StagedOperand {
-    static constexpr int GROUPS = ROWS / 8, LOADS = (GROUPS + kProductWaves - 1) / kProductWaves;  // 1 KiB each; of a wavefront
-    static constexpr int UNITS = ACROSS ? 64 : 8;  // of the reduction in a stage: elements, 16-byte pieces
-    static constexpr int BYTES = ROWS * 128;
+    static constexpr int GROUPS = ROWS * STEPS / 16, LOADS = (GROUPS + kProductWaves - 1) / kProductWaves;  // 1 KiB each; of a wavefront
+    static constexpr int UNITS = ACROSS ? 32 * STEPS : 8;  // of the reduction in a stage: elements, 16-byte pieces
+    static constexpr int BYTES = ROWS * 64 * STEPS;
+    static_assert(STEPS == 2 || ACROSS, "a row of a stage along the reduction is 128 bytes");
     static constexpr int PITCH = ROWS * 2;         // across: bytes of a reduction element in LDS
     static_assert(GROUPS >= kProductWaves && GROUPS % 2 == 0, "every wavefront has a group of its own parity");
     static_assert(!ACROSS || (ROWS & (ROWS - 1)) == 0, "rows across are a power of two");
@@ -101,7 +103,7 @@ struct StagedOperand {
                 off[i] = static_cast<uint32_t>(min(g * 8 + (lane >> 3), rows - 1)) * static_cast<uint32_t>(ld) + static_cast<uint32_t>(place) * 16u;
             }
         }
-        step = ACROSS ? 64 * ld : 128;
+        step = ACROSS ? UNITS * ld : 128;
         total = units;
         left = units - k0 * UNITS;
         todo = (units + UNITS - 1) / UNITS;
@@ -225,23 +227,24 @@ struct NoScales {
 };
 
 // ONCE: the weights are loaded with the streaming hint (see rows_tile).
-template <int H, int NT, ProductKind KIND, bool ONCE = false, int STAGES = 8>
+template <int H, int NT, ProductKind KIND, bool ONCE = false, int STAGES = 8, int STEPS = 2>
 struct ProductTile {
     static constexpr bool MX = KIND == kMx4;
     static constexpr int WAVES = kProductWaves;
     static constexpr int WN = wave_columns(H, NT, WAVES), WM = WAVES / WN;
-    static constexpr int ROW = stage_row_bytes(KIND);
+    static constexpr int ROW = stage_row_bytes(KIND) * STEPS / 2;
     static constexpr int SA = product_row_stages(H, NT, ROW, STAGES), SB = product_stages(H, NT, ROW, STAGES);
     static constexpr int WTM = H / WM, WTN = NT / WN, TM = WTM / 16, TN = WTN / 16;  // outputs of a wavefront
     static constexpr int SLOTS = TM * TN, HALF = SLOTS / 2;  // matrix instructions of a K step (two a stage); of the last one in front of the hand-over
-    typedef StagedOperand<H, KIND == kWeightGradient> OpA;
-    typedef StagedOperand<NT, KIND == kRowsGradient || KIND == kWeightGradient, ONCE> OpW;
+    typedef StagedOperand<H, KIND == kWeightGradient, false, STEPS> OpA;
+    typedef StagedOperand<NT, KIND == kRowsGradient || KIND == kWeightGradient, ONCE, STEPS> OpW;
     typedef typename std::conditional<MX, StagedScales<H>, NoScales>::type ScA;
     typedef typename std::conditional<MX, StagedScales<NT>, NoScales>::type ScW;
     static constexpr int A_BYTES = OpA::BYTES + ScA::BYTES, W_BYTES = OpW::BYTES + ScW::BYTES;
     static constexpr int LA = OpA::LOADS + ScA::LOADS, LW = OpW::LOADS + ScW::LOADS, LPW = LA + LW;  // loads of a wavefront a stage
     static constexpr int IN_FLIGHT = (SA > SB ? LA : 0) + (SB - 2) * LPW;  // behind the next stage at a hand-over
-    static constexpr int ACC_HALF = 256 / WAVES;
+    // (Few accumulators are ordinary registers: moves from and to the accumulator half are a good part of a short reduction's time.)
+    static constexpr int ACC_HALF = KIND == kWeightGradient && SLOTS <= 16 ? 0 : 256 / WAVES;
     template <typename TO>
     static constexpr int stores() { return TM * TN / (sizeof(TO) == 4 ? 1 : 2); }  // of a lane, by store()
     static_assert(TN % 2 == 0 && TM * 16 * WM == H && TN * 16 * WN == NT, "outputs of a wavefront");
@@ -249,15 +252,15 @@ struct ProductTile {
     static_assert(product_ring_bytes(H, NT, ROW, STAGES) <= kLdsBytes, "LDS of a compute unit");
 
     f32x4_t acc[TM][TN];
-    bf16x8_t fw[2][TN], fa[TM];
-    int sw[2][TN], sa[TM];  // scales (4 bits)
+    bf16x8_t fw[STEPS][TN], fa[TM];
+    int sw[STEPS][TN], sa[TM];  // scales (4 bits)
     f32x4_t sum[TM];        // of the rows over the reduction, where asked for: multiplied by ones
     bf16x8_t ones;
     OpA a;
     OpW w;
     ScA as;
     ScW ws;
-    uint32_t from_a[2], from_w[2], from_as, from_ws;
+    uint32_t from_a[STEPS], from_w[STEPS], from_as, from_ws;
     uint32_t smem_addr;
     int wave;
 
@@ -349,12 +352,13 @@ struct ProductTile {
     //   feed: steps both operands on to the stage that is loaded next.
     //   STREAM: tiles in one stream, STORES of a lane behind each.  A refill is complete in front of the next stage, because behind the last
     //   stage of a tile come its stores, which a load behind them would have to wait for.
-    template <bool NEXT, bool STREAM, int STORES, typename Feed>
+    template <bool NEXT, bool STREAM, int STORES, bool SUMS, typename Feed>
     __device__ __forceinline__ void stage(unsigned ends, bool sums, Feed&& feed)
     {
+        static_assert(STEPS == 2 || STREAM, "a refill is spread over two K steps");
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const bool last = ks == 1;
+        for (int ks = 0; ks < STEPS; ++ks) {
+            const bool last = ks == STEPS - 1;
 #pragma unroll
             for (int m = 0; m < SLOTS; ++m) {
                 const int r = m % TN, b = m / TN;
@@ -366,17 +370,20 @@ struct ProductTile {
                     feed(*this);
                 }
                 multiply(b, r, ks);
-                if (KIND == kWeightGradient && sums && r == TN - 1) mfma_16x16x32<false>(ones, fa[b], sum[b]);
+                if (KIND == kWeightGradient && SUMS && sums && r == TN - 1) mfma_16x16x32<false>(ones, fa[b], sum[b]);
                 __builtin_amdgcn_sched_barrier(0);
-                if (!last) {
+                if constexpr (STEPS == 2) if (!last) {
                     if (r == TN - 1) fetch_a(ra.cur, b, 1);
 #pragma unroll
                     for (int q = 0; q < TN; ++q)
                         if (m == (q * SLOTS / TN + 1 < SLOTS ? q * SLOTS / TN + 1 : SLOTS - 1)) fetch_w(rw.cur, q, 1);
-                } else if (NEXT) {
+                }
+                if (last && NEXT) {
 #pragma unroll
                     for (int q = 0; q < TN; ++q) {
-                        const int p = HALF + 2 * q < SLOTS ? HALF + 2 * q : SLOTS - 1;
+                        const int free = STEPS > 1 ? 0 : (TM - 1) * TN + q;  // (one K step a stage: these registers, too, are in use till then)
+                        const int want = HALF + 2 * q > free ? HALF + 2 * q : free;
+                        const int p = want < SLOTS ? want : SLOTS - 1;
                         if (m == p) fetch_w(rw.nxt, q, 0);
                     }
 #pragma unroll
@@ -428,7 +435,7 @@ struct ProductTile {
     {
         const int wm = wave / WN, wn = wave % WN;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int ks = 0; ks < STEPS; ++ks) {
             from_a[ks] = OpA::fetch_base(wm * WTM, ks);
             from_w[ks] = OpW::fetch_base(wn * WTN, ks);
         }
@@ -468,10 +475,10 @@ struct ProductTile {
             t.step_w();
         };
         for (int kt = 1; kt < nk; ++kt) {
-            stage<true, false, 0>(0u, sums, on);
+            stage<true, false, 0, true>(0u, sums, on);
             next_stage();
         }
-        stage<false, false, 0>(0u, sums, on);
+        stage<false, false, 0, true>(0u, sums, on);
         wait_vmcnt<0>();  // (loads into LDS that nobody waited for)
         pin_accumulators();
     }
@@ -565,15 +572,23 @@ struct ProductTile {
                     }
                 }
                 const int row = wm * WTM + b * 16, col = wn * WTN + r * 16 + in_unit;
+                // Rows that begin anywhere in a line leave lines in part to the next tile: those stay in the L2 until they are whole (weight gradients, us with the
+                // streaming hint and without: fp32, 235 rows, 8 experts of 1240 x 11752 229 and 113, bf16, 291 rows, 15 of 1432 x 2264 44 and 40; of whole
+                // lines, fp32, 16384 rows, 32 of 8192 x 2048 837 and 882).
+                const bool plain = ldo * static_cast<int>(sizeof(TO)) % 128 != 0;
+                auto put = [&](TO* at, uint4 v) {
+                    if (plain) *reinterpret_cast<uint4*>(at) = v;
+                    else store_stream16(reinterpret_cast<uint4*>(at), v);
+                };
                 if constexpr (PAIRS) {
                     uint4 lo, hi;
                     trade(u[0], u[PER - 1], lo, hi);
                     const int row_lo = row + (in16 & 7), col_of = col + (in16 >> 3) * BLOCKS * 16;
                     TO* to = out + row_lo * ldo + col_of;
-                    if (WHOLE || (row_lo < rows && col_of < cols)) store_stream16(reinterpret_cast<uint4*>(to), lo);
-                    if (WHOLE || (row_lo + 8 < rows && col_of < cols)) store_stream16(reinterpret_cast<uint4*>(to + 8 * ldo), hi);
+                    if (WHOLE || (row_lo < rows && col_of < cols)) put(to, lo);
+                    if (WHOLE || (row_lo + 8 < rows && col_of < cols)) put(to + 8 * ldo, hi);
                 } else if (WHOLE || (row + in16 < rows && col < cols)) {
-                    store_stream16(reinterpret_cast<uint4*>(out + (row + in16) * ldo + col), make_uint4(u[0][0], u[0][1], u[0][2], u[0][3]));
+                    put(out + (row + in16) * ldo + col, make_uint4(u[0][0], u[0][1], u[0][2], u[0][3]));
                 }
             }
         }

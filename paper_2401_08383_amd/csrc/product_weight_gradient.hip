@@ -94,19 +94,20 @@ __global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_tiles_kernel(
     t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols, nullptr);
 }
 
-// A stream of tiles, not split.  What the loads know of a tile goes to the multiplication through a queue in the lanes of a few registers.
-template <int H, int NT, int STAGES, typename TO>
-__global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_stream_kernel(const WeightTiles p)
+// A stream of tiles, not split; PER_UNIT workgroups a compute unit.  What the loads know of a tile goes to the multiplication through a queue in the lanes of a few registers.
+template <int H, int NT, int STAGES, int STEPS, int PER_UNIT, bool SUMS, typename TO>
+__global__ __launch_bounds__(kProductWaves * kWave, PER_UNIT) void weight_stream_kernel(const WeightTiles p)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    typedef ProductTile<H, NT, kWeightGradient, false, STAGES> T;
+    typedef ProductTile<H, NT, kWeightGradient, false, STAGES, STEPS> T;
+    constexpr int DEPTH = 32 * STEPS;  // rows a stage
     constexpr int STORES = T::template stores<TO>();
     static_assert(T::SA == T::SB, "both operands are loaded of the same stage");
     const int64_t N = p.N, K = p.K;
     WeightOrder<H, NT> order;
     order.begin(p);
     const unsigned step_rank = uniform_udiv(gridDim.x, order.tiles), step_tile = gridDim.x - step_rank * order.tiles;
-    const unsigned index = blockIdx.x % kXcdCount * kGroupTiles + blockIdx.x / kXcdCount, experts = static_cast<unsigned>(p.E_local);
+    const unsigned index = blockIdx.x % kXcdCount * (gridDim.x / kXcdCount) + blockIdx.x / kXcdCount, experts = static_cast<unsigned>(p.E_local);
     unsigned rank = uniform_udiv(index, order.tiles), tile = index - rank * order.tiles;
     int queue_stages = 0, queue_expert = 0, queue_row = 0, queue_col = 0;
     unsigned in = 0u, out = 0u;  // tiles that have entered it and left
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_stream_kernel
         t.a.begin(p.dy + begin * N + row0, N * 2, min(H, p.N - row0), n, 0, t.wave);
         t.w.begin(p.x + begin * K + col0, K * 2, min(NT, p.K - col0), n, 0, t.wave);
         const bool mine = lane_id() == static_cast<int>(in % kWave);
-        queue_stages = mine ? (n + 63) / 64 : queue_stages;
+        queue_stages = mine ? (n + DEPTH - 1) / DEPTH : queue_stages;
         queue_expert = mine ? e : queue_expert;
         queue_row = mine ? row0 : queue_row;
         queue_col = mine ? col0 : queue_col;
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_stream_kernel
     auto store = [&](int e, int row0, int col0) {
         const int rows = min(H, p.N - row0), cols = min(NT, p.K - col0);
         const int64_t result = e * N + row0;
-        if (p.sums != nullptr && col0 == 0) t.store_sums(static_cast<TO*>(p.sums) + result, rows);
+        if (SUMS && col0 == 0) t.store_sums(static_cast<TO*>(p.sums) + result, rows);
         t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols, nullptr);
         return rows == H && cols == NT ? 1u : 0u;
     };
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_stream_kernel
         const int row0 = wave_read_lane(queue_row, out % kWave), col0 = wave_read_lane(queue_col, out % kWave);
         t.clear();
         for (int kt = 0; kt < stages; ++kt) {
-            t.template stage<true, true, STORES>(ends, p.sums != nullptr && col0 == 0, feed);
+            t.template stage<true, true, STORES, SUMS>(ends, col0 == 0, feed);
             t.next_stage();
             ends <<= 1;
         }
@@ -175,7 +176,9 @@ __global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_stream_kernel
 
 static int64_t tiles_in(int64_t n, int64_t k, int64_t size) { return ((n + size - 1) / size) * ((k + size - 1) / size); }
 
-// Large tiles where they fill the compute units twice and their reductions are long enough to be worth it.
+// Large tiles where they fill the compute units twice and their reductions are long enough to be worth it.  32 experts of 2048 x 1024, us as large tiles and
+// as a stream of small ones: 128 rows an expert 54.5 and 49.0, 200 61.1 and 57.4, 256 65.9 and 64.8, 512 98.7 and 119.3 (results in fp32 76.5 and 62.7, 83.6 and
+// 74.4, 87.5 and 82.8, 121.3 and 151.2).
 static bool large_tiles(int64_t A, int n, int k, int E_local)
 {
     return E_local * tiles_in(n, k, 256) >= 2 * kComputeUnits && A >= 256 * E_local;
@@ -191,21 +194,31 @@ int weight_gradient_splits(int64_t A, int n, int k, int E_local)
     return static_cast<int>(s < 2 ? 1 : (s > kMostSplits ? kMostSplits : s));
 }
 
-// STAGES: of a stream's ring (0: a workgroup a tile).
-template <int H, int NT, int STAGES, typename TO>
-static int launch_weight_as(const WeightTiles& p, hipStream_t stream)
+static int launch_weight_kernel(void (*kern)(WeightTiles), int64_t grid, size_t lds, std::atomic<uint64_t>& allowed, const WeightTiles& p, hipStream_t stream)
 {
-    constexpr size_t lds = product_ring_bytes(H, NT, 128, STAGES > 0 ? STAGES : 8);
-    const int64_t tiles = static_cast<int64_t>((p.N + H - 1) / H) * ((p.K + NT - 1) / NT), groups = (tiles * p.E_local * p.splits + kGroupTiles - 1) / kGroupTiles;
-    const int64_t grid = STAGES > 0 ? kComputeUnits : (groups + kXcdCount - 1) / kXcdCount * kXcdCount * kGroupTiles;
-    if (tiles >= kMostTiles || grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
-    void (*kern)(WeightTiles);
-    if constexpr (STAGES > 0) kern = weight_stream_kernel<H, NT, STAGES, TO>;
-    else kern = weight_tiles_kernel<H, NT, TO>;
-    static std::atomic<uint64_t> allowed{0};
     if (int rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, "moe_grouped_product_dw")) return rc;
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(kProductWaves * kWave), lds, stream, p);
     return EXF_OK;
+}
+static int64_t tiles_of(const WeightTiles& p, int H, int NT) { return static_cast<int64_t>((p.N + H - 1) / H) * ((p.K + NT - 1) / NT); }
+
+template <int H, int NT, typename TO>
+static int launch_weight_as(const WeightTiles& p, hipStream_t stream)
+{
+    const int64_t tiles = tiles_of(p, H, NT), groups = (tiles * p.E_local * p.splits + kGroupTiles - 1) / kGroupTiles;
+    const int64_t grid = (groups + kXcdCount - 1) / kXcdCount * kXcdCount * kGroupTiles;
+    if (tiles >= kMostTiles || grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
+    static std::atomic<uint64_t> allowed{0};
+    return launch_weight_kernel(weight_tiles_kernel<H, NT, TO>, grid, product_ring_bytes(H, NT, 128), allowed, p, stream);
+}
+template <int H, int NT, int STAGES, int STEPS, int PER_UNIT, typename TO>
+static int launch_weight_stream(const WeightTiles& p, hipStream_t stream)
+{
+    constexpr size_t lds = product_ring_bytes(H, NT, 64 * STEPS, STAGES);
+    if (tiles_of(p, H, NT) >= kMostTiles) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
+    static std::atomic<uint64_t> allowed{0}, allowed_sums{0};
+    if (p.sums != nullptr) return launch_weight_kernel(weight_stream_kernel<H, NT, STAGES, STEPS, PER_UNIT, true, TO>, PER_UNIT * kComputeUnits, lds, allowed_sums, p, stream);
+    return launch_weight_kernel(weight_stream_kernel<H, NT, STAGES, STEPS, PER_UNIT, false, TO>, PER_UNIT * kComputeUnits, lds, allowed, p, stream);
 }
 
 template <typename TO>
@@ -215,11 +228,16 @@ static int launch_weight_tiles(const WeightGradient& g, hipStream_t stream)
     float* parts = static_cast<float*>(g.workspace);
     const int64_t each = static_cast<int64_t>(g.E_local) * g.N * g.K, sums = static_cast<int64_t>(g.E_local) * g.N;
     WeightTiles p{static_cast<const bf16_t*>(g.dy), static_cast<const bf16_t*>(g.x), g.offsets, g.dw, g.db, g.max_rows, g.N, g.K, g.E_local, splits};
-    if (large_tiles(g.max_rows, g.N, g.K, g.E_local)) return launch_weight_as<256, 256, 0, TO>(p, stream);
-    if (splits == 1) return launch_weight_as<128, 128, 4, TO>(p, stream);
+    if (large_tiles(g.max_rows, g.N, g.K, g.E_local)) return launch_weight_as<256, 256, TO>(p, stream);
+    if (splits == 1) {
+        // Stages of 32 rows, four in a ring, or of 64, two: the same, us: 16 rows an expert 29.8 and 32.5, 32 31.9 and 35.4, 64 36.8 and 37.2, 128 49.0 and
+        // 49.5, 200 60.8 and 57.4, 256 69.8 and 64.8.  (One workgroup a compute unit with a ring twice as deep: 42.7, 42.9, 48.1, 59.7, 72.9, 82.4.)
+        if (g.max_rows <= 128ll * g.E_local) return launch_weight_stream<128, 128, 4, 1, 2, TO>(p, stream);
+        return launch_weight_stream<128, 128, 2, 2, 2, TO>(p, stream);
+    }
     p.out = parts;
     if (p.sums != nullptr) p.sums = parts + splits * each;
-    if (int rc = launch_weight_as<128, 128, 0, float>(p, stream)) return rc;
+    if (int rc = launch_weight_as<128, 128, float>(p, stream)) return rc;
     return launch_join_parts(parts, each, g.dw, parts + splits * each, g.db != nullptr ? sums : 0, g.db, splits, sizeof(TO) == 4 ? EXF_F32 : EXF_BF16, stream);
 }
 
