@@ -408,18 +408,44 @@ struct ProductTile {
         }
     }
 
-    __device__ __forceinline__ void clear()
+    // The accumulators begin with the bias of their columns, or with zeros.  The bias comes on the scalar path: a load to vector registers would be awaited
+    // together with all stages of the ring.
+    __device__ __forceinline__ void begin_sums(const bf16_t* bias, int cols)
     {
 #pragma unroll
-        for (int b = 0; b < TM; ++b)
+        for (int r = 0; r < TN; ++r) {
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#if defined(__HIP_DEVICE_COMPILE__)
+            const int quad = lane_id() >> 4;
+            if (bias != nullptr) {
+                uint32_t pair[2][2];  // of this lane's columns, if they lie in the lower or in the upper eight of 16
 #pragma unroll
-            for (int r = 0; r < TN; ++r) acc[b][r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int h = 0; h < 2; ++h) {
+                    const int col = __builtin_amdgcn_readfirstlane(min(wave % WN * WTN + r * 16 + h * 8, cols - 8));
+                    const auto* at = (const __attribute__((address_space(4))) uint32_t*)uniform_ptr(reinterpret_cast<const unsigned char*>(bias + col));
+                    uint32_t d[4] = {at[0], at[1], at[2], at[3]};
+                    asm volatile("" : "+s"(d[0]), "+s"(d[1]), "+s"(d[2]), "+s"(d[3]));
+                    pair[h][0] = (quad & 1) != 0 ? d[2] : d[0];
+                    pair[h][1] = (quad & 1) != 0 ? d[3] : d[1];
+                }
+                const uint32_t x = quad > 1 ? pair[1][0] : pair[0][0], y = quad > 1 ? pair[1][1] : pair[0][1];
+                v = f32x4_t{__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u), __uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u)};
+            }
+#endif
+#pragma unroll
+            for (int b = 0; b < TM; ++b) acc[b][r] = v;
+        }
         if constexpr (KIND == kWeightGradient) {
 #pragma unroll
             for (int b = 0; b < TM; ++b) sum[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             ones = __builtin_bit_cast(bf16x8_t, u32x4_v{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
             asm volatile("" : "+v"(ones));  // (in its registers from here on: a matrix instruction must not follow its operand's write at once)
         }
+        pin_registers();
+    }
+    __device__ __forceinline__ void clear()
+    {
+        begin_sums(nullptr, 0);
         pin_accumulators();
     }
 
@@ -430,8 +456,9 @@ struct ProductTile {
     }
     // The ring is filled as if the stage before the first one had handed over (all but the late loads of its last stage), and the first operands
     // are fetched.
-    template <bool STREAM, typename FeedA, typename FeedW>
-    __device__ __forceinline__ void begin_ring(FeedA&& feed_a, FeedW&& feed_w)
+    //   meanwhile: what is done while the first loads are on their way.
+    template <bool STREAM, typename FeedA, typename FeedW, typename Meanwhile>
+    __device__ __forceinline__ void begin_ring(FeedA&& feed_a, FeedW&& feed_w, Meanwhile&& meanwhile)
     {
         const int wm = wave / WN, wn = wave % WN;
 #pragma unroll
@@ -454,6 +481,7 @@ struct ProductTile {
                 if (i >= LW && (s < SA - 1 || i < EARLY)) issue_a(static_cast<uint32_t>(s * A_BYTES), i >= LW ? i - LW : 0);
             }
         }
+        meanwhile();
         wait_vmcnt<(SB - 2) * LW + (SA - 2) * LA + EARLY>();  // the first stage is complete when only what follows it is in flight
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -466,10 +494,10 @@ struct ProductTile {
     }
 
     // All of a reduction of nk stages, at least one.  Behind it the accumulators hold the sums.
-    __device__ __forceinline__ void reduce(int nk, bool sums = false)
+    __device__ __forceinline__ void reduce(int nk, bool sums = false, const bf16_t* bias = nullptr, int cols = 0)
     {
-        begin_ring<false>([](ProductTile& t) { t.step_a(); }, [](ProductTile& t) { t.step_w(); });
-        clear();
+        begin_ring<false>([](ProductTile& t) { t.step_a(); }, [](ProductTile& t) { t.step_w(); }, [&]() { begin_sums(bias, cols); });
+        pin_accumulators();
         auto on = [](ProductTile& t) {
             t.step_a();
             t.step_w();
@@ -483,12 +511,10 @@ struct ProductTile {
         pin_accumulators();
     }
 
-    // The accumulators are there before an instruction reads them, and the last one is done before they are read (the
-    // compiler sees neither).
-    __device__ __forceinline__ void pin_accumulators()
+    // (the compiler sees neither that the matrix instructions read the accumulators nor that they write them)
+    __device__ __forceinline__ void pin_registers()
     {
 #if defined(__HIP_DEVICE_COMPILE__)
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
         for (int b = 0; b < TM; ++b)
 #pragma unroll
@@ -500,6 +526,14 @@ struct ProductTile {
 #pragma unroll
             for (int b = 0; b < TM; ++b) asm volatile("" : "+v"(sum[b]));
         }
+#endif
+    }
+    // The accumulators are there before an instruction reads them, and the last one is done before they are read.
+    __device__ __forceinline__ void pin_accumulators()
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        pin_registers();
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #endif
     }
@@ -518,34 +552,25 @@ struct ProductTile {
         hi = make_uint4(h[0], h[1], h[2], h[3]);
     }
 
-    // out[row][col] (+ bias[col]) of the tile's rows and columns that there are, leading dimension ldo.  A lane holds, of the 16 x 16 block
+    // out[row][col] of the tile's rows and columns that there are, leading dimension ldo.  A lane holds, of the 16 x 16 block
     // (b, r), row lane%16 and columns 4 (lane/16) .. +3: in fp32 16 bytes, 64 of the row with the other lanes.  bf16: of two
     // blocks side by side the odd rows of 16 lanes of the first trade with the even ones of the second, and every lane has
     // eight consecutive columns of one block.
-    //   A whole tile's stores have no condition, and without a bias nothing is added: where a wavefront is alone on its SIMD every
-    //   instruction here is time.
+    //   A whole tile's stores have no condition: where a wavefront is alone on its SIMD every instruction here is time.
     template <typename TO>
-    __device__ __forceinline__ void store(TO* out, int64_t ldo, int rows, int cols, const bf16_t* bias) const
+    __device__ __forceinline__ void store(TO* out, int64_t ldo, int rows, int cols) const
     {
-        const bool whole = rows == H && cols == NT;
-        if (bias != nullptr) store_as<TO, true, false>(out, ldo, rows, cols, bias);
-        else if (whole) store_as<TO, false, true>(out, ldo, rows, cols, nullptr);
-        else store_as<TO, false, false>(out, ldo, rows, cols, nullptr);
+        if (rows == H && cols == NT) store_as<TO, true>(out, ldo, rows, cols);
+        else store_as<TO, false>(out, ldo, rows, cols);
     }
-    template <typename TO, bool BIAS, bool WHOLE>
-    __device__ __forceinline__ void store_as(TO* out, int64_t ldo, int rows, int cols, const bf16_t* bias) const
+    template <typename TO, bool WHOLE>
+    __device__ __forceinline__ void store_as(TO* out, int64_t ldo, int rows, int cols) const
     {
         constexpr int BLOCKS = sizeof(TO) == 4 ? 1 : 2;                // of a unit
         constexpr bool PAIRS = TN % (2 * BLOCKS) == 0;
         constexpr int PER = PAIRS ? 2 : 1;                              // units of a store
         const int quad = lane_id() >> 4, in16 = lane_id() & 15, wm = wave / WN, wn = wave % WN;
         const int in_unit = BLOCKS == 1 ? quad * 4 : (quad & 1) * 16 + (quad >> 1) * 8;
-        float bias_v[TN][4];
-#pragma unroll
-        for (int r = 0; r < TN; ++r)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) bias_v[r][v] = BIAS ? bf16_to_f32(bias[min(wn * WTN + r * 16 + quad * 4 + v, cols - 1)]) : 0.0f;
-        auto value = [&](int b, int r, int v) { return BIAS ? acc[b][r][v] + bias_v[r][v] : acc[b][r][v]; };
         // (row by row: rows are often a power of two bytes apart, and column by column all compute units would write to few memory channels at a time)
 #pragma unroll
         for (int b = 0; b < TM; ++b) {
@@ -556,7 +581,7 @@ struct ProductTile {
                 for (int i = 0; i < PER; ++i) {
                     if constexpr (BLOCKS == 1) {
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) u[i][v] = __float_as_uint(value(b, r + i, v));
+                        for (int v = 0; v < 4; ++v) u[i][v] = __float_as_uint(acc[b][r + i][v]);
                     } else {
                         uint32_t p[2][2];
 #pragma unroll
@@ -564,7 +589,7 @@ struct ProductTile {
 #pragma unroll
                             for (int v = 0; v < 2; ++v) {
                                 const int c = r + 2 * i + q;
-                                p[q][v] = pack_bf16x2(value(b, c, 2 * v), value(b, c, 2 * v + 1));
+                                p[q][v] = pack_bf16x2(acc[b][c][2 * v], acc[b][c][2 * v + 1]);
                             }
                         const auto s0 = __builtin_amdgcn_permlane16_swap(p[0][0], p[1][0], false, false);
                         const auto s1 = __builtin_amdgcn_permlane16_swap(p[0][1], p[1][1], false, false);
@@ -648,8 +673,8 @@ __device__ __forceinline__ void rows_tile(const RowsTiles& p, const Tile2D& tile
         t.as.begin(p.row_scale + static_cast<int64_t>(tile.row_begin) * 8, p.max_rows, rows, nk, k0, t.wave);
         t.ws.begin(p.weight_scale + (tile.expert * N + tile.n0) * 8, p.E_local * N, cols, nk, k0, t.wave);
     }
-    t.reduce(nk);
-    t.store(p.out + tile.row_begin * N + tile.n0, N, rows, cols, p.bias != nullptr ? p.bias + tile.expert * N + tile.n0 : nullptr);
+    t.reduce(nk, false, p.bias != nullptr ? p.bias + tile.expert * N + tile.n0 : nullptr, cols);
+    t.store(p.out + tile.row_begin * N + tile.n0, N, rows, cols);
 }
 
 // A whole tile of 320 rows and 256 columns in 4 bits has no registers left for the scales (it would spill 44 of them): there tiles take one

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(kProductWaves * kWave, 1) void weight_tiles_kernel(
         t.clear();
     }
     if (sums) t.store_sums(static_cast<TO*>(p.sums) + result, rows);
-    t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols, nullptr);
+    t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols);
 }
 
 // A stream of tiles, not split; PER_UNIT workgroups a compute unit.  What the loads know of a tile goes to the multiplication through a queue in the lanes of a few registers.
@@ -146,10 +146,10 @@ __global__ __launch_bounds__(kProductWaves * kWave, PER_UNIT) void weight_stream
         const int rows = min(H, p.N - row0), cols = min(NT, p.K - col0);
         const int64_t result = e * N + row0;
         if (SUMS && col0 == 0) t.store_sums(static_cast<TO*>(p.sums) + result, rows);
-        t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols, nullptr);
+        t.store(static_cast<TO*>(p.out) + result * K + col0, K, rows, cols);
         return rows == H && cols == NT ? 1u : 0u;
     };
-    if (enter()) t.template begin_ring<true>(feed, [](T&) {});
+    if (enter()) t.template begin_ring<true>(feed, [](T&) {}, []() {});
     unsigned ends = 0u;
     for (; out != in; ++out) {
         const int stages = wave_read_lane(queue_stages, out % kWave), e = wave_read_lane(queue_expert, out % kWave);
