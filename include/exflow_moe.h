@@ -244,7 +244,7 @@ int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorted, const in
  * Shapes: rows >= 0, k >= 32 and k % 32 == 0.  q and scale must be 16-byte aligned.
  * ------------------------------------------------------------------------------------- */
 #define EXF_MX4_BLOCK 32
-#define EXF_MX4_INLINE_ROWS 8  /* up to so many rows moe_grouped_product_mx4 quantises as it goes, without a workspace */
+#define EXF_MX4_INLINE_ROWS 8  /* up to so many rows moe_grouped_product_mx4 needs no workspace */
 size_t mx4_scale_bytes(int64_t rows, int k);
 int mx4_quantize(const void* x, int64_t rows, int k, int dt, uint8_t* q, uint8_t* scale, void* stream);
 int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t rows, int k, int dt, void* out, void* stream);
@@ -253,13 +253,13 @@ int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t rows, int k, 
  * moe_grouped_product_mx4 — moe_grouped_product of operands held as mx4_quantize writes them.
  *   w [E_local,n,k/2], w_scale: E_local*n rows of k.
  *   x_scale != NULL: x_sorted [A,k/2], x_scale: A rows of k.
- *   x_scale == NULL: x_sorted [A,k] dt; the call quantises it into the workspace.
+ *   x_scale == NULL: x_sorted [A,k] dt; the call quantises it (the same values).
  *   bias [E_local,n] dt or NULL;  y_sorted [A,n] dt.  Sums in fp32, rounded once.
  * Shapes: 0 <= A < 2^31; k >= 32, k % 32 == 0; n >= 1, a multiple of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
- * workspace: moe_grouped_product_mx4_workspace_bytes(A, k) bytes with x_scale == NULL, 0 for A <= EXF_MX4_INLINE_ROWS; otherwise none
- * (NULL).
+ * workspace: moe_grouped_product_mx4_workspace_bytes(A, n, k) bytes with x_scale == NULL (0 for small products, which quantise the rows as
+ * they go, and whenever A <= EXF_MX4_INLINE_ROWS), otherwise none (NULL).
  * ------------------------------------------------------------------------------------- */
-size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k);
+size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int n, int k);
 int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_scale, const int32_t* expert_offsets, const uint8_t* w,
                             const uint8_t* w_scale, const void* bias, int64_t A, int n, int k, int E_local, int dt,
                             void* y_sorted, void* workspace, size_t workspace_bytes, void* stream);

@@ -55,7 +55,7 @@ SIGNATURES = {
     "mx4_scale_bytes": (_sz, [_i64, _i]),
     "mx4_quantize": (_i, [_vp, _i64, _i, _i, _vp, _vp, _vp]),
     "mx4_dequantize": (_i, [_vp, _vp, _i64, _i, _i, _vp, _vp]),
-    "moe_grouped_product_mx4_workspace_bytes": (_sz, [_i64, _i]),
+    "moe_grouped_product_mx4_workspace_bytes": (_sz, [_i64, _i, _i]),
     "moe_grouped_product_mx4": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i, _vp, _vp, _sz, _vp]),
     "moe_layer_forward": (_i, [_vp, _vp]),
     "affinity_histogram_workspace_bytes": (_sz, [_i, _i64, _i]),
@@ -438,7 +438,8 @@ def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, 
         bias = _expect("bias", bias, (E, n), dtype, dev).data_ptr()
     out = torch.empty((A, n), dtype=dtype, device=rows.device) if out is None else _expect("out", out, (A, n), dtype, dev)
     if workspace is None and not held and A > EXF_MX4_INLINE_ROWS:
-        workspace = _workspace(lib().moe_grouped_product_mx4_workspace_bytes(A, k), rows.device)
+        need = lib().moe_grouped_product_mx4_workspace_bytes(A, n, k)
+        workspace = _workspace(need, rows.device) if need else None
     rc = lib().moe_grouped_product_mx4(rows.data_ptr(), x_scale, expert_offsets.data_ptr(), w.q.data_ptr(), w.scale.data_ptr(), bias, A, n, k, E, code,
                                        out.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
     if rc:

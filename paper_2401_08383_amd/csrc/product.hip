@@ -126,9 +126,9 @@ extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorte
     return rc == EXF_OK ? check_launch(fn) : rc;
 }
 
-extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int k)
+extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int n, int k)
 {
-    if (A <= EXF_MX4_INLINE_ROWS || k < 1) return 0;
+    if (A < 0 || n < 1 || k < 1 || exf::mx4_product_is_small(A, n, k)) return 0;
     return exf::align_up(static_cast<size_t>(A) * k / 2, 256) + exf::align_up(mx4_scale_bytes(A, k), 256);
 }
 
@@ -152,7 +152,7 @@ extern "C" int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_sc
     EXF_CHECK_ALIGNED(fn, y_sorted);
     if (x_scale != nullptr) EXF_CHECK_ALIGNED(fn, x_scale);
     if (bias != nullptr) EXF_CHECK_ALIGNED(fn, bias);
-    const size_t need = x_scale == nullptr ? moe_grouped_product_mx4_workspace_bytes(A, k) : 0;
+    const size_t need = x_scale == nullptr ? moe_grouped_product_mx4_workspace_bytes(A, n, k) : 0;
     if (need > 0) {
         EXF_CHECK_PTR(fn, workspace);
         EXF_CHECK_ALIGNED(fn, workspace);
@@ -177,8 +177,8 @@ extern "C" int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_sc
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     int rc;
-    if (A <= EXF_MX4_INLINE_ROWS) {
-        rc = launch_mx4_few_rows(p, dt, s);
+    if (mx4_product_is_small(A, n, k)) {
+        rc = launch_mx4_small(p, dt, s);
     } else if (dt == EXF_BF16) {
         rc = launch_mx4_tiles({p.rows, expert_offsets, w, static_cast<const bf16_t*>(bias), static_cast<bf16_t*>(y_sorted), p.row_scale, w_scale, static_cast<int>(A), k, n, E_local}, s);
     } else {

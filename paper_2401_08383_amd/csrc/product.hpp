@@ -26,7 +26,7 @@ struct WeightGradient {
 };
 // out[rows of e, N] = rows[rows of e, K] W_e^T (+ bias_e) of operands held by mx4_quantize; scales: [ceil(K/256), rows, 8].
 struct Mx4Product {
-    const uint8_t* rows;      // (few rows: of the result's type where row_scale is null)
+    const uint8_t* rows;
     const uint8_t* row_scale;
     const int32_t* offsets;
     const uint8_t* weight;
@@ -43,7 +43,9 @@ int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local);
 // The sums of `splits` parts of n (and of m) values each, in order, in the type `dt`.
 int launch_join_parts(const float* parts, int64_t n, void* out, const float* more, int64_t m, void* more_out, int splits, int dt, hipStream_t stream);
 int launch_mx4_product(const Mx4Product& p, hipStream_t stream);  // result in fp32
-int launch_mx4_few_rows(const Mx4Product& p, int dt, hipStream_t stream);  // at most EXF_MX4_INLINE_ROWS
+// Small products: one launch, rows quantised where they are needed (rows of the result's type where row_scale is null).
+bool mx4_product_is_small(int64_t A, int n, int k);
+int launch_mx4_small(const Mx4Product& p, int dt, hipStream_t stream);
 
 // Bytes [a, a + n) and [b, b + m) overlap (nothing overlaps a null pointer).
 inline bool overlap(const void* a, size_t n, const void* b, size_t m)

@@ -75,21 +75,28 @@ __global__ __launch_bounds__(64) void mx4_rows_kernel(const Mx4Product p, int co
         }
 }
 
-// ---------------------------------------------------------------------------- few rows
-// At most EXF_MX4_INLINE_ROWS rows in all: a workgroup has 16 columns of one expert, its four wavefronts share the reduction and join their sums through
-// LDS.  A lane's operand is one block of one row, so rows that are not held in 4 bits are quantised where they are needed, by
-// the lane that needs them, without a word to any other lane: one launch instead of two, and no workspace.
+// ---------------------------------------------------------------------------- small products
+// A workgroup has 16 rows and 16 columns of one expert, its four wavefronts share the reduction and join their sums through LDS.  A lane's operand is
+// one block of one row, so rows that are not held in 4 bits are quantised where they are needed, by the lane that needs them, without a
+// word to any other lane: one launch instead of two, and no workspace.
+//   Every 16 columns quantise the rows again, so the products are small ones, of at most kSmallTurns rows times reduction times column tiles.  One call as
+// this and as two launches with a workspace, us: 490 rows over 2 of 128 x 288 8.5 and 13.0, 256 over 8 of 1024 x 1024 11.3 and 13.3, 64 over 8 of
+// 1024 x 4096 (2^24) 11.1 and 14.0, of 4096 x 1024 (2^24) 14 and 14, 128 of these (2^25) 20.6 and 13.0.
+constexpr int64_t kSmallTurns = 1ll << 24;
+bool mx4_product_is_small(int64_t A, int n, int k) { return A <= EXF_MX4_INLINE_ROWS || (n + 15ll) / 16 <= kSmallTurns / (A * k); }
+
 constexpr int kFewWaves = 4, kFewAhead = 2;
 template <bool BF16, bool HELD>
-__global__ __launch_bounds__(kFewWaves* kWave) void mx4_few_rows_kernel(const Mx4Product p, int col_tiles)
+__global__ __launch_bounds__(kFewWaves* kWave) void mx4_small_kernel(const Mx4Product p, int col_tiles)
 {
     __shared__ f32x4_t part[kFewWaves][kWave];
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
-    unsigned long long busy = __ballot(range.hi > range.lo);
-    for (unsigned skip = blockIdx.x / static_cast<unsigned>(col_tiles); skip > 0; --skip) busy &= busy - 1;
-    if (busy == 0ull) return;
-    const int e = __builtin_ctzll(busy), col0 = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles)) * 16;
-    const int lo = wave_read_lane(range.lo, e), rows = wave_read_lane(range.hi, e) - lo;
+    const int tiles = (range.hi - range.lo + 15) / 16, upto = wave_inclusive_scan(tiles);
+    const int row_tile = static_cast<int>(blockIdx.x / static_cast<unsigned>(col_tiles)), col0 = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles)) * 16;
+    const unsigned long long owner = __ballot(row_tile < upto);
+    if (owner == 0ull) return;
+    const int e = __builtin_ctzll(owner), lo = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * 16;
+    const int rows = min(16, wave_read_lane(range.hi, e) - lo);
     const int lane = lane_id(), in16 = lane & 15, quad = lane >> 4, wave = threadIdx.x / kWave;
     const int64_t N = p.N, weight_rows = p.E_local * N, half = p.K / 2;
     const int64_t col = e * N + min(col0 + in16, p.N - 1), row = lo + min(in16, rows - 1);
@@ -156,12 +163,12 @@ __global__ __launch_bounds__(kFewWaves* kWave) void mx4_few_rows_kernel(const Mx
     }
 }
 
-int launch_mx4_few_rows(const Mx4Product& p, int dt, hipStream_t stream)
+int launch_mx4_small(const Mx4Product& p, int dt, hipStream_t stream)
 {
-    const int64_t cols = (p.N + 15) / 16, grid = (p.max_rows < p.E_local ? p.max_rows : p.E_local) * cols;
+    const int64_t cols = (p.N + 15) / 16, grid = (p.max_rows / 16 + (p.max_rows < p.E_local ? p.max_rows : p.E_local)) * cols;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_mx4: too many tiles");
     auto run = [&](auto bf16, auto held) {
-        hipLaunchKernelGGL((mx4_few_rows_kernel<decltype(bf16)::value, decltype(held)::value>), dim3(static_cast<unsigned>(grid)), dim3(kFewWaves * kWave), 0, stream, p,
+        hipLaunchKernelGGL((mx4_small_kernel<decltype(bf16)::value, decltype(held)::value>), dim3(static_cast<unsigned>(grid)), dim3(kFewWaves * kWave), 0, stream, p,
                            static_cast<int>(cols));
     };
     const std::true_type yes;

@@ -88,13 +88,16 @@ def test_blocks():
 
 def test_workspaces():
     lib = exf.lib()
-    need = lib.moe_grouped_product_mx4_workspace_bytes(1000, 96)
+    need = lib.moe_grouped_product_mx4_workspace_bytes(1000, 4096, 96)
     assert need >= 1000 * 48 + 1000 * 8
-    assert _mx4(xs=None, A=1000, k=96) == B.EXF_ERR_NULL_PTR
-    assert _mx4(xs=None, A=1000, k=96, work=_p(8), size=need - 1) == B.EXF_ERR_WORKSPACE_TOO_SMALL
-    assert _mx4(xs=None, A=1000, k=96, work=ODD, size=need) == B.EXF_ERR_MISALIGNED
-    assert _mx4(xs=None, A=1000, k=96, work=_p(0), size=need) == B.EXF_ERR_BAD_SHAPE  # over the rows
-    assert lib.moe_grouped_product_mx4_workspace_bytes(-1, 96) == 0
+    big = dict(xs=None, A=1000, n=4096, k=96)
+    assert _mx4(**big) == B.EXF_ERR_NULL_PTR
+    assert _mx4(**big, work=_p(8), size=need - 1) == B.EXF_ERR_WORKSPACE_TOO_SMALL
+    assert _mx4(**big, work=ODD, size=need) == B.EXF_ERR_MISALIGNED
+    assert _mx4(**big, work=_p(0), size=need) == B.EXF_ERR_BAD_SHAPE  # over the rows
+    assert lib.moe_grouped_product_mx4_workspace_bytes(-1, 64, 96) == 0
+    assert lib.moe_grouped_product_mx4_workspace_bytes(B.EXF_MX4_INLINE_ROWS, 1 << 20, 1 << 14) == 0  # whatever the weights
+    assert lib.moe_grouped_product_mx4_workspace_bytes(100, 64, 96) == 0
     for dt in (B.EXF_F32, B.EXF_BF16):
         need = lib.moe_grouped_product_dw_workspace_bytes(1 << 20, 64, 64, 1, dt)
         if need:
