@@ -61,6 +61,7 @@ extern "C" {
 #define EXF_MAX_TOPK 2
 #define EXF_DISPATCH_STATIC_MAX_ASSIGNMENTS (1ll << 20)  /* largest T*k of moe_dispatch_static */
 #define EXF_MAX_TRACE_LAYERS 256
+#define EXF_MAX_PRODUCT_WIDTH (1 << 21)  /* n and k of moe_grouped_product and its kin */
 
 /* Library version (major*10000 + minor*100 + patch). */
 int exf_version(void);
@@ -208,15 +209,14 @@ int moe_combine(const void* y_sorted, const int32_t* sorted_of_src, const float*
  *   dx[s][u]    = sum_v dy[s][v] * w[e][v][u]                       moe_grouped_product_dx
  *   dw[e][v][u] = sum_s dy[s][v] * x[s][u]                          moe_grouped_product_dw
  *   db[e][v]    = sum_s dy[s][v]
- * Rows outside all experts' ranges are neither read nor written; dw and db of an expert without rows are zero.  Each row's
- * result depends on that row and its expert alone, and every sum has an order that depends on the sizes and the
- * offsets only: the same call gives the same bits.
+ * Rows outside all experts' ranges are neither read nor written; dw and db of an expert without rows are zero.  The order of
+ * every sum depends on the sizes and the offsets only: the same call gives the same bits.
  *
  *   x_sorted, dx_sorted [A,k] dt;  y_sorted, dy_sorted [A,n] dt;  w [E_local,n,k] dt;  bias [E_local,n] dt or NULL;
  *   dw [E_local,n,k], db [E_local,n] (NULL: not wanted) of type grad_dt, EXF_F32 or dt, overwritten, not accumulated.
  *   A must be an upper bound on expert_offsets[E_local].  Outputs must not overlap inputs.
  * All sums are kept in fp32 and rounded once.
- * Shapes: 0 <= A < 2^31; n, k >= 1, multiples of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
+ * Shapes: 0 <= A < 2^31; 1 <= n, k <= EXF_MAX_PRODUCT_WIDTH, multiples of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
  * workspace: moe_grouped_product_dw_workspace_bytes(A, n, k, E_local, dt) bytes (partial sums of a long reduction).
  * ------------------------------------------------------------------------------------- */
 int moe_grouped_product(const void* x_sorted, const int32_t* expert_offsets, const void* w, const void* bias, int64_t A,
@@ -255,7 +255,7 @@ int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t rows, int k, 
  *   x_scale != NULL: x_sorted [A,k/2], x_scale: A rows of k.
  *   x_scale == NULL: x_sorted [A,k] dt; the call quantises it (the same values).
  *   bias [E_local,n] dt or NULL;  y_sorted [A,n] dt.  Sums in fp32, rounded once.
- * Shapes: 0 <= A < 2^31; k >= 32, k % 32 == 0; n >= 1, a multiple of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
+ * Shapes: as moe_grouped_product, and k % 32 == 0.
  * workspace: moe_grouped_product_mx4_workspace_bytes(A, n, k) bytes with x_scale == NULL (0 for small products, which quantise the rows as
  * they go, and whenever A <= EXF_MX4_INLINE_ROWS), otherwise none (NULL).
  * ------------------------------------------------------------------------------------- */

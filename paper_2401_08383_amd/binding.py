@@ -283,6 +283,17 @@ def _expect(name, t, shape, dtype, dev):
     _bad(f"{name} must be contiguous and on device {dev}")
 
 
+_INT32, _UINT8 = torch.int32, torch.uint8
+
+
+def _fits(rows, width, offsets, E, w, out, out_shape, dt, dev):
+    """The rows [A,width], offsets, weights and result of a product are dense, of these shapes and types and on device number `dev` (one
+    expression: a call of a few microseconds spends a third of them on its checks)."""
+    return (rows.shape[1] == width and offsets.shape == (E + 1,) and out.shape == out_shape and w.dtype is dt and out.dtype is dt and offsets.dtype is _INT32
+            and rows.is_contiguous() and w.is_contiguous() and out.is_contiguous() and offsets.is_contiguous()
+            and w.get_device() == out.get_device() == offsets.get_device() == dev)
+
+
 def _grouped(rows, w_shape):
     """(E_local, n, k, A, type, its code, device number) of a product of `rows` [A,*] with weights of this shape."""
     if len(w_shape) != 3 or len(rows.shape) != 2:
@@ -294,15 +305,23 @@ def _grouped(rows, w_shape):
     return (*w_shape, rows.shape[0], dt, code, rows.get_device())
 
 
+def _misfit(rows, rows_shape, offsets, E, w, out, out_shape, dt, dev):
+    """Raises for what _fits() found."""
+    _expect("the rows", rows, rows_shape, dt, dev)
+    _expect("expert_offsets", offsets, (E + 1,), _INT32, dev)
+    _expect("w", w, w.shape, dt, dev)
+    _expect("out", out, out_shape, dt, dev)
+
+
 def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
     """y[s] = x_sorted[s] W_e^T (+ bias[e]) for the rows of every expert; w [E_local,n,k]."""
     E, n, k, A, dt, code, dev = _grouped(x_sorted, w.shape)
-    _expect("x_sorted", x_sorted, (A, k), dt, dev)
-    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, dev)
-    _expect("w", w, (E, n, k), dt, dev)
+    if out is None:
+        out = torch.empty((A, n), dtype=dt, device=x_sorted.device)
+    if not _fits(x_sorted, k, expert_offsets, E, w, out, (A, n), dt, dev):
+        _misfit(x_sorted, (A, k), expert_offsets, E, w, out, (A, n), dt, dev)
     if bias is not None:
         bias = _expect("bias", bias, (E, n), dt, dev).data_ptr()
-    out = torch.empty((A, n), dtype=dt, device=x_sorted.device) if out is None else _expect("out", out, (A, n), dt, dev)
     rc = lib().moe_grouped_product(x_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), bias, A, n, k, E, code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -312,10 +331,10 @@ def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
 def moe_grouped_product_dx(dy_sorted, expert_offsets, w, out=None):
     """Gradient of moe_grouped_product's rows: dx[s] = dy_sorted[s] W_e; w [E_local,n,k]."""
     E, n, k, A, dt, code, dev = _grouped(dy_sorted, w.shape)
-    _expect("dy_sorted", dy_sorted, (A, n), dt, dev)
-    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, dev)
-    _expect("w", w, (E, n, k), dt, dev)
-    out = torch.empty((A, k), dtype=dt, device=dy_sorted.device) if out is None else _expect("out", out, (A, k), dt, dev)
+    if out is None:
+        out = torch.empty((A, k), dtype=dt, device=dy_sorted.device)
+    if not _fits(dy_sorted, n, expert_offsets, E, w, out, (A, k), dt, dev):
+        _misfit(dy_sorted, (A, n), expert_offsets, E, w, out, (A, k), dt, dev)
     rc = lib().moe_grouped_product_dx(dy_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), A, n, k, E, code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -367,13 +386,14 @@ class Mx4:
 
 
 def _expect_mx4(name, m, shape, dev):
-    """`m` holds this shape on device number `dev`."""
-    k = shape[-1]
-    rows = 1
-    for length in shape[:-1]:
-        rows *= length
-    _expect(f"{name}.q", m.q, (*shape[:-1], k // 2), torch.uint8, dev)
-    _expect(f"{name}.scale", m.scale, ((k + 255) // 256, rows, 8), torch.uint8, dev)
+    """`m` holds this shape on device number `dev`; -> its rows."""
+    q, scale = m.q, m.scale
+    rows, k = q.numel() * 2 // max(shape[-1], 1), shape[-1]
+    if (q.shape == (*shape[:-1], k // 2) and scale.shape == ((k + 255) // 256, rows, 8) and q.dtype is _UINT8 and scale.dtype is _UINT8 and q.is_contiguous()
+            and scale.is_contiguous() and q.get_device() == scale.get_device() == dev):
+        return rows
+    _expect(f"{name}.q", q, (*shape[:-1], k // 2), _UINT8, dev)
+    _expect(f"{name}.scale", scale, ((k + 255) // 256, rows, 8), _UINT8, dev)
     return rows
 
 
@@ -414,14 +434,14 @@ def mx4_dequantize(m, dtype=torch.bfloat16, out=None):
 def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, out=None, workspace=None):
     """moe_grouped_product with weights held in 4 bits: w an Mx4 [E_local,n,k]; x_sorted an Mx4 [A,k], or rows of `dtype` that the call
     quantises.  The result has the type of the rows, or `dtype` (bf16)."""
-    shape = w.shape
     held = isinstance(x_sorted, Mx4)
     rows = x_sorted.q if held else x_sorted
-    if len(shape) != 3 or len(rows.shape) != 2:
-        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {tuple(shape)}")
-    E, n, k = shape
+    if len(w.q.shape) != 3 or len(rows.shape) != 2:
+        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {tuple(w.shape)}")
+    E, n, k = w.q.shape
+    k *= 2
     A, dev = rows.shape[0], rows.get_device()
-    _expect_mx4("w", w, shape, dev)
+    _expect_mx4("w", w, (E, n, k), dev)
     if held:
         _expect_mx4("x_sorted", x_sorted, (A, k), dev)
         x_scale = x_sorted.scale.data_ptr()
@@ -433,7 +453,7 @@ def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, 
     code = _CODES.get(dtype)
     if code is None:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dtype}")
-    _expect("expert_offsets", expert_offsets, (E + 1,), torch.int32, dev)
+    _expect("expert_offsets", expert_offsets, (E + 1,), _INT32, dev)
     if bias is not None:
         bias = _expect("bias", bias, (E, n), dtype, dev).data_ptr()
     out = torch.empty((A, n), dtype=dtype, device=rows.device) if out is None else _expect("out", out, (A, n), dtype, dev)

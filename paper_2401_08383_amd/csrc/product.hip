@@ -11,6 +11,8 @@ static int check_sizes(const char* fn, int64_t A, int n, int k, int E_local, int
     const int gran = dt == EXF_BF16 ? 8 : 4;
     if (n < gran || n % gran != 0 || k < gran || k % gran != 0)
         return fail(EXF_ERR_BAD_SHAPE, "%s: n = %d and k = %d must be positive multiples of %d", fn, n, k, gran);
+    if (n > EXF_MAX_PRODUCT_WIDTH || k > EXF_MAX_PRODUCT_WIDTH)  // the tiles address their rows with 32-bit byte offsets
+        return fail(EXF_ERR_BAD_SHAPE, "%s: n = %d and k = %d must not exceed %d", fn, n, k, EXF_MAX_PRODUCT_WIDTH);
     return EXF_OK;
 }
 

@@ -42,6 +42,7 @@ __device__ __forceinline__ void lds_buffer_16B(u32x4_v rsrc, uint32_t voff, uint
 #endif
 }
 constexpr uint32_t kBufferReach = 0x80000000u;  // offsets from here on deliver zeros
+static_assert(static_cast<uint64_t>(kTallestTile) * EXF_MAX_PRODUCT_WIDTH * 2 < kBufferReach, "all offsets of a tile lie below");
 
 template <typename T>
 __device__ __forceinline__ T lds_fetch(uint32_t addr)
@@ -751,11 +752,15 @@ static int launch_rows_tiles_as(const RowsTiles& p, hipStream_t stream, const ch
     return EXF_OK;
 }
 
-// Weights too many to stay in the memory-side cache of 256 MB from call to call, and so few rows that many experts have one row tile.
+// Weights too many to stay in the memory-side cache of 256 MB from call to call, and so few rows that many experts have one row tile (the lines of
+// ffn.hip).  512 rows, 64 experts of 16384 x 4096 as tiles 1481 us without and 1367 with; in 4 bits 384 and 361.
+//   Not where weight rows begin off the lines: two loads share a line then, and the second one has to find it in the L2 (501 rows, 7 experts of 6664 x 11816
+// 320 us without and 365 with; 2864 in 4 bits, 36 of 6032 x 4288 150 and 177).
 inline bool streams_weights(const RowsTiles& p, ProductKind kind)
 {
-    const int64_t bytes = static_cast<int64_t>(p.E_local) * p.K * p.N * (kind == kMx4 ? 1 : 4) / 2;
-    return p.max_rows <= 1024ll * p.E_local && bytes >= 128ll << 20;
+    const int64_t row = static_cast<int64_t>(kind == kRowsGradient ? p.N : p.K) * (kind == kMx4 ? 1 : 4) / 2;
+    const int64_t bytes = row * p.E_local * (kind == kRowsGradient ? p.K : p.N);
+    return row % 128 == 0 && p.max_rows <= 1024ll * p.E_local && bytes >= 128ll << 20;
 }
 template <int NT, ProductKind KIND>
 static int launch_rows_tiles(const RowsTiles& p, hipStream_t stream, const char* fn)

@@ -39,7 +39,7 @@ def _dequantise(q=_p(1), s=_p(2), rows=4, k=64, dt=B.EXF_BF16, out=_p(0)):
     return exf.lib().mx4_dequantize(q, s, rows, k, dt, out, None)
 
 
-SHAPES = [dict(A=-1), dict(A=1 << 31), dict(n=0), dict(n=-8), dict(n=60), dict(k=0), dict(k=36), dict(E=0), dict(E=65), dict(dt=B.EXF_F32, n=62)]
+SHAPES = [dict(A=-1), dict(A=1 << 31), dict(n=0), dict(n=-8), dict(n=60), dict(k=0), dict(k=36), dict(E=0), dict(E=65), dict(dt=B.EXF_F32, n=62), dict(n=(1 << 21) + 8), dict(k=(1 << 21) + 32)]
 
 
 @pytest.mark.parametrize("call", [_product, _dx, _dw, _mx4])
