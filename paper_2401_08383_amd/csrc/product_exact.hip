@@ -117,44 +117,63 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
 // ---- small problems: 32 x 32 outputs a workgroup, whose four wavefronts share the reduction (16 elements each in turn) and join their sums
 // through LDS.  Operands come straight from memory into the registers that the matrix instructions read, kAhead turns early.
 constexpr int kSmallTile = 32, kAhead = 3;
+//   A wavefront's 16 reduction elements of a turn begin at a place that is the same in all lanes, and a lane's elements at a
+// 32-bit distance from there that never changes; past the end of the reduction a lane reads the turn's first element instead.
 template <bool ACROSS>
-__device__ __forceinline__ f32x4_t small_operand(const float* base, int64_t ld, int row, int r, int depth)
-{
-    if constexpr (!ACROSS) {  // depth is a multiple of four: all four or none
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(base + row * ld + (r < depth ? r : 0));
-        return r < depth ? v : f32x4_t{0.f, 0.f, 0.f, 0.f};
-    } else {
-        f32x4_t v;
+struct SmallOperand {
+    static constexpr int N = ACROSS ? 4 : 1;
+    const float* base;
+    int64_t ld;
+    int depth;
+    uint32_t off[2][N], first[2];  // of two groups of 16 rows
+
+    __device__ __forceinline__ SmallOperand(const float* b, int64_t l, int rows, int d) : base(b), ld(l), depth(d)
+    {
+        const int in16 = lane_id() & 15, quad = lane_id() >> 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float x = base[(r + j < depth ? r + j : 0) * ld + row];
-            v[j] = r + j < depth ? x : 0.0f;
+        for (int i = 0; i < 2; ++i) {
+            const int row = min(i * 16 + in16, rows - 1);
+            first[i] = static_cast<uint32_t>(ACROSS ? row : row * ld);
+#pragma unroll
+            for (int j = 0; j < N; ++j) off[i][j] = first[i] + static_cast<uint32_t>(ACROSS ? (quad * 4 + j) * ld : quad * 4);
         }
-        return v;
     }
-}
+    // elements begin + 4 (lane/16) .. +3
+    __device__ __forceinline__ void load(int begin, f32x4_t (&v)[2]) const
+    {
+        const int at = min(begin, (depth - 1) / 16 * 16), quad4 = (lane_id() >> 4) * 4;
+        const float* from = base + (ACROSS ? at * ld : at);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if constexpr (!ACROSS) {  // depth is a multiple of four: all four or none
+                v[i] = *reinterpret_cast<const f32x4_t*>(from + (at + quad4 < depth ? off[i][0] : first[i]));
+                if (begin + quad4 >= depth) v[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[i][j] = from[at + quad4 + j < depth ? off[i][j] : first[i]];
+                    if (begin + quad4 + j >= depth) v[i][j] = 0.0f;
+                }
+            }
+        }
+    }
+};
 template <bool A_ACROSS, bool W_ACROSS>
 __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows, const float* w, int64_t ldw, int cols, int depth, float* out, int64_t ldo, float* sums)
 {
     constexpr int STRIDE = kSmallTile + 4;
     __shared__ __attribute__((aligned(16))) float part[4][kSmallTile * STRIDE];
     __shared__ float part_sum[4][kSmallTile];
-    const int lane = lane_id(), wave = threadIdx.x / kWave, in16 = lane & 15, quad = lane >> 4;
-    int row[2], col[2];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), in16 = lane & 15, quad = lane >> 4;
+    const SmallOperand<A_ACROSS> oa(a, lda, rows, depth);
+    const SmallOperand<W_ACROSS> ow(w, ldw, cols, depth);
     f32x4_t acc[2][2], fa[kAhead][2], fw[kAhead][2];
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        row[i] = min(i * 16 + in16, rows - 1);
-        col[i] = min(i * 16 + in16, cols - 1);
-        acc[i][0] = acc[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int i = 0; i < 2; ++i) acc[i][0] = acc[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     auto load = [&](int turn, int s) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            fa[s][i] = small_operand<A_ACROSS>(a, lda, row[i], (turn * 4 + wave) * 16 + quad * 4, depth);
-            fw[s][i] = small_operand<W_ACROSS>(w, ldw, col[i], (turn * 4 + wave) * 16 + quad * 4, depth);
-        }
+        oa.load((turn * 4 + wave) * 16, fa[s]);
+        ow.load((turn * 4 + wave) * 16, fw[s]);
     };
     const int turns = depth > wave * 16 ? (depth - wave * 16 + 63) / 64 : 0;
     if (turns > 0) {
