@@ -114,66 +114,65 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
         }
 }
 
-// ---- small problems: 32 x 32 outputs a workgroup, whose four wavefronts share the reduction (16 elements each in turn) and join their sums
+// ---- small problems: 32 x 64 outputs a workgroup, whose four wavefronts share the reduction (16 elements each in turn) and join their sums
 // through LDS.  Operands come straight from memory into the registers that the matrix instructions read, kAhead turns early.
-constexpr int kSmallTile = 32, kAhead = 3;
-//   A wavefront's 16 reduction elements of a turn begin at a place that is the same in all lanes, and a lane's elements at a
-// 32-bit distance from there that never changes; past the end of the reduction a lane reads the turn's first element instead.
-template <bool ACROSS>
-struct SmallOperand {
-    static constexpr int N = ACROSS ? 4 : 1;
-    const float* base;
-    int64_t ld;
-    int depth;
-    uint32_t off[2][N], first[2];  // of two groups of 16 rows
+//   An operand across the reduction is loaded as it lies: a lane takes 16 bytes of a reduction element, four columns, and each of the four
+// is the operand of a matrix instruction of its own, whose 16 columns are then four apart.  (Loads of 4 bytes for 16 adjacent columns are
+// four times as many: gradient of 777 rows, 5 experts of 520 x 264 9.6 us with them.)  Loads past the end deliver zeros (see product_tiles.hpp).
+constexpr int kSmallTileRows = 32, kSmallCols = 64, kAhead = 3;
+constexpr int kSmallStride = kSmallCols + 4;
 
-    __device__ __forceinline__ SmallOperand(const float* b, int64_t l, int rows, int d) : base(b), ld(l), depth(d)
-    {
-        const int in16 = lane_id() & 15, quad = lane_id() >> 4;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = min(i * 16 + in16, rows - 1);
-            first[i] = static_cast<uint32_t>(ACROSS ? row : row * ld);
-#pragma unroll
-            for (int j = 0; j < N; ++j) off[i][j] = first[i] + static_cast<uint32_t>(ACROSS ? (quad * 4 + j) * ld : quad * 4);
-        }
-    }
-    // elements begin + 4 (lane/16) .. +3
-    __device__ __forceinline__ void load(int begin, f32x4_t (&v)[2]) const
-    {
-        const int at = min(begin, (depth - 1) / 16 * 16), quad4 = (lane_id() >> 4) * 4;
-        const float* from = base + (ACROSS ? at * ld : at);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if constexpr (!ACROSS) {  // depth is a multiple of four: all four or none
-                v[i] = *reinterpret_cast<const f32x4_t*>(from + (at + quad4 < depth ? off[i][0] : first[i]));
-                if (begin + quad4 >= depth) v[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[i][j] = from[at + quad4 + j < depth ? off[i][j] : first[i]];
-                    if (begin + quad4 + j >= depth) v[i][j] = 0.0f;
-                }
-            }
-        }
-    }
-};
-template <bool A_ACROSS, bool W_ACROSS>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const float* base, int64_t floats)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, static_cast<int>(floats * 4), 0x00020000);
+}
+
+// A_ACROSS: a's element (row, r) at a[r * lda + row], otherwise a[row * lda + r]; w's element (col, r) at w[r * ldw + col].
+template <bool A_ACROSS>
 __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows, const float* w, int64_t ldw, int cols, int depth, float* out, int64_t ldo, float* sums)
 {
-    constexpr int STRIDE = kSmallTile + 4;
-    __shared__ __attribute__((aligned(16))) float part[4][kSmallTile * STRIDE];
-    __shared__ float part_sum[4][kSmallTile];
+    __shared__ __attribute__((aligned(16))) float part[4][kSmallTileRows * kSmallStride];
+    __shared__ float part_sum[4][kSmallTileRows];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), in16 = lane & 15, quad = lane >> 4;
-    const SmallOperand<A_ACROSS> oa(a, lda, rows, depth);
-    const SmallOperand<W_ACROSS> ow(w, ldw, cols, depth);
-    f32x4_t acc[2][2], fa[kAhead][2], fw[kAhead][2];
+    // byte distances from the first of the 16 reduction elements
+    int off_w[4], off_a[A_ACROSS ? 4 : 2];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        off_w[q] = static_cast<int>(((quad * 4 + q) * ldw + min(in16 * 4, cols - 4)) * 4);
+        if constexpr (A_ACROSS) off_a[q] = static_cast<int>(((quad * 4 + q) * lda + min(in16 * 2, rows - 2)) * 4);
+    }
+    if constexpr (!A_ACROSS)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) off_a[i] = static_cast<int>((min(i * 16 + in16, rows - 1) * lda + quad * 4) * 4);
+    f32x4_t acc[2][4], fw[kAhead][4];  // [row group][column of a lane's four], [reduction element]
+    float fa[kAhead][2][4];            // [row group][reduction element]
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) acc[i][0] = acc[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     auto load = [&](int turn, int s) {
-        oa.load((turn * 4 + wave) * 16, fa[s]);
-        ow.load((turn * 4 + wave) * 16, fw[s]);
+        const int begin = (turn * 4 + wave) * 16, left = depth - begin, last = min(left, 16) - 1;
+        const auto from_w = buffer_of(w + begin * ldw, left > 0 ? last * ldw + cols : 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) fw[s][q] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from_w, off_w[q], 0, 0));
+        if constexpr (A_ACROSS) {
+            const auto from_a = buffer_of(a + begin * lda, left > 0 ? last * lda + rows : 0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const auto v = __builtin_amdgcn_raw_buffer_load_b64(from_a, off_a[q], 0, 0);
+                fa[s][0][q] = __uint_as_float(v[0]);
+                fa[s][1][q] = __uint_as_float(v[1]);
+            }
+        } else {  // depth is a multiple of four: all four or none
+            const auto from_a = buffer_of(a + begin, left > 0 ? (rows - 1) * lda + left : 0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const f32x4_t v = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from_a, quad * 4 < left ? off_a[i] : -16, 0, 0));
+#pragma unroll
+                for (int q = 0; q < 4; ++q) fa[s][i][q] = v[q];
+            }
+        }
     };
     const int turns = depth > wave * 16 ? (depth - wave * 16 + 63) / 64 : 0;
     if (turns > 0) {
@@ -187,49 +186,55 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[s][j][q], fa[s][i][q], acc[i][j], 0, 0, 0);
-                if (sums != nullptr)
+                        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[s][q][j], fa[s][i][q], acc[i][j], 0, 0, 0);
+                if (A_ACROSS && sums != nullptr)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) sum[i] += (fa[s][i][0] + fa[s][i][1]) + (fa[s][i][2] + fa[s][i][3]);
                 load(t + s + kAhead, s);
             }
         }
     }
+    // a lane holds, of row group i, columns 16 quad + 4 v + j
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+        const int row = A_ACROSS ? in16 * 2 + i : i * 16 + in16;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) *reinterpret_cast<f32x4_t*>(&part[wave][(i * 16 + in16) * STRIDE + j * 16 + quad * 4]) = acc[i][j];
-        if (sums != nullptr) {
+        for (int v = 0; v < 4; ++v)
+            *reinterpret_cast<f32x4_t*>(&part[wave][row * kSmallStride + quad * 16 + v * 4]) = f32x4_t{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]};
+        if (A_ACROSS && sums != nullptr) {
             sum[i] = butterfly_add<16>(butterfly_add<32>(sum[i]));
-            if (quad == 0) part_sum[wave][i * 16 + in16] = sum[i];
+            if (quad == 0) part_sum[wave][row] = sum[i];
         }
     }
     __syncthreads();
-    const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 4, at = r * STRIDE + c;
-    auto of = [&](int wv) { return *reinterpret_cast<const f32x4_t*>(&part[wv][at]); };
-    if (r < rows && c < cols) *reinterpret_cast<f32x4_t*>(out + r * ldo + c) = (of(0) + of(1)) + (of(2) + of(3));
-    if (sums != nullptr && threadIdx.x < kSmallTile && static_cast<int>(threadIdx.x) < rows)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 4 + h * 32, at = r * kSmallStride + c;
+        auto of = [&](int wv) { return *reinterpret_cast<const f32x4_t*>(&part[wv][at]); };
+        if (r < rows && c < cols) *reinterpret_cast<f32x4_t*>(out + r * ldo + c) = (of(0) + of(1)) + (of(2) + of(3));
+    }
+    if (A_ACROSS && sums != nullptr && static_cast<int>(threadIdx.x) < min(kSmallTileRows, rows))
         sums[threadIdx.x] = (part_sum[0][threadIdx.x] + part_sum[1][threadIdx.x]) + (part_sum[2][threadIdx.x] + part_sum[3][threadIdx.x]);
 }
 
 template <bool SMALL>
 __global__ __launch_bounds__(256) void exact_rows_gradient_kernel(const RowsGradient p, int col_tiles)
 {
-    constexpr int TILE = SMALL ? kSmallTile : kExactTile;
+    constexpr int ROWS = SMALL ? kSmallTileRows : kExactTile, COLS = SMALL ? kSmallCols : kExactTile;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
-    const int tiles = (range.hi - range.lo + TILE - 1) / TILE;
+    const int tiles = (range.hi - range.lo + ROWS - 1) / ROWS;
     const int upto = wave_inclusive_scan(tiles);
     const int row_tile = static_cast<int>(blockIdx.x / static_cast<unsigned>(col_tiles)), col_tile = static_cast<int>(blockIdx.x % static_cast<unsigned>(col_tiles));
     const unsigned long long owner = __ballot(row_tile < upto);
     if (owner == 0ull) return;
     const int e = __builtin_ctzll(owner);
     const int hi = wave_read_lane(range.hi, e);
-    const int row = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * TILE;
-    const int col = col_tile * TILE, rows = min(TILE, hi - row), cols = min(TILE, p.N - col);
+    const int row = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * ROWS;
+    const int col = col_tile * COLS, rows = min(ROWS, hi - row), cols = min(COLS, p.N - col);
     const int64_t K = p.K, N = p.N;
     const float *a = static_cast<const float*>(p.rows) + row * K, *w = static_cast<const float*>(p.weight) + e * N * K + col;
     float* out = static_cast<float*>(p.out) + row * N + col;
-    if constexpr (SMALL) small_tile<false, true>(a, K, rows, w, N, cols, p.K, out, N, nullptr);
+    if constexpr (SMALL) small_tile<false>(a, K, rows, w, N, cols, p.K, out, N, nullptr);
     else exact_tile(ExactOperand<false>{a, K, rows, p.K, {}}, ExactOperand<true>{w, N, cols, p.K, {}}, out, N, nullptr);
 }
 
@@ -240,18 +245,18 @@ __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient 
     const unsigned per_expert = static_cast<unsigned>(row_tiles) * static_cast<unsigned>(col_tiles);
     const int e = static_cast<int>(blockIdx.x / per_expert);
     const unsigned t = blockIdx.x % per_expert;
-    constexpr int TILE = SMALL ? kSmallTile : kExactTile;
-    const int row = static_cast<int>(t / static_cast<unsigned>(col_tiles)) * TILE, col = static_cast<int>(t % static_cast<unsigned>(col_tiles)) * TILE;
+    constexpr int ROWS = SMALL ? kSmallTileRows : kExactTile, COLS = SMALL ? kSmallCols : kExactTile;
+    const int row = static_cast<int>(t / static_cast<unsigned>(col_tiles)) * ROWS, col = static_cast<int>(t % static_cast<unsigned>(col_tiles)) * COLS;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
     const int lo = wave_read_lane(range.lo, e), all = wave_read_lane(range.hi, e) - lo;
     const int stages = (all + kExactDepth - 1) / kExactDepth;
     const int first = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / gridDim.y) * kExactDepth;
     const int n = max(min(all, static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / gridDim.y) * kExactDepth) - first, 0);
     const int64_t N = p.N, K = p.K, begin = lo + first, at = static_cast<int64_t>(blockIdx.y) * p.E_local + e;
-    const int rows = min(TILE, p.N - row), cols = min(TILE, p.K - col);
+    const int rows = min(ROWS, p.N - row), cols = min(COLS, p.K - col);
     const float *a = static_cast<const float*>(p.dy) + begin * N + row, *w = static_cast<const float*>(p.x) + begin * K + col;
     float *out = static_cast<float*>(p.dw) + (at * N + row) * K + col, *sums = p.db != nullptr && col == 0 ? static_cast<float*>(p.db) + at * N + row : nullptr;
-    if constexpr (SMALL) small_tile<true, true>(a, N, rows, w, K, cols, n, out, K, sums);
+    if constexpr (SMALL) small_tile<true>(a, N, rows, w, K, cols, n, out, K, sums);
     else exact_tile(ExactOperand<true>{a, N, rows, n, {}}, ExactOperand<true>{w, K, cols, n, {}}, out, K, sums);
 }
 
@@ -286,29 +291,30 @@ static bool small_tiles(int64_t large) { return large < 2 * 256; }
 int launch_exact_rows_gradient(const RowsGradient& p, hipStream_t stream)
 {
     const int64_t most_experts = p.max_rows < p.E_local ? p.max_rows : p.E_local;
-    auto tiles = [&](int64_t size) { return (p.max_rows / size + most_experts) * ((p.N + size - 1) / size); };
+    auto tiles = [&](int64_t rows) { return (p.max_rows / rows + most_experts) * ((p.N + kExactTile - 1) / kExactTile); };
     const bool small = small_tiles(tiles(kExactTile));
-    const int64_t grid = tiles(small ? kSmallTile : kExactTile);
+    const int64_t grid = tiles(small ? kSmallTileRows : kExactTile);
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dx: too many tiles");
-    if (small) hipLaunchKernelGGL(exact_rows_gradient_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kSmallTile - 1) / kSmallTile);
+    if (small) hipLaunchKernelGGL(exact_rows_gradient_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kSmallCols - 1) / kSmallCols);
     else hipLaunchKernelGGL(exact_rows_gradient_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kExactTile - 1) / kExactTile);
     return EXF_OK;
 }
 
 // Parts of at least 256 rows until two workgroups a compute unit have one.
-static int64_t weight_tiles(int n, int k, int E_local, int size) { return static_cast<int64_t>(E_local) * ((n + size - 1) / size) * ((k + size - 1) / size); }
+static_assert(kSmallCols == kExactTile, "both kinds of tiles have as many columns");
+static int64_t weight_tiles(int n, int k, int E_local, int rows) { return static_cast<int64_t>(E_local) * ((n + rows - 1) / rows) * ((k + kExactTile - 1) / kExactTile); }
 int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local)
 {
     const bool small = small_tiles(weight_tiles(n, k, E_local, kExactTile));
-    const int64_t wanted = 512 / weight_tiles(n, k, E_local, small ? kSmallTile : kExactTile), most = A / (256 * E_local);
+    const int64_t wanted = 512 / weight_tiles(n, k, E_local, small ? kSmallTileRows : kExactTile), most = A / (256 * E_local);
     const int64_t s = wanted < most ? wanted : most;
     return static_cast<int>(s < 2 ? 1 : (s > 16 ? 16 : s));
 }
 int launch_exact_weight_gradient(const WeightGradient& g, hipStream_t stream)
 {
     const bool small = small_tiles(weight_tiles(g.N, g.K, g.E_local, kExactTile));
-    const int size = small ? kSmallTile : kExactTile;
-    const int64_t grid = weight_tiles(g.N, g.K, g.E_local, size), each = static_cast<int64_t>(g.E_local) * g.N * g.K;
+    const int tile_rows = small ? kSmallTileRows : kExactTile;
+    const int64_t grid = weight_tiles(g.N, g.K, g.E_local, tile_rows), each = static_cast<int64_t>(g.E_local) * g.N * g.K;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
     const int splits = exact_weight_gradient_splits(g.max_rows, g.N, g.K, g.E_local);
     float* parts = static_cast<float*>(g.workspace);
@@ -318,7 +324,7 @@ int launch_exact_weight_gradient(const WeightGradient& g, hipStream_t stream)
         if (p.db != nullptr) p.db = parts + splits * each;
     }
     const dim3 blocks(static_cast<unsigned>(grid), static_cast<unsigned>(splits));
-    const int rows = (g.N + size - 1) / size, cols = (g.K + size - 1) / size;
+    const int rows = (g.N + tile_rows - 1) / tile_rows, cols = (g.K + kExactTile - 1) / kExactTile;
     if (small) hipLaunchKernelGGL(exact_weight_kernel<true>, blocks, dim3(256), 0, stream, p, rows, cols);
     else hipLaunchKernelGGL(exact_weight_kernel<false>, blocks, dim3(256), 0, stream, p, rows, cols);
     if (splits == 1) return EXF_OK;
