@@ -114,12 +114,14 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
         }
 }
 
-// ---- small problems: 32 x 64 outputs a workgroup, whose four wavefronts share the reduction (16 elements each in turn) and join their sums
+// ---- small problems: 16 (rows' gradient) or 32 (weights' gradient) x 64 outputs a workgroup, whose four wavefronts share the reduction (16 elements each in turn) and join their sums
 // through LDS.  Operands come straight from memory into the registers that the matrix instructions read, kAhead turns early.
 //   An operand across the reduction is loaded as it lies: a lane takes 16 bytes of a reduction element, four columns, and each of the four
 // is the operand of a matrix instruction of its own, whose 16 columns are then four apart.  (Loads of 4 bytes for 16 adjacent columns are
 // four times as many: gradient of 777 rows, 5 experts of 520 x 264 9.6 us with them.)  Loads past the end deliver zeros (see product_tiles.hpp).
-constexpr int kSmallTileRows = 32, kSmallCols = 64, kAhead = 3;
+//   A 16 x 16 x 4 product in fp32 takes 32 cycles, and few tiles are as fast as one of them: rows' gradients, whose experts often have few rows, take 16.
+constexpr int kSmallCols = 64, kAhead = 3;
+constexpr int small_rows(bool across) { return across ? 32 : 16; }
 constexpr int kSmallStride = kSmallCols + 4;
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const float* base, int64_t floats)
@@ -131,11 +133,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const float* base, i
 template <bool A_ACROSS>
 __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows, const float* w, int64_t ldw, int cols, int depth, float* out, int64_t ldo, float* sums)
 {
-    __shared__ __attribute__((aligned(16))) float part[4][kSmallTileRows * kSmallStride];
-    __shared__ float part_sum[4][kSmallTileRows];
+    constexpr int ROWS = small_rows(A_ACROSS), R = ROWS / 16;  // row groups
+    __shared__ __attribute__((aligned(16))) float part[4][ROWS * kSmallStride];
+    __shared__ float part_sum[4][ROWS];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), in16 = lane & 15, quad = lane >> 4;
     // byte distances from the first of the 16 reduction elements
-    int off_w[4], off_a[A_ACROSS ? 4 : 2];
+    int off_w[4], off_a[A_ACROSS ? 4 : R];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         off_w[q] = static_cast<int>(((quad * 4 + q) * ldw + min(in16 * 4, cols - 4)) * 4);
@@ -143,12 +146,12 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
     }
     if constexpr (!A_ACROSS)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) off_a[i] = static_cast<int>((min(i * 16 + in16, rows - 1) * lda + quad * 4) * 4);
-    f32x4_t acc[2][4], fw[kAhead][4];  // [row group][column of a lane's four], [reduction element]
-    float fa[kAhead][2][4];            // [row group][reduction element]
-    float sum[2] = {0.0f, 0.0f};
+        for (int i = 0; i < R; ++i) off_a[i] = static_cast<int>((min(i * 16 + in16, rows - 1) * lda + quad * 4) * 4);
+    f32x4_t acc[R][4], fw[kAhead][4];  // [row group][column of a lane's four], [reduction element]
+    float fa[kAhead][R][4];            // [row group][reduction element]
+    float sum[R] = {};
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     auto load = [&](int turn, int s) {
@@ -167,7 +170,7 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
         } else {  // depth is a multiple of four: all four or none
             const auto from_a = buffer_of(a + begin, left > 0 ? (rows - 1) * lda + left : 0);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < R; ++i) {
                 const f32x4_t v = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from_a, quad * 4 < left ? off_a[i] : -16, 0, 0));
 #pragma unroll
                 for (int q = 0; q < 4; ++q) fa[s][i][q] = v[q];
@@ -184,19 +187,19 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < R; ++i)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[s][q][j], fa[s][i][q], acc[i][j], 0, 0, 0);
                 if (A_ACROSS && sums != nullptr)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) sum[i] += (fa[s][i][0] + fa[s][i][1]) + (fa[s][i][2] + fa[s][i][3]);
+                    for (int i = 0; i < R; ++i) sum[i] += (fa[s][i][0] + fa[s][i][1]) + (fa[s][i][2] + fa[s][i][3]);
                 load(t + s + kAhead, s);
             }
         }
     }
     // a lane holds, of row group i, columns 16 quad + 4 v + j
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < R; ++i) {
         const int row = A_ACROSS ? in16 * 2 + i : i * 16 + in16;
 #pragma unroll
         for (int v = 0; v < 4; ++v)
@@ -208,19 +211,19 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
     }
     __syncthreads();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 4 + h * 32, at = r * kSmallStride + c;
+    for (int h = 0; h < R; ++h) {
+        const int r = threadIdx.x / 16 + h * 16, c = threadIdx.x % 16 * 4, at = r * kSmallStride + c;
         auto of = [&](int wv) { return *reinterpret_cast<const f32x4_t*>(&part[wv][at]); };
         if (r < rows && c < cols) *reinterpret_cast<f32x4_t*>(out + r * ldo + c) = (of(0) + of(1)) + (of(2) + of(3));
     }
-    if (A_ACROSS && sums != nullptr && static_cast<int>(threadIdx.x) < min(kSmallTileRows, rows))
+    if (A_ACROSS && sums != nullptr && static_cast<int>(threadIdx.x) < min(ROWS, rows))
         sums[threadIdx.x] = (part_sum[0][threadIdx.x] + part_sum[1][threadIdx.x]) + (part_sum[2][threadIdx.x] + part_sum[3][threadIdx.x]);
 }
 
 template <bool SMALL>
 __global__ __launch_bounds__(256) void exact_rows_gradient_kernel(const RowsGradient p, int col_tiles)
 {
-    constexpr int ROWS = SMALL ? kSmallTileRows : kExactTile, COLS = SMALL ? kSmallCols : kExactTile;
+    constexpr int ROWS = SMALL ? small_rows(false) : kExactTile, COLS = SMALL ? kSmallCols : kExactTile;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
     const int tiles = (range.hi - range.lo + ROWS - 1) / ROWS;
     const int upto = wave_inclusive_scan(tiles);
@@ -245,7 +248,7 @@ __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient 
     const unsigned per_expert = static_cast<unsigned>(row_tiles) * static_cast<unsigned>(col_tiles);
     const int e = static_cast<int>(blockIdx.x / per_expert);
     const unsigned t = blockIdx.x % per_expert;
-    constexpr int ROWS = SMALL ? kSmallTileRows : kExactTile, COLS = SMALL ? kSmallCols : kExactTile;
+    constexpr int ROWS = SMALL ? small_rows(true) : kExactTile, COLS = SMALL ? kSmallCols : kExactTile;
     const int row = static_cast<int>(t / static_cast<unsigned>(col_tiles)) * ROWS, col = static_cast<int>(t % static_cast<unsigned>(col_tiles)) * COLS;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
     const int lo = wave_read_lane(range.lo, e), all = wave_read_lane(range.hi, e) - lo;
@@ -293,7 +296,7 @@ int launch_exact_rows_gradient(const RowsGradient& p, hipStream_t stream)
     const int64_t most_experts = p.max_rows < p.E_local ? p.max_rows : p.E_local;
     auto tiles = [&](int64_t rows) { return (p.max_rows / rows + most_experts) * ((p.N + kExactTile - 1) / kExactTile); };
     const bool small = small_tiles(tiles(kExactTile));
-    const int64_t grid = tiles(small ? kSmallTileRows : kExactTile);
+    const int64_t grid = tiles(small ? small_rows(false) : kExactTile);
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dx: too many tiles");
     if (small) hipLaunchKernelGGL(exact_rows_gradient_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kSmallCols - 1) / kSmallCols);
     else hipLaunchKernelGGL(exact_rows_gradient_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kExactTile - 1) / kExactTile);
@@ -306,14 +309,14 @@ static int64_t weight_tiles(int n, int k, int E_local, int rows) { return static
 int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local)
 {
     const bool small = small_tiles(weight_tiles(n, k, E_local, kExactTile));
-    const int64_t wanted = 512 / weight_tiles(n, k, E_local, small ? kSmallTileRows : kExactTile), most = A / (256 * E_local);
+    const int64_t wanted = 512 / weight_tiles(n, k, E_local, small ? small_rows(true) : kExactTile), most = A / (256 * E_local);
     const int64_t s = wanted < most ? wanted : most;
     return static_cast<int>(s < 2 ? 1 : (s > 16 ? 16 : s));
 }
 int launch_exact_weight_gradient(const WeightGradient& g, hipStream_t stream)
 {
     const bool small = small_tiles(weight_tiles(g.N, g.K, g.E_local, kExactTile));
-    const int tile_rows = small ? kSmallTileRows : kExactTile;
+    const int tile_rows = small ? small_rows(true) : kExactTile;
     const int64_t grid = weight_tiles(g.N, g.K, g.E_local, tile_rows), each = static_cast<int64_t>(g.E_local) * g.N * g.K;
     if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dw: too many tiles");
     const int splits = exact_weight_gradient_splits(g.max_rows, g.N, g.K, g.E_local);
