@@ -114,8 +114,9 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
         }
 }
 
-// ---- small problems: 16 (rows' gradient) or 32 (weights' gradient) x 64 outputs a workgroup, whose four wavefronts share the reduction (16 elements each in turn) and join their sums
-// through LDS.  Operands come straight from memory into the registers that the matrix instructions read, kAhead turns early.
+// ---- small problems: 16 (rows' gradient) or 32 (weights' gradient) x 64 outputs a workgroup, whose four wavefronts share the reduction
+// (16 elements each in turn) and join their sums through LDS.  Operands come straight from memory into the registers that the matrix
+// instructions read, kAhead turns early.
 //   An operand across the reduction is loaded as it lies: a lane takes 16 bytes of a reduction element, four columns, and each of the four
 // is the operand of a matrix instruction of its own, whose 16 columns are then four apart.  (Loads of 4 bytes for 16 adjacent columns are
 // four times as many: gradient of 777 rows, 5 experts of 520 x 264 9.6 us with them.)  Loads past the end deliver zeros (see product_tiles.hpp).
