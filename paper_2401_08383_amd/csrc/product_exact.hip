@@ -119,8 +119,10 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
 // instructions read, kAhead turns early.
 //   An operand across the reduction is loaded as it lies: a lane takes 16 bytes of a reduction element, four columns, and each of the four
 // is the operand of a matrix instruction of its own, whose 16 columns are then four apart.  (Loads of 4 bytes for 16 adjacent columns are
-// four times as many: gradient of 777 rows, 5 experts of 520 x 264 9.6 us with them.)  Loads past the end deliver zeros (see product_tiles.hpp).
-//   A 16 x 16 x 4 product in fp32 takes 32 cycles, and few tiles are as fast as one of them: rows' gradients, whose experts often have few rows, take 16.
+// four times as many: gradient of 777 rows, 5 experts of 520 x 264 9.6 us with them, 8.9 without; with 16 rows a tile 7.3 to 8.1.)
+// Loads past the end deliver zeros (see product_tiles.hpp).
+//   A 16 x 16 x 4 product in fp32 takes 32 cycles, and few tiles are as fast as one of them: rows' gradients, whose experts often have few
+// rows, take 16.
 constexpr int kSmallCols = 64, kAhead = 3;
 constexpr int small_rows(bool across) { return across ? 32 : 16; }
 constexpr int kSmallStride = kSmallCols + 4;
