@@ -45,6 +45,12 @@ static bool streams_forward(int64_t A, int n, int k, int E_local)
     return n % 64 == 0 && k % 64 == 0 && A <= 28ll * E_local && A * widest < (1ll << 31) && static_cast<int64_t>(n) * k < (1ll << 31);
 }
 
+// fp32 with more rows an expert, the more the longer the reduction is: tiles (product_exact.hip).  Streams and tiles, us: 8 experts of
+// 1024 x 1024, 4096 rows 177 and 104; 32 of 512 x 512, 16384 rows 158 and 93; of 24 rows an expert 40 of 1024 x 1024 90 and 63, 8 of 2048 x 1024 36
+// and 31, 4 of 1024 x 4096 31 and 38 (48 rows: 61 and 39), 2 of 256 x 8192 30 and 72 (96 rows: 42 and 72, 500: 115 and 73); of 16 rows 40 of
+// 1024 x 1024 47 and 62.
+static bool exact_forward_in_tiles(int64_t A, int k, int E_local) { return A >= (k <= 2048 ? 24ll : (k <= 4096 ? 48ll : 128ll)) * E_local; }
+
 }  // namespace exf
 
 extern "C" int moe_grouped_product(const void* x_sorted, const int32_t* expert_offsets, const void* w, const void* bias, int64_t A, int n, int k,
@@ -55,7 +61,9 @@ extern "C" int moe_grouped_product(const void* x_sorted, const int32_t* expert_o
     if (A == 0) return EXF_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     int rc;
-    if (dt == EXF_F32 || streams_forward(A, n, k, E_local)) {
+    if (dt == EXF_F32 && exact_forward_in_tiles(A, k, E_local)) {
+        rc = launch_exact_product({x_sorted, expert_offsets, w, bias, y_sorted, static_cast<int>(A), k, n, E_local}, s);
+    } else if (dt == EXF_F32 || streams_forward(A, n, k, E_local)) {
         StreamGemm g{};
         g.act = x_sorted, g.weight = w, g.bias = bias, g.out = y_sorted, g.offsets = expert_offsets;
         g.max_rows = static_cast<int>(A), g.K = k, g.N = n, g.E_local = E_local, g.epi = kEpiNone;
@@ -77,7 +85,7 @@ extern "C" int moe_grouped_product_dx(const void* dy_sorted, const int32_t* expe
     if (dt == EXF_BF16) {
         rc = launch_rows_gradient_tiles({dy_sorted, expert_offsets, w, nullptr, static_cast<bf16_t*>(dx_sorted), nullptr, nullptr, static_cast<int>(A), n, k, E_local}, s);
     } else {
-        rc = launch_exact_rows_gradient({dy_sorted, expert_offsets, w, dx_sorted, static_cast<int>(A), n, k, E_local}, s);
+        rc = launch_exact_rows_gradient({dy_sorted, expert_offsets, w, nullptr, dx_sorted, static_cast<int>(A), n, k, E_local}, s);
     }
     return rc == EXF_OK ? check_launch("moe_grouped_product_dx") : rc;
 }

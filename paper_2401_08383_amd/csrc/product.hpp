@@ -5,11 +5,12 @@
 
 namespace exf {
 
-// out[rows of e, N] = rows[rows of e, K] W_e, a sorted row at a time; weight [E_local,K,N].
-struct RowsGradient {
+// out[rows of e, N] = rows[rows of e, K] W_e^T (+ bias_e), weight [E_local,N,K], or in a rows' gradient rows W_e, weight [E_local,K,N].
+struct ExactRows {
     const void* rows;         // [A,K]
     const int32_t* offsets;   // [E_local+1]
     const void* weight;
+    const void* bias;         // [E_local,N] or null
     void* out;                // [A,N]
     int max_rows;             // A
     int K, N, E_local;
@@ -37,7 +38,8 @@ struct Mx4Product {
 };
 
 // fp32 (product_exact.hip).
-int launch_exact_rows_gradient(const RowsGradient& p, hipStream_t stream);
+int launch_exact_product(const ExactRows& p, hipStream_t stream);
+int launch_exact_rows_gradient(const ExactRows& p, hipStream_t stream);
 int launch_exact_weight_gradient(const WeightGradient& p, hipStream_t stream);
 int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local);
 // The sums of `splits` parts of n (and of m) values each, in order, in the type `dt`.

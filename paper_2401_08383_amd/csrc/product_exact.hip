@@ -51,9 +51,9 @@ struct ExactOperand {
 };
 
 // D[row][col] = sum_r a(row, r) w(col, r), written where row < a.rows and col < w.rows; sums[row] = sum_r a(row, r) where wanted
-// (a across).
+// (a across); bias[col] is added where there is one.
 template <bool A_ACROSS, bool W_ACROSS>
-__device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperand<W_ACROSS> w, float* out, int64_t ldo, float* sums)
+__device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperand<W_ACROSS> w, float* out, int64_t ldo, float* sums, const float* bias)
 {
     typedef ExactOperand<A_ACROSS> OA;
     typedef ExactOperand<W_ACROSS> OW;
@@ -110,19 +110,20 @@ __device__ __forceinline__ void exact_tile(ExactOperand<A_ACROSS> a, ExactOperan
         for (int j = 0; j < 2; ++j) {
             const int row = row0 + i * 16 + in16, col = col0 + j * 16 + quad * 4;
             if (row >= a.rows || col >= w.rows) continue;
-            *reinterpret_cast<f32x4_t*>(out + static_cast<int64_t>(row) * ldo + col) = acc[0][i][j] + acc[1][i][j];
+            const f32x4_t sum = acc[0][i][j] + acc[1][i][j];
+            *reinterpret_cast<f32x4_t*>(out + static_cast<int64_t>(row) * ldo + col) = bias != nullptr ? sum + load4(bias + col) : sum;
         }
 }
 
-// ---- small problems: 16 (rows' gradient) or 32 (weights' gradient) x 64 outputs a workgroup, whose four wavefronts share the reduction
+// ---- small problems: 16 (products, rows' gradients) or 32 (weights' gradient) x 64 outputs a workgroup, whose four wavefronts share the reduction
 // (16 elements each in turn) and join their sums through LDS.  Operands come straight from memory into the registers that the matrix
 // instructions read, kAhead turns early.
 //   An operand across the reduction is loaded as it lies: a lane takes 16 bytes of a reduction element, four columns, and each of the four
 // is the operand of a matrix instruction of its own, whose 16 columns are then four apart.  (Loads of 4 bytes for 16 adjacent columns are
 // four times as many: gradient of 777 rows, 5 experts of 520 x 264 9.6 us with them, 8.9 without; with 16 rows a tile 7.3 to 8.1.)
 // Loads past the end deliver zeros (see product_tiles.hpp).
-//   A 16 x 16 x 4 product in fp32 takes 32 cycles, and few tiles are as fast as one of them: rows' gradients, whose experts often have few
-// rows, take 16.
+//   A 16 x 16 x 4 product in fp32 takes 32 cycles, and few tiles are as fast as one of them: products and rows' gradients, whose
+// experts often have few rows, take 16.
 constexpr int kSmallCols = 64, kAhead = 3;
 constexpr int small_rows(bool across) { return across ? 32 : 16; }
 constexpr int kSmallStride = kSmallCols + 4;
@@ -132,9 +133,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const float* base, i
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, static_cast<int>(floats * 4), 0x00020000);
 }
 
-// A_ACROSS: a's element (row, r) at a[r * lda + row], otherwise a[row * lda + r]; w's element (col, r) at w[r * ldw + col].
-template <bool A_ACROSS>
-__device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows, const float* w, int64_t ldw, int cols, int depth, float* out, int64_t ldo, float* sums)
+// A_ACROSS: a's element (row, r) at a[r * lda + row], otherwise a[row * lda + r]; W_ACROSS and w's element (col, r) alike.
+template <bool A_ACROSS, bool W_ACROSS>
+__device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows, const float* w, int64_t ldw, int cols, int depth, float* out, int64_t ldo, float* sums,
+                                           const float* bias)
 {
     constexpr int ROWS = small_rows(A_ACROSS), R = ROWS / 16;  // row groups
     __shared__ __attribute__((aligned(16))) float part[4][ROWS * kSmallStride];
@@ -144,14 +146,15 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
     int off_w[4], off_a[A_ACROSS ? 4 : R];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        off_w[q] = static_cast<int>(((quad * 4 + q) * ldw + min(in16 * 4, cols - 4)) * 4);
+        off_w[q] = static_cast<int>((W_ACROSS ? (quad * 4 + q) * ldw + min(in16 * 4, cols - 4) : min(q * 16 + in16, cols - 1) * ldw + quad * 4) * 4);
         if constexpr (A_ACROSS) off_a[q] = static_cast<int>(((quad * 4 + q) * lda + min(in16 * 2, rows - 2)) * 4);
     }
     if constexpr (!A_ACROSS)
 #pragma unroll
         for (int i = 0; i < R; ++i) off_a[i] = static_cast<int>((min(i * 16 + in16, rows - 1) * lda + quad * 4) * 4);
-    f32x4_t acc[R][4], fw[kAhead][4];  // [row group][column of a lane's four], [reduction element]
-    float fa[kAhead][R][4];            // [row group][reduction element]
+    f32x4_t acc[R][4];
+    f32x4_t fw[kAhead][4];   // across: [reduction element] of a lane's four columns; along: [16 columns] of its four reduction elements
+    float fa[kAhead][R][4];  // [row group][reduction element]
     float sum[R] = {};
 #pragma unroll
     for (int i = 0; i < R; ++i)
@@ -159,9 +162,10 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
         for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     auto load = [&](int turn, int s) {
         const int begin = (turn * 4 + wave) * 16, left = depth - begin, last = min(left, 16) - 1;
-        const auto from_w = buffer_of(w + begin * ldw, left > 0 ? last * ldw + cols : 0);
+        const auto from_w = W_ACROSS ? buffer_of(w + begin * ldw, left > 0 ? last * ldw + cols : 0) : buffer_of(w + begin, left > 0 ? (cols - 1) * ldw + left : 0);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) fw[s][q] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from_w, off_w[q], 0, 0));
+        for (int q = 0; q < 4; ++q)  // (a depth along memory is a multiple of four: all four or none)
+            fw[s][q] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from_w, W_ACROSS || quad * 4 < left ? off_w[q] : -16, 0, 0));
         if constexpr (A_ACROSS) {
             const auto from_a = buffer_of(a + begin * lda, left > 0 ? last * lda + rows : 0);
 #pragma unroll
@@ -170,7 +174,7 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
                 fa[s][0][q] = __uint_as_float(v[0]);
                 fa[s][1][q] = __uint_as_float(v[1]);
             }
-        } else {  // depth is a multiple of four: all four or none
+        } else {
             const auto from_a = buffer_of(a + begin, left > 0 ? (rows - 1) * lda + left : 0);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
@@ -192,7 +196,7 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
 #pragma unroll
                     for (int i = 0; i < R; ++i)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[s][q][j], fa[s][i][q], acc[i][j], 0, 0, 0);
+                        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(W_ACROSS ? fw[s][q][j] : fw[s][j][q], fa[s][i][q], acc[i][j], 0, 0, 0);
                 if (A_ACROSS && sums != nullptr)
 #pragma unroll
                     for (int i = 0; i < R; ++i) sum[i] += (fa[s][i][0] + fa[s][i][1]) + (fa[s][i][2] + fa[s][i][3]);
@@ -200,13 +204,14 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
             }
         }
     }
-    // a lane holds, of row group i, columns 16 quad + 4 v + j
+    // a lane holds in acc[i][j][v], of row group i, column 16 quad + 4 v + j of a w across, 16 j + 4 quad + v of one along
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int row = A_ACROSS ? in16 * 2 + i : i * 16 + in16;
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-            *reinterpret_cast<f32x4_t*>(&part[wave][row * kSmallStride + quad * 16 + v * 4]) = f32x4_t{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]};
+            *reinterpret_cast<f32x4_t*>(&part[wave][row * kSmallStride + (W_ACROSS ? quad * 16 + v * 4 : v * 16 + quad * 4)]) =
+                W_ACROSS ? f32x4_t{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]} : acc[i][v];
         if (A_ACROSS && sums != nullptr) {
             sum[i] = butterfly_add<16>(butterfly_add<32>(sum[i]));
             if (quad == 0) part_sum[wave][row] = sum[i];
@@ -217,14 +222,17 @@ __device__ __forceinline__ void small_tile(const float* a, int64_t lda, int rows
     for (int h = 0; h < R; ++h) {
         const int r = threadIdx.x / 16 + h * 16, c = threadIdx.x % 16 * 4, at = r * kSmallStride + c;
         auto of = [&](int wv) { return *reinterpret_cast<const f32x4_t*>(&part[wv][at]); };
-        if (r < rows && c < cols) *reinterpret_cast<f32x4_t*>(out + r * ldo + c) = (of(0) + of(1)) + (of(2) + of(3));
+        if (r >= rows || c >= cols) continue;
+        const f32x4_t sum = (of(0) + of(1)) + (of(2) + of(3));
+        *reinterpret_cast<f32x4_t*>(out + r * ldo + c) = bias != nullptr ? sum + load4(bias + c) : sum;
     }
     if (A_ACROSS && sums != nullptr && static_cast<int>(threadIdx.x) < min(ROWS, rows))
         sums[threadIdx.x] = (part_sum[0][threadIdx.x] + part_sum[1][threadIdx.x]) + (part_sum[2][threadIdx.x] + part_sum[3][threadIdx.x]);
 }
 
-template <bool SMALL>
-__global__ __launch_bounds__(256) void exact_rows_gradient_kernel(const RowsGradient p, int col_tiles)
+// W_ACROSS: rows' gradients; otherwise products.
+template <bool SMALL, bool W_ACROSS>
+__global__ __launch_bounds__(256) void exact_rows_kernel(const ExactRows p, int col_tiles)
 {
     constexpr int ROWS = SMALL ? small_rows(false) : kExactTile, COLS = SMALL ? kSmallCols : kExactTile;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
@@ -238,10 +246,12 @@ __global__ __launch_bounds__(256) void exact_rows_gradient_kernel(const RowsGrad
     const int row = wave_read_lane(range.lo, e) + (row_tile - wave_read_lane(upto - tiles, e)) * ROWS;
     const int col = col_tile * COLS, rows = min(ROWS, hi - row), cols = min(COLS, p.N - col);
     const int64_t K = p.K, N = p.N;
-    const float *a = static_cast<const float*>(p.rows) + row * K, *w = static_cast<const float*>(p.weight) + e * N * K + col;
+    const float *a = static_cast<const float*>(p.rows) + row * K, *w = static_cast<const float*>(p.weight) + (e * N * K + (W_ACROSS ? col : col * K));
     float* out = static_cast<float*>(p.out) + row * N + col;
-    if constexpr (SMALL) small_tile<false>(a, K, rows, w, N, cols, p.K, out, N, nullptr);
-    else exact_tile(ExactOperand<false>{a, K, rows, p.K, {}}, ExactOperand<true>{w, N, cols, p.K, {}}, out, N, nullptr);
+    const float* bias = !W_ACROSS && p.bias != nullptr ? static_cast<const float*>(p.bias) + e * N + col : nullptr;
+    const int64_t ldw = W_ACROSS ? N : K;
+    if constexpr (SMALL) small_tile<false, W_ACROSS>(a, K, rows, w, ldw, cols, p.K, out, N, nullptr, bias);
+    else exact_tile(ExactOperand<false>{a, K, rows, p.K, {}}, ExactOperand<W_ACROSS>{w, ldw, cols, p.K, {}}, out, N, nullptr, bias);
 }
 
 // Parts of the reduction (blockIdx.y) go to [part][E_local][N,K] and sums to [part][E_local][N].
@@ -262,8 +272,8 @@ __global__ __launch_bounds__(256) void exact_weight_kernel(const WeightGradient 
     const int rows = min(ROWS, p.N - row), cols = min(COLS, p.K - col);
     const float *a = static_cast<const float*>(p.dy) + begin * N + row, *w = static_cast<const float*>(p.x) + begin * K + col;
     float *out = static_cast<float*>(p.dw) + (at * N + row) * K + col, *sums = p.db != nullptr && col == 0 ? static_cast<float*>(p.db) + at * N + row : nullptr;
-    if constexpr (SMALL) small_tile<true>(a, N, rows, w, K, cols, n, out, K, sums);
-    else exact_tile(ExactOperand<true>{a, N, rows, n, {}}, ExactOperand<true>{w, K, cols, n, {}}, out, K, sums);
+    if constexpr (SMALL) small_tile<true, true>(a, N, rows, w, K, cols, n, out, K, sums, nullptr);
+    else exact_tile(ExactOperand<true>{a, N, rows, n, {}}, ExactOperand<true>{w, K, cols, n, {}}, out, K, sums, nullptr);
 }
 
 template <typename TO>
@@ -294,17 +304,21 @@ int launch_join_parts(const float* parts, int64_t n, void* out, const float* mor
 // Small tiles where larger ones would leave compute units without one.
 static bool small_tiles(int64_t large) { return large < 2 * 256; }
 
-int launch_exact_rows_gradient(const RowsGradient& p, hipStream_t stream)
+template <bool W_ACROSS>
+static int launch_exact_rows(const ExactRows& p, hipStream_t stream, const char* fn)
 {
     const int64_t most_experts = p.max_rows < p.E_local ? p.max_rows : p.E_local;
     auto tiles = [&](int64_t rows) { return (p.max_rows / rows + most_experts) * ((p.N + kExactTile - 1) / kExactTile); };
     const bool small = small_tiles(tiles(kExactTile));
     const int64_t grid = tiles(small ? small_rows(false) : kExactTile);
-    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_grouped_product_dx: too many tiles");
-    if (small) hipLaunchKernelGGL(exact_rows_gradient_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kSmallCols - 1) / kSmallCols);
-    else hipLaunchKernelGGL(exact_rows_gradient_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, (p.N + kExactTile - 1) / kExactTile);
+    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "%s: too many tiles", fn);
+    const int col_tiles = (p.N + kExactTile - 1) / kExactTile;
+    if (small) hipLaunchKernelGGL((exact_rows_kernel<true, W_ACROSS>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, col_tiles);
+    else hipLaunchKernelGGL((exact_rows_kernel<false, W_ACROSS>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, col_tiles);
     return EXF_OK;
 }
+int launch_exact_product(const ExactRows& p, hipStream_t stream) { return launch_exact_rows<false>(p, stream, "moe_grouped_product"); }
+int launch_exact_rows_gradient(const ExactRows& p, hipStream_t stream) { return launch_exact_rows<true>(p, stream, "moe_grouped_product_dx"); }
 
 // Parts of at least 256 rows until two workgroups a compute unit have one.
 static_assert(kSmallCols == kExactTile, "both kinds of tiles have as many columns");

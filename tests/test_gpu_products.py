@@ -130,6 +130,17 @@ def test_rows_in_tiles(kind, sizes, n, k):
         _rows_case(kind, sizes, k, n, "bf16")
 
 
+# fp32 with few tiles and with many; reductions and widths that end inside a step; both sides of the rows an expert that choose the kernel
+@pytest.mark.parametrize("kind", ["product", "dx"])
+@pytest.mark.parametrize("sizes,n,k", [
+    ([30, 0, 45], 4, 4), ([24], 68, 12), ([23, 25, 24], 60, 20), ([1, 70], 132, 36), ([200], 64, 68), ([47, 49], 128, 2052), ([40, 50], 72, 2048),
+    ([140, 120], 36, 4100), ([127, 0, 300], 100, 8196), ([700, 0, 333, 67], 2052, 100), ([64] * 40, 1028, 44), ([1500, 1, 63], 4096, 260),
+])
+def test_rows_in_fp32_tiles(kind, sizes, n, k):
+    _rows_case(kind, sizes, n, k, "f32", bias=kind == "product")
+    _rows_case(kind, sizes, n, k, "f32", before=3, behind=2, shift=1)
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_rows_of_random_sizes(seed):
     g = torch.Generator()
