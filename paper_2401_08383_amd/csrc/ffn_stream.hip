@@ -822,15 +822,23 @@ __device__ __forceinline__ void exact_units(const float* __restrict__ wexp, cons
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int k = u * kExactUnit + h * 16 + g * 4;  // K % 4 == 0: a piece is inside or outside as a whole
-            const bool in = k < K;
-            const int at = in ? k : 0;
+            const int at = k < K ? k : 0;
 #pragma unroll
             for (int c = 0; c < C; ++c) w[s][c][h] = *reinterpret_cast<const f32x4_t*>(row_w[c] + at);
 #pragma unroll
-            for (int m = 0; m < M; ++m) {
-                const f32x4_t v = *reinterpret_cast<const f32x4_t*>(row_a[m] + at);
-                a[s][m][h] = in ? v : f32x4_t{0.f, 0.f, 0.f, 0.f};
-            }
+            for (int m = 0; m < M; ++m) a[s][m][h] = *reinterpret_cast<const f32x4_t*>(row_a[m] + at);
+        }
+    };
+    // What the last unit has past the end is zero in both operands: an infinite weight times an activation's zero would be a NaN.
+    auto end = [&](int u, int s) {
+        if (u * kExactUnit + kExactUnit <= K) return;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bool in = u * kExactUnit + h * 16 + g * 4 < K;
+#pragma unroll
+            for (int c = 0; c < C; ++c) w[s][c][h] = in ? w[s][c][h] : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < M; ++m) a[s][m][h] = in ? a[s][m][h] : f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
     };
     // a lane holds four consecutive columns of one row
@@ -900,7 +908,10 @@ __device__ __forceinline__ void exact_units(const float* __restrict__ wexp, cons
         }
 #pragma unroll
         for (int s = 0; s < D; ++s)
-            if (u + s < u_end) compute(u + s, s);
+            if (u + s < u_end) {
+                end(u + s, s);
+                compute(u + s, s);
+            }
     }
     if constexpr (SUB > 1) {
         if (SUB == kExactParts || first_parts) {
@@ -1172,13 +1183,17 @@ struct PairWeights {
     {
         const int g = lane_id() >> 4;
         const float* row_a = act + (lane_id() & 15) * stride;
-        auto compute = [&](int u, int s) {
+        auto compute = [&](int u, int s, bool last) {  // last: the unit may end past the reduction
             f32x4_t a[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k = u * kExactUnit + h * 16 + g * 4;  // K % 4 == 0: a piece is inside or outside as a whole
                 a[h] = *reinterpret_cast<const f32x4_t*>(row_a + (k < K ? k : 0));
-                if (k >= K) a[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+            if (last && u * kExactUnit + kExactUnit > K) {  // what lies past the end is zero in both: an infinite weight times zero would be a NaN
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (u * kExactUnit + h * 16 + g * 4 >= K) a[h] = w[s][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -1190,7 +1205,7 @@ struct PairWeights {
         for (; u + kPairAhead < u_end; u += kPairAhead) {
 #pragma unroll
             for (int s = 0; s < kPairAhead; ++s) {
-                compute(u + s, s);
+                compute(u + s, s, false);
                 __builtin_amdgcn_sched_barrier(0);
                 load(min(u + kPairAhead + s, u_end - 1), s);
                 __builtin_amdgcn_sched_barrier(0);
@@ -1198,7 +1213,7 @@ struct PairWeights {
         }
 #pragma unroll
         for (int s = 0; s < kPairAhead; ++s)
-            if (u + s < u_end) compute(u + s, s);
+            if (u + s < u_end) compute(u + s, s, true);
     }
 };
 __host__ __device__ constexpr size_t pair_floats(int d, int f) { return static_cast<size_t>(kPairRows) * (f + 4) + static_cast<size_t>(kPairParts) * kPairRows * (d + 4); }
