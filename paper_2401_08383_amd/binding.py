@@ -273,7 +273,7 @@ def _bad(message: str):
 
 
 def _expect(name, t, shape, dtype, dev):
-    """`t` is a dense tensor of this shape and type on device number `dev` (-1: the host)."""
+    """`t` is a dense tensor of this shape and type on device number `dev` (-1: the host, see _on_device)."""
     if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
         return t
     if t.shape != shape:
@@ -283,15 +283,30 @@ def _expect(name, t, shape, dtype, dev):
     _bad(f"{name} must be contiguous and on device {dev}")
 
 
+def _on_device(dev):
+    """The arguments, all of them on device number `dev`, are where a kernel can reach them."""
+    if dev < 0:
+        _bad("the arguments must be on a GPU, they are on the host")
+
+
+def _bytes_of(workspace, dev):
+    """(address, size) of a caller's workspace, of any type."""
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous() or workspace.get_device() != dev:
+        _bad(f"workspace must be contiguous and on device {dev}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 _INT32, _UINT8 = torch.int32, torch.uint8
 
 
 def _fits(rows, width, offsets, E, w, out, out_shape, dt, dev):
-    """The rows [A,width], offsets, weights and result of a product are dense, of these shapes and types and on device number `dev` (one
+    """The rows [A,width], offsets, weights and result of a product are dense, of these shapes and types and on device number `dev`, a GPU (one
     expression: a call of a few microseconds spends a third of them on its checks)."""
     return (rows.shape[1] == width and offsets.shape == (E + 1,) and out.shape == out_shape and w.dtype is dt and out.dtype is dt and offsets.dtype is _INT32
             and rows.is_contiguous() and w.is_contiguous() and out.is_contiguous() and offsets.is_contiguous()
-            and w.get_device() == out.get_device() == offsets.get_device() == dev)
+            and w.get_device() == out.get_device() == offsets.get_device() == dev >= 0)
 
 
 def _grouped(rows, w_shape):
@@ -311,6 +326,7 @@ def _misfit(rows, rows_shape, offsets, E, w, out, out_shape, dt, dev):
     _expect("expert_offsets", offsets, (E + 1,), _INT32, dev)
     _expect("w", w, w.shape, dt, dev)
     _expect("out", out, out_shape, dt, dev)
+    _on_device(dev)
 
 
 def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
@@ -318,10 +334,10 @@ def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
     E, n, k, A, dt, code, dev = _grouped(x_sorted, w.shape)
     if out is None:
         out = torch.empty((A, n), dtype=dt, device=x_sorted.device)
-    if not _fits(x_sorted, k, expert_offsets, E, w, out, (A, n), dt, dev):
-        _misfit(x_sorted, (A, k), expert_offsets, E, w, out, (A, n), dt, dev)
     if bias is not None:
         bias = _expect("bias", bias, (E, n), dt, dev).data_ptr()
+    if not _fits(x_sorted, k, expert_offsets, E, w, out, (A, n), dt, dev):
+        _misfit(x_sorted, (A, k), expert_offsets, E, w, out, (A, n), dt, dev)
     rc = lib().moe_grouped_product(x_sorted.data_ptr(), expert_offsets.data_ptr(), w.data_ptr(), bias, A, n, k, E, code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -359,11 +375,13 @@ def moe_grouped_product_dw(dy_sorted, x_sorted, expert_offsets, want_bias=False,
         _expect("out_bias", out_bias, (E, n), grad_dtype, dev)
     elif want_bias:
         out_bias = torch.empty((E, n), dtype=grad_dtype, device=x_sorted.device)
+    _on_device(dev)
     if workspace is None:
         need = lib().moe_grouped_product_dw_workspace_bytes(A, n, k, E, code)
         workspace = _workspace(need, x_sorted.device) if need else None
+    workspace, size = _bytes_of(workspace, dev)
     rc = lib().moe_grouped_product_dw(dy_sorted.data_ptr(), x_sorted.data_ptr(), expert_offsets.data_ptr(), A, n, k, E, code, _CODES[grad_dtype], out.data_ptr(),
-                                      _ptr(out_bias), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+                                      _ptr(out_bias), workspace, size, _stream())
     if rc:
         _check(rc)
     return out, out_bias
@@ -411,6 +429,7 @@ def mx4_quantize(x, out=None):
                   torch.empty(((k + 255) // 256, rows, 8), dtype=torch.uint8, device=x.device))
     else:
         rows = _expect_mx4("out", out, shape, x.get_device())
+    _on_device(x.get_device())
     rc = lib().mx4_quantize(x.data_ptr(), rows, k, code, out.q.data_ptr(), out.scale.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -425,6 +444,7 @@ def mx4_dequantize(m, dtype=torch.bfloat16, out=None):
     code = _CODES.get(out.dtype)
     if code is None:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {out.dtype}")
+    _on_device(dev)
     rc = lib().mx4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), rows, shape[-1], code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -457,11 +477,13 @@ def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, 
     if bias is not None:
         bias = _expect("bias", bias, (E, n), dtype, dev).data_ptr()
     out = torch.empty((A, n), dtype=dtype, device=rows.device) if out is None else _expect("out", out, (A, n), dtype, dev)
+    _on_device(dev)
     if workspace is None and not held and A > EXF_MX4_INLINE_ROWS:
         need = lib().moe_grouped_product_mx4_workspace_bytes(A, n, k)
         workspace = _workspace(need, rows.device) if need else None
+    workspace, size = _bytes_of(workspace, dev)
     rc = lib().moe_grouped_product_mx4(rows.data_ptr(), x_scale, expert_offsets.data_ptr(), w.q.data_ptr(), w.scale.data_ptr(), bias, A, n, k, E, code,
-                                       out.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+                                       out.data_ptr(), workspace, size, _stream())
     if rc:
         _check(rc)
     return out
