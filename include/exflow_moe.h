@@ -62,6 +62,7 @@ extern "C" {
 #define EXF_DISPATCH_STATIC_MAX_ASSIGNMENTS (1ll << 20)  /* largest T*k of moe_dispatch_static */
 #define EXF_MAX_TRACE_LAYERS 256
 #define EXF_MAX_PRODUCT_WIDTH (1 << 21)  /* n and k of moe_grouped_product and its kin */
+#define EXF_MAX_PRODUCT_ROWS ((1ll << 31) - 1024)  /* A of these: rows are rounded up to tiles and stages in 32 bits */
 
 /* Library version (major*10000 + minor*100 + patch). */
 int exf_version(void);
@@ -216,7 +217,7 @@ int moe_combine(const void* y_sorted, const int32_t* sorted_of_src, const float*
  *   dw [E_local,n,k], db [E_local,n] (NULL: not wanted) of type grad_dt, EXF_F32 or dt, overwritten, not accumulated.
  *   A must be an upper bound on expert_offsets[E_local].  Outputs must not overlap inputs.
  * All sums are kept in fp32 and rounded once.
- * Shapes: 0 <= A < 2^31; 1 <= n, k <= EXF_MAX_PRODUCT_WIDTH, multiples of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
+ * Shapes: 0 <= A <= EXF_MAX_PRODUCT_ROWS; 1 <= n, k <= EXF_MAX_PRODUCT_WIDTH, multiples of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
  * workspace: moe_grouped_product_dw_workspace_bytes(A, n, k, E_local, dt) bytes (partial sums of a long reduction).
  * ------------------------------------------------------------------------------------- */
 int moe_grouped_product(const void* x_sorted, const int32_t* expert_offsets, const void* w, const void* bias, int64_t A,

@@ -6,7 +6,7 @@ namespace exf {
 static int check_sizes(const char* fn, int64_t A, int n, int k, int E_local, int dt)
 {
     if (dt != EXF_F32 && dt != EXF_BF16) return fail(EXF_ERR_BAD_DTYPE, "%s: dt = %d", fn, dt);
-    if (A < 0 || A >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "%s: A = %lld outside [0,2^31)", fn, static_cast<long long>(A));
+    if (A < 0 || A > EXF_MAX_PRODUCT_ROWS) return fail(EXF_ERR_BAD_SHAPE, "%s: A = %lld outside [0,%lld]", fn, static_cast<long long>(A), EXF_MAX_PRODUCT_ROWS);
     if (E_local < 1 || E_local > EXF_MAX_EXPERTS) return fail(EXF_ERR_BAD_SHAPE, "%s: E_local = %d outside [1,%d]", fn, E_local, EXF_MAX_EXPERTS);
     const int gran = dt == EXF_BF16 ? 8 : 4;
     if (n < gran || n % gran != 0 || k < gran || k % gran != 0)

@@ -1,0 +1,34 @@
+"""Sizes at the ends of what the experts' products take, without a GPU: what the kernels' arithmetic cannot hold is refused."""
+import ctypes
+
+import pytest
+
+import paper_2401_08383_amd as exf
+from paper_2401_08383_amd import binding as B
+
+
+def _p(i):  # aligned, never dereferenced
+    return ctypes.c_void_p((i + 1) << 40)
+
+
+ROWS = (1 << 31) - 1024  # EXF_MAX_PRODUCT_ROWS
+CALLS = {  # the result is NULL: sizes that are taken come back with that error, and nothing is launched
+    "product": lambda A, dt: exf.lib().moe_grouped_product(_p(0), _p(1), _p(2), None, A, 8, 8, 1, dt, None, None),
+    "dx": lambda A, dt: exf.lib().moe_grouped_product_dx(_p(0), _p(1), _p(2), A, 8, 8, 1, dt, None, None),
+    "dw": lambda A, dt: exf.lib().moe_grouped_product_dw(_p(0), _p(1), _p(2), A, 8, 8, 1, dt, dt, None, None, _p(3), 1 << 40, None),
+    "mx4": lambda A, dt: exf.lib().moe_grouped_product_mx4(_p(0), _p(1), _p(2), _p(3), _p(4), None, A, 8, 32, 1, dt, None, None, 0, None),
+}
+
+
+@pytest.mark.parametrize("dt", [B.EXF_BF16, B.EXF_F32])
+@pytest.mark.parametrize("call", list(CALLS))
+def test_rows(call, dt):
+    """An expert with all rows: they are rounded up to tiles of 320 rows and stages of 64 in 32 bits.  With 2^31 - 63 rows and more the weights'
+    gradient had a negative number of stages, and came out as zeros."""
+    for rows in (ROWS + 1, (1 << 31) - 64, (1 << 31) - 1):
+        assert CALLS[call](rows, dt) == B.EXF_ERR_BAD_SHAPE, rows
+    assert CALLS[call](ROWS, dt) == B.EXF_ERR_NULL_PTR
+    int32 = lambda v: ctypes.c_int32(v).value  # noqa: E731
+    assert int32((1 << 31) - 63 + 63) < 0  # what they were
+    for step in (64, 320, 12 * 64):  # a stage, the tallest tile, the stages that small tiles look ahead
+        assert int32(ROWS + step) == ROWS + step
