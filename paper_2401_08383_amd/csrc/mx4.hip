@@ -11,6 +11,8 @@ namespace exf {
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2_t;
 
 constexpr int kScaleTile = 256;
+constexpr int scale_tiles(int k) { return (k - 1) / kScaleTile + 1; }  // (k at least 1)
+static_assert(scale_tiles(1) == 1 && scale_tiles(256) == 1 && scale_tiles(257) == 2 && scale_tiles(0x7fffffff) == 1 << 23, "any k there is");
 
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, int64_t rows, int k, int tiles, uint32_t* __restrict__ q,
@@ -93,7 +95,7 @@ static int check_mx4(const char* fn, const void* x, int64_t rows, int k, int dt,
 extern "C" size_t mx4_scale_bytes(int64_t rows, int k)
 {
     if (rows < 0 || k < 1) return 0;
-    return static_cast<size_t>((k + exf::kScaleTile - 1) / exf::kScaleTile) * static_cast<size_t>(rows) * (exf::kScaleTile / EXF_MX4_BLOCK);
+    return static_cast<size_t>(exf::scale_tiles(k)) * static_cast<size_t>(rows) * (exf::kScaleTile / EXF_MX4_BLOCK);
 }
 
 extern "C" int mx4_quantize(const void* x, int64_t rows, int k, int dt, uint8_t* q, uint8_t* scale, void* stream)
@@ -101,7 +103,7 @@ extern "C" int mx4_quantize(const void* x, int64_t rows, int k, int dt, uint8_t*
     using namespace exf;
     if (int rc = check_mx4("mx4_quantize", x, rows, k, dt, q, scale)) return rc;
     if (rows == 0) return EXF_OK;
-    const int tiles = (k + kScaleTile - 1) / kScaleTile;
+    const int tiles = scale_tiles(k);
     const int64_t items = (rows + 1) / 2 * tiles;
     const unsigned grid = static_cast<unsigned>(items / 4 + 1 < 4 * kStreamWorkgroups ? items / 4 + 1 : 4 * kStreamWorkgroups);
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -115,7 +117,7 @@ extern "C" int mx4_dequantize(const uint8_t* q, const uint8_t* scale, int64_t ro
     using namespace exf;
     if (int rc = check_mx4("mx4_dequantize", out, rows, k, dt, q, scale)) return rc;
     if (rows == 0) return EXF_OK;
-    const int tiles = (k + kScaleTile - 1) / kScaleTile;
+    const int tiles = scale_tiles(k);
     const int64_t items = (rows + 1) / 2 * tiles;
     const unsigned grid = static_cast<unsigned>(items / 4 + 1 < 4 * kStreamWorkgroups ? items / 4 + 1 : 4 * kStreamWorkgroups);
     hipStream_t s = static_cast<hipStream_t>(stream);
