@@ -218,7 +218,7 @@ int moe_combine(const void* y_sorted, const int32_t* sorted_of_src, const float*
  *   A must be an upper bound on expert_offsets[E_local].  Outputs must not overlap inputs.
  * All sums are kept in fp32 and rounded once.
  * Shapes: 0 <= A <= EXF_MAX_PRODUCT_ROWS; 1 <= n, k <= EXF_MAX_PRODUCT_WIDTH, multiples of 8 (bf16) / 4 (fp32); 1 <= E_local <= EXF_MAX_EXPERTS.
- * workspace: moe_grouped_product_dw_workspace_bytes(A, n, k, E_local, dt) bytes (partial sums of a long reduction).
+ * workspace: moe_grouped_product_dw_workspace_bytes(A, n, k, E_local, dt) bytes (partial sums of a long reduction; 0 for sizes that the call refuses).
  * ------------------------------------------------------------------------------------- */
 int moe_grouped_product(const void* x_sorted, const int32_t* expert_offsets, const void* w, const void* bias, int64_t A,
                         int n, int k, int E_local, int dt, void* y_sorted, void* stream);

@@ -90,9 +90,15 @@ extern "C" int moe_grouped_product_dx(const void* dy_sorted, const int32_t* expe
     return rc == EXF_OK ? check_launch("moe_grouped_product_dx") : rc;
 }
 
+// Sizes that a workspace is computed for: others are refused by the call, and would overflow on the way.
+static bool sizes_fit(int64_t A, int n, int k)
+{
+    return A >= 1 && A <= EXF_MAX_PRODUCT_ROWS && n >= 1 && n <= EXF_MAX_PRODUCT_WIDTH && k >= 1 && k <= EXF_MAX_PRODUCT_WIDTH;
+}
+
 extern "C" size_t moe_grouped_product_dw_workspace_bytes(int64_t A, int n, int k, int E_local, int dt)
 {
-    if (A < 1 || n < 1 || k < 1 || E_local < 1 || (dt != EXF_BF16 && dt != EXF_F32)) return 0;
+    if (!sizes_fit(A, n, k) || E_local < 1 || E_local > EXF_MAX_EXPERTS || (dt != EXF_BF16 && dt != EXF_F32)) return 0;
     const int splits = dt == EXF_BF16 ? exf::weight_gradient_splits(A, n, k, E_local) : exf::exact_weight_gradient_splits(A, n, k, E_local);
     return splits > 1 ? exf::align_up(static_cast<size_t>(splits) * E_local * n * (static_cast<size_t>(k) + 1) * 4, 256) : 0;  // dw's and db's
 }
@@ -138,7 +144,7 @@ extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorte
 
 extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int n, int k)
 {
-    if (A < 0 || n < 1 || k < 1 || exf::mx4_product_is_small(A, n, k)) return 0;
+    if (!sizes_fit(A, n, k) || exf::mx4_product_is_small(A, n, k)) return 0;
     return exf::align_up(static_cast<size_t>(A) * k / 2, 256) + exf::align_up(mx4_scale_bytes(A, k), 256);
 }
 

@@ -1,10 +1,15 @@
 """Sizes at the ends of what the experts' products take, without a GPU: what the kernels' arithmetic cannot hold is refused."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
 import paper_2401_08383_amd as exf
 from paper_2401_08383_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def _p(i):  # aligned, never dereferenced
@@ -32,3 +37,12 @@ def test_rows(call, dt):
     assert int32((1 << 31) - 63 + 63) < 0  # what they were
     for step in (64, 320, 12 * 64):  # a stage, the tallest tile, the stages that small tiles look ahead
         assert int32(ROWS + step) == ROWS + step
+
+
+# Sizes that no call takes, some of which overflow to zero on the way to a division.
+@pytest.mark.parametrize("query", ["mx4_workspace_bytes(1 << 62, 64, 4)", "mx4_workspace_bytes(1 << 40, 1 << 30, 1 << 24)", "mx4_workspace_bytes(-1, 64, 32)",
+                                   "dw_workspace_bytes(1000, 8, 8, 1 << 24, 0)", "dw_workspace_bytes(1000, 8, 8, 1 << 24, 1)", "dw_workspace_bytes(1 << 62, 2147483647, 8, 1, 0)",
+                                   "dw_workspace_bytes(1 << 20, 64, 2147483647, 1, 1)", "dw_workspace_bytes(1 << 20, 64, 64, 65, 0)", "dw_workspace_bytes(1 << 20, 64, 64, 1, 7)"])
+def test_queries_of_sizes_that_no_call_takes(query):
+    code = f"import paper_2401_08383_amd as exf; assert exf.lib().moe_grouped_product_{query} == 0"
+    assert subprocess.run([sys.executable, "-c", code], cwd=ROOT).returncode == 0
