@@ -298,6 +298,13 @@ def _bytes_of(workspace, dev):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+def _untracked(name):
+    """An argument requires a gradient, which a result of these calls does not carry on."""
+    if torch.is_grad_enabled():
+        raise ExflowError(EXF_ERR_NOT_IMPLEMENTED, f"{name} records no autograd history and an argument requires a gradient: call it under torch.no_grad(), or in the "
+                                                   "forward of a torch.autograd.Function whose backward calls moe_grouped_product_dx and moe_grouped_product_dw")
+
+
 _INT32, _UINT8 = torch.int32, torch.uint8
 
 
@@ -330,7 +337,11 @@ def _misfit(rows, rows_shape, offsets, E, w, out, out_shape, dt, dev):
 
 
 def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
-    """y[s] = x_sorted[s] W_e^T (+ bias[e]) for the rows of every expert; w [E_local,n,k]."""
+    """y[s] = x_sorted[s] W_e^T (+ bias[e]) for the rows of every expert; w [E_local,n,k].
+
+    No autograd history is recorded: in grad mode an argument that requires a gradient is refused (here and in the calls below)."""
+    if x_sorted.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad):
+        _untracked("moe_grouped_product")
     E, n, k, A, dt, code, dev = _grouped(x_sorted, w.shape)
     if out is None:
         out = torch.empty((A, n), dtype=dt, device=x_sorted.device)
@@ -346,6 +357,8 @@ def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
 
 def moe_grouped_product_dx(dy_sorted, expert_offsets, w, out=None):
     """Gradient of moe_grouped_product's rows: dx[s] = dy_sorted[s] W_e; w [E_local,n,k]."""
+    if dy_sorted.requires_grad or w.requires_grad:
+        _untracked("moe_grouped_product_dx")
     E, n, k, A, dt, code, dev = _grouped(dy_sorted, w.shape)
     if out is None:
         out = torch.empty((A, k), dtype=dt, device=dy_sorted.device)
@@ -360,6 +373,8 @@ def moe_grouped_product_dx(dy_sorted, expert_offsets, w, out=None):
 def moe_grouped_product_dw(dy_sorted, x_sorted, expert_offsets, want_bias=False, grad_dtype=None, workspace=None, out=None, out_bias=None):
     """Gradients of moe_grouped_product's weights and bias: (dw [E_local,n,k], db [E_local,n] or None), both of `grad_dtype` (that of
     ``out``, or the rows')."""
+    if dy_sorted.requires_grad or x_sorted.requires_grad:
+        _untracked("moe_grouped_product_dw")
     if len(dy_sorted.shape) != 2 or len(x_sorted.shape) != 2 or len(expert_offsets.shape) != 1:
         _bad("rows are [A,n] and [A,k], expert_offsets [E_local+1]")
     E, n, k, A, dt, code, dev = _grouped(x_sorted, (expert_offsets.shape[0] - 1, dy_sorted.shape[1], x_sorted.shape[1]))
@@ -456,6 +471,8 @@ def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, 
     quantises.  The result has the type of the rows, or `dtype` (bf16)."""
     held = isinstance(x_sorted, Mx4)
     rows = x_sorted.q if held else x_sorted
+    if rows.requires_grad or (bias is not None and bias.requires_grad):
+        _untracked("moe_grouped_product_mx4")
     if len(w.q.shape) != 3 or len(rows.shape) != 2:
         _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {tuple(w.shape)}")
     E, n, k = w.q.shape
