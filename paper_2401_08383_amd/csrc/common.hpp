@@ -278,10 +278,17 @@ __device__ __forceinline__ void lds_dma_16B_stream(const unsigned char* base, ui
 
 // One wavefront-wide direct-to-LDS load of 4 bytes per lane: lane i fetches base + voff and the word
 // lands at LDS byte address lds_addr + 4*i.
+//   A memory instruction must follow five wait states behind a vector instruction that wrote a scalar register it reads, and the compiler, which looks
+// into no assembly, does not see to it: FRESH waits them out, whatever stands in front (v_readfirstlane; v_readlane of a spilled register).  Loads of a loop
+// whose bases are stepped by scalar instructions go without, as the loads of 16 bytes do; the built code is checked for all of them.
+template <bool FRESH = true>
 __device__ __forceinline__ void lds_dma_4B(const unsigned char* base, uint32_t voff, uint32_t lds_addr)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n" : : "v"(voff), "s"(base), "s"(lds_addr) : "memory");
+    if constexpr (FRESH)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dword %0, %1\n" : : "v"(voff), "s"(base), "s"(lds_addr) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n" : : "v"(voff), "s"(base), "s"(lds_addr) : "memory");
 #else
     (void)base; (void)voff; (void)lds_addr;
 #endif

@@ -64,7 +64,11 @@ __device__ __forceinline__ const unsigned char* probe_uniform(const unsigned cha
     const uint64_t v = reinterpret_cast<uint64_t>(p);
     const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
     const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
-    return reinterpret_cast<const unsigned char*>((static_cast<uint64_t>(hi) << 32) | lo);
+    uint64_t u = (static_cast<uint64_t>(hi) << 32) | lo;
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_nop 3" : "+s"(u));  // (five wait states between these and the memory instructions in probe_dma_16B, which the compiler does not see)
+#endif
+    return reinterpret_cast<const unsigned char*>(u);
 }
 constexpr int kLoopExperts = 8, kLoopRows = 1024, kLoopCols = 4096, kLoopK = 1024;
 constexpr size_t kLoopActBytes = static_cast<size_t>(kLoopExperts) * kLoopRows * kLoopK * 2;

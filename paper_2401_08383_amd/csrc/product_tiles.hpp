@@ -186,7 +186,7 @@ struct StagedScales {
         if (todo > 0) base += left == 1 ? back : step;  // (behind the last stage it is loaded again: nobody reads it)
         left -= 1;
     }
-    __device__ __forceinline__ void load(int i, uint32_t lds_addr, int wave) { lds_dma_4B(base, off[i], lds_addr + group(i, wave) * 256); }
+    __device__ __forceinline__ void load(int i, uint32_t lds_addr, int wave) { lds_dma_4B<false>(base, off[i], lds_addr + group(i, wave) * 256); }
     __device__ __forceinline__ static uint32_t fetch_base(int row0) { return static_cast<uint32_t>((row0 + (lane_id() & 15)) * 8 + (lane_id() >> 4)); }
     __device__ __forceinline__ static int fetch(uint32_t stage, uint32_t from, int b, int ks) { return lds_fetch<uint8_t>(stage + from + static_cast<uint32_t>(b * 128 + ks * 4)); }
 };
