@@ -708,44 +708,44 @@ __global__ __launch_bounds__(W * 64) void stream_gemm_kernel(const StreamGemm p)
 }
 
 template <int C8, int W, StreamRows ROWS, StreamKeep KEEP, bool SECOND>
-static int launch_stream_as(const StreamGemm& p, hipStream_t stream)
+static int launch_stream_as(const StreamGemm& p, hipStream_t stream, const char* fn)
 {
     constexpr size_t lds = static_cast<size_t>(stream_ring_bytes(C8, W)) + W * kStreamIdBytes + (ROWS == kRowsInline ? sizeof(InlineDispatch) : (ROWS == kRowsEight ? W * stream_sums_bytes(C8) : 0));
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     auto kern = stream_gemm_kernel<C8, W, ROWS, KEEP, SECOND>;
     static std::atomic<uint64_t> allowed{0};
-    if (int rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, "moe_expert_ffn")) return rc;
+    if (int rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, fn)) return rc;
     hipLaunchKernelGGL(kern, dim3(kStreamGrid), dim3(W * kWave), lds, stream, p);
     return EXF_OK;
 }
 
 enum StreamWant { kWantResult, kWantSorted, kWantPairs };  // the last: rows that meet in p.exchange
 template <int C8, int W, StreamRows ROWS, StreamWant WANT>
-static int launch_stream_rows(const StreamGemm& p, hipStream_t stream)
+static int launch_stream_rows(const StreamGemm& p, hipStream_t stream, const char* fn)
 {
     const bool second = p.epi == kEpiNone;
     if constexpr (WANT == kWantResult) {
         if constexpr (ROWS != kRowsInline) {  // (a first contraction)
-            if (second) return launch_stream_as<C8, W, ROWS, kKeepNone, true>(p, stream);
+            if (second) return launch_stream_as<C8, W, ROWS, kKeepNone, true>(p, stream, fn);
         }
-        return launch_stream_as<C8, W, ROWS, kKeepNone, false>(p, stream);
+        return launch_stream_as<C8, W, ROWS, kKeepNone, false>(p, stream, fn);
     } else {
         if constexpr (WANT == kWantSorted && ROWS != kRowsSorted) {  // (rows that are there in sorted order are not wanted again)
-            if (!second && p.sorted_act != nullptr) return launch_stream_as<C8, W, ROWS, kKeepAct, false>(p, stream);
+            if (!second && p.sorted_act != nullptr) return launch_stream_as<C8, W, ROWS, kKeepAct, false>(p, stream, fn);
         }
         if constexpr (WANT == kWantSorted && ROWS != kRowsInline) {
-            if (second && p.sorted_out != nullptr) return launch_stream_as<C8, W, ROWS, kKeepOut, true>(p, stream);
+            if (second && p.sorted_out != nullptr) return launch_stream_as<C8, W, ROWS, kKeepOut, true>(p, stream, fn);
         }
-        if constexpr (WANT == kWantPairs && ROWS != kRowsInline) return launch_stream_as<C8, W, ROWS, kKeepPairs, true>(p, stream);
-        return fail(EXF_ERR_BAD_SHAPE, "moe_expert_ffn: sorted rows of a contraction that has none");
+        if constexpr (WANT == kWantPairs && ROWS != kRowsInline) return launch_stream_as<C8, W, ROWS, kKeepPairs, true>(p, stream, fn);
+        return fail(EXF_ERR_BAD_SHAPE, "%s: sorted rows of a contraction that has none", fn);
     }
 }
 template <int C8, int W, StreamWant WANT>
-static int launch_stream(const StreamGemm& p, hipStream_t stream)
+static int launch_stream(const StreamGemm& p, hipStream_t stream, const char* fn)
 {
-    if (p.topk_idx == nullptr) return launch_stream_rows<C8, W, kRowsSorted, WANT>(p, stream);
-    if (p.max_rows <= 8) return launch_stream_rows<C8, W, kRowsEight, WANT>(p, stream);
-    return p.max_rows <= kFewAssignments ? launch_stream_rows<C8, W, kRowsFew, WANT>(p, stream) : launch_stream_rows<C8, W, kRowsInline, WANT>(p, stream);
+    if (p.topk_idx == nullptr) return launch_stream_rows<C8, W, kRowsSorted, WANT>(p, stream, fn);
+    if (p.max_rows <= 8) return launch_stream_rows<C8, W, kRowsEight, WANT>(p, stream, fn);
+    return p.max_rows <= kFewAssignments ? launch_stream_rows<C8, W, kRowsFew, WANT>(p, stream, fn) : launch_stream_rows<C8, W, kRowsInline, WANT>(p, stream, fn);
 }
 
 // Columns per block, by a model of the launch (blocks of 8 columns: one row of 4096 x 1024 has 128 of them for 256 workgroups
@@ -757,7 +757,7 @@ static int launch_stream(const StreamGemm& p, hipStream_t stream)
 // kFewAssignments in all (four experts of 512 x 2048, 120 rows 20.7 us with them and 18.5) and 28 an expert (two of 768 x 3072, 60
 // rows 23.0 and 20.4; 48 rows 16.4 and 16.9).
 template <StreamWant WANT>
-static int launch_stream_bf16(const StreamGemm& p, hipStream_t stream)
+static int launch_stream_bf16(const StreamGemm& p, hipStream_t stream, const char* fn)
 {
     const double A = p.max_rows, E = p.E_local;
     const double touched = E * (1.0 - exp(A * log1p(-1.0 / E)));  // experts with rows, if A rows fall on E experts at random
@@ -774,10 +774,10 @@ static int launch_stream_bf16(const StreamGemm& p, hipStream_t stream)
             best = c;
         }
     }
-    if (best == 8) return launch_stream<8, 4, WANT>(p, stream);
-    if (best == 4) return launch_stream<4, 4, WANT>(p, stream);
-    if (best == 2) return launch_stream<2, 8, WANT>(p, stream);
-    return launch_stream<1, 8, WANT>(p, stream);
+    if (best == 8) return launch_stream<8, 4, WANT>(p, stream, fn);
+    if (best == 4) return launch_stream<4, 4, WANT>(p, stream, fn);
+    if (best == 2) return launch_stream<2, 8, WANT>(p, stream, fn);
+    return launch_stream<1, 8, WANT>(p, stream, fn);
 }
 
 // ---------------------------------------------------------------------------- fp32
@@ -1059,36 +1059,36 @@ __global__ __launch_bounds__(WK* WI * 64) void exact_gemm_kernel(const StreamGem
 }
 
 template <int C, int M, int WK, int WI, int D, bool INLINE, StreamKeep KEEP>
-static int launch_exact_as(const StreamGemm& p, hipStream_t stream)
+static int launch_exact_as(const StreamGemm& p, hipStream_t stream, const char* fn)
 {
     constexpr int TILE_ROWS = 16 * M;
     constexpr size_t lds = static_cast<size_t>(exact_slots(WK) * WI) * TILE_ROWS * (16 * C + 4) * sizeof(float) + (INLINE ? sizeof(InlineDispatch) : 0);
     auto kern = exact_gemm_kernel<C, M, WK, WI, D, INLINE, KEEP>;
     static std::atomic<uint64_t> allowed{0};
-    if (int rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, "moe_expert_ffn")) return rc;
+    if (int rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, fn)) return rc;
     // row tiles: whole ones and at most one partial tile per expert with rows
     const int64_t A = p.max_rows;
     const int64_t row_tiles = A / TILE_ROWS + (A < p.E_local ? A : p.E_local);
     const int64_t share = row_tiles * ((p.N + 16 * C - 1) / (16 * C)) / kXcdCount + 1;  // items of an XCD at most
     const int64_t grid = (share + WI - 1) / WI * kXcdCount;
-    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_expert_ffn: too many tiles");
+    if (grid >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "%s: too many tiles", fn);
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(WK * WI * kWave), lds, stream, p);
     return EXF_OK;
 }
 
 template <int C, int M, int WK, int WI, int D>
-static int launch_exact(const StreamGemm& p, hipStream_t stream)
+static int launch_exact(const StreamGemm& p, hipStream_t stream, const char* fn)
 {
     if (p.topk_idx != nullptr) {
-        if (p.sorted_act != nullptr) return launch_exact_as<C, M, WK, WI, D, true, kKeepAct>(p, stream);
-        return launch_exact_as<C, M, WK, WI, D, true, kKeepNone>(p, stream);
+        if (p.sorted_act != nullptr) return launch_exact_as<C, M, WK, WI, D, true, kKeepAct>(p, stream, fn);
+        return launch_exact_as<C, M, WK, WI, D, true, kKeepNone>(p, stream, fn);
     }
     if (p.exchange != nullptr) {
-        if (p.sorted_out != nullptr) return fail(EXF_ERR_BAD_SHAPE, "moe_expert_ffn: sorted rows of a contraction that keeps none");
-        return launch_exact_as<C, M, WK, WI, D, false, kKeepPairs>(p, stream);
+        if (p.sorted_out != nullptr) return fail(EXF_ERR_BAD_SHAPE, "%s: sorted rows of a contraction that keeps none", fn);
+        return launch_exact_as<C, M, WK, WI, D, false, kKeepPairs>(p, stream, fn);
     }
-    if (p.sorted_out != nullptr) return launch_exact_as<C, M, WK, WI, D, false, kKeepOut>(p, stream);
-    return launch_exact_as<C, M, WK, WI, D, false, kKeepNone>(p, stream);
+    if (p.sorted_out != nullptr) return launch_exact_as<C, M, WK, WI, D, false, kKeepOut>(p, stream, fn);
+    return launch_exact_as<C, M, WK, WI, D, false, kKeepNone>(p, stream, fn);
 }
 
 // Enough tiles of 64 columns x 16 M rows for the chip: one wavefront per tile of 64 rows where the reduction is short (nothing to
@@ -1099,12 +1099,12 @@ constexpr int64_t kExactFewTiles = 384;
 constexpr int kExactShortReduction = 1024;
 static int64_t exact_tiles(int64_t A, int N, int E_local, int rows) { return ((A < E_local ? A : E_local) + A / rows) * ((N + 63) / 64); }
 template <int M>
-static int launch_exact_rows(const StreamGemm& p, hipStream_t stream)
+static int launch_exact_rows(const StreamGemm& p, hipStream_t stream, const char* fn)
 {
-    if (exact_tiles(p.max_rows, p.N, p.E_local, 16 * M) < kExactFewTiles) return launch_exact<1, 1, 4, 1, 2>(p, stream);
-    if (p.K > kExactShortReduction) return launch_exact<4, M, 4, 1, 2>(p, stream);
-    if constexpr (M == 1) return launch_exact<2, 1, 2, 2, 2>(p, stream);
-    else return launch_exact<4, M, 1, 4, 2>(p, stream);
+    if (exact_tiles(p.max_rows, p.N, p.E_local, 16 * M) < kExactFewTiles) return launch_exact<1, 1, 4, 1, 2>(p, stream, fn);
+    if (p.K > kExactShortReduction) return launch_exact<4, M, 4, 1, 2>(p, stream, fn);
+    if constexpr (M == 1) return launch_exact<2, 1, 2, 2, 2>(p, stream, fn);
+    else return launch_exact<4, M, 1, 4, 2>(p, stream, fn);
 }
 
 // What an fp32 contraction [A,K] x [N,K] takes in launch_exact_rows<tall ? 4 : 1>, us.  Fitted to both contractions of 1540 lists (1025 to 100000 rows,
@@ -1436,14 +1436,14 @@ bool stream_path_fits(int64_t A, int d, int f, int E_local, int dt)
     return rows * d * f <= 120000ll * (static_cast<int64_t>(d) + f);
 }
 
-int launch_stream_gemm(const StreamGemm& p, int dt, hipStream_t stream)
+int launch_stream_gemm(const StreamGemm& p, int dt, hipStream_t stream, const char* fn)
 {
     if (dt == EXF_BF16) {
-        if (p.epi == kEpiNone && p.exchange != nullptr) return launch_stream_bf16<kWantPairs>(p, stream);
-        if (p.sorted_act == nullptr && p.sorted_out == nullptr) return launch_stream_bf16<kWantResult>(p, stream);
-        return launch_stream_bf16<kWantSorted>(p, stream);
+        if (p.epi == kEpiNone && p.exchange != nullptr) return launch_stream_bf16<kWantPairs>(p, stream, fn);
+        if (p.sorted_act == nullptr && p.sorted_out == nullptr) return launch_stream_bf16<kWantResult>(p, stream, fn);
+        return launch_stream_bf16<kWantSorted>(p, stream, fn);
     }
-    return tall_exact_tiles(p.max_rows, p.K, p.N, p.E_local, p.epi != kEpiNone) ? launch_exact_rows<4>(p, stream) : launch_exact_rows<1>(p, stream);
+    return tall_exact_tiles(p.max_rows, p.K, p.N, p.E_local, p.epi != kEpiNone) ? launch_exact_rows<4>(p, stream, fn) : launch_exact_rows<1>(p, stream, fn);
 }
 
 }  // namespace exf

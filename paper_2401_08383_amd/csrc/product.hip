@@ -67,7 +67,7 @@ extern "C" int moe_grouped_product(const void* x_sorted, const int32_t* expert_o
         StreamGemm g{};
         g.act = x_sorted, g.weight = w, g.bias = bias, g.out = y_sorted, g.offsets = expert_offsets;
         g.max_rows = static_cast<int>(A), g.K = k, g.N = n, g.E_local = E_local, g.epi = kEpiNone;
-        rc = launch_stream_gemm(g, dt, s);
+        rc = launch_stream_gemm(g, dt, s, "moe_grouped_product");
     } else {
         rc = launch_forward_tiles({x_sorted, expert_offsets, w, static_cast<const bf16_t*>(bias), static_cast<bf16_t*>(y_sorted), nullptr, nullptr, static_cast<int>(A), k, n, E_local}, s);
     }

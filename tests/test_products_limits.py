@@ -5,6 +5,7 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
 import paper_2401_08383_amd as exf
 from paper_2401_08383_amd import binding as B
@@ -46,3 +47,10 @@ def test_rows(call, dt):
 def test_queries_of_sizes_that_no_call_takes(query):
     code = f"import paper_2401_08383_amd as exf; assert exf.lib().moe_grouped_product_{query} == 0"
     assert subprocess.run([sys.executable, "-c", code], cwd=ROOT).returncode == 0
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="what fails here is that there is no GPU")
+def test_errors_name_the_call():
+    """bf16 with few rows an expert goes to the weight streams, whose other user is moe_expert_ffn."""
+    rc = exf.lib().moe_grouped_product(_p(0), _p(1), _p(2), None, 4, 64, 64, 1, B.EXF_BF16, _p(3), None)
+    assert rc == B.EXF_ERR_HIP and B.last_error().startswith("moe_grouped_product:")
