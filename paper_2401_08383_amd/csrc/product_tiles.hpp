@@ -1,5 +1,5 @@
 // The experts' products in tiles, a workgroup of four wavefronts a tile (product_forward.hip, product_rows_gradient.hip,
-// product_weight_gradient.hip, product_mx4.hip instantiate it).
+// product_weight_gradient.hip, product_mx4_tiles.hip instantiate it).
 //
 // As in ffn_tiles.hpp, whose row tiles and whose map from workgroups to them are used: H x NT outputs in 16x16 accumulators in the accumulator
 // half of the registers, operands by direct-to-LDS loads into a ring of stages, one workgroup barrier a stage.  What differs:
