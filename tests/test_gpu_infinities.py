@@ -31,7 +31,7 @@ def _same(got, ref, mag, terms, what):
 # Rows an expert on both sides of what chooses the kernel; reductions that end 4, 12, 20 or 28 elements into a step of 32; few tiles and many, one wavefront
 # a tile and several.
 PRODUCTS = [([5, 0, 9], 40, 36), ([40, 3], 72, 100), ([90, 30], 136, 44), ([12] * 8, 64, 1156), ([20, 3] * 8, 260, 1036), ([10] * 30, 516, 92), ([500, 9], 264, 140),
-            ([100, 41], 64, 2068), ([20, 2] * 20, 1028, 60), ([18, 0, 23], 1040, 2052)]
+            ([100, 41], 64, 2068), ([20, 2] * 20, 1028, 60), ([18, 0, 23], 1040, 2052), ([20] * 30, 1040, 300), ([20] * 30, 1040, 1036)]
 
 
 def _operands(sizes, n, k, dt, seed):
@@ -91,7 +91,7 @@ def test_blocks_of_4_bits(dtype, sizes, n, k):
 
 # both contractions in a launch each, of tiles of 16 x 16, 16 x 32, 64 x 64, long reductions, and both in one launch (from 1025 rows on)
 @pytest.mark.parametrize("sizes,d,f", [([5, 0, 9], 36, 100), ([60, 30], 132, 396), ([12] * 8, 1036, 1156), ([400] * 9 + [124], 120, 444), ([1500, 13, 1504], 92, 188),
-                                       ([300, 0, 700, 200], 516, 1044)])
+                                       ([300, 0, 700, 200], 516, 1044), ([1600, 0, 700, 500], 516, 1044)])
 def test_expert_ffn_in_fp32(sizes, d, f):
     print(f"[case] ffn sizes={sizes} d={d} f={f}", flush=True)
     E, A, dt = len(sizes), sum(sizes), torch.float32
