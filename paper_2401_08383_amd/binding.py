@@ -273,7 +273,7 @@ def _bad(message: str):
 
 
 def _expect(name, t, shape, dtype, dev):
-    """`t` is a dense tensor of this shape and type on device number `dev` (-1: the host, see _on_device)."""
+    """`t` is a dense tensor of this shape and type on device number `dev` (-1: the host, which the calls refuse by themselves)."""
     if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
         return t
     if t.shape != shape:
@@ -283,16 +283,13 @@ def _expect(name, t, shape, dtype, dev):
     _bad(f"{name} must be contiguous and on device {dev}")
 
 
-def _on_device(dev):
-    """The arguments, all of them on device number `dev`, are where a kernel can reach them."""
-    if dev < 0:
-        _bad("the arguments must be on a GPU, they are on the host")
+def _on_host():
+    """The arguments' device number is -1: no kernel can reach them."""
+    _bad("the arguments must be on a GPU, they are on the host")
 
 
 def _bytes_of(workspace, dev):
-    """(address, size) of a caller's workspace, of any type."""
-    if workspace is None:
-        return None, 0
+    """(address, size) of a workspace, of any type."""
     if not workspace.is_contiguous() or workspace.get_device() != dev:
         _bad(f"workspace must be contiguous and on device {dev}")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -333,14 +330,14 @@ def _misfit(rows, rows_shape, offsets, E, w, out, out_shape, dt, dev):
     _expect("expert_offsets", offsets, (E + 1,), _INT32, dev)
     _expect("w", w, w.shape, dt, dev)
     _expect("out", out, out_shape, dt, dev)
-    _on_device(dev)
+    _on_host()
 
 
 def moe_grouped_product(x_sorted, expert_offsets, w, bias=None, out=None):
     """y[s] = x_sorted[s] W_e^T (+ bias[e]) for the rows of every expert; w [E_local,n,k].
 
     No autograd history is recorded: in grad mode an argument that requires a gradient is refused (here and in the calls below)."""
-    if x_sorted.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad):
+    if x_sorted.requires_grad or w.requires_grad or bias is not None and bias.requires_grad:
         _untracked("moe_grouped_product")
     E, n, k, A, dt, code, dev = _grouped(x_sorted, w.shape)
     if out is None:
@@ -390,11 +387,12 @@ def moe_grouped_product_dw(dy_sorted, x_sorted, expert_offsets, want_bias=False,
         _expect("out_bias", out_bias, (E, n), grad_dtype, dev)
     elif want_bias:
         out_bias = torch.empty((E, n), dtype=grad_dtype, device=x_sorted.device)
-    _on_device(dev)
+    if dev < 0:
+        _on_host()
     if workspace is None:
         need = lib().moe_grouped_product_dw_workspace_bytes(A, n, k, E, code)
         workspace = _workspace(need, x_sorted.device) if need else None
-    workspace, size = _bytes_of(workspace, dev)
+    workspace, size = (None, 0) if workspace is None else _bytes_of(workspace, dev)
     rc = lib().moe_grouped_product_dw(dy_sorted.data_ptr(), x_sorted.data_ptr(), expert_offsets.data_ptr(), A, n, k, E, code, _CODES[grad_dtype], out.data_ptr(),
                                       _ptr(out_bias), workspace, size, _stream())
     if rc:
@@ -435,7 +433,7 @@ def mx4_quantize(x, out=None):
     shape, code = x.shape, _CODES.get(x.dtype)
     if code is None:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {x.dtype}")
-    k = shape[-1] if len(shape) else 0
+    k, dev = shape[-1] if len(shape) else 0, x.get_device()
     if k < EXF_MX4_BLOCK or k % EXF_MX4_BLOCK or not x.is_contiguous():
         _bad(f"mx4_quantize: contiguous rows of a multiple of {EXF_MX4_BLOCK} elements expected, got {tuple(shape)}")
     if out is None:
@@ -443,8 +441,9 @@ def mx4_quantize(x, out=None):
         out = Mx4(torch.empty((*shape[:-1], k // 2), dtype=torch.uint8, device=x.device),
                   torch.empty(((k + 255) // 256, rows, 8), dtype=torch.uint8, device=x.device))
     else:
-        rows = _expect_mx4("out", out, shape, x.get_device())
-    _on_device(x.get_device())
+        rows = _expect_mx4("out", out, shape, dev)
+    if dev < 0:
+        _on_host()
     rc = lib().mx4_quantize(x.data_ptr(), rows, k, code, out.q.data_ptr(), out.scale.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -459,7 +458,8 @@ def mx4_dequantize(m, dtype=torch.bfloat16, out=None):
     code = _CODES.get(out.dtype)
     if code is None:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {out.dtype}")
-    _on_device(dev)
+    if dev < 0:
+        _on_host()
     rc = lib().mx4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), rows, shape[-1], code, out.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -494,11 +494,12 @@ def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, 
     if bias is not None:
         bias = _expect("bias", bias, (E, n), dtype, dev).data_ptr()
     out = torch.empty((A, n), dtype=dtype, device=rows.device) if out is None else _expect("out", out, (A, n), dtype, dev)
-    _on_device(dev)
+    if dev < 0:
+        _on_host()
     if workspace is None and not held and A > EXF_MX4_INLINE_ROWS:
         need = lib().moe_grouped_product_mx4_workspace_bytes(A, n, k)
         workspace = _workspace(need, rows.device) if need else None
-    workspace, size = _bytes_of(workspace, dev)
+    workspace, size = (None, 0) if workspace is None else _bytes_of(workspace, dev)
     rc = lib().moe_grouped_product_mx4(rows.data_ptr(), x_scale, expert_offsets.data_ptr(), w.q.data_ptr(), w.scale.data_ptr(), bias, A, n, k, E, code,
                                        out.data_ptr(), workspace, size, _stream())
     if rc:

@@ -48,7 +48,6 @@ def test_host_tensors_are_refused(monkeypatch, call, dt):
 
 
 def test_workspaces():
-    assert B._bytes_of(None, 0) == (None, 0)
     some = torch.zeros(64, dtype=F32)
     assert B._bytes_of(some, -1) == (some.data_ptr(), 256)
     for bad, dev in ((some, 0), (torch.zeros(64, 2)[:, 0], -1)):
