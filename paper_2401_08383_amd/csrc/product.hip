@@ -38,17 +38,21 @@ static int check_rows_product(const char* fn, const void* rows, const int32_t* o
     return EXF_OK;
 }
 
-// Few rows an expert: a stream of weights (ffn_stream.hip), in its sizes.
+// Few rows an expert: a stream of weights (ffn_stream.hip), in its sizes.  Tiles and streams, us, rows spread evenly: 64 experts of 4096 x 1024 with 16 rows
+// each 87 and 82, 24 89 and 89, 28 90 and 92, 48 91 and 113; 64 of 1024 x 4096 24 84 and 82, 48 86 and 93; 8 of 8192 x 2048 16 41 and 42, 28 41 and 43; 8 of
+// 4096 x 1024 24 14.2 and 12.0, 48 14.3 and 14.8; 4 of 2048 x 8192 28 41 and 25, 48 41 and 47; 32 of 512 x 512 6.6 and 6.1, with 64 rows 6.8 and 6.2.
+//   The rule knows the mean only.  Skewed, 24 rows an expert: 64 of 4096 x 1024, rows as 1/rank 96 and 111, all 1536 on one, whose weights every tile of 64
+// rows reads again, 19.6 and 47.4; 8 of 4096 x 1024 15.6 and 15.4, on one 10.0 and 8.4; 16 of 1024 x 1024 12.5 and 10.5, on one 9.8 and 8.2.
 static bool streams_forward(int64_t A, int n, int k, int E_local)
 {
     const int64_t widest = n > k ? n : k;
     return n % 64 == 0 && k % 64 == 0 && A <= 28ll * E_local && A * widest < (1ll << 31) && static_cast<int64_t>(n) * k < (1ll << 31);
 }
 
-// fp32 with more rows an expert, the more the longer the reduction is: tiles (product_exact.hip).  Streams and tiles, us: 8 experts of
-// 1024 x 1024, 4096 rows 177 and 104; 32 of 512 x 512, 16384 rows 158 and 93; of 24 rows an expert 40 of 1024 x 1024 90 and 63, 8 of 2048 x 1024 36
-// and 31, 4 of 1024 x 4096 31 and 38 (48 rows: 61 and 39), 2 of 256 x 8192 30 and 72 (96 rows: 42 and 72, 500: 115 and 73); of 16 rows 40 of
-// 1024 x 1024 47 and 62.
+// fp32 with more rows an expert, the more the longer the reduction is: tiles (product_exact.hip).  Streams and tiles, us, rows skewed (and even): 8 experts of
+// 1024 x 1024, 4096 rows 149 and 95 (79 and 78); 32 of 512 x 512, 16384 rows 130 and 87 (91 and 85); of 24 rows an expert 40 of 1024 x 1024 78 and 60 (47 and 58),
+// 20 of 2048 x 256 29 and 18 (17 and 17), 8 of 2048 x 1024 31 and 22 (30 and 22), 4 of 1024 x 4096 31 and 38 (of 48 rows 58 and 39), 2 of 256 x 8192 30 and 72 (96
+// rows 31 and 72, 500 rows 114 and 73); of 16 rows 40 of 1024 x 1024 44 and 59 (35 and 59).
 static bool exact_forward_in_tiles(int64_t A, int k, int E_local) { return A >= (k <= 2048 ? 24ll : (k <= 4096 ? 48ll : 128ll)) * E_local; }
 
 }  // namespace exf

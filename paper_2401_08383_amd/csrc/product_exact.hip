@@ -301,7 +301,11 @@ int launch_join_parts(const float* parts, int64_t n, void* out, const float* mor
 }
 
 
-// Small tiles where larger ones would leave compute units without one.
+// Small tiles where larger ones would leave compute units without one.  Large and small, us, and how many large ones there are: gradients of rows 1024 rows, 8
+// experts of 512 x 256 (96) 15.8 and 5.7; 2048, 8 of 1024 x 256 (160) 29.3 and 13.9; 8192, 8 of 512 x 128 (272) 16.4 and 14.2; 2048, 8 of 512 x 512 (320)
+// 16.5 and 14.5; 4096 (576) 24.8 and 27.2.  Products, whose weights lie along the reduction, fall behind sooner: 512, 8 of 256 x 256 (64) 9.1 and 5.9; 1024, 8 of
+// 512 x 256 (192) 9.3 and 8.7; but 2048, 8 of 512 x 512 (320) 16.5 and 22.6; 3000, 16 of 512 x 128 (496) 8.6 and 13.0; 4096, 8 of 512 x 512 (576) 24 and 42.
+// Gradients of weights: 8192 rows, 8 of 512 x 128 (128) 18.7 and 18.1; 3000, 16 of 512 x 128 (256) 8.6 and 7.6; 2048, 8 of 512 x 512 (512) 15.1 and 21.3.
 static bool small_tiles(int64_t large) { return large < 2 * 256; }
 
 template <bool W_ACROSS>
@@ -320,7 +324,10 @@ static int launch_exact_rows(const ExactRows& p, hipStream_t stream, const char*
 int launch_exact_product(const ExactRows& p, hipStream_t stream) { return launch_exact_rows<false>(p, stream, "moe_grouped_product"); }
 int launch_exact_rows_gradient(const ExactRows& p, hipStream_t stream) { return launch_exact_rows<true>(p, stream, "moe_grouped_product_dx"); }
 
-// Parts of at least 256 rows until two workgroups a compute unit have one.
+// Parts of at least 256 rows until two workgroups a compute unit have one, at most 16.  us with parts of 128, 256 and 512 rows: 2048 rows, one expert of 256 x 256
+// 13.9, 12.6, 12.8 (not split 20.0); 8192, 4 of 256 x 64 13.6, 12.3, 12.4; 2048, one of 64 x 64 12.5, 12.4, 14.3; but of few rows a second
+// launch costs more than it saves: 512, one of 256 x 256 12.5, 12.6, 7.9; 2048, 4 of 256 x 64 12.5, 12.5, 7.9.  At most 8, 16 and 32 parts: 8192 rows, one of 64 x 64
+// 16.0, 13.8, 17.5, 32768 rows 39.9, 26.0, 23.4 (not split 256).
 static_assert(kSmallCols == kExactTile, "both kinds of tiles have as many columns");
 static int64_t weight_tiles(int n, int k, int E_local, int rows) { return static_cast<int64_t>(E_local) * ((n + rows - 1) / rows) * ((k + kExactTile - 1) / kExactTile); }
 int exact_weight_gradient_splits(int64_t A, int n, int k, int E_local)

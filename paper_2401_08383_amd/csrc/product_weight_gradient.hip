@@ -184,6 +184,10 @@ static bool large_tiles(int64_t A, int n, int k, int E_local)
     return E_local * tiles_in(n, k, 256) >= 2 * kComputeUnits && A >= 256 * E_local;
 }
 
+// Parts of at least 512 rows, at most 16.  Results in fp32, us, with parts of 256, 512 and 1024 rows: 4096 rows, one expert of 512 x 512 21.0, 17.3, 18.9; 2 of
+// 1024 x 512 28.6, 20.3, 20.6; 16384 rows, 8 of 256 x 256 20.9, 17.9, 19.2; 1024 rows, one of 512 x 512 12.6, 12.9, 16.3 (not split 16.6).  With at most 8, 16 and 32
+// parts: 16384 rows, one of 512 x 512 31.3, 24.7, 36.6, 65536 rows 85, 53, 64 (not split 705); one of 256 x 256 88, 52, 42.
+//   As many parts as fill the compute units twice are not always best: 16384 rows, 2 of 1024 x 512 38 in 8 parts and 31 in 4, 65536, 8 of 256 x 256 33 in 16, 23 in 8.
 constexpr int kMostSplits = 16;
 constexpr int64_t kRowsOfAPart = 512;
 int weight_gradient_splits(int64_t A, int n, int k, int E_local)
