@@ -242,6 +242,8 @@ int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorted, const in
  *   q     [rows,k/2]: elements 2i (low half) and 2i+1 of a row in byte i
  *   scale [ceil(k/256),rows,8]: byte (t,r,j) belongs to elements 256 t + 32 j .. +31 of row r; bytes past the end of a row
  *         are zero (the contraction reads them).  mx4_scale_bytes(rows, k) bytes.
+ *         The rows of one expert are no contiguous part of it: weights of some of the experts are quantised by a call of their own, or their
+ *         scale bytes gathered, tile by tile.
  * Shapes: rows >= 0, k >= 32 and k % 32 == 0.  q and scale must be 16-byte aligned.
  * ------------------------------------------------------------------------------------- */
 #define EXF_MX4_BLOCK 32

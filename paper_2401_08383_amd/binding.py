@@ -401,7 +401,9 @@ def moe_grouped_product_dw(dy_sorted, x_sorted, expert_offsets, want_bias=False,
 
 
 class Mx4:
-    """Rows in microscaled 4-bit floating point: ``q`` uint8 [..., k/2] and ``scale`` uint8 [ceil(k/256), rows, 8] (see mx4_quantize)."""
+    """Rows in microscaled 4-bit floating point: ``q`` uint8 [..., k/2] and ``scale`` uint8 [ceil(k/256), rows, 8] (see mx4_quantize).
+
+    Experts a .. b-1 of weights [E,n,k] are ``Mx4(m.q[a:b], m.scale[:, a * n:b * n].contiguous())``."""
     __slots__ = ("q", "scale")
 
     def __init__(self, q, scale):

@@ -174,3 +174,15 @@ def test_weights_beyond_4_gib(dtype, A):
     for at in (0, 65024, n - 8):
         ref, mag, _, _, terms = R.weight_gradient(dy[:, at:at + 8].contiguous(), x, off)
         R.assert_sums_close(dw[:, at:at + 8].contiguous(), ref, mag, terms, "dw")
+
+
+def test_some_of_the_experts():
+    """Experts 1 and 2 of four, cut out of the others' 4-bit weights as Mx4 says, and quantised by themselves."""
+    n, k, off = 72, 544, torch.tensor([0, 30, 41], dtype=torch.int32, device=DEV)
+    w, x = _normal((4, n, k), 0.1, BF, 1), _normal((41, k), 1.0, BF, 2)
+    m = exf.mx4_quantize(w)
+    cut, own = exf.Mx4(m.q[1:3], m.scale[:, n:3 * n].contiguous()), exf.mx4_quantize(w[1:3])
+    assert torch.equal(cut.q, own.q) and torch.equal(cut.scale, own.scale)
+    assert torch.equal(exf.moe_grouped_product_mx4(x, off, cut), exf.moe_grouped_product_mx4(x, off, own))
+    with pytest.raises(exf.ExflowError):
+        exf.moe_grouped_product_mx4(x, off, exf.Mx4(m.q[1:3], m.scale[:, n:3 * n]))
