@@ -372,7 +372,7 @@ def moe_grouped_product_dw(dy_sorted, x_sorted, expert_offsets, want_bias=False,
     ``out``, or the rows')."""
     if dy_sorted.requires_grad or x_sorted.requires_grad:
         _untracked("moe_grouped_product_dw")
-    if len(dy_sorted.shape) != 2 or len(x_sorted.shape) != 2 or len(expert_offsets.shape) != 1:
+    if len(dy_sorted.shape) != 2 or len(x_sorted.shape) != 2 or len(expert_offsets.shape) != 1 or expert_offsets.shape[0] < 2:
         _bad("rows are [A,n] and [A,k], expert_offsets [E_local+1]")
     E, n, k, A, dt, code, dev = _grouped(x_sorted, (expert_offsets.shape[0] - 1, dy_sorted.shape[1], x_sorted.shape[1]))
     _expect("x_sorted", x_sorted, (A, k), dt, dev)
@@ -411,7 +411,8 @@ class Mx4:
 
     @property
     def shape(self):
-        return (*self.q.shape[:-1], 2 * self.q.shape[-1])
+        s = self.q.shape
+        return (*s[:-1], *(2 * k for k in s[-1:]))
 
     @property
     def rows(self):
@@ -421,6 +422,8 @@ class Mx4:
 def _expect_mx4(name, m, shape, dev):
     """`m` holds this shape on device number `dev`; -> its rows."""
     q, scale = m.q, m.scale
+    if not len(shape):
+        _bad(f"{name} has no rows")
     rows, k = q.numel() * 2 // max(shape[-1], 1), shape[-1]
     if (q.shape == (*shape[:-1], k // 2) and scale.shape == ((k + 255) // 256, rows, 8) and q.dtype is _UINT8 and scale.dtype is _UINT8 and q.is_contiguous()
             and scale.is_contiguous() and q.get_device() == scale.get_device() == dev):

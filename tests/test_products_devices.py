@@ -1,4 +1,4 @@
-"""Tensors that no kernel of the experts' products may be given: well-formed ones on the host, workspaces on the host."""
+"""Tensors that no kernel of the experts' products may be given: well-formed ones on the host, workspaces on the host, and what has no rows or experts to speak of."""
 import pytest
 import torch
 
@@ -45,6 +45,18 @@ def test_host_tensors_are_refused(monkeypatch, call, dt):
     monkeypatch.setattr(B, "_stream", lambda: None)
     with pytest.raises(exf.ExflowError, match="on the host"):
         run()
+
+
+def test_what_has_no_axes_is_refused():
+    """... by the binding's own error."""
+    x, dy, off, nothing = torch.zeros(4, 64, dtype=BF), torch.zeros(4, 64, dtype=BF), torch.zeros(4, dtype=torch.int32), torch.zeros((), dtype=torch.uint8)
+    held, flat = exf.Mx4(torch.zeros(3, 64, 32, dtype=torch.uint8), torch.zeros(1, 192, 8, dtype=torch.uint8)), exf.Mx4(nothing, torch.zeros(1, 1, 8, dtype=torch.uint8))
+    bad = [lambda: exf.moe_grouped_product_dw(dy, x, off[:0]), lambda: exf.moe_grouped_product_dw(dy, x, off[:1]), lambda: exf.mx4_dequantize(flat),
+           lambda: exf.mx4_quantize(nothing.to(BF)), lambda: exf.moe_grouped_product_mx4(flat, off, held), lambda: exf.moe_grouped_product_mx4(x, off, flat)]
+    for i, call in enumerate(bad):
+        with pytest.raises(exf.ExflowError) as caught:
+            call()
+        assert caught.value.code == B.EXF_ERR_BAD_SHAPE, i
 
 
 def test_workspaces():
