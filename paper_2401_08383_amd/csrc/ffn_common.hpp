@@ -117,8 +117,8 @@ constexpr int kInlineDispatchMax = 1024;  // assignments a workgroup sorts for i
 constexpr int kRoutedTilesMax = 4096;     // ... in a contraction in tiles
 // Is the path taken for A rows of `dt` spread over E_local experts?
 bool stream_path_fits(int64_t A, int d, int f, int E_local, int dt);
-// fn: the call that errors name.
-int launch_stream_gemm(const StreamGemm& g, int dt, hipStream_t stream, const char* fn = "moe_expert_ffn");
+int launch_stream_gemm(const StreamGemm& g, int dt, hipStream_t stream);                  // errors name moe_expert_ffn
+int launch_stream_gemm(const StreamGemm& g, int dt, hipStream_t stream, const char* fn);  // ... this call
 // fp32: are both contractions one launch, and that launch (out of the first one is not written).
 bool exact_pair_fits(int64_t A, int d, int f, int E_local);
 bool exact_pair_routed_fits(int64_t A, int d, int f, int E, int E_local);  // (that sorts; its rows do not meet, see StreamGemm::exchange)

@@ -1445,5 +1445,6 @@ int launch_stream_gemm(const StreamGemm& p, int dt, hipStream_t stream, const ch
     }
     return tall_exact_tiles(p.max_rows, p.K, p.N, p.E_local, p.epi != kEpiNone) ? launch_exact_rows<4>(p, stream, fn) : launch_exact_rows<1>(p, stream, fn);
 }
+int launch_stream_gemm(const StreamGemm& p, int dt, hipStream_t stream) { return launch_stream_gemm(p, dt, stream, "moe_expert_ffn"); }
 
 }  // namespace exf
