@@ -310,7 +310,7 @@ __device__ __forceinline__ int place_direct(const int32_t* __restrict__ topk_idx
     auto local = [&](int id, bool there) {
         const bool ok = there && id >= 0 && id < E;
         int m = id;
-        if (expert_map != nullptr) m = __shfl(map, ok ? id : 0, kWave);
+        if (expert_map != nullptr) m = E <= kWave ? __shfl(map, ok ? id : 0, kWave) : expert_map[ok ? id : 0];
         return ok && m >= 0 && m < E_local ? m : -1;
     };
     __syncthreads();
