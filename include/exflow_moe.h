@@ -3,11 +3,14 @@
  * context-coherent Mixture-of-Experts inference with inter-layer expert affinity
  * (arXiv 2401.08383).
  *
- * Four groups of calls:
+ * Five groups of calls:
  *   MoE expert layer  : moe_gate_topk -> moe_dispatch -> moe_expert_ffn -> moe_combine, or
  *                       moe_gate_topk -> moe_dispatch (index maps only) -> moe_expert_ffn_fused
+ *   many experts      : moe_route -> moe_dispatch_topk -> (experts' products) -> moe_combine_topk, and the gradients
+ *                       moe_combine_backward, moe_combine_topk (of the dispatch), moe_route_backward
  *   experts' products : moe_grouped_product and its gradients, moe_grouped_product_mx4 (operands in 4 bits:
- *                       mx4_quantize, mx4_dequantize)
+ *                       mx4_quantize, mx4_dequantize), moe_grouped_product_q4 (weights in 4-bit integers with group
+ *                       scales: q4_quantize, q4_dequantize)
  *   affinity statistic: affinity_histogram, placement_locality (both in one pass: affinity_statistics),
  *                       affinity_multihop, routing_transfers
  *   placement search  : placement_locality_from_counts (GPU scoring), exf_placement_search (host)
@@ -57,8 +60,14 @@ extern "C" {
 #define EXF_ACT_GELU_ERF 0  /* z/2 * (1 + erf(z/sqrt 2)) */
 #define EXF_ACT_GELU_TANH 1 /* z/2 * (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
 
+#define EXF_SCORE_SOFTMAX 0 /* exp(l_e) / sum exp(l) */
+#define EXF_SCORE_SIGMOID 1 /* 1 / (1 + exp(-l_e)) */
+
 #define EXF_MAX_EXPERTS 64   /* gate width E, local experts E_local and trace alphabet E */
 #define EXF_MAX_TOPK 2
+#define EXF_MAX_ROUTE_EXPERTS 512  /* E of moe_route (a GPU holds at most EXF_MAX_EXPERTS of them) */
+#define EXF_MAX_ROUTE_TOPK 16      /* k of moe_route, moe_dispatch_topk, moe_combine_topk and the gradients */
+#define EXF_MAX_ROUTE_GROUPS 64
 #define EXF_DISPATCH_STATIC_MAX_ASSIGNMENTS (1ll << 20)  /* largest T*k of moe_dispatch_static */
 #define EXF_MAX_TRACE_LAYERS 256
 #define EXF_MAX_PRODUCT_WIDTH (1 << 21)  /* n and k of moe_grouped_product and its kin */
@@ -266,6 +275,83 @@ size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int n, int k);
 int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_scale, const int32_t* expert_offsets, const uint8_t* w,
                             const uint8_t* w_scale, const void* bias, int64_t A, int n, int k, int E_local, int dt,
                             void* y_sorted, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * moe_route, moe_route_backward — routing to many experts from the gate's logits, and its gradient (Background, "Gating
+ * Strategies and Optimizations": softmax-based gating; here with the forms that layers of many small experts use).
+ *   s[t][e]   = softmax(logits[t][:])[e]  or  1 / (1 + exp(-logits[t][e]))          (`score`)
+ *   key[t][e] = s[t][e] + bias[e]; without a bias the logits themselves are compared.  Keys decide as if they were computed in
+ *               64 bits.  A logit of -inf or NaN, or a bias that makes the key -inf or NaN, takes the expert out.
+ *   groups > 1: the experts lie in groups of E / groups consecutive ones; the top_groups groups stay whose group_best (1 or 2) highest keys
+ *               have the largest sum (with group_best == 2 and no bias: scores), ties to the lowest group.
+ *   slot j    = the j-th largest key of the groups that stay, ties to the LOWEST expert id
+ *   topk_w[t][j] = scale * s[t][e_j]                             if k == 1 or renormalize == 0
+ *                = scale * s[t][e_j] / sum_j' s[t][e_j']         otherwise
+ * Slots that no expert is left for have id -1 (which moe_dispatch_topk does not keep) and weight 0.  A row with a NaN, or under the
+ * softmax with +inf, has NaN weights; its ids are -1 or in [0,E).
+ *
+ *   logits [T,E] dt;  bias [E] fp32 or NULL;  topk_idx [T,k] int32;  topk_w [T,k] fp32;  scores_out [T,E] fp32 (s), may be NULL
+ *
+ * moe_route_backward: dlogits[t][e] = the derivative by logits[t][e] of  sum_j dtopk_w[t][j] topk_w[t][j] + sum_e dscores[t][e] s[t][e]
+ * with the ids held (the bias has no gradient).  Slots whose id is outside [0,E) contribute nothing; an id that stands twice counts twice;
+ * masked experts (logit -inf) get 0.
+ *   dtopk_w [T,k] fp32;  topk_idx [T,k];  dscores fp32 or NULL: [T,E] with dscores_stride == E, or one row for all tokens, [E], with
+ *   dscores_stride == 0 (a balance loss);  dlogits [T,E] dt, overwritten.
+ * All in fp32, rounded once.
+ * Shapes: T >= 0, T*k < 2^31, 1 <= E <= EXF_MAX_ROUTE_EXPERTS, 1 <= k <= min(E, EXF_MAX_ROUTE_TOPK), scale finite; 1 <= groups <=
+ *         EXF_MAX_ROUTE_GROUPS divides E, 1 <= top_groups <= groups, k <= top_groups * E / groups.  Results must not overlap inputs.
+ * ------------------------------------------------------------------------------------- */
+int moe_route(const void* logits, const float* bias, int64_t T, int E, int k, int score, int groups, int top_groups,
+              int group_best, int renormalize, float scale, int dt, int32_t* topk_idx, float* topk_w, float* scores_out,
+              void* stream);
+int moe_route_backward(const float* dtopk_w, const void* logits, const int32_t* topk_idx, const float* dscores,
+                       int64_t dscores_stride, int64_t T, int E, int k, int score, int renormalize, float scale, int dt,
+                       void* dlogits, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * moe_dispatch_topk, moe_combine_topk, moe_combine_backward — moe_dispatch and moe_combine for 1 <= k <= EXF_MAX_ROUTE_TOPK
+ * assignments a token, and the gradients of both.
+ *   moe_dispatch_topk     as moe_dispatch, with its workspace
+ *   moe_combine_topk      as moe_combine; topk_w NULL: weights of one, which is the gradient of the dispatch,
+ *                           dx[t][:] = sum_j dx_sorted[ sorted_of_src[t*k+j] ][:]
+ *   moe_combine_backward  dy_sorted[ sorted_of_src[t*k+j] ][:] = topk_w[t][j] * dout[t][:]   (rows that no assignment has: untouched)
+ *                         dtopk_w[t][j] = sum_c dout[t][c] * y_sorted[ sorted_of_src[t*k+j] ][c], 0 for position -1
+ *     dout [T,d] dt;  dy_sorted [T*k,d] dt or NULL (not wanted: topk_w may be NULL too);  dtopk_w [T,k] fp32 or NULL (y_sorted may be NULL too)
+ * Sums in fp32 in an order that depends on the sizes only, rounded once.  Results must not overlap inputs.
+ * Shapes: T*k < 2^31, d % 8 == 0 (bf16) / d % 4 == 0 (fp32), of the combines d <= EXF_MAX_PRODUCT_WIDTH.
+ * ------------------------------------------------------------------------------------- */
+int moe_dispatch_topk(const void* x, const int32_t* topk_idx, const int32_t* expert_map, int64_t T, int d, int k, int E,
+                      int E_local, int dt, void* x_sorted, int32_t* src_of_sorted, int32_t* sorted_of_src,
+                      int32_t* expert_counts, int32_t* expert_offsets, void* workspace, size_t workspace_bytes, void* stream);
+int moe_combine_topk(const void* y_sorted, const int32_t* sorted_of_src, const float* topk_w, int64_t T, int d, int k, int dt,
+                     void* out, void* stream);
+int moe_combine_backward(const void* dout, const void* y_sorted, const int32_t* sorted_of_src, const float* topk_w, int64_t T,
+                         int d, int k, int dt, void* dy_sorted, float* dtopk_w, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * q4_quantize, q4_dequantize, moe_grouped_product_q4 — weights in 4-bit integers: `group` (32, 64 or 128) consecutive elements of a row share
+ * a scale and a zero point.  Rows of activations stay in bf16 or fp32.
+ *   value = scale * (code - zero), code 0 .. 15, zero 0 .. 255 (as q4_quantize writes it 0 .. 15); zero == NULL: 8 throughout
+ *   q4_quantize, zero != NULL: lo = min(0, least x), hi = max(0, largest x);  scale = (hi - lo) / 15, rounded to fp32 and dt;
+ *                              zero = nearest(-lo / scale), at most 15
+ *                zero == NULL: scale = largest |x| / 7, rounded in the same way
+ *                code = nearest(x / scale) + zero within 0 .. 15; nearest: the nearest integer to the exact quotient, halfway the even one
+ *                A group with scale 0: all codes are the zero point (0, or 8).  One that holds an infinity or a NaN: its scale is NaN.
+ *   q4_dequantize: the values, rounded to dt
+ *   moe_grouped_product_q4: y[s][v] = sum_u x[s][u] * value[e][v][u] + bias[e][v] for rows s of expert e, as moe_grouped_product; sums in
+ *                fp32, rounded once, in an order that depends on the sizes and the offsets only.  For few rows an expert: weights are read once
+ *                for every 16 rows or more.
+ *
+ *   x, out [rows,k] dt;  q [rows,k/2]: elements 2i (low half) and 2i+1 of a row in byte i;  scale [rows,k/group] dt;  zero [rows,k/group]
+ *   x_sorted [A,k] dt;  w [E_local,n,k/2], w_scale, w_zero (or NULL): E_local*n rows of k;  bias [E_local,n] dt or NULL;  y_sorted [A,n] dt
+ * Shapes: rows >= 0, k >= group, k % group == 0; the product's as moe_grouped_product.  All arrays 16-byte aligned.
+ * ------------------------------------------------------------------------------------- */
+int q4_quantize(const void* x, int64_t rows, int k, int group, int dt, uint8_t* q, void* scale, uint8_t* zero, void* stream);
+int q4_dequantize(const uint8_t* q, const void* scale, const uint8_t* zero, int64_t rows, int k, int group, int dt, void* out,
+                  void* stream);
+int moe_grouped_product_q4(const void* x_sorted, const int32_t* expert_offsets, const uint8_t* w, const void* w_scale,
+                           const uint8_t* w_zero, const void* bias, int64_t A, int n, int k, int group, int E_local, int dt,
+                           void* y_sorted, void* stream);
 
 /* ---------------------------------------------------------------------------------------
  * moe_layer_forward — one pass of the whole expert layer (the calls above in sequence) for callers that

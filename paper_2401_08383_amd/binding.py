@@ -26,6 +26,9 @@ EXF_F32 = 0
 EXF_BF16 = 1
 EXF_ACT_GELU_ERF = 0
 EXF_ACT_GELU_TANH = 1
+EXF_SCORE_SOFTMAX = 0
+EXF_SCORE_SIGMOID = 1
+EXF_MAX_TOPK = 2
 EXF_MX4_BLOCK = 32
 EXF_MX4_INLINE_ROWS = 8
 
@@ -57,6 +60,14 @@ SIGNATURES = {
     "mx4_dequantize": (_i, [_vp, _vp, _i64, _i, _i, _vp, _vp]),
     "moe_grouped_product_mx4_workspace_bytes": (_sz, [_i64, _i, _i]),
     "moe_grouped_product_mx4": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i, _vp, _vp, _sz, _vp]),
+    "moe_route": (_i, [_vp, _vp, _i64, _i, _i, _i, _i, _i, _i, _i, ctypes.c_float, _i, _vp, _vp, _vp, _vp]),
+    "moe_route_backward": (_i, [_vp, _vp, _vp, _vp, _i64, _i64, _i, _i, _i, _i, ctypes.c_float, _i, _vp, _vp]),
+    "moe_dispatch_topk": (_i, [_vp, _vp, _vp, _i64, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "moe_combine_topk": (_i, [_vp, _vp, _vp, _i64, _i, _i, _i, _vp, _vp]),
+    "moe_combine_backward": (_i, [_vp, _vp, _vp, _vp, _i64, _i, _i, _i, _vp, _vp, _vp]),
+    "q4_quantize": (_i, [_vp, _i64, _i, _i, _i, _vp, _vp, _vp, _vp]),
+    "q4_dequantize": (_i, [_vp, _vp, _vp, _i64, _i, _i, _i, _vp, _vp]),
+    "moe_grouped_product_q4": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i, _i, _vp, _vp]),
     "moe_layer_forward": (_i, [_vp, _vp]),
     "affinity_histogram_workspace_bytes": (_sz, [_i, _i64, _i]),
     "affinity_histogram": (_i, [_vp, _i, _i64, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -176,7 +187,7 @@ class DispatchResult:
 
 
 def moe_dispatch(x, topk_idx, E, E_local=None, expert_map=None, out=None, workspace=None, gather=True):
-    """Stable dispatch of the assignments; returns a DispatchResult of device tensors.
+    """Stable dispatch of the assignments (up to 16 a token); returns a DispatchResult of device tensors.
 
     Entries of ``src_of_sorted`` / rows of ``x_sorted`` at or beyond ``expert_offsets[E_local]``
     are left untouched by the library.  ``out`` may carry a previous DispatchResult to reuse.
@@ -197,10 +208,40 @@ def moe_dispatch(x, topk_idx, E, E_local=None, expert_map=None, out=None, worksp
         )
     if workspace is None:
         workspace = _workspace(lib().moe_dispatch_workspace_bytes(T, k, E_local), dev)
-    _check(lib().moe_dispatch(_ptr(x), _ptr(topk_idx), _ptr(expert_map), T, d, k, E, E_local, dtype_code(x),
-                              _ptr(out.x_sorted), _ptr(out.src_of_sorted), _ptr(out.sorted_of_src),
-                              _ptr(out.expert_counts), _ptr(out.expert_offsets), _ptr(workspace), workspace.numel(), _stream()))
+    if k <= EXF_MAX_TOPK:
+        call = lib().moe_dispatch
+    else:
+        call = lib().moe_dispatch_topk
+        workspace = _dispatch_topk_fits(x, topk_idx, expert_map, E, E_local, out, workspace)
+    _check(call(_ptr(x), _ptr(topk_idx), _ptr(expert_map), T, d, k, E, E_local, dtype_code(x), _ptr(out.x_sorted), _ptr(out.src_of_sorted),
+                _ptr(out.sorted_of_src), _ptr(out.expert_counts), _ptr(out.expert_offsets), _ptr(workspace), workspace.numel(), _stream()))
     return out
+
+
+def _dispatch_topk_fits(x, topk_idx, expert_map, E, E_local, out, workspace):
+    """Checks of what the library cannot see of a dispatch of more than two assignments a token; -> the workspace as bytes."""
+    T, k = topk_idx.shape
+    dev = topk_idx.get_device()
+    if x.requires_grad:
+        _untracked("moe_dispatch", "moe_dispatch_backward")
+    _expect("x", x, (T, x.shape[1]), x.dtype, dev)
+    if expert_map is not None:
+        _expect("expert_map", expert_map, (E,), _INT32, dev)
+    if out.x_sorted is not None:
+        _expect("out.x_sorted", out.x_sorted, (T * k, x.shape[1]), x.dtype, dev)
+    _expect("out.src_of_sorted", out.src_of_sorted, (T * k,), _INT32, dev)
+    _expect("out.sorted_of_src", out.sorted_of_src, (T * k,), _INT32, dev)
+    _expect("out.expert_counts", out.expert_counts, (E_local,), _INT32, dev)
+    _expect("out.expert_offsets", out.expert_offsets, (E_local + 1,), _INT32, dev)
+    if dev < 0:
+        _on_host()
+    _bytes_of(workspace, dev)
+    return workspace.view(-1).view(_UINT8)
+
+
+def moe_dispatch_backward(dx_sorted, sorted_of_src, k, out=None):
+    """Gradient of moe_dispatch's rows: dx[t] = sum of the rows of dx_sorted [T*k,d] that token t's k assignments went to."""
+    return _combine_rows("moe_dispatch_backward", dx_sorted, sorted_of_src, None, k, out)
 
 
 def moe_dispatch_static(x, topk_idx, E, out, E_local=None, expert_map=None):
@@ -255,13 +296,137 @@ def moe_expert_ffn_fused(x, src_of_sorted, sorted_of_src, topk_w, expert_offsets
 
 
 def moe_combine(y_sorted, sorted_of_src, topk_w, out=None):
+    """out[t] = sum of token t's rows of y_sorted, each by its weight; topk_w [T,k], k up to 16."""
     T, k = topk_w.shape
+    if k > EXF_MAX_TOPK:
+        return _combine_rows("moe_combine", y_sorted, sorted_of_src, topk_w, k, out)
     d = y_sorted.shape[1]
     assert sorted_of_src.numel() == T * k and y_sorted.is_contiguous() and topk_w.dtype == torch.float32
     if out is None:
         out = torch.empty((T, d), dtype=y_sorted.dtype, device=y_sorted.device)
     _check(lib().moe_combine(_ptr(y_sorted), _ptr(sorted_of_src), _ptr(topk_w), T, d, k, dtype_code(y_sorted), _ptr(out),
                              _stream()))
+    return out
+
+
+def _combine_rows(name, y_sorted, sorted_of_src, topk_w, k, out):
+    if y_sorted.requires_grad or topk_w is not None and topk_w.requires_grad:
+        _untracked(name, "moe_combine_backward" if name == "moe_combine" else "moe_dispatch")
+    T, A, d, code, dev = _assigned(y_sorted, sorted_of_src, k)
+    dt = y_sorted.dtype
+    out = torch.empty((T, d), dtype=dt, device=y_sorted.device) if out is None else _expect("out", out, (T, d), dt, dev)
+    _expect("the sorted rows", y_sorted, (A, d), dt, dev)
+    if topk_w is not None:
+        topk_w = _expect("topk_w", topk_w, (T, k), torch.float32, dev).data_ptr()
+    if dev < 0:
+        _on_host()
+    rc = lib().moe_combine_topk(y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w, T, d, k, code, out.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+def _assigned(rows, sorted_of_src, k):
+    """(T, T*k, d, type's code, device number) of sorted rows and the positions of T tokens' k assignments."""
+    if len(rows.shape) != 2 or len(sorted_of_src.shape) not in (1, 2):
+        _bad(f"sorted rows are [T*k,d] and positions [T*k], got {tuple(rows.shape)} and {tuple(sorted_of_src.shape)}")
+    A, dev = sorted_of_src.numel(), rows.get_device()
+    if k < 1 or A % k or len(sorted_of_src.shape) == 2 and sorted_of_src.shape[1] != k:
+        _bad(f"positions of k = {k} assignments a token expected, got {tuple(sorted_of_src.shape)}")
+    code = _CODES.get(rows.dtype)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {rows.dtype}")
+    _expect("sorted_of_src", sorted_of_src, sorted_of_src.shape, _INT32, dev)
+    return A // k, A, rows.shape[1], code, dev
+
+
+def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, want_weights=True, out=None, out_weights=None):
+    """Gradients of moe_combine: (dy_sorted [T*k,d] or None, dtopk_w [T,k] or None).  Rows of dy_sorted that no assignment has are left as they were
+    (``out``), or zero."""
+    if dout.requires_grad or y_sorted.requires_grad or topk_w.requires_grad:
+        _untracked("moe_combine_backward", "none: there is no second derivative")
+    if len(topk_w.shape) != 2:
+        _bad(f"topk_w is [T,k], got {tuple(topk_w.shape)}")
+    k = topk_w.shape[1]
+    T, A, d, code, dev = _assigned(y_sorted, sorted_of_src, k)
+    dt = y_sorted.dtype
+    _expect("dout", dout, (T, d), dt, dev)
+    _expect("y_sorted", y_sorted, (A, d), dt, dev)
+    _expect("topk_w", topk_w, (T, k), torch.float32, dev)
+    if out is not None:
+        _expect("out", out, (A, d), dt, dev)
+    elif want_rows:
+        out = torch.zeros((A, d), dtype=dt, device=dout.device)
+    if out_weights is not None:
+        _expect("out_weights", out_weights, (T, k), torch.float32, dev)
+    elif want_weights:
+        out_weights = torch.empty((T, k), dtype=torch.float32, device=dout.device)
+    if dev < 0:
+        _on_host()
+    rc = lib().moe_combine_backward(dout.data_ptr(), y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w.data_ptr(), T, d, k, code, _ptr(out), _ptr(out_weights),
+                                    _stream())
+    if rc:
+        _check(rc)
+    return out, out_weights
+
+
+def moe_route(logits, k, bias=None, score=EXF_SCORE_SOFTMAX, renormalize=False, scale=1.0, groups=1, top_groups=None, group_best=1, want_scores=False, out=None):
+    """Experts of every token from the gate's logits [T,E], E up to 512: (topk_idx int32 [T,k], topk_w fp32 [T,k], scores fp32 [T,E] or None).
+
+    The k (up to 16) largest of the scores plus ``bias`` (fp32 [E]) are chosen, of the ``top_groups`` best of ``groups`` groups of experts, a group being as
+    good as the sum of its ``group_best`` best; the weights are the scores without the bias, renormalised to a sum of one (k > 1), times ``scale``.
+    ``out``: (topk_idx, topk_w) to write to."""
+    if logits.requires_grad:
+        _untracked("moe_route", "moe_route_backward")
+    shape, dt, dev = logits.shape, logits.dtype, logits.get_device()
+    code = _CODES.get(dt)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
+    if len(shape) != 2 or not logits.is_contiguous():
+        _bad(f"logits: contiguous [T,E] expected, got {tuple(shape)}")
+    T, E = shape
+    if bias is not None:
+        bias = _expect("bias", bias, (E,), torch.float32, dev).data_ptr()
+    if dev < 0:
+        _on_host()
+    if out is None:
+        idx, w = torch.empty((T, k), dtype=_INT32, device=logits.device), torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    else:
+        idx, w = out
+        _expect("topk_idx", idx, (T, k), _INT32, dev)
+        _expect("topk_w", w, (T, k), torch.float32, dev)
+    scores = torch.empty((T, E), dtype=torch.float32, device=logits.device) if want_scores else None
+    rc = lib().moe_route(logits.data_ptr(), bias, T, E, k, score, groups, groups if top_groups is None else top_groups, group_best, 1 if renormalize else 0, scale, code,
+                         idx.data_ptr(), w.data_ptr(), _ptr(scores), _stream())
+    if rc:
+        _check(rc)
+    return idx, w, scores
+
+
+def moe_route_backward(dtopk_w, logits, topk_idx, score=EXF_SCORE_SOFTMAX, renormalize=False, scale=1.0, dscores=None, out=None):
+    """Gradient of moe_route's logits, of their type, from that of the weights, fp32 [T,k], and of the scores, fp32 [T,E] or one row [E] for all tokens."""
+    if dtopk_w.requires_grad or logits.requires_grad or dscores is not None and dscores.requires_grad:
+        _untracked("moe_route_backward", "none: there is no second derivative")
+    shape, dt, dev = logits.shape, logits.dtype, logits.get_device()
+    code = _CODES.get(dt)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
+    if len(shape) != 2 or len(topk_idx.shape) != 2 or not logits.is_contiguous():
+        _bad(f"logits: contiguous [T,E] expected, topk_idx [T,k], got {tuple(shape)} and {tuple(topk_idx.shape)}")
+    T, E = shape
+    k, stride, at = topk_idx.shape[1], 0, None
+    _expect("dtopk_w", dtopk_w, (T, k), torch.float32, dev)
+    _expect("topk_idx", topk_idx, (T, k), _INT32, dev)
+    if dscores is not None:
+        stride = E if len(dscores.shape) == 2 else 0
+        at = _expect("dscores", dscores, (T, E) if stride else (E,), torch.float32, dev).data_ptr()
+    out = torch.empty(shape, dtype=dt, device=logits.device) if out is None else _expect("out", out, shape, dt, dev)
+    if dev < 0:
+        _on_host()
+    rc = lib().moe_route_backward(dtopk_w.data_ptr(), logits.data_ptr(), topk_idx.data_ptr(), at, stride, T, E, k, score, 1 if renormalize else 0, scale, code,
+                                  out.data_ptr(), _stream())
+    if rc:
+        _check(rc)
     return out
 
 
@@ -295,11 +460,11 @@ def _bytes_of(workspace, dev):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _untracked(name):
+def _untracked(name, backward="moe_grouped_product_dx and moe_grouped_product_dw"):
     """An argument requires a gradient, which a result of these calls does not carry on."""
     if torch.is_grad_enabled():
         raise ExflowError(EXF_ERR_NOT_IMPLEMENTED, f"{name} records no autograd history and an argument requires a gradient: call it under torch.no_grad(), or in the "
-                                                   "forward of a torch.autograd.Function whose backward calls moe_grouped_product_dx and moe_grouped_product_dw")
+                                                   f"forward of a torch.autograd.Function whose backward calls {backward}")
 
 
 _INT32, _UINT8 = torch.int32, torch.uint8
@@ -507,6 +672,101 @@ def moe_grouped_product_mx4(x_sorted, expert_offsets, w, bias=None, dtype=None, 
     workspace, size = (None, 0) if workspace is None else _bytes_of(workspace, dev)
     rc = lib().moe_grouped_product_mx4(rows.data_ptr(), x_scale, expert_offsets.data_ptr(), w.q.data_ptr(), w.scale.data_ptr(), bias, A, n, k, E, code,
                                        out.data_ptr(), workspace, size, _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+class Q4:
+    """Rows in 4-bit integers: ``q`` uint8 [..., k/2], ``scale`` [..., k/group] of the rows' type, ``zero`` uint8 [..., k/group] or None (8 throughout); see
+    q4_quantize.  Experts a .. b-1 of weights [E,n,k] are ``Q4(m.q[a:b], m.scale[a:b], m.zero[a:b])``."""
+    __slots__ = ("q", "scale", "zero")
+
+    def __init__(self, q, scale, zero=None):
+        self.q, self.scale, self.zero = q, scale, zero
+
+    @property
+    def shape(self):
+        s = self.q.shape
+        return (*s[:-1], *(2 * k for k in s[-1:]))
+
+    @property
+    def group(self):
+        return self.shape[-1] // max(self.scale.shape[-1], 1)
+
+
+def _expect_q4(name, m, shape, dtype, dev):
+    """`m` holds this shape with scales of `dtype` on device number `dev`; -> its group, which the library checks."""
+    q, scale, zero = m.q, m.scale, m.zero
+    if not len(shape) or not len(scale.shape) or not scale.shape[-1]:
+        _bad(f"{name} has no groups")
+    groups = (*shape[:-1], scale.shape[-1])
+    if shape[-1] % groups[-1]:
+        _bad(f"{name}: rows of {shape[-1]} in {groups[-1]} groups")
+    if not (q.shape == (*shape[:-1], shape[-1] // 2) and scale.shape == groups and q.dtype is _UINT8 and scale.dtype is dtype and q.is_contiguous() and scale.is_contiguous()
+            and q.get_device() == scale.get_device() == dev):
+        _expect(f"{name}.q", q, (*shape[:-1], shape[-1] // 2), _UINT8, dev)
+        _expect(f"{name}.scale", scale, groups, dtype, dev)
+    if zero is not None:
+        _expect(f"{name}.zero", zero, groups, _UINT8, dev)
+    return shape[-1] // groups[-1]
+
+
+def q4_quantize(x, group=128, symmetric=False, out=None):
+    """Rows x [..., k] (k a multiple of the group: 32, 64 or 128) -> Q4, with zero points unless ``symmetric`` (``out`` says that by what it holds)."""
+    shape, dt = x.shape, x.dtype
+    code = _CODES.get(dt)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
+    k, dev = shape[-1] if len(shape) else 0, x.get_device()
+    if k < 1 or group < 1 or k % group or not x.is_contiguous():
+        _bad(f"q4_quantize: contiguous rows of a multiple of {group} elements expected, got {tuple(shape)}")
+    if out is None:
+        groups = (*shape[:-1], k // group)
+        out = Q4(torch.empty((*shape[:-1], k // 2), dtype=_UINT8, device=x.device), torch.empty(groups, dtype=dt, device=x.device),
+                 None if symmetric else torch.empty(groups, dtype=_UINT8, device=x.device))
+    elif _expect_q4("out", out, shape, dt, dev) != group or (out.zero is None) != bool(symmetric):
+        _bad("q4_quantize: out holds other groups, or zero points where none are asked for")
+    if dev < 0:
+        _on_host()
+    rc = lib().q4_quantize(x.data_ptr(), x.numel() // k, k, group, code, out.q.data_ptr(), out.scale.data_ptr(), _ptr(out.zero), _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+def q4_dequantize(m, out=None):
+    """The values a Q4 stands for, in its scales' type."""
+    shape, dt, dev = m.shape, m.scale.dtype, m.q.get_device()
+    code = _CODES.get(dt)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
+    group = _expect_q4("m", m, shape, dt, dev)
+    out = torch.empty(shape, dtype=dt, device=m.q.device) if out is None else _expect("out", out, shape, dt, dev)
+    if dev < 0:
+        _on_host()
+    rc = lib().q4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), _ptr(m.zero), m.q.numel() * 2 // max(shape[-1], 1), shape[-1], group, code, out.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return out
+
+
+def moe_grouped_product_q4(x_sorted, expert_offsets, w, bias=None, out=None):
+    """moe_grouped_product with weights in 4-bit integers: w a Q4 [E_local,n,k] with scales of the rows' type."""
+    if x_sorted.requires_grad or bias is not None and bias.requires_grad or w.scale.requires_grad:
+        _untracked("moe_grouped_product_q4", "none: weights in 4 bits are not trained")
+    if len(w.q.shape) != 3:
+        _bad(f"weights are [E_local,n,k], got {w.shape}")
+    E, n, k, A, dt, code, dev = _grouped(x_sorted, w.shape)
+    group = _expect_q4("w", w, (E, n, k), dt, dev)
+    if out is None:
+        out = torch.empty((A, n), dtype=dt, device=x_sorted.device)
+    if bias is not None:
+        bias = _expect("bias", bias, (E, n), dt, dev).data_ptr()
+    if not _fits(x_sorted, k, expert_offsets, E, w.scale, out, (A, n), dt, dev):
+        _misfit(x_sorted, (A, k), expert_offsets, E, w.scale, out, (A, n), dt, dev)
+    rc = lib().moe_grouped_product_q4(x_sorted.data_ptr(), expert_offsets.data_ptr(), w.q.data_ptr(), w.scale.data_ptr(), _ptr(w.zero), bias, A, n, k, group, E, code,
+                                      out.data_ptr(), _stream())
     if rc:
         _check(rc)
     return out

@@ -509,49 +509,54 @@ extern "C" size_t moe_dispatch_workspace_bytes(int64_t T, int k, int E_local)
 
 namespace exf {
 
-int check_dispatch(const void* x, const int32_t* topk_idx, int64_t T, int d, int k, int E, int E_local, int dt, const void* x_sorted,
-                   const int32_t* src_of_sorted, const int32_t* sorted_of_src, const int32_t* expert_counts, const int32_t* expert_offsets,
-                   const void* workspace, size_t workspace_bytes)
+static int check_dispatch_of(const char* fn, int most, const void* x, const int32_t* topk_idx, int64_t T, int d, int k, int E, int E_local, int dt,
+                             const void* x_sorted, const int32_t* src_of_sorted, const int32_t* sorted_of_src, const int32_t* expert_counts,
+                             const int32_t* expert_offsets, const void* workspace, size_t workspace_bytes)
 {
-    if (dt != EXF_F32 && dt != EXF_BF16) return fail(EXF_ERR_BAD_DTYPE, "moe_dispatch: dt = %d", dt);
-    if (T < 0) return fail(EXF_ERR_BAD_SHAPE, "moe_dispatch: T = %lld < 0", static_cast<long long>(T));
-    if (k < 1 || k > EXF_MAX_TOPK) return fail(EXF_ERR_BAD_SHAPE, "moe_dispatch: k = %d outside [1,%d]", k, EXF_MAX_TOPK);
-    if (E < 1) return fail(EXF_ERR_BAD_SHAPE, "moe_dispatch: E = %d < 1", E);
+    if (dt != EXF_F32 && dt != EXF_BF16) return fail(EXF_ERR_BAD_DTYPE, "%s: dt = %d", fn, dt);
+    if (T < 0) return fail(EXF_ERR_BAD_SHAPE, "%s: T = %lld < 0", fn, static_cast<long long>(T));
+    if (k < 1 || k > most) return fail(EXF_ERR_BAD_SHAPE, "%s: k = %d outside [1,%d]", fn, k, most);
+    if (E < 1) return fail(EXF_ERR_BAD_SHAPE, "%s: E = %d < 1", fn, E);
     if (E_local < 1 || E_local > EXF_MAX_EXPERTS)
-        return fail(EXF_ERR_BAD_SHAPE, "moe_dispatch: E_local = %d outside [1,%d]", E_local, EXF_MAX_EXPERTS);
+        return fail(EXF_ERR_BAD_SHAPE, "%s: E_local = %d outside [1,%d]", fn, E_local, EXF_MAX_EXPERTS);
+    if (T >= (1ll << 31) || T * k >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "%s: T*k must be below 2^31", fn);
     const int64_t A = T * k;
-    if (A >= (1ll << 31)) return fail(EXF_ERR_BAD_SHAPE, "moe_dispatch: T*k must be below 2^31");
     const int gran = dt == EXF_BF16 ? 8 : 4;
     if (x_sorted != nullptr && (d < gran || d % gran != 0))
-        return fail(EXF_ERR_BAD_SHAPE, "moe_dispatch: d = %d must be a positive multiple of %d", d, gran);
-    EXF_CHECK_PTR("moe_dispatch", expert_counts);
-    EXF_CHECK_PTR("moe_dispatch", expert_offsets);
-    EXF_CHECK_PTR("moe_dispatch", workspace);
+        return fail(EXF_ERR_BAD_SHAPE, "%s: d = %d must be a positive multiple of %d", fn, d, gran);
+    EXF_CHECK_PTR(fn, expert_counts);
+    EXF_CHECK_PTR(fn, expert_offsets);
+    EXF_CHECK_PTR(fn, workspace);
     if (workspace_bytes < moe_dispatch_workspace_bytes(T, k, E_local))
-        return fail(EXF_ERR_WORKSPACE_TOO_SMALL, "moe_dispatch: workspace %zu < %zu bytes", workspace_bytes,
+        return fail(EXF_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu < %zu bytes", fn, workspace_bytes,
                     moe_dispatch_workspace_bytes(T, k, E_local));
     if (A > 0) {
-        EXF_CHECK_PTR("moe_dispatch", topk_idx);
-        EXF_CHECK_PTR("moe_dispatch", src_of_sorted);
-        EXF_CHECK_PTR("moe_dispatch", sorted_of_src);
+        EXF_CHECK_PTR(fn, topk_idx);
+        EXF_CHECK_PTR(fn, src_of_sorted);
+        EXF_CHECK_PTR(fn, sorted_of_src);
         if (x_sorted != nullptr) {
-            EXF_CHECK_PTR("moe_dispatch", x);
-            EXF_CHECK_ALIGNED("moe_dispatch", x);
-            EXF_CHECK_ALIGNED("moe_dispatch", x_sorted);
+            EXF_CHECK_PTR(fn, x);
+            EXF_CHECK_ALIGNED(fn, x);
+            EXF_CHECK_ALIGNED(fn, x_sorted);
         }
     }
     return EXF_OK;
 }
 
-// Validation and launches shared by moe_dispatch (chunk counts in the caller's workspace) and
-// moe_dispatch_static (chunk counts in this library's own device array).
-static int dispatch_run(const void* x, const int32_t* topk_idx, const int32_t* expert_map, int64_t T, int d, int k, int E, int E_local,
-                        int dt, void* x_sorted, int32_t* src_of_sorted, int32_t* sorted_of_src, int32_t* expert_counts,
-                        int32_t* expert_offsets, void* workspace, size_t workspace_bytes, void* stream)
+int check_dispatch(const void* x, const int32_t* topk_idx, int64_t T, int d, int k, int E, int E_local, int dt, const void* x_sorted,
+                   const int32_t* src_of_sorted, const int32_t* sorted_of_src, const int32_t* expert_counts, const int32_t* expert_offsets,
+                   const void* workspace, size_t workspace_bytes)
 {
-    if (int rc = check_dispatch(x, topk_idx, T, d, k, E, E_local, dt, x_sorted, src_of_sorted, sorted_of_src, expert_counts, expert_offsets,
-                                workspace, workspace_bytes))
-        return rc;
+    return check_dispatch_of("moe_dispatch", EXF_MAX_TOPK, x, topk_idx, T, d, k, E, E_local, dt, x_sorted, src_of_sorted, sorted_of_src, expert_counts,
+                             expert_offsets, workspace, workspace_bytes);
+}
+
+// Launches shared by moe_dispatch and moe_dispatch_topk (chunk counts in the caller's workspace) and
+// moe_dispatch_static (chunk counts in this library's own device array).
+static int dispatch_launch(const char* fn, const void* x, const int32_t* topk_idx, const int32_t* expert_map, int64_t T, int d, int k, int E, int E_local,
+                        int dt, void* x_sorted, int32_t* src_of_sorted, int32_t* sorted_of_src, int32_t* expert_counts,
+                        int32_t* expert_offsets, void* workspace, void* stream)
+{
     const int64_t A = T * k;
     hipStream_t s = static_cast<hipStream_t>(stream);
     int32_t* block_counts = static_cast<int32_t*>(workspace);
@@ -565,7 +570,7 @@ static int dispatch_run(const void* x, const int32_t* topk_idx, const int32_t* e
         else if (A <= 4 * kDirectThreads) EXF_LAUNCH_DIRECT(4);
         else EXF_LAUNCH_DIRECT(8);
 #undef EXF_LAUNCH_DIRECT
-        return check_launch("moe_dispatch");
+        return check_launch(fn);
     }
     if (A > 0 && x_sorted != nullptr && A <= (vec_per_row < kDirectRowVecs ? kDirectShortRows : kDirectRows)) {
 #define EXF_LAUNCH_DIRECT(MOVE)                                                                                                                        \
@@ -575,7 +580,7 @@ static int dispatch_run(const void* x, const int32_t* topk_idx, const int32_t* e
         if (A <= kDirectRows8) EXF_LAUNCH_DIRECT(8);
         else EXF_LAUNCH_DIRECT(16);
 #undef EXF_LAUNCH_DIRECT
-        return check_launch("moe_dispatch");
+        return check_launch(fn);
     }
     if (n_blocks > 0)
         hipLaunchKernelGGL(dispatch_count_kernel, dim3(n_blocks), dim3(kDispThreads), 0, s, topk_idx, expert_map, A, E, E_local,
@@ -610,7 +615,18 @@ static int dispatch_run(const void* x, const int32_t* topk_idx, const int32_t* e
 #undef EXF_LAUNCH_PLACE
         }
     }
-    return check_launch("moe_dispatch");
+    return check_launch(fn);
+}
+
+static int dispatch_run(const void* x, const int32_t* topk_idx, const int32_t* expert_map, int64_t T, int d, int k, int E, int E_local,
+                        int dt, void* x_sorted, int32_t* src_of_sorted, int32_t* sorted_of_src, int32_t* expert_counts,
+                        int32_t* expert_offsets, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (int rc = check_dispatch(x, topk_idx, T, d, k, E, E_local, dt, x_sorted, src_of_sorted, sorted_of_src, expert_counts, expert_offsets,
+                                workspace, workspace_bytes))
+        return rc;
+    return dispatch_launch("moe_dispatch", x, topk_idx, expert_map, T, d, k, E, E_local, dt, x_sorted, src_of_sorted, sorted_of_src, expert_counts,
+                           expert_offsets, workspace, stream);
 }
 
 // ---- the entry point that allocates nothing --------------------------------------------------
@@ -653,6 +669,18 @@ extern "C" int moe_dispatch(const void* x, const int32_t* topk_idx, const int32_
 {
     return exf::dispatch_run(x, topk_idx, expert_map, T, d, k, E, E_local, dt, x_sorted, src_of_sorted, sorted_of_src, expert_counts,
                              expert_offsets, workspace, workspace_bytes, stream);
+}
+
+extern "C" int moe_dispatch_topk(const void* x, const int32_t* topk_idx, const int32_t* expert_map, int64_t T, int d, int k, int E, int E_local, int dt,
+                                 void* x_sorted, int32_t* src_of_sorted, int32_t* sorted_of_src, int32_t* expert_counts, int32_t* expert_offsets,
+                                 void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace exf;
+    if (int rc = check_dispatch_of("moe_dispatch_topk", EXF_MAX_ROUTE_TOPK, x, topk_idx, T, d, k, E, E_local, dt, x_sorted, src_of_sorted, sorted_of_src,
+                                   expert_counts, expert_offsets, workspace, workspace_bytes))
+        return rc;
+    return dispatch_launch("moe_dispatch_topk", x, topk_idx, expert_map, T, d, k, E, E_local, dt, x_sorted, src_of_sorted, sorted_of_src, expert_counts,
+                           expert_offsets, workspace, stream);
 }
 
 extern "C" int moe_dispatch_static(const void* x, const int32_t* topk_idx, const int32_t* expert_map, int64_t T, int d, int k, int E,

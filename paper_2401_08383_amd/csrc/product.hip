@@ -3,7 +3,7 @@
 
 namespace exf {
 
-static int check_sizes(const char* fn, int64_t A, int n, int k, int E_local, int dt)
+int check_product_sizes(const char* fn, int64_t A, int n, int k, int E_local, int dt)
 {
     if (dt != EXF_F32 && dt != EXF_BF16) return fail(EXF_ERR_BAD_DTYPE, "%s: dt = %d", fn, dt);
     if (A < 0 || A > EXF_MAX_PRODUCT_ROWS) return fail(EXF_ERR_BAD_SHAPE, "%s: A = %lld outside [0,%lld]", fn, static_cast<long long>(A), EXF_MAX_PRODUCT_ROWS);
@@ -21,7 +21,7 @@ static size_t type_bytes(int dt) { return dt == EXF_BF16 ? 2 : 4; }
 static int check_rows_product(const char* fn, const void* rows, const int32_t* offsets, const void* w, const void* bias, int64_t A, int n, int k,
                               int E_local, int dt, bool gradient, const void* out)
 {
-    if (int rc = check_sizes(fn, A, n, k, E_local, dt)) return rc;
+    if (int rc = check_product_sizes(fn, A, n, k, E_local, dt)) return rc;
     if (A == 0) return EXF_OK;
     EXF_CHECK_PTR(fn, rows);
     EXF_CHECK_PTR(fn, offsets);
@@ -112,7 +112,7 @@ extern "C" int moe_grouped_product_dw(const void* dy_sorted, const void* x_sorte
 {
     using namespace exf;
     const char* fn = "moe_grouped_product_dw";
-    if (int rc = check_sizes(fn, A, n, k, E_local, dt)) return rc;
+    if (int rc = check_product_sizes(fn, A, n, k, E_local, dt)) return rc;
     if (grad_dt != EXF_F32 && grad_dt != dt) return fail(EXF_ERR_BAD_DTYPE, "%s: grad_dt = %d with dt = %d", fn, grad_dt, dt);
     if (A > 0) {
         EXF_CHECK_PTR(fn, dy_sorted);
@@ -158,7 +158,7 @@ extern "C" int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_sc
 {
     using namespace exf;
     const char* fn = "moe_grouped_product_mx4";
-    if (int rc = check_sizes(fn, A, n, k, E_local, dt)) return rc;
+    if (int rc = check_product_sizes(fn, A, n, k, E_local, dt)) return rc;
     if (k % EXF_MX4_BLOCK != 0) return fail(EXF_ERR_BAD_SHAPE, "%s: k = %d must be a multiple of %d", fn, k, EXF_MX4_BLOCK);
     if (A == 0) return EXF_OK;
     EXF_CHECK_PTR(fn, x_sorted);

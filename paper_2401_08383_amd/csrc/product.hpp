@@ -37,6 +37,9 @@ struct Mx4Product {
     int max_rows, K, N, E_local;
 };
 
+// What the products refuse of their sizes.
+int check_product_sizes(const char* fn, int64_t A, int n, int k, int E_local, int dt);
+
 // fp32 (product_exact.hip).
 int launch_exact_product(const ExactRows& p, hipStream_t stream);
 int launch_exact_rows_gradient(const ExactRows& p, hipStream_t stream);
