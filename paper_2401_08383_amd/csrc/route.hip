@@ -59,22 +59,86 @@ __device__ __forceinline__ double token_sum64(double v)
     return v;
 }
 
-// V logits of experts first .. first + V - 1 of a row, -inf past the last one.
 template <bool BF16>
 __device__ __forceinline__ float load_logit(const void* row, int e)
 {
     if constexpr (BF16) return bf16_to_f32(static_cast<const bf16_t*>(row)[e]);
     else return static_cast<const float*>(row)[e];
 }
+// A logit's place in the order of all bf16 numbers, from 1 on; 0 for -inf and NaN.
+__device__ __forceinline__ uint32_t ordered(float l)
+{
+    const uint32_t u = __float_as_uint(l + 0.0f) >> 16;  // (-0 is 0)
+    return l > -INFINITY ? ((u & 0x8000u) != 0u ? 0xffffu - u : u + 0x8000u) + 1u : 0u;
+}
 template <bool BF16>
 __device__ __forceinline__ const void* row_at(const void* p, int64_t i) { return static_cast<const uint8_t*>(p) + i * (BF16 ? 2 : 4); }
+// V values of experts first .. first + V - 1 of a row, `none` past the last one; four at a time where rows are a multiple of that.
 template <int V, bool BF16>
-__device__ __forceinline__ void load_logits(const void* row, int first, int E, float (&l)[V])
+__device__ __forceinline__ void load_row(const void* row, int first, int E, float none, float (&l)[V])
 {
 #pragma unroll
-    for (int v = 0; v < V; ++v) l[v] = first + v < E ? load_logit<BF16>(row, first + v) : -INFINITY;
+    for (int v = 0; v < V; ++v) l[v] = none;
+    if (E % 4 == 0) {
+#pragma unroll
+        for (int v = 0; v < V; v += 4)
+            if (first + v < E) {
+                if constexpr (BF16) {
+                    const uint2 t = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(row) + first + v);
+                    l[v] = __uint_as_float(t.x << 16), l[v + 1] = __uint_as_float(t.x & 0xffff0000u);
+                    l[v + 2] = __uint_as_float(t.y << 16), l[v + 3] = __uint_as_float(t.y & 0xffff0000u);
+                } else {
+                    const float4 t = *reinterpret_cast<const float4*>(static_cast<const float*>(row) + first + v);
+                    l[v] = t.x, l[v + 1] = t.y, l[v + 2] = t.z, l[v + 3] = t.w;
+                }
+            }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float x = load_logit<BF16>(row, min(first + v, E - 1));
+            l[v] = first + v < E ? x : none;
+        }
+    }
+}
+template <int V, bool BF16>
+__device__ __forceinline__ void store_row(void* row, int first, int E, const float (&l)[V])
+{
+    if (E % 4 == 0) {
+#pragma unroll
+        for (int v = 0; v < V; v += 4)
+            if (first + v < E) {
+                if constexpr (BF16) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(row) + first + v) = make_uint2(pack_bf16x2(l[v], l[v + 1]), pack_bf16x2(l[v + 2], l[v + 3]));
+                else *reinterpret_cast<float4*>(static_cast<float*>(row) + first + v) = make_float4(l[v], l[v + 1], l[v + 2], l[v + 3]);
+            }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (first + v < E) {
+                if constexpr (BF16) static_cast<bf16_t*>(row)[first + v] = f32_to_bf16(l[v]);
+                else static_cast<float*>(row)[first + v] = l[v];
+            }
+    }
 }
 
+// exp(x) for x <= 0 (0 below -200), to less than two units: what the argument loses on its way to base 2 is put back, and results below the normal range are
+// kept (the instruction flushes them).
+__device__ __forceinline__ float exp_below(float x)
+{
+    x = fmaxf(x, -200.0f);
+    const float t = x * 1.442695041f, rest = fmaf(x, 1.925963033e-8f, fmaf(x, 1.442695041f, -t)), whole = rintf(t);
+    return ldexpf(__builtin_amdgcn_exp2f((t - whole) + rest), static_cast<int>(whole));
+}
+// a / b for b in [1, 2], to a unit.
+__device__ __forceinline__ float quotient(float a, float b)
+{
+    const float r = __builtin_amdgcn_rcpf(b), q = a * r;
+    return fmaf(fmaf(-b, q, a), r, q);
+}
+__device__ __forceinline__ float sigmoid(float l)
+{
+    const float t = exp_below(-fabsf(l));
+    return l != l ? l : quotient(l >= 0.0f ? 1.0f : t, 1.0f + t);
+}
 // Weights of the chosen experts, lane j of the token with logit l of its own (live: there is one); `most` and `sum`: the largest logit of the
 // token and the sum of exp(l - most).
 //   Renormalised scores are u_j / sum u with any u proportional to the scores: exp(l - the largest chosen l) for the softmax, and for the sigmoid
@@ -89,11 +153,6 @@ __device__ __forceinline__ float chosen_share(float l, bool live)
     if (!live) u = 0.0f;
     const float all = token_sum<L>(u);
     return live ? u / all : 0.0f;
-}
-__device__ __forceinline__ float sigmoid(float l)
-{
-    const float t = expf(-fabsf(l));
-    return (l >= 0.0f ? 1.0f : t) / (1.0f + t);
 }
 __device__ __forceinline__ double sigmoid64(double l)
 {
@@ -115,69 +174,43 @@ __device__ __forceinline__ void best_over_token(double& key, int& at)
     }
 }
 
-template <int V, int L, bool BF16, bool SIGMOID>
-__global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
+// Ids by keys in 64 bits, in the order of the definition; slot j in lane j.  `keys`: the lane's logits, kWave apart.  In LDS and in loops:
+// wavefronts that need none of it would have to leave room for its registers (245 instead of 90 with 16 experts a lane, two wavefronts a SIMD: 32768 tokens of 256
+// experts in groups 50 us).
+template <int V, int L, bool SIGMOID, bool SCORES, bool GROUPS>
+__device__ __forceinline__ int choose_exactly(const RouteCall& p, double* keys, int first, int in, float base)
 {
-    const int lane = lane_id(), in = lane % L;
-    constexpr int kTokens = kRouteThreads / L;
-    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < p.T; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
-    const int64_t t = t0 + threadIdx.x / L;
-    const bool there = t < p.T;
-    const int64_t row = min(t, p.T - 1);
-    const void* at = row_at<BF16>(p.logits, row * p.E);
-    const int first = in * V;
-    float l[V];
-    load_logits<V, BF16>(at, first, p.E, l);
-    float most = -INFINITY;
-    bool broken = false;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        most = fmaxf(most, l[v]);  // (ignores a NaN)
-        broken |= l[v] != l[v];
-    }
-    most = token_max<L>(most);
-    broken = token_max<L>(broken ? 1.0f : 0.0f) > 0.0f || (!SIGMOID && most == INFINITY);
-    const float base = most == -INFINITY ? 0.0f : most;
-    float sum = 0.0f;
-    if constexpr (!SIGMOID) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum += expf(l[v] - base);
-        sum = token_sum<L>(sum);
-    }
-    if (p.scores != nullptr && there) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (first + v < p.E) p.scores[row * p.E + first + v] = SIGMOID ? sigmoid(l[v]) : (most == -INFINITY ? 0.0f : expf(l[v] - base) / sum);
-    }
-
-    // keys in 64 bits
-    double key[V];
-    const bool wide = p.bias != nullptr || (p.groups > 1 && p.group_best == 2);
+    const bool by_score = SCORES && p.bias == nullptr;  // (of groups)
     double sum64 = 0.0;
-    if (wide && !SIGMOID) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum64 += l[v] > -INFINITY ? exp(static_cast<double>(l[v]) - base) : 0.0;
+    if constexpr (SCORES && !SIGMOID) {
+#pragma unroll 1
+        for (int v = 0; v < V; ++v) {
+            const double x = keys[v * kWave];
+            sum64 += x > -INFINITY ? exp(x - base) : 0.0;
+        }
         sum64 = token_sum64<L>(sum64);
     }
-    auto score64 = [&](float v) -> double { return SIGMOID ? sigmoid64(v) : exp(static_cast<double>(v) - base) / sum64; };
-#pragma unroll
+    auto score64 = [&](double x) -> double { return SIGMOID ? sigmoid64(x) : exp(x - base) / sum64; };
+#pragma unroll 1
     for (int v = 0; v < V; ++v) {
-        key[v] = l[v];
-        if (p.bias != nullptr) key[v] = score64(l[v]) + p.bias[min(first + v, p.E - 1)];
-        if (!(l[v] > -INFINITY) || !(key[v] > -INFINITY)) key[v] = -INFINITY;  // (also a NaN)
+        const double x = keys[v * kWave];
+        double key = x;
+        if (SCORES && p.bias != nullptr) key = score64(x) + p.bias[min(first + v, p.E - 1)];
+        keys[v * kWave] = x > -INFINITY && key > -INFINITY ? key : -INFINITY;  // (out: also a NaN)
     }
-    if (p.groups > 1) {
-        const int size = p.E / p.groups;
-        unsigned long long stay = ~0ull;
+    unsigned long long stay = ~0ull;
+    const int size = p.E / p.groups;
+    if constexpr (GROUPS) {
         double mine[kWave / L];  // values of groups in, in + L, ...
 #pragma unroll
         for (int q = 0; q < kWave / L; ++q) mine[q] = -INFINITY;
+#pragma unroll 1
         for (int g = 0; g < p.groups; ++g) {
             double a = -INFINITY, b = -INFINITY;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const bool member = first + v >= g * size && first + v < (g + 1) * size && key[v] > -INFINITY;
-                const double s = member ? (p.bias == nullptr && p.group_best == 2 ? score64(l[v]) : key[v]) : -INFINITY;
+#pragma unroll 1
+            for (int v = max(g * size - first, 0); v < min((g + 1) * size - first, V); ++v) {
+                double s = keys[v * kWave];
+                if (by_score && s > -INFINITY) s = score64(s);
                 b = fmax(b, fmin(a, s));
                 a = fmax(a, s);
             }
@@ -193,6 +226,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
                 if (g == in + q * L) mine[q] = a;
         }
         stay = 0ull;
+#pragma unroll 1
         for (int j = 0; j < p.top_groups; ++j) {
             double a = -INFINITY;
             int g = kWave;
@@ -205,34 +239,463 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
             for (int q = 0; q < kWave / L; ++q)
                 if (g == in + q * L) mine[q] = -INFINITY;
         }
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (((stay >> min((first + v) / size, kWave - 1)) & 1ull) == 0ull) key[v] = -INFINITY;
     }
-
     int chosen = -1;
+#pragma unroll 1
     for (int j = 0; j < p.k; ++j) {
         double a = -INFINITY;
         int e = 1 << 20;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (key[v] > a) a = key[v], e = first + v;
+#pragma unroll 1
+        for (int v = 0; v < V; ++v) {
+            const double key = keys[v * kWave];
+            if (key > a && (!GROUPS || ((stay >> min((first + v) / size, kWave - 1)) & 1ull) != 0ull)) a = key, e = first + v;
+        }
         best_over_token<L>(a, e);
         if (in == j && a > -INFINITY) chosen = e;
+        if (e >= first && e < first + V) keys[(e - first) * kWave] = -INFINITY;
+    }
+    return chosen;
+}
+
+// ---- the same by whole numbers of 32 bits, where they are sure of the order
+// A key's place between the least and the largest of its token, in 2^22 steps, is its class; the number (class, 511 - id) is unique, the largest one is found
+// with one instruction a step, and equals go to the lowest id.  Where the classes of two experts that follow one another - the last chosen one and the next
+// included - are further apart than the classes' own error, so are the keys; otherwise the wavefront begins again in 64 bits.
+//   bf16 logits without a bias: a class is the logit itself, and always sure.
+constexpr int kIdBits = 9;
+static_assert(EXF_MAX_ROUTE_EXPERTS <= 1 << kIdBits, "an id has its bits");
+constexpr float kClasses = 4194304.0f;  // 2^22
+
+template <int L>
+__device__ __forceinline__ uint32_t token_max_u32(uint32_t v)
+{
+    uint32_t a, b;
+    if constexpr (L >= 32) butterfly<16>(v, a, b), v = max(a, b);
+    butterfly<8>(v, a, b), v = max(a, b);
+    butterfly<4>(v, a, b), v = max(a, b);
+    butterfly<2>(v, a, b), v = max(a, b);
+    butterfly<1>(v, a, b), v = max(a, b);
+    return v;
+}
+
+// Sorted, the largest first (odd-even merge sort).
+template <int V>
+__device__ __forceinline__ void sort_keys(uint32_t (&s)[V])
+{
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (first + v == e) key[v] = -INFINITY;
+    for (int p = 1; p < V; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < V; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < V && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const uint32_t a = s[i + j], b = s[i + j + k];
+                        s[i + j] = max(a, b), s[i + j + k] = min(a, b);
+                    }
+}
+
+// The keys of lanes i and i ^ OFF, the same pair in both of them; lanes that differ in lower bits agree already.
+template <int OFF>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v)
+{
+    if constexpr (OFF == 1) return __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true);        // quad_perm 1,0,3,2
+    else if constexpr (OFF == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true);   // quad_perm 2,3,0,1
+    else if constexpr (OFF == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);  // row_half_mirror
+    else if constexpr (OFF == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);  // row_mirror
+    else return static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), OFF, kWave));
+}
+template <int OFF>
+__device__ __forceinline__ void best_two(uint32_t& a, uint32_t& b)
+{
+    const uint32_t a2 = other_lane<OFF>(a), b2 = other_lane<OFF>(b);
+    b = max(max(b, b2), min(a, a2));
+    a = max(a, a2);
+}
+
+// Largest of the finite values above the lowest that stand for masks, the least of them, and 2^22 steps between them.
+struct Classes {
+    float most, step;
+};
+template <int V, int L>
+__device__ __forceinline__ Classes classes_of(const float (&key)[V])
+{
+    float most = -INFINITY, least = INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        most = fmaxf(most, key[v]);
+        least = fminf(least, key[v] > -1e30f ? key[v] : INFINITY);
+    }
+    most = token_max<L>(most);
+    least = -token_max<L>(-least);
+    const float range = most - least;
+    return {most, range > 0.0f && range < 1e30f ? (kClasses - 2.0f) * __builtin_amdgcn_rcpf(range) : 0.0f};
+}
+// 0: out; 1: at the least, or below; otherwise in order, to within one.
+__device__ __forceinline__ uint32_t class_of(float key, Classes c)
+{
+    const float at = fmaf(key - c.most, c.step, kClasses);
+    return key > -INFINITY ? static_cast<uint32_t>(fmaxf(at, 1.0f)) : 0u;
+}
+
+// LDS of a wavefront is written and read in order; this keeps the compiler from moving either.
+__device__ __forceinline__ void lds_in_order()
+{
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// Where a group's lanes are, if not those that hold its experts: `parts` lanes a group, each with a share of its experts (at most L groups).
+template <int L>
+struct GroupParts {
+    int parts, mine, begin, end;  // my group; its experts that are mine
+    __device__ GroupParts(int E, int groups, int in)
+    {
+        const int size = E / groups;
+        parts = L;
+        while (parts * groups > L) parts >>= 1;
+        mine = in / parts;
+        const int share = (size + parts - 1) / parts, part = in % parts;
+        begin = mine * size + min(part * share, size);
+        end = mine < groups ? mine * size + min((part + 1) * share, size) : begin;
+    }
+};
+
+// The logits of the token's lanes as they lie in a row, at `mine`, for all of them.
+template <int V, int L>
+__device__ __forceinline__ void share_logits(const float (&l)[V], float* token, int first)
+{
+    lds_in_order();
+#pragma unroll
+    for (int v = 0; v < V; ++v) token[first + v] = l[v];
+    lds_in_order();
+}
+
+// Score and key of a logit in 64 bits; -inf: out.
+template <int V, int L, bool SIGMOID, bool SCORES>
+struct ExactKeys {
+    const float* bias;
+    float base;
+    double sum;
+    __device__ ExactKeys(const float* bias, const float* token, int first, float base) : bias(bias), base(base), sum(0.0)
+    {
+        if constexpr (SCORES && !SIGMOID) {
+#pragma unroll 1
+            for (int v = 0; v < V; ++v) {
+                const float x = token[first + v];
+                sum += x > -INFINITY ? exp(static_cast<double>(x) - base) : 0.0;
+            }
+            sum = token_sum64<L>(sum);
+        }
+    }
+    __device__ double score(float x) const { return SIGMOID ? sigmoid64(x) : exp(static_cast<double>(x) - base) / sum; }
+    __device__ double key(float x, int e) const
+    {
+        const double k = SCORES && bias != nullptr ? score(x) + bias[e] : x;
+        return x > -INFINITY && k > -INFINITY ? k : -INFINITY;
+    }
+};
+
+// Whether this lane's group (by parts) stays, by values in 64 bits.
+template <int V, int L, bool SIGMOID, bool SCORES>
+__device__ __forceinline__ bool group_stays_exactly(const float* bias, const float* token, int E, int groups, int top_groups, int group_best, float base)
+{
+    const int in = lane_id() % L, first = in * V;
+    const GroupParts<L> g(E, groups, in);
+    const ExactKeys<V, L, SIGMOID, SCORES> keys(bias, token, first, base);
+    double a = -INFINITY, b = -INFINITY;
+#pragma unroll 1
+    for (int e = g.begin; e < g.end; ++e) {
+        double s = keys.key(token[e], e);
+        if (SCORES && bias == nullptr && s > -INFINITY) s = keys.score(token[e]);
+        b = fmax(b, fmin(a, s));
+        a = fmax(a, s);
+    }
+    for (int off = 1; off < g.parts; off *= 2) {
+        const double a2 = __shfl_xor(a, off, kWave), b2 = __shfl_xor(b, off, kWave);
+        b = fmax(fmax(b, b2), fmin(a, a2));
+        a = fmax(a, a2);
+    }
+    if (group_best == 2 && b > -INFINITY) a += b;
+    int ahead = 0;
+#pragma unroll 1
+    for (int i = 0; i < groups; ++i) {
+        const double other = __shfl(a, (lane_id() & ~(L - 1)) + i * g.parts, kWave);
+        ahead += other > a || (other == a && i < g.mine) ? 1 : 0;
+    }
+    return ahead < top_groups && a > -INFINITY;
+}
+
+__device__ __forceinline__ int id_of(uint32_t n) { return (1 << kIdBits) - 1 - static_cast<int>(n & ((1u << kIdBits) - 1u)); }
+
+// Candidates, one a lane (0: none), in the order of their keys in 64 bits.
+template <int V, int L, bool SIGMOID, bool SCORES>
+__device__ __forceinline__ uint32_t order_exactly(const float* bias, float* token, uint32_t mine, float base)
+{
+    const int in = lane_id() % L, from = lane_id() & ~(L - 1), e = id_of(mine);
+    const ExactKeys<V, L, SIGMOID, SCORES> keys(bias, token, in * V, base);
+    const double exact = mine != 0u ? keys.key(token[mine != 0u ? e : 0], e) : -INFINITY;
+    int ahead = 0;
+#pragma unroll 4
+    for (int i = 0; i < L; ++i) {
+        const double other = __shfl(exact, from + i, kWave);
+        const int id = __shfl(e, from + i, kWave);
+        ahead += other > exact || (other == exact && id < e) ? 1 : 0;
+    }
+    uint32_t* order = reinterpret_cast<uint32_t*>(token);
+    lds_in_order();
+    order[in] = 0u;
+    lds_in_order();
+    if (exact > -INFINITY) order[ahead] = mine;
+    lds_in_order();
+    mine = order[in];
+    lds_in_order();
+    return mine;
+}
+
+template <int V>
+__device__ __forceinline__ void load_bias(const RouteCall& p, int first, float (&bias)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) bias[v] = 0.0f;
+    if (p.bias == nullptr) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) bias[v] = p.bias[min(first + v, p.E - 1)];
+}
+
+// `token`: room for the token's logits in LDS.  sure: whether the lane's part of the choice is the definition's.
+template <int V, int L, bool BF16, bool SIGMOID, bool SCORES, bool GROUPS>
+__device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void* row, float (&l)[V], float (&bias)[V], float* token, int first, int in, float base,
+                                                 float inverse, bool& sure)
+{
+    auto score = [&](float v) {
+        if constexpr (SIGMOID) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));
+        else return __builtin_amdgcn_exp2f((v - base) * 1.44269504f) * inverse;
+    };
+    uint32_t key[V];
+    sure = true;
+    float apart = 0.0f;  // classes that are no further apart say nothing
+    Classes c{0.0f, 0.0f};
+    // A sigmoid is off by less than 2^-21 (half a unit of 2^-23 and less from the exponent and its argument, one from the sum and two from the reciprocal), a
+    // softmax by less than 2^-19 of the largest score (21 sums of terms that are off by two units each), and a sum with a bias by half a last place more.
+    auto classes_of_scores = [&]() {
+        float f[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            f[v] = score(l[v]);
+            if (SCORES && p.bias != nullptr) f[v] += bias[v];
+            f[v] = l[v] > -INFINITY && f[v] > -INFINITY ? f[v] : -INFINITY;
+        }
+        c = classes_of<V, L>(f);
+        const float error = (SIGMOID ? 0x1p-21f : 0x1p-19f * inverse) + 0x1p-23f * fmaxf(fabsf(c.most), fabsf(c.most - kClasses * __builtin_amdgcn_rcpf(c.step)));
+        apart = c.step > 0.0f ? 4.0f + 2.0f * error * c.step : 2.0f * kClasses;
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = class_of(f[v], c);
+    };
+    auto classes_of_logits = [&]() {
+        if constexpr (BF16) {
+            apart = -1.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = ordered(l[v]);
+        } else {
+            c = classes_of<V, L>(l);
+            apart = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = class_of(l[v], c);
+        }
+    };
+    if constexpr (SCORES) classes_of_scores();
+    else classes_of_logits();
+
+    unsigned long long stay = ~0ull;  // lanes whose experts stay, or whose group does where groups have `parts` lanes
+    int parts = 0;
+    const int size = p.E / p.groups, lanes = size / V;
+    const bool aligned = lanes * V == size && (lanes & (lanes - 1)) == 0;  // a group has lanes of its own, a power of two
+    if constexpr (GROUPS) {
+        uint32_t a = 0u, b = 0u;
+        int group;
+        const GroupParts<L> g(p.E, p.groups, in);
+        if (aligned) {
+            group = in / lanes;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                b = max(b, min(a, key[v]));
+                a = max(a, key[v]);
+            }
+            if (lanes > 1) best_two<1>(a, b);
+            if (lanes > 2) best_two<2>(a, b);
+            if (lanes > 4) best_two<4>(a, b);
+            if (lanes > 8) best_two<8>(a, b);
+            if (L > 16 && lanes > 16) best_two<16>(a, b);
+        } else {
+            group = g.mine;
+            uint32_t* classes = reinterpret_cast<uint32_t*>(token);
+            lds_in_order();
+#pragma unroll
+            for (int v = 0; v < V; ++v) classes[first + v] = key[v];
+            lds_in_order();
+#pragma unroll 4
+            for (int e = g.begin; e < g.end; ++e) {
+                const uint32_t k = classes[e];
+                b = max(b, min(a, k));
+                a = max(a, k);
+            }
+            if (g.parts > 1) best_two<1>(a, b);
+            if (g.parts > 2) best_two<2>(a, b);
+            if (g.parts > 4) best_two<4>(a, b);
+            if (g.parts > 8) best_two<8>(a, b);
+            if (L > 16 && g.parts > 16) best_two<16>(a, b);
+        }
+        const uint32_t own = group < p.groups ? (p.group_best == 2 ? a + b : a) << 6 | static_cast<uint32_t>(63 - group) : 0u;
+        uint32_t left = own, last = 0u, next = 0u;
+        for (int j = 0; j <= p.top_groups; ++j) {
+            last = next;
+            next = token_max_u32<L>(left);
+            if (left == next) left = 0u;
+        }
+        bool stays = own >= last;
+        // (a class of one may be anything below; sums of one and of two classes do not compare)
+        const float gap = static_cast<float>((last >> 6) - (next >> 6)), need = p.group_best == 2 ? 2.0f * apart : apart;
+        bool certain = (gap > need && (last >> 6) > 1u) || (BF16 && !SCORES);
+        if (p.group_best == 2 && b <= 1u && a != 0u) certain = false;
+        bool by_parts = !aligned;
+        if (!(BF16 && !SCORES) && __ballot(!certain) != 0ull) {
+            share_logits<V, L>(l, token, first);
+            stays = group_stays_exactly<V, L, SIGMOID, SCORES>(p.bias, token, p.E, p.groups, p.top_groups, p.group_best, base);
+            by_parts = true;
+            // (Classes and what they are made from are formed again, for what is rarely needed: held meanwhile, they cost registers always.)
+            load_row<V, BF16>(row, first, p.E, -INFINITY, l);
+            if constexpr (SCORES) load_bias<V>(p, first, bias), classes_of_scores();
+            else classes_of_logits();
+        }
+        stay = __ballot(stays) >> (lane_id() & ~(L - 1));
+        if (SCORES && p.bias == nullptr) classes_of_logits();
+        parts = by_parts ? g.parts : 0;
+    }
+    // in place of the experts that do not stay, nothing; classes with their ids, sorted
+    auto number = [&]() {
+        if constexpr (GROUPS) {
+            if (parts == 0) {
+                const bool mine = ((stay >> in) & 1ull) != 0ull;
+#pragma unroll
+                for (int v = 0; v < V; ++v) key[v] = mine ? key[v] : 0u;
+            } else {
+                int q = first / size, rest = first - q * size;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if (((stay >> min(q * parts, kWave - 1)) & 1ull) == 0ull) key[v] = 0u;
+                    if (++rest == size) ++q, rest = 0;
+                }
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = key[v] != 0u ? key[v] << kIdBits | static_cast<uint32_t>((1 << kIdBits) - 1 - first - v) : 0u;
+        sort_keys<V>(key);
+    };
+    uint32_t mine = 0u, next = 0u;
+    // the `count` largest: the largest of all heads is taken off its lane's list, of which M places are moved
+    auto take = [&](auto places, int count) {
+        constexpr int M = decltype(places)::value;
+        for (int j = 0; j < count; ++j) {
+            next = token_max_u32<L>(key[0]);
+            mine = in == j ? next : mine;
+            const bool taken = key[0] == next;
+#pragma unroll
+            for (int v = 0; v < M; ++v) key[v] = taken ? (v + 1 < V ? key[v + 1] : 0u) : key[v];
+        }
+    };
+    const std::integral_constant<int, V> all;
+    const std::integral_constant<int, (V > 9 ? 9 : V)> nine;
+    number();
+    if (V > 9 && p.k <= 8) take(nine, p.k + 1);
+    else take(all, p.k + 1);
+    const uint32_t right = static_cast<uint32_t>(__shfl_down(static_cast<int>(mine), 1, kWave)), after = in == p.k - 1 ? next : right;
+    const float gap = static_cast<float>(mine >> kIdBits) - static_cast<float>(after >> kIdBits);
+    const bool certain = in >= p.k || mine == 0u || (BF16 && p.bias == nullptr) || (gap > apart && mine >> kIdBits > 1u);
+    if (!(BF16 && !SCORES) && __ballot(!certain) != 0ull) {
+        // Neighbours that classes do not tell apart: the L best by class, a lane each, put in order by their keys in 64 bits.  The k best are among them if the
+        // last one is clearly behind the k-th, or there are no more.
+        const uint32_t behind_all = next;
+        load_row<V, BF16>(row, first, p.E, -INFINITY, l);
+        if constexpr (SCORES) load_bias<V>(p, first, bias);
+        if (SCORES && p.bias != nullptr) classes_of_scores();
+        else classes_of_logits();
+        number();
+        mine = 0u;
+        take(all, L);
+        const int from = lane_id() & ~(L - 1);
+        const uint32_t kth = static_cast<uint32_t>(__shfl(static_cast<int>(mine), from + p.k - 1, kWave)) >> kIdBits;
+        const uint32_t end = static_cast<uint32_t>(__shfl(static_cast<int>(mine), from + L - 1, kWave)) >> kIdBits;
+        const uint32_t behind = p.k == L ? behind_all >> kIdBits : end;
+        sure = behind == 0u || kth == 0u || (static_cast<float>(kth) - static_cast<float>(behind) > apart && kth > 1u);
+        share_logits<V, L>(l, token, first);
+        mine = order_exactly<V, L, SIGMOID, SCORES>(p.bias, token, mine, base);
+    }
+    return in < p.k && mine != 0u ? id_of(mine) : -1;
+}
+
+template <int V, int L, bool BF16, bool SIGMOID, bool SCORES, bool GROUPS>
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
+{
+    __shared__ double keys[V * kRouteThreads];  // of the exact choice, or a token's logits or classes
+    const int in = lane_id() % L, first = in * V;
+    constexpr int kTokens = kRouteThreads / L;
+    const bool by_classes = !GROUPS || p.groups <= L;
+    double* mine_in_lds = keys + threadIdx.x / kWave * (V * kWave);
+    float* token = reinterpret_cast<float*>(mine_in_lds) + lane_id() / L * (L * V);
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kTokens;
+    if (t0 >= p.T) return;
+    const int64_t t = t0 + threadIdx.x / L;
+    const bool there = t < p.T;
+    const int64_t row = min(t, p.T - 1);
+    const void* at = row_at<BF16>(p.logits, row * p.E);
+    float l[V], bias[V];
+    load_row<V, BF16>(at, first, p.E, -INFINITY, l);
+    if constexpr (SCORES) load_bias<V>(p, first, bias);
+    float most = -INFINITY;
+    uint32_t bits = 0u;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        most = fmaxf(most, l[v]);  // (ignores a NaN)
+        bits = max(bits, __float_as_uint(l[v]) & 0x7fffffffu);
+    }
+    most = token_max<L>(most);
+    const bool broken = token_max_u32<L>(bits) > 0x7f800000u || (!SIGMOID && most == INFINITY);
+    const float base = most == -INFINITY ? 0.0f : most;
+    const bool share = p.renormalize && p.k > 1;
+    float sum = 0.0f;
+    if (!SIGMOID && (SCORES || !share || p.scores != nullptr)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum += exp_below(l[v] - base);
+        sum = token_sum<L>(sum);
+    }
+    const float inverse = 1.0f / sum;
+    if (p.scores != nullptr && there) {
+        float s[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) s[v] = SIGMOID ? sigmoid(l[v]) : (most == -INFINITY ? 0.0f : exp_below(l[v] - base) * inverse);
+        store_row<V, false>(p.scores + row * p.E, first, p.E, s);
+    }
+    int chosen = -1;
+    bool sure = false;
+    if (by_classes) chosen = choose_by_classes<V, L, BF16, SIGMOID, SCORES, GROUPS>(p, at, l, bias, token, first, in, base, inverse, sure);
+    if ((GROUPS || !(BF16 && !SCORES)) && __ballot(!sure) != 0ull) {
+        load_row<V, BF16>(at, first, p.E, -INFINITY, l);
+        lds_in_order();  // (the place held the tokens' logits)
+#pragma unroll
+        for (int v = 0; v < V; ++v) mine_in_lds[v * kWave + lane_id()] = l[v];
+        chosen = choose_exactly<V, L, SIGMOID, SCORES, GROUPS>(p, mine_in_lds + lane_id(), first, in, base);
     }
     const bool live = chosen >= 0;
     const float mine = live ? load_logit<BF16>(at, chosen) : -INFINITY;
     float w;
-    if (p.renormalize && p.k > 1) w = chosen_share<L, SIGMOID>(mine, live);
+    if (share) w = chosen_share<L, SIGMOID>(mine, live);
     else if (!live) w = 0.0f;
-    else w = SIGMOID ? sigmoid(mine) : expf(mine - base) / sum;
+    else w = SIGMOID ? sigmoid(mine) : exp_below(mine - base) * inverse;
     if (there && in < p.k) {
         p.idx[row * p.k + in] = chosen;
         p.w[row * p.k + in] = broken ? NAN : p.scale * w;
-    }
     }
 }
 
@@ -246,7 +709,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
 {
     const int lane = lane_id(), in = lane % L;
     constexpr int kTokens = kRouteThreads / L;
-    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < p.T; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kTokens;
+    if (t0 >= p.T) return;
     const int64_t t = t0 + threadIdx.x / L;
     const bool there = t < p.T;
     const int64_t row = min(t, p.T - 1);
@@ -264,9 +728,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
     float l[V], d[V];
     const bool all = p.dscores != nullptr || (!SIGMOID && !renormalize);
     if (all) {
-        load_logits<V, BF16>(at, first, p.E, l);
+        load_row<V, BF16>(at, first, p.E, -INFINITY, l);
 #pragma unroll
-        for (int v = 0; v < V; ++v) d[v] = p.dscores != nullptr && first + v < p.E ? p.dscores[row * p.dscores_stride + first + v] : 0.0f;
+        for (int v = 0; v < V; ++v) d[v] = 0.0f;
+        if (p.dscores != nullptr) load_row<V, false>(p.dscores + row * p.dscores_stride, first, p.E, 0.0f, d);
         if constexpr (!SIGMOID) {
             most = l[0];
 #pragma unroll
@@ -276,7 +741,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
             sum = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                l[v] = expf(l[v] - most);
+                l[v] = exp_below(l[v] - most);
                 sum += l[v];
             }
             sum = token_sum<L>(sum);
@@ -315,13 +780,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
         for (int v = 0; v < V; ++v)
             if (first + v == ej) out[v] += cj;
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (there && first + v < p.E) {
-            if constexpr (BF16) static_cast<bf16_t*>(p.dlogits)[row * p.E + first + v] = f32_to_bf16(out[v]);
-            else static_cast<float*>(p.dlogits)[row * p.E + first + v] = out[v];
-        }
-    }
+    if (there) store_row<V, BF16>(static_cast<uint8_t*>(p.dlogits) + row * p.E * (BF16 ? 2 : 4), first, p.E, out);
 }
 
 // Calls run(V, L, type, score) with the instance for E experts.
@@ -342,10 +801,11 @@ static void pick_route(int E, int dt, int score, F run)
     else with(std::integral_constant<int, 16>(), l32);
 }
 
-static unsigned route_grid(int64_t T, int tokens)
+// (Not a loop over the tokens: what the rare paths need would be made ready in front of it.)
+static dim3 route_grid(int64_t T, int tokens)
 {
-    const int64_t blocks = (T + tokens - 1) / tokens;
-    return static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20);
+    const int64_t blocks = (T + tokens - 1) / tokens, wide = blocks < (1 << 20) ? blocks : 1 << 20;
+    return dim3(static_cast<unsigned>(wide), static_cast<unsigned>((blocks + wide - 1) / wide));
 }
 
 static int check_route(const char* fn, int64_t T, int E, int k, int score, float scale, int dt)
@@ -391,10 +851,17 @@ extern "C" int moe_route(const void* logits, const float* bias, int64_t T, int E
             if (overlap(out[i].at, out[i].bytes, out[j].at, out[j].bytes)) return fail(EXF_ERR_BAD_SHAPE, "%s: results must not overlap", fn);
     }
     const RouteCall p{logits, bias, topk_idx, topk_w, scores_out, T, E, k, groups == top_groups ? 1 : groups, top_groups, group_best, renormalize, scale};
+    const bool in_groups = p.groups > 1, by_scores = bias != nullptr || (in_groups && group_best == 2);
     pick_route(E, dt, score, [&](auto v, auto l, auto bf16, auto sigmoid) {
         constexpr int kTokens = kRouteThreads / decltype(l)::value;
-        hipLaunchKernelGGL((route_kernel<decltype(v)::value, decltype(l)::value, decltype(bf16)::value, decltype(sigmoid)::value>),
-                           dim3(route_grid(T, kTokens)), dim3(kRouteThreads), 0, static_cast<hipStream_t>(stream), p);
+        auto launch = [&](auto scores, auto grouped) {
+            hipLaunchKernelGGL((route_kernel<decltype(v)::value, decltype(l)::value, decltype(bf16)::value, decltype(sigmoid)::value, decltype(scores)::value, decltype(grouped)::value>),
+                               route_grid(T, kTokens), dim3(kRouteThreads), 0, static_cast<hipStream_t>(stream), p);
+        };
+        const std::true_type yes;
+        const std::false_type no;
+        if (by_scores) in_groups ? launch(yes, yes) : launch(yes, no);
+        else in_groups ? launch(no, yes) : launch(no, no);
     });
     return check_launch(fn);
 }
@@ -423,7 +890,7 @@ extern "C" int moe_route_backward(const float* dtopk_w, const void* logits, cons
     pick_route(E, dt, score, [&](auto v, auto l, auto bf16, auto sigmoid) {
         constexpr int kTokens = kRouteThreads / decltype(l)::value;
         hipLaunchKernelGGL((route_backward_kernel<decltype(v)::value, decltype(l)::value, decltype(bf16)::value, decltype(sigmoid)::value>),
-                           dim3(route_grid(T, kTokens)), dim3(kRouteThreads), 0, static_cast<hipStream_t>(stream), p);
+                           route_grid(T, kTokens), dim3(kRouteThreads), 0, static_cast<hipStream_t>(stream), p);
     });
     return check_launch(fn);
 }
