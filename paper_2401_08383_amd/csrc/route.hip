@@ -73,8 +73,13 @@ __device__ __forceinline__ uint32_t ordered(float l)
 }
 template <bool BF16>
 __device__ __forceinline__ const void* row_at(const void* p, int64_t i) { return static_cast<const uint8_t*>(p) + i * (BF16 ? 2 : 4); }
-// V values of experts first .. first + V - 1 of a row, `none` past the last one; four at a time where rows are a multiple of that.
-template <int V, bool BF16>
+// A lane's experts are first + place(0), first + place(1), ..: pieces of four, P apart.  Next to each other (4), so that a group of experts has lanes of its own, or with
+// those of the other lanes between them (4 L), so that neighbouring lanes load what lies together: 64 accesses to the L1 of a load, or 16.
+template <int P>
+__host__ __device__ constexpr int place(int v) { return v / 4 * P + v % 4; }
+
+// The lane's V values of a row, `none` past the last one; four at a time where rows are a multiple of that.
+template <int V, int P, bool BF16>
 __device__ __forceinline__ void load_row(const void* row, int first, int E, float none, float (&l)[V])
 {
 #pragma unroll
@@ -82,40 +87,40 @@ __device__ __forceinline__ void load_row(const void* row, int first, int E, floa
     if (E % 4 == 0) {
 #pragma unroll
         for (int v = 0; v < V; v += 4)
-            if (first + v < E) {
+            if (first + place<P>(v) < E) {
                 if constexpr (BF16) {
-                    const uint2 t = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(row) + first + v);
+                    const uint2 t = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(row) + first + place<P>(v));
                     l[v] = __uint_as_float(t.x << 16), l[v + 1] = __uint_as_float(t.x & 0xffff0000u);
                     l[v + 2] = __uint_as_float(t.y << 16), l[v + 3] = __uint_as_float(t.y & 0xffff0000u);
                 } else {
-                    const float4 t = *reinterpret_cast<const float4*>(static_cast<const float*>(row) + first + v);
+                    const float4 t = *reinterpret_cast<const float4*>(static_cast<const float*>(row) + first + place<P>(v));
                     l[v] = t.x, l[v + 1] = t.y, l[v + 2] = t.z, l[v + 3] = t.w;
                 }
             }
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float x = load_logit<BF16>(row, min(first + v, E - 1));
-            l[v] = first + v < E ? x : none;
+            const float x = load_logit<BF16>(row, min(first + place<P>(v), E - 1));
+            l[v] = first + place<P>(v) < E ? x : none;
         }
     }
 }
-template <int V, bool BF16>
+template <int V, int P, bool BF16>
 __device__ __forceinline__ void store_row(void* row, int first, int E, const float (&l)[V])
 {
     if (E % 4 == 0) {
 #pragma unroll
         for (int v = 0; v < V; v += 4)
-            if (first + v < E) {
-                if constexpr (BF16) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(row) + first + v) = make_uint2(pack_bf16x2(l[v], l[v + 1]), pack_bf16x2(l[v + 2], l[v + 3]));
-                else *reinterpret_cast<float4*>(static_cast<float*>(row) + first + v) = make_float4(l[v], l[v + 1], l[v + 2], l[v + 3]);
+            if (first + place<P>(v) < E) {
+                if constexpr (BF16) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(row) + first + place<P>(v)) = make_uint2(pack_bf16x2(l[v], l[v + 1]), pack_bf16x2(l[v + 2], l[v + 3]));
+                else *reinterpret_cast<float4*>(static_cast<float*>(row) + first + place<P>(v)) = make_float4(l[v], l[v + 1], l[v + 2], l[v + 3]);
             }
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (first + v < E) {
-                if constexpr (BF16) static_cast<bf16_t*>(row)[first + v] = f32_to_bf16(l[v]);
-                else static_cast<float*>(row)[first + v] = l[v];
+            if (first + place<P>(v) < E) {
+                if constexpr (BF16) static_cast<bf16_t*>(row)[first + place<P>(v)] = f32_to_bf16(l[v]);
+                else static_cast<float*>(row)[first + place<P>(v)] = l[v];
             }
     }
 }
@@ -124,7 +129,7 @@ __device__ __forceinline__ void store_row(void* row, int first, int E, const flo
 // kept (the instruction flushes them).
 __device__ __forceinline__ float exp_below(float x)
 {
-    x = fmaxf(x, -200.0f);
+    x = x < -200.0f ? -200.0f : x;
     const float t = x * 1.442695041f, rest = fmaf(x, 1.925963033e-8f, fmaf(x, 1.442695041f, -t)), whole = rintf(t);
     return ldexpf(__builtin_amdgcn_exp2f((t - whole) + rest), static_cast<int>(whole));
 }
@@ -137,7 +142,13 @@ __device__ __forceinline__ float quotient(float a, float b)
 __device__ __forceinline__ float sigmoid(float l)
 {
     const float t = exp_below(-fabsf(l));
-    return l != l ? l : quotient(l >= 0.0f ? 1.0f : t, 1.0f + t);
+    return quotient(l >= 0.0f ? 1.0f : t, 1.0f + t);
+}
+// s (1 - s) of s = sigmoid(l), also where s is next to 1.
+__device__ __forceinline__ float sigmoid_slope(float l)
+{
+    const float t = exp_below(-fabsf(l)), q = quotient(1.0f, 1.0f + t);
+    return t * q * q;
 }
 // Weights of the chosen experts, lane j of the token with logit l of its own (live: there is one); `most` and `sum`: the largest logit of the
 // token and the sum of exp(l - most).
@@ -177,7 +188,7 @@ __device__ __forceinline__ void best_over_token(double& key, int& at)
 // Ids by keys in 64 bits, in the order of the definition; slot j in lane j.  `keys`: the lane's logits, kWave apart.  In LDS and in loops:
 // wavefronts that need none of it would have to leave room for its registers (245 instead of 90 with 16 experts a lane, two wavefronts a SIMD: 32768 tokens of 256
 // experts in groups 50 us).
-template <int V, int L, bool SIGMOID, bool SCORES, bool GROUPS>
+template <int V, int P, int L, bool SIGMOID, bool SCORES, bool GROUPS>
 __device__ __forceinline__ int choose_exactly(const RouteCall& p, double* keys, int first, int in, float base)
 {
     const bool by_score = SCORES && p.bias == nullptr;  // (of groups)
@@ -195,7 +206,7 @@ __device__ __forceinline__ int choose_exactly(const RouteCall& p, double* keys, 
     for (int v = 0; v < V; ++v) {
         const double x = keys[v * kWave];
         double key = x;
-        if (SCORES && p.bias != nullptr) key = score64(x) + p.bias[min(first + v, p.E - 1)];
+        if (SCORES && p.bias != nullptr) key = score64(x) + p.bias[min(first + place<P>(v), p.E - 1)];
         keys[v * kWave] = x > -INFINITY && key > -INFINITY ? key : -INFINITY;  // (out: also a NaN)
     }
     unsigned long long stay = ~0ull;
@@ -208,7 +219,7 @@ __device__ __forceinline__ int choose_exactly(const RouteCall& p, double* keys, 
         for (int g = 0; g < p.groups; ++g) {
             double a = -INFINITY, b = -INFINITY;
 #pragma unroll 1
-            for (int v = max(g * size - first, 0); v < min((g + 1) * size - first, V); ++v) {
+            for (int v = max(g * size - first, 0); v < min((g + 1) * size - first, V); ++v) {  // (in groups P is 4)
                 double s = keys[v * kWave];
                 if (by_score && s > -INFINITY) s = score64(s);
                 b = fmax(b, fmin(a, s));
@@ -248,11 +259,12 @@ __device__ __forceinline__ int choose_exactly(const RouteCall& p, double* keys, 
 #pragma unroll 1
         for (int v = 0; v < V; ++v) {
             const double key = keys[v * kWave];
-            if (key > a && (!GROUPS || ((stay >> min((first + v) / size, kWave - 1)) & 1ull) != 0ull)) a = key, e = first + v;
+            if (key > a && (!GROUPS || ((stay >> min((first + place<P>(v)) / size, kWave - 1)) & 1ull) != 0ull)) a = key, e = first + place<P>(v);
         }
         best_over_token<L>(a, e);
         if (in == j && a > -INFINITY) chosen = e;
-        if (e >= first && e < first + V) keys[(e - first) * kWave] = -INFINITY;
+        const int off = e - first, slot = off / P * 4 + off % P;
+        if (off >= 0 && off % P < 4 && slot < V) keys[slot * kWave] = -INFINITY;
     }
     return chosen;
 }
@@ -363,17 +375,17 @@ struct GroupParts {
 };
 
 // The logits of the token's lanes as they lie in a row, at `mine`, for all of them.
-template <int V, int L>
+template <int V, int P, int L>
 __device__ __forceinline__ void share_logits(const float (&l)[V], float* token, int first)
 {
     lds_in_order();
 #pragma unroll
-    for (int v = 0; v < V; ++v) token[first + v] = l[v];
+    for (int v = 0; v < V; ++v) token[first + place<P>(v)] = l[v];
     lds_in_order();
 }
 
 // Score and key of a logit in 64 bits; -inf: out.
-template <int V, int L, bool SIGMOID, bool SCORES>
+template <int V, int P, int L, bool SIGMOID, bool SCORES>
 struct ExactKeys {
     const float* bias;
     float base;
@@ -383,7 +395,7 @@ struct ExactKeys {
         if constexpr (SCORES && !SIGMOID) {
 #pragma unroll 1
             for (int v = 0; v < V; ++v) {
-                const float x = token[first + v];
+                const float x = token[first + place<P>(v)];
                 sum += x > -INFINITY ? exp(static_cast<double>(x) - base) : 0.0;
             }
             sum = token_sum64<L>(sum);
@@ -398,12 +410,12 @@ struct ExactKeys {
 };
 
 // Whether this lane's group (by parts) stays, by values in 64 bits.
-template <int V, int L, bool SIGMOID, bool SCORES>
+template <int V, int P, int L, bool SIGMOID, bool SCORES>
 __device__ __forceinline__ bool group_stays_exactly(const float* bias, const float* token, int E, int groups, int top_groups, int group_best, float base)
 {
     const int in = lane_id() % L, first = in * V;
     const GroupParts<L> g(E, groups, in);
-    const ExactKeys<V, L, SIGMOID, SCORES> keys(bias, token, first, base);
+    const ExactKeys<V, P, L, SIGMOID, SCORES> keys(bias, token, first, base);
     double a = -INFINITY, b = -INFINITY;
 #pragma unroll 1
     for (int e = g.begin; e < g.end; ++e) {
@@ -430,11 +442,11 @@ __device__ __forceinline__ bool group_stays_exactly(const float* bias, const flo
 __device__ __forceinline__ int id_of(uint32_t n) { return (1 << kIdBits) - 1 - static_cast<int>(n & ((1u << kIdBits) - 1u)); }
 
 // Candidates, one a lane (0: none), in the order of their keys in 64 bits.
-template <int V, int L, bool SIGMOID, bool SCORES>
-__device__ __forceinline__ uint32_t order_exactly(const float* bias, float* token, uint32_t mine, float base)
+template <int V, int P, int L, bool SIGMOID, bool SCORES>
+__device__ __forceinline__ uint32_t order_exactly(const float* bias, float* token, uint32_t mine, int first, float base)
 {
     const int in = lane_id() % L, from = lane_id() & ~(L - 1), e = id_of(mine);
-    const ExactKeys<V, L, SIGMOID, SCORES> keys(bias, token, in * V, base);
+    const ExactKeys<V, P, L, SIGMOID, SCORES> keys(bias, token, first, base);
     const double exact = mine != 0u ? keys.key(token[mine != 0u ? e : 0], e) : -INFINITY;
     int ahead = 0;
 #pragma unroll 4
@@ -454,18 +466,18 @@ __device__ __forceinline__ uint32_t order_exactly(const float* bias, float* toke
     return mine;
 }
 
-template <int V>
+template <int V, int P>
 __device__ __forceinline__ void load_bias(const RouteCall& p, int first, float (&bias)[V])
 {
 #pragma unroll
     for (int v = 0; v < V; ++v) bias[v] = 0.0f;
     if (p.bias == nullptr) return;
 #pragma unroll
-    for (int v = 0; v < V; ++v) bias[v] = p.bias[min(first + v, p.E - 1)];
+    for (int v = 0; v < V; ++v) bias[v] = p.bias[min(first + place<P>(v), p.E - 1)];
 }
 
 // `token`: room for the token's logits in LDS.  sure: whether the lane's part of the choice is the definition's.
-template <int V, int L, bool BF16, bool SIGMOID, bool SCORES, bool GROUPS>
+template <int V, int P, int L, bool BF16, bool SIGMOID, bool SCORES, bool GROUPS>
 __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void* row, float (&l)[V], float (&bias)[V], float* token, int first, int in, float base,
                                                  float inverse, bool& sure)
 {
@@ -533,7 +545,7 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
             uint32_t* classes = reinterpret_cast<uint32_t*>(token);
             lds_in_order();
 #pragma unroll
-            for (int v = 0; v < V; ++v) classes[first + v] = key[v];
+            for (int v = 0; v < V; ++v) classes[first + place<P>(v)] = key[v];
             lds_in_order();
 #pragma unroll 4
             for (int e = g.begin; e < g.end; ++e) {
@@ -561,12 +573,12 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         if (p.group_best == 2 && b <= 1u && a != 0u) certain = false;
         bool by_parts = !aligned;
         if (!(BF16 && !SCORES) && __ballot(!certain) != 0ull) {
-            share_logits<V, L>(l, token, first);
-            stays = group_stays_exactly<V, L, SIGMOID, SCORES>(p.bias, token, p.E, p.groups, p.top_groups, p.group_best, base);
+            share_logits<V, P, L>(l, token, first);
+            stays = group_stays_exactly<V, P, L, SIGMOID, SCORES>(p.bias, token, p.E, p.groups, p.top_groups, p.group_best, base);
             by_parts = true;
             // (Classes and what they are made from are formed again, for what is rarely needed: held meanwhile, they cost registers always.)
-            load_row<V, BF16>(row, first, p.E, -INFINITY, l);
-            if constexpr (SCORES) load_bias<V>(p, first, bias), classes_of_scores();
+            load_row<V, P, BF16>(row, first, p.E, -INFINITY, l);
+            if constexpr (SCORES) load_bias<V, P>(p, first, bias), classes_of_scores();
             else classes_of_logits();
         }
         stay = __ballot(stays) >> (lane_id() & ~(L - 1));
@@ -590,7 +602,7 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
             }
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = key[v] != 0u ? key[v] << kIdBits | static_cast<uint32_t>((1 << kIdBits) - 1 - first - v) : 0u;
+        for (int v = 0; v < V; ++v) key[v] = key[v] != 0u ? key[v] << kIdBits | static_cast<uint32_t>((1 << kIdBits) - 1 - first - place<P>(v)) : 0u;
         sort_keys<V>(key);
     };
     uint32_t mine = 0u, next = 0u;
@@ -617,8 +629,8 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         // Neighbours that classes do not tell apart: the L best by class, a lane each, put in order by their keys in 64 bits.  The k best are among them if the
         // last one is clearly behind the k-th, or there are no more.
         const uint32_t behind_all = next;
-        load_row<V, BF16>(row, first, p.E, -INFINITY, l);
-        if constexpr (SCORES) load_bias<V>(p, first, bias);
+        load_row<V, P, BF16>(row, first, p.E, -INFINITY, l);
+        if constexpr (SCORES) load_bias<V, P>(p, first, bias);
         if (SCORES && p.bias != nullptr) classes_of_scores();
         else classes_of_logits();
         number();
@@ -629,8 +641,8 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         const uint32_t end = static_cast<uint32_t>(__shfl(static_cast<int>(mine), from + L - 1, kWave)) >> kIdBits;
         const uint32_t behind = p.k == L ? behind_all >> kIdBits : end;
         sure = behind == 0u || kth == 0u || (static_cast<float>(kth) - static_cast<float>(behind) > apart && kth > 1u);
-        share_logits<V, L>(l, token, first);
-        mine = order_exactly<V, L, SIGMOID, SCORES>(p.bias, token, mine, base);
+        share_logits<V, P, L>(l, token, first);
+        mine = order_exactly<V, P, L, SIGMOID, SCORES>(p.bias, token, mine, first, base);
     }
     return in < p.k && mine != 0u ? id_of(mine) : -1;
 }
@@ -639,7 +651,8 @@ template <int V, int L, bool BF16, bool SIGMOID, bool SCORES, bool GROUPS>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
 {
     __shared__ double keys[V * kRouteThreads];  // of the exact choice, or a token's logits or classes
-    const int in = lane_id() % L, first = in * V;
+    constexpr int P = GROUPS ? 4 : 4 * L;
+    const int in = lane_id() % L, first = in * (GROUPS ? V : 4);
     constexpr int kTokens = kRouteThreads / L;
     const bool by_classes = !GROUPS || p.groups <= L;
     double* mine_in_lds = keys + threadIdx.x / kWave * (V * kWave);
@@ -651,8 +664,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
     const int64_t row = min(t, p.T - 1);
     const void* at = row_at<BF16>(p.logits, row * p.E);
     float l[V], bias[V];
-    load_row<V, BF16>(at, first, p.E, -INFINITY, l);
-    if constexpr (SCORES) load_bias<V>(p, first, bias);
+    load_row<V, P, BF16>(at, first, p.E, -INFINITY, l);
+    if constexpr (SCORES) load_bias<V, P>(p, first, bias);
     float most = -INFINITY;
     uint32_t bits = 0u;
 #pragma unroll
@@ -675,17 +688,17 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
         float s[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) s[v] = SIGMOID ? sigmoid(l[v]) : (most == -INFINITY ? 0.0f : exp_below(l[v] - base) * inverse);
-        store_row<V, false>(p.scores + row * p.E, first, p.E, s);
+        store_row<V, P, false>(p.scores + row * p.E, first, p.E, s);
     }
     int chosen = -1;
     bool sure = false;
-    if (by_classes) chosen = choose_by_classes<V, L, BF16, SIGMOID, SCORES, GROUPS>(p, at, l, bias, token, first, in, base, inverse, sure);
+    if (by_classes) chosen = choose_by_classes<V, P, L, BF16, SIGMOID, SCORES, GROUPS>(p, at, l, bias, token, first, in, base, inverse, sure);
     if ((GROUPS || !(BF16 && !SCORES)) && __ballot(!sure) != 0ull) {
-        load_row<V, BF16>(at, first, p.E, -INFINITY, l);
+        load_row<V, P, BF16>(at, first, p.E, -INFINITY, l);
         lds_in_order();  // (the place held the tokens' logits)
 #pragma unroll
         for (int v = 0; v < V; ++v) mine_in_lds[v * kWave + lane_id()] = l[v];
-        chosen = choose_exactly<V, L, SIGMOID, SCORES, GROUPS>(p, mine_in_lds + lane_id(), first, in, base);
+        chosen = choose_exactly<V, P, L, SIGMOID, SCORES, GROUPS>(p, mine_in_lds + lane_id(), first, in, base);
     }
     const bool live = chosen >= 0;
     const float mine = live ? load_logit<BF16>(at, chosen) : -INFINITY;
@@ -707,6 +720,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
 template <int V, int L, bool BF16, bool SIGMOID>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteGradient p)
 {
+    __shared__ __attribute__((aligned(16))) float changes[V * kRouteThreads];
     const int lane = lane_id(), in = lane % L;
     constexpr int kTokens = kRouteThreads / L;
     const int64_t t0 = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kTokens;
@@ -715,7 +729,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
     const bool there = t < p.T;
     const int64_t row = min(t, p.T - 1);
     const void* at = row_at<BF16>(p.logits, row * p.E);
-    const int first = in * V;
+    constexpr int P = 4 * L;
+    const int first = in * 4;
     const bool renormalize = p.renormalize && p.k > 1;
     const int e = in < p.k ? p.idx[row * p.k + in] : -1;
     const bool live = e >= 0 && e < p.E;
@@ -728,10 +743,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
     float l[V], d[V];
     const bool all = p.dscores != nullptr || (!SIGMOID && !renormalize);
     if (all) {
-        load_row<V, BF16>(at, first, p.E, -INFINITY, l);
+        load_row<V, P, BF16>(at, first, p.E, -INFINITY, l);
 #pragma unroll
         for (int v = 0; v < V; ++v) d[v] = 0.0f;
-        if (p.dscores != nullptr) load_row<V, false>(p.dscores + row * p.dscores_stride, first, p.E, 0.0f, d);
+        if (p.dscores != nullptr) load_row<V, P, false>(p.dscores + row * p.dscores_stride, first, p.E, 0.0f, d);
         if constexpr (!SIGMOID) {
             most = l[0];
 #pragma unroll
@@ -746,9 +761,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
             }
             sum = token_sum<L>(sum);
             if (sum == 0.0f) sum = 1.0f;
+            const float inverse = 1.0f / sum;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                l[v] /= sum;
+                l[v] *= inverse;
                 less += l[v] != 0.0f ? l[v] * d[v] : 0.0f;  // (a score of a masked expert, whatever its gradient)
             }
             less = token_sum<L>(less);
@@ -760,7 +776,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
         change = p.scale * u * (g - mean);
         if constexpr (SIGMOID) change *= sigmoid(-mine);
     } else if constexpr (SIGMOID) {
-        change = p.scale * g * sigmoid(mine) * sigmoid(-mine);
+        change = p.scale * g * sigmoid_slope(mine);
     } else {
         change = p.scale * g * (expf(mine - most) / sum);
         less += token_sum<L>(change);
@@ -769,18 +785,30 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
     if (all) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float slope = SIGMOID ? sigmoid(l[v]) * sigmoid(-l[v]) : l[v];
+            const float slope = SIGMOID ? sigmoid_slope(l[v]) : l[v];
             out[v] = slope != 0.0f ? slope * (SIGMOID ? d[v] : d[v] - less) : 0.0f;
         }
     }
+    // An expert's changes, in the order of the slots; each in its place of the row in LDS, from where the expert's lane takes it.
+    float mine_all = 0.0f;
+    const int id = live ? e : -1;
     for (int j = 0; j < p.k; ++j) {
-        const int ej = __shfl(live ? e : -1, (lane & ~(L - 1)) + j, kWave);
-        const float cj = __shfl(change, (lane & ~(L - 1)) + j, kWave);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (first + v == ej) out[v] += cj;
+        const int other = __shfl(id, (lane & ~(L - 1)) + j, kWave);
+        const float c = __shfl(change, (lane & ~(L - 1)) + j, kWave);
+        mine_all += other == id ? c : 0.0f;
     }
-    if (there) store_row<V, BF16>(static_cast<uint8_t*>(p.dlogits) + row * p.E * (BF16 ? 2 : 4), first, p.E, out);
+    float* token = changes + threadIdx.x / L * (L * V);
+#pragma unroll
+    for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(token + first + place<P>(v)) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    lds_in_order();
+    if (live) token[e] = mine_all;
+    lds_in_order();
+#pragma unroll
+    for (int v = 0; v < V; v += 4) {
+        const float4 c = *reinterpret_cast<const float4*>(token + first + place<P>(v));
+        out[v] += c.x, out[v + 1] += c.y, out[v + 2] += c.z, out[v + 3] += c.w;
+    }
+    if (there) store_row<V, P, BF16>(static_cast<uint8_t*>(p.dlogits) + row * p.E * (BF16 ? 2 : 4), first, p.E, out);
 }
 
 // Calls run(V, L, type, score) with the instance for E experts.
