@@ -135,6 +135,147 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const CombineGrad
         }
 }
 
+// Rows of more than 32 pieces: a token a wavefront, or `waves` (1, 2, 4) of them a token, which share its columns: a row is read at one time.  Its positions and weights are fetched by a lane each and handed out on the scalar path, those of the
+// wavefront's next token while this one's rows travel, and U pieces a lane of every row are in flight.
+constexpr int kRowsPieces = 2;
+
+struct Assigned {  // what lane j has of slot j
+    int at;
+    float w;
+};
+__device__ __forceinline__ Assigned assigned(const int32_t* position, const float* w, int64_t t, int64_t T, int k, int64_t A, int lane)
+{
+    Assigned r{-1, 1.0f};
+    if (t < T && lane < k) {
+        const int64_t s = position[t * k + lane];
+        r.at = s < A ? static_cast<int>(s) : -1;
+        if (w != nullptr) r.w = w[t * k + lane];
+    }
+    return r;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void combine_wave_kernel(const CombineCall p, int waves)
+{
+    constexpr int N = BF16 ? 8 : 4, U = kRowsPieces;
+    const int lane = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), share = wave & (waves - 1), tokens = 4 / waves;
+    const int64_t A = p.T * p.k, step = static_cast<int64_t>(gridDim.x) * tokens;
+    int64_t t = static_cast<int64_t>(blockIdx.x) * tokens + wave / waves;
+    Assigned next = assigned(p.position, p.w, t, p.T, p.k, A, lane);
+    for (; t < p.T; t += step) {
+        const Assigned mine = next;
+        next = assigned(p.position, p.w, t + step, p.T, p.k, A, lane);
+        for (int c0 = share * kWave * U + lane; c0 < p.vecs; c0 += waves * kWave * U) {
+            Piece<BF16> sum[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[u].v[i] = 0.0f;
+            for (int j0 = 0; j0 < p.k; j0 += kRowsAhead) {
+                uint4 v[kRowsAhead][U];
+#pragma unroll
+                for (int j = 0; j < kRowsAhead; ++j) {
+                    const int s = wave_read_lane(mine.at, j0 + j);  // (-1 past the last slot)
+                    const uint4* row = p.y + static_cast<int64_t>(max(s, 0)) * p.vecs;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        v[j][u] = make_uint4(0u, 0u, 0u, 0u);
+                        if (s >= 0 && c0 + u * kWave < p.vecs) v[j][u] = load_stream16(row + (c0 + u * kWave));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kRowsAhead; ++j) {
+                    const bool there = wave_read_lane(mine.at, j0 + j) >= 0;
+                    const float w = there ? __int_as_float(wave_read_lane(__float_as_int(mine.w), j0 + j)) : 0.0f;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const Piece<BF16> r = unpack<BF16>(v[j][u]);
+#pragma unroll
+                        for (int i = 0; i < N; ++i) sum[u].v[i] = fmaf(w, r.v[i], sum[u].v[i]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c0 + u * kWave < p.vecs) store_stream16(p.out + t * p.vecs + c0 + u * kWave, pack<BF16>(sum[u]));
+        }
+    }
+}
+
+// Gradients: the wavefronts of a token join their sums through LDS, in order.
+template <bool BF16>
+__global__ __launch_bounds__(256) void combine_backward_wave_kernel(const CombineGradient p, int waves)
+{
+    __shared__ float part[4][kRowsAhead];
+    constexpr int N = BF16 ? 8 : 4;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), share = wave & (waves - 1);
+    const int64_t A = p.T * p.k, tokens = 4 / waves, step = static_cast<int64_t>(gridDim.x) * tokens;
+    int64_t t = static_cast<int64_t>(blockIdx.x) * tokens + wave / waves;
+    Assigned next = assigned(p.position, p.w, t, p.T, p.k, A, lane);
+    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * tokens; t0 < p.T; t0 += step, t += step) {  // (the same number of times for all wavefronts)
+        const Assigned mine = next;
+        next = assigned(p.position, p.w, t + step, p.T, p.k, A, lane);
+        const int vecs = t < p.T ? p.vecs : 0;
+        for (int j0 = 0; j0 < p.k; j0 += kRowsAhead) {
+            float dot[kRowsAhead];
+#pragma unroll
+            for (int j = 0; j < kRowsAhead; ++j) dot[j] = 0.0f;
+            for (int c = share * kWave + lane; c < vecs; c += waves * kWave) {
+                const uint4 g4 = p.dout[t * p.vecs + c];
+                uint4 v[kRowsAhead];
+                if (p.dw != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < kRowsAhead; ++j) {
+                        const int s = wave_read_lane(mine.at, j0 + j);
+                        v[j] = make_uint4(0u, 0u, 0u, 0u);
+                        if (s >= 0) v[j] = load_stream16(p.y + static_cast<int64_t>(s) * p.vecs + c);
+                    }
+                }
+                const Piece<BF16> g = unpack<BF16>(g4);
+                if (p.dy != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < kRowsAhead; ++j) {
+                        const int s = wave_read_lane(mine.at, j0 + j);
+                        if (s < 0) continue;
+                        const float w = __int_as_float(wave_read_lane(__float_as_int(mine.w), j0 + j));
+                        Piece<BF16> r;
+#pragma unroll
+                        for (int i = 0; i < N; ++i) r.v[i] = w * g.v[i];
+                        store_stream16(p.dy + static_cast<int64_t>(s) * p.vecs + c, pack<BF16>(r));
+                    }
+                }
+                if (p.dw != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < kRowsAhead; ++j) {
+                        if (wave_read_lane(mine.at, j0 + j) < 0) continue;
+                        const Piece<BF16> r = unpack<BF16>(v[j]);
+#pragma unroll
+                        for (int i = 0; i < N; ++i) dot[j] = fmaf(g.v[i], r.v[i], dot[j]);
+                    }
+                }
+            }
+            if (p.dw == nullptr) continue;
+            float all = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kRowsAhead; ++j) {
+                const float sum = wave_sum(dot[j]);
+                all = lane == j ? sum : all;
+            }
+            if (waves > 1) {
+                if (lane < kRowsAhead) part[wave][lane] = all;
+                __syncthreads();
+                if (lane < kRowsAhead) {
+                    all = part[wave - share][lane] + part[wave - share + 1][lane];
+                    if (waves == 4) all += part[2][lane] + part[3][lane];
+                }
+                __syncthreads();
+            }
+            if (t < p.T && share == 0 && lane < kRowsAhead && j0 + lane < p.k) p.dw[t * p.k + j0 + lane] = all;
+        }
+    }
+}
+
 static int check_rows(const char* fn, int64_t T, int d, int k, int dt)
 {
     if (dt != EXF_F32 && dt != EXF_BF16) return fail(EXF_ERR_BAD_DTYPE, "%s: dt = %d", fn, dt);
@@ -180,7 +321,12 @@ extern "C" int moe_combine_topk(const void* y_sorted, const int32_t* sorted_of_s
     const CombineCall p{static_cast<const uint4*>(y_sorted), sorted_of_src, topk_w, static_cast<uint4*>(out), T, k, vecs, lanes};
     const dim3 grid(rows_grid(T, lanes));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dt == EXF_BF16) hipLaunchKernelGGL(combine_topk_kernel<true>, grid, dim3(256), 0, s, p);
+    // Rows of 4 KiB of 16384 x 8 assignments 105 us with one wavefront a token and with two, of 8192 x 8 56 and 52, of 8 KiB of 8192 x 2 42 and 37, of 1 KiB of 65536 x 4
+    // 64 and 82; of 4 KiB of 333 x 6 6.1, 4.9 and with four 4.0.
+    const int waves = vecs <= 2 * kWave ? 1 : (T < 1024 ? 4 : 2);
+    if (lanes == kWave && dt == EXF_BF16) hipLaunchKernelGGL(combine_wave_kernel<true>, dim3(rows_grid(T, lanes * waves)), dim3(256), 0, s, p, waves);
+    else if (lanes == kWave) hipLaunchKernelGGL(combine_wave_kernel<false>, dim3(rows_grid(T, lanes * waves)), dim3(256), 0, s, p, waves);
+    else if (dt == EXF_BF16) hipLaunchKernelGGL(combine_topk_kernel<true>, grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(combine_topk_kernel<false>, grid, dim3(256), 0, s, p);
     return check_launch(fn);
 }
@@ -216,7 +362,12 @@ extern "C" int moe_combine_backward(const void* dout, const void* y_sorted, cons
                             T, k, vecs, lanes};
     const dim3 grid(rows_grid(T, lanes));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dt == EXF_BF16) hipLaunchKernelGGL(combine_backward_kernel<true>, grid, dim3(256), 0, s, p);
+    // Rows of 4 KiB of 8192 x 8 assignments 119 us with one wavefront a token, 109 with two, 104 with four; of 8 KiB of 8192 x 2 67, 61 and 56; of 1 KiB of 65536 x 4 103, 111
+    // and 155; of 2 KiB of 129 x 3 6.2, 5.1 and 4.2.
+    const int waves = vecs > 2 * kWave ? 4 : (vecs > kWave ? 2 : 1);
+    if (lanes == kWave && dt == EXF_BF16) hipLaunchKernelGGL(combine_backward_wave_kernel<true>, dim3(rows_grid(T, lanes * waves)), dim3(256), 0, s, p, waves);
+    else if (lanes == kWave) hipLaunchKernelGGL(combine_backward_wave_kernel<false>, dim3(rows_grid(T, lanes * waves)), dim3(256), 0, s, p, waves);
+    else if (dt == EXF_BF16) hipLaunchKernelGGL(combine_backward_kernel<true>, grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(combine_backward_kernel<false>, grid, dim3(256), 0, s, p);
     return check_launch(fn);
 }
