@@ -309,15 +309,22 @@ def moe_combine(y_sorted, sorted_of_src, topk_w, out=None):
     return out
 
 
+def _rows(T, width, dtype, device):
+    """A new dense [T, width] (torch.empty takes a microsecond more)."""
+    return torch.empty_strided((T, width), (width, 1), dtype=dtype, device=device)
+
+
 def _combine_rows(name, y_sorted, sorted_of_src, topk_w, k, out):
     if y_sorted.requires_grad or topk_w is not None and topk_w.requires_grad:
         _untracked(name, "moe_combine_backward" if name == "moe_combine" else "moe_dispatch")
-    T, A, d, code, dev = _assigned(y_sorted, sorted_of_src, k)
-    dt = y_sorted.dtype
-    out = torch.empty((T, d), dtype=dt, device=y_sorted.device) if out is None else _expect("out", out, (T, d), dt, dev)
-    _expect("the sorted rows", y_sorted, (A, d), dt, dev)
+    T, A, d, dt, code, dev = _assigned(y_sorted, sorted_of_src, k)
+    if out is None:
+        out = _rows(T, d, dt, y_sorted.device)
+    if not (y_sorted.shape[0] == A and out.shape == (T, d) and out.dtype is dt and y_sorted.is_contiguous() and out.is_contiguous() and out.get_device() == dev >= 0):
+        _expect("out", out, (T, d), dt, dev)
+        _expect("the sorted rows", y_sorted, (A, d), dt, dev)
     if topk_w is not None:
-        topk_w = _expect("topk_w", topk_w, (T, k), torch.float32, dev).data_ptr()
+        topk_w = _expect("topk_w", topk_w, (T, k), _FLOAT, dev).data_ptr()
     if dev < 0:
         _on_host()
     rc = lib().moe_combine_topk(y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w, T, d, k, code, out.data_ptr(), _stream())
@@ -327,17 +334,19 @@ def _combine_rows(name, y_sorted, sorted_of_src, topk_w, k, out):
 
 
 def _assigned(rows, sorted_of_src, k):
-    """(T, T*k, d, type's code, device number) of sorted rows and the positions of T tokens' k assignments."""
-    if len(rows.shape) != 2 or len(sorted_of_src.shape) not in (1, 2):
-        _bad(f"sorted rows are [T*k,d] and positions [T*k], got {tuple(rows.shape)} and {tuple(sorted_of_src.shape)}")
-    A, dev = sorted_of_src.numel(), rows.get_device()
-    if k < 1 or A % k or len(sorted_of_src.shape) == 2 and sorted_of_src.shape[1] != k:
-        _bad(f"positions of k = {k} assignments a token expected, got {tuple(sorted_of_src.shape)}")
-    code = _CODES.get(rows.dtype)
+    """(T, T*k, d, type, its code, device number) of sorted rows and the positions of T tokens' k assignments."""
+    shape, at = rows.shape, sorted_of_src.shape
+    if len(shape) != 2 or len(at) not in (1, 2):
+        _bad(f"sorted rows are [T*k,d] and positions [T*k], got {tuple(shape)} and {tuple(at)}")
+    A, dev, dt = sorted_of_src.numel(), rows.get_device(), rows.dtype
+    if k < 1 or A % k or len(at) == 2 and at[1] != k:
+        _bad(f"positions of k = {k} assignments a token expected, got {tuple(at)}")
+    code = _CODES.get(dt)
     if code is None:
-        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {rows.dtype}")
-    _expect("sorted_of_src", sorted_of_src, sorted_of_src.shape, _INT32, dev)
-    return A // k, A, rows.shape[1], code, dev
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
+    if not (sorted_of_src.dtype is _INT32 and sorted_of_src.is_contiguous() and sorted_of_src.get_device() == dev):
+        _expect("sorted_of_src", sorted_of_src, at, _INT32, dev)
+    return A // k, A, shape[1], dt, code, dev
 
 
 def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, want_weights=True, out=None, out_weights=None):
@@ -348,19 +357,20 @@ def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, 
     if len(topk_w.shape) != 2:
         _bad(f"topk_w is [T,k], got {tuple(topk_w.shape)}")
     k = topk_w.shape[1]
-    T, A, d, code, dev = _assigned(y_sorted, sorted_of_src, k)
-    dt = y_sorted.dtype
-    _expect("dout", dout, (T, d), dt, dev)
-    _expect("y_sorted", y_sorted, (A, d), dt, dev)
-    _expect("topk_w", topk_w, (T, k), torch.float32, dev)
+    T, A, d, dt, code, dev = _assigned(y_sorted, sorted_of_src, k)
+    if not (dout.shape == (T, d) and y_sorted.shape[0] == A and topk_w.shape[0] == T and dout.dtype is dt and topk_w.dtype is _FLOAT and dout.is_contiguous()
+            and y_sorted.is_contiguous() and topk_w.is_contiguous() and dout.get_device() == topk_w.get_device() == dev):
+        _expect("dout", dout, (T, d), dt, dev)
+        _expect("y_sorted", y_sorted, (A, d), dt, dev)
+        _expect("topk_w", topk_w, (T, k), _FLOAT, dev)
     if out is not None:
         _expect("out", out, (A, d), dt, dev)
     elif want_rows:
         out = torch.zeros((A, d), dtype=dt, device=dout.device)
     if out_weights is not None:
-        _expect("out_weights", out_weights, (T, k), torch.float32, dev)
+        _expect("out_weights", out_weights, (T, k), _FLOAT, dev)
     elif want_weights:
-        out_weights = torch.empty((T, k), dtype=torch.float32, device=dout.device)
+        out_weights = _rows(T, k, _FLOAT, dout.device)
     if dev < 0:
         _on_host()
     rc = lib().moe_combine_backward(dout.data_ptr(), y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w.data_ptr(), T, d, k, code, _ptr(out), _ptr(out_weights),
@@ -386,16 +396,19 @@ def moe_route(logits, k, bias=None, score=EXF_SCORE_SOFTMAX, renormalize=False, 
         _bad(f"logits: contiguous [T,E] expected, got {tuple(shape)}")
     T, E = shape
     if bias is not None:
-        bias = _expect("bias", bias, (E,), torch.float32, dev).data_ptr()
+        bias = _expect("bias", bias, (E,), _FLOAT, dev).data_ptr()
     if dev < 0:
         _on_host()
     if out is None:
-        idx, w = torch.empty((T, k), dtype=_INT32, device=logits.device), torch.empty((T, k), dtype=torch.float32, device=logits.device)
+        if k < 1:
+            _bad(f"k = {k}")
+        device = logits.device
+        idx, w = _rows(T, k, _INT32, device), _rows(T, k, _FLOAT, device)
     else:
         idx, w = out
         _expect("topk_idx", idx, (T, k), _INT32, dev)
-        _expect("topk_w", w, (T, k), torch.float32, dev)
-    scores = torch.empty((T, E), dtype=torch.float32, device=logits.device) if want_scores else None
+        _expect("topk_w", w, (T, k), _FLOAT, dev)
+    scores = _rows(T, E, _FLOAT, logits.device) if want_scores else None
     rc = lib().moe_route(logits.data_ptr(), bias, T, E, k, score, groups, groups if top_groups is None else top_groups, group_best, 1 if renormalize else 0, scale, code,
                          idx.data_ptr(), w.data_ptr(), _ptr(scores), _stream())
     if rc:
@@ -415,12 +428,14 @@ def moe_route_backward(dtopk_w, logits, topk_idx, score=EXF_SCORE_SOFTMAX, renor
         _bad(f"logits: contiguous [T,E] expected, topk_idx [T,k], got {tuple(shape)} and {tuple(topk_idx.shape)}")
     T, E = shape
     k, stride, at = topk_idx.shape[1], 0, None
-    _expect("dtopk_w", dtopk_w, (T, k), torch.float32, dev)
-    _expect("topk_idx", topk_idx, (T, k), _INT32, dev)
+    if not (topk_idx.shape[0] == T and dtopk_w.shape == topk_idx.shape and topk_idx.dtype is _INT32 and dtopk_w.dtype is _FLOAT and topk_idx.is_contiguous()
+            and dtopk_w.is_contiguous() and topk_idx.get_device() == dtopk_w.get_device() == dev):
+        _expect("topk_idx", topk_idx, (T, k), _INT32, dev)
+        _expect("dtopk_w", dtopk_w, (T, k), _FLOAT, dev)
     if dscores is not None:
         stride = E if len(dscores.shape) == 2 else 0
-        at = _expect("dscores", dscores, (T, E) if stride else (E,), torch.float32, dev).data_ptr()
-    out = torch.empty(shape, dtype=dt, device=logits.device) if out is None else _expect("out", out, shape, dt, dev)
+        at = _expect("dscores", dscores, (T, E) if stride else (E,), _FLOAT, dev).data_ptr()
+    out = _rows(T, E, dt, logits.device) if out is None else _expect("out", out, shape, dt, dev)
     if dev < 0:
         _on_host()
     rc = lib().moe_route_backward(dtopk_w.data_ptr(), logits.data_ptr(), topk_idx.data_ptr(), at, stride, T, E, k, score, 1 if renormalize else 0, scale, code,
@@ -431,6 +446,7 @@ def moe_route_backward(dtopk_w, logits, topk_idx, score=EXF_SCORE_SOFTMAX, renor
 
 
 _CODES = {torch.float32: EXF_F32, torch.bfloat16: EXF_BF16}
+_FLOAT = torch.float32
 
 
 def _bad(message: str):
@@ -700,16 +716,18 @@ def _expect_q4(name, m, shape, dtype, dev):
     q, scale, zero = m.q, m.scale, m.zero
     if not len(shape) or not len(scale.shape) or not scale.shape[-1]:
         _bad(f"{name} has no groups")
-    groups = (*shape[:-1], scale.shape[-1])
-    if shape[-1] % groups[-1]:
-        _bad(f"{name}: rows of {shape[-1]} in {groups[-1]} groups")
-    if not (q.shape == (*shape[:-1], shape[-1] // 2) and scale.shape == groups and q.dtype is _UINT8 and scale.dtype is dtype and q.is_contiguous() and scale.is_contiguous()
-            and q.get_device() == scale.get_device() == dev):
-        _expect(f"{name}.q", q, (*shape[:-1], shape[-1] // 2), _UINT8, dev)
+    k, n = shape[-1], scale.shape[-1]
+    if k % n:
+        _bad(f"{name}: rows of {k} in {n} groups")
+    groups = (*shape[:-1], n)
+    if not (q.shape == (*shape[:-1], k // 2) and scale.shape == groups and q.dtype is _UINT8 and scale.dtype is dtype and q.is_contiguous() and scale.is_contiguous()
+            and q.get_device() == scale.get_device() == dev
+            and (zero is None or zero.shape == groups and zero.dtype is _UINT8 and zero.is_contiguous() and zero.get_device() == dev)):
+        _expect(f"{name}.q", q, (*shape[:-1], k // 2), _UINT8, dev)
         _expect(f"{name}.scale", scale, groups, dtype, dev)
-    if zero is not None:
-        _expect(f"{name}.zero", zero, groups, _UINT8, dev)
-    return shape[-1] // groups[-1]
+        if zero is not None:
+            _expect(f"{name}.zero", zero, groups, _UINT8, dev)
+    return k // n
 
 
 def q4_quantize(x, group=128, symmetric=False, out=None):
@@ -755,17 +773,24 @@ def moe_grouped_product_q4(x_sorted, expert_offsets, w, bias=None, out=None):
     """moe_grouped_product with weights in 4-bit integers: w a Q4 [E_local,n,k] with scales of the rows' type."""
     if x_sorted.requires_grad or bias is not None and bias.requires_grad or w.scale.requires_grad:
         _untracked("moe_grouped_product_q4", "none: weights in 4 bits are not trained")
-    if len(w.q.shape) != 3:
-        _bad(f"weights are [E_local,n,k], got {w.shape}")
-    E, n, k, A, dt, code, dev = _grouped(x_sorted, w.shape)
+    q, scale, zero, shape = w.q, w.scale, w.zero, w.q.shape
+    if len(shape) != 3 or len(x_sorted.shape) != 2:
+        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {w.shape}")
+    E, n, k = shape
+    k *= 2
+    A, dt, dev = x_sorted.shape[0], x_sorted.dtype, x_sorted.get_device()
+    code = _CODES.get(dt)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
     group = _expect_q4("w", w, (E, n, k), dt, dev)
     if out is None:
-        out = torch.empty((A, n), dtype=dt, device=x_sorted.device)
+        out = _rows(A, n, dt, x_sorted.device)
     if bias is not None:
         bias = _expect("bias", bias, (E, n), dt, dev).data_ptr()
-    if not _fits(x_sorted, k, expert_offsets, E, w.scale, out, (A, n), dt, dev):
-        _misfit(x_sorted, (A, k), expert_offsets, E, w.scale, out, (A, n), dt, dev)
-    rc = lib().moe_grouped_product_q4(x_sorted.data_ptr(), expert_offsets.data_ptr(), w.q.data_ptr(), w.scale.data_ptr(), _ptr(w.zero), bias, A, n, k, group, E, code,
+    if not (x_sorted.shape[1] == k and expert_offsets.shape == (E + 1,) and out.shape == (A, n) and out.dtype is dt and expert_offsets.dtype is _INT32
+            and x_sorted.is_contiguous() and out.is_contiguous() and expert_offsets.is_contiguous() and out.get_device() == expert_offsets.get_device() == dev >= 0):
+        _misfit(x_sorted, (A, k), expert_offsets, E, scale, out, (A, n), dt, dev)
+    rc = lib().moe_grouped_product_q4(x_sorted.data_ptr(), expert_offsets.data_ptr(), q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), bias, A, n, k, group, E, code,
                                       out.data_ptr(), _stream())
     if rc:
         _check(rc)
