@@ -4,14 +4,14 @@
 // an access of its own to the L1, 64 a load, and the L1 is the bound.  Copied to LDS first, in units of 256 elements - 128 bytes of a column, 512 of a row -
 // neighbouring lanes fetch what lies together, and a load of a wavefront is 16 accesses.  Pieces of 16 bytes trade places inside a column's (row's) part of a
 // unit so that the 16 lanes that read one piece each of 16 columns (rows) meet all banks once.
-//   A workgroup has 16 R rows and 4 x 16 C columns of an expert, a wavefront all rows and 16 C of the columns, with a ring of D units of codes, scales and
-// zero points of its own; the rows' ring is shared, each wavefront copies a quarter.  One barrier a unit: behind it the unit is there for all, and the slot of
-// the unit before is free.
+//   A workgroup has 16 R rows and 4 x 16 C columns of an expert, a wavefront all rows and 16 C of the columns, with two slots of codes, scales and
+// zero points of its own; the rows' two are shared, each wavefront copies a quarter of the rows there are (what a slot holds of others goes into sums that are not
+// stored).  One barrier a unit: behind it the unit is there for all, and the slot of the unit before is free.
 #include "q4.hpp"
 
 namespace exf {
 
-template <int GROUP, int U, int R, int C, int D, bool ZERO>
+template <int GROUP, int U, int R, int C, bool ZERO>
 struct Q4Ring {
     static constexpr int kUnit = U, kSteps = U / 128, kGroups = kUnit / GROUP, kColumns = 16 * C;
     // words of a column's unit, that hold its scales and its zero points
@@ -21,14 +21,13 @@ struct Q4Ring {
     static constexpr int kCodeLoads = kCodes / 1024, kRowLoads = kRows / 4096;
     static constexpr int kScaleLanes = kScaleWords == 4 ? kColumns : kColumns * kScaleWords, kScaleLoads = (kScaleLanes + 63) / 64;
     static constexpr int kZeroLanes = kColumns * kZeroWords, kZeroLoads = ZERO ? (kZeroLanes + 63) / 64 : 0;
-    static constexpr int kLoads = kCodeLoads + kRowLoads + kScaleLoads + kZeroLoads;  // of a wavefront a unit
-    static constexpr int kBytes = D * (kRows + 4 * kWave64);
+    static constexpr int kBytes = 2 * (kRows + 4 * kWave64);
 };
 
-template <int GROUP, int U, int R, int C, int D, bool ZERO>
-__global__ __launch_bounds__(256) void q4_stream_kernel(const Q4Product p, int col_tiles)
+template <int GROUP, int U, int R, int C, bool PAST, bool ZERO>
+__global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, int col_tiles)
 {
-    using Ring = Q4Ring<GROUP, U, R, C, D, ZERO>;
+    using Ring = Q4Ring<GROUP, U, R, C, ZERO>;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const uint32_t smem_addr = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
     const int lane = lane_id(), in16 = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -36,7 +35,7 @@ __global__ __launch_bounds__(256) void q4_stream_kernel(const Q4Product p, int c
     const int tiles = (range.hi - range.lo + 16 * R - 1) / (16 * R), upto = wave_inclusive_scan(tiles);
     const int64_t N = p.N, groups = p.K / GROUP;
     const int units = p.K / Ring::kUnit;
-    const uint32_t rows_at = smem_addr, mine_at = smem_addr + D * Ring::kRows + wave * (D * Ring::kWave64);
+    const uint32_t rows_at = smem_addr, mine_at = smem_addr + 2 * Ring::kRows + wave * (2 * Ring::kWave64);
     const CodeBits bits = code_bits();
     for (int64_t tile = blockIdx.x;; tile += gridDim.x) {
         const int row_tile = static_cast<int>(tile / col_tiles);
@@ -60,16 +59,20 @@ __global__ __launch_bounds__(256) void q4_stream_kernel(const Q4Product p, int c
 #pragma unroll
         for (int i = 0; i < Ring::kRowLoads; ++i) {
             constexpr int kPieces = U / 8;  // of a row
-            const int r = (wave * Ring::kRowLoads + i) * (64 / kPieces) + lane / kPieces;
+            const int r = (i * 4 + wave) * (64 / kPieces) + lane / kPieces;
             row_at[i] = static_cast<uint32_t>(min(r, rows - 1)) * static_cast<uint32_t>(p.K * 2) + ((lane % kPieces) ^ (r & 15)) * 16;
         }
         auto issue = [&](int u) {
-            const int slot = u % D;
+            const int slot = u % 2;
             const uint32_t mine = mine_at + slot * Ring::kWave64;
 #pragma unroll
-            for (int i = 0; i < Ring::kCodeLoads; ++i) lds_dma_16B(codes + u * (Ring::kUnit / 2), code_at[i], mine + i * 1024);
+            for (int i = 0; i < Ring::kCodeLoads; ++i) {
+                if constexpr (PAST) lds_dma_16B_stream(codes + u * (Ring::kUnit / 2), code_at[i], mine + i * 1024);
+                else lds_dma_16B(codes + u * (Ring::kUnit / 2), code_at[i], mine + i * 1024);
+            }
 #pragma unroll
-            for (int i = 0; i < Ring::kRowLoads; ++i) lds_dma_16B(x + u * (Ring::kUnit * 2), row_at[i], rows_at + slot * Ring::kRows + (wave * Ring::kRowLoads + i) * 1024);
+            for (int i = 0; i < Ring::kRowLoads; ++i)
+                if ((i * 4 + wave) * (512 / U) < rows) lds_dma_16B(x + u * (Ring::kUnit * 2), row_at[i], rows_at + slot * Ring::kRows + (i * 4 + wave) * 1024);
 #pragma unroll
             for (int i = 0; i < Ring::kScaleLoads; ++i) {
                 const int l = i * 64 + lane;
@@ -95,8 +98,8 @@ __global__ __launch_bounds__(256) void q4_stream_kernel(const Q4Product p, int c
 #pragma unroll
             for (int c = 0; c < C; ++c) total[r][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         auto multiply = [&](int u) {
-            const int slot = u % D;
-            const unsigned char *mine = smem + D * Ring::kRows + wave * (D * Ring::kWave64) + slot * Ring::kWave64, *shared = smem + slot * Ring::kRows;
+            const int slot = u % 2;
+            const unsigned char *mine = smem + 2 * Ring::kRows + wave * (2 * Ring::kWave64) + slot * Ring::kWave64, *shared = smem + slot * Ring::kRows;
             float scale[C][Ring::kGroups], zero[C][Ring::kGroups];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -160,13 +163,11 @@ __global__ __launch_bounds__(256) void q4_stream_kernel(const Q4Product p, int c
                 }
             }
         };
-        wait_vmcnt<0>();
-        for (int u = 0; u < D - 1 && u < units; ++u) issue(u);
+        issue(0);
         for (int u = 0; u < units; ++u) {
-            if (u + D - 2 < units) wait_vmcnt<(D - 2) * Ring::kLoads>();
-            else wait_vmcnt<0>();
+            wait_vmcnt<0>();
             barrier_for_lds();
-            if (u + D - 1 < units) issue(u + D - 1);
+            if (u + 1 < units) issue(u + 1);
             multiply(u);
         }
 #pragma unroll
@@ -187,23 +188,27 @@ __global__ __launch_bounds__(256) void q4_stream_kernel(const Q4Product p, int c
 }
 
 // Whole steps of 128 elements, and workgroups of 128 columns for half of the compute units at least.  Streamed and not, us: 512 rows over 64 experts of 16384 x
-// 4096 433 and 946, 64 rows 394 and 715; one row, 16384 x 4096 13.2 and 14; 8 over 8 of 4096 x 1024 6.4 and 9.5; one of 4096 x 1024 4.9 and 3.9; 16 over 2 of 2048 x
+// 4096 411 and 946, 64 rows 385 and 715; one row, 16384 x 4096 13.2 and 14; 8 over 8 of 4096 x 1024 6.4 and 9.5; one of 4096 x 1024 4.9 and 3.9; 16 over 2 of 2048 x
 // 8192 22 and 12.5.
 bool q4_streams(int64_t A, int n, int k, int E_local) { return k % 128 == 0 && (n + 127) / 128 * (A < E_local ? A : E_local) >= 128; }
 
+// Tiles, us.  Few rows a tile read the weights once (1024 rows over 64 experts of 4096 x 1024: 31.6 with 16 x 128 a workgroup, 39.1 with 32 x 256), many share
+// what it costs to turn codes into numbers (2048 rows over the same 49.6 and 43.7; over 8 of 4096 x 4096 157.7 and 114.7).  Units of 256 elements are a whole line
+// of a column; those of 128 are for the columns that end inside one (512 rows over 64 of 16384 x 4096: 433 and 557).  A third slot in LDS costs a workgroup a
+// compute unit (488).  Weights that the 256 MB behind the L2 cannot hold until the next call go past the caches: 411 us for 512 rows over 64 of 16384 x 4096, 426
+// otherwise (64 rows: 385 and 402); weights that it can hold do not, 31.2 and 36.1 (1024 rows over 64 of 4096 x 1024, called again and again).
 int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
 {
-    const char* fn = "moe_grouped_product_q4";
     int rc = EXF_OK;
-    auto run = [&](auto size, auto unit, auto row_tiles, auto col_tiles, auto depth, auto zero) {
-        constexpr int G = decltype(size)::value, U = decltype(unit)::value, R = decltype(row_tiles)::value, C = decltype(col_tiles)::value, D = decltype(depth)::value;
-        constexpr bool ZERO = decltype(zero)::value;
-        constexpr size_t lds = Q4Ring<G, U, R, C, D, ZERO>::kBytes;
+    auto run = [&](auto size, auto unit, auto row_tiles, auto col_tiles, auto past, auto zero) {
+        constexpr int G = decltype(size)::value, U = decltype(unit)::value, R = decltype(row_tiles)::value, C = decltype(col_tiles)::value;
+        constexpr bool PAST = decltype(past)::value, ZERO = decltype(zero)::value;
+        constexpr size_t lds = Q4Ring<G, U, R, C, ZERO>::kBytes;
         static_assert(lds <= 160 * 1024, "a CU has 160 KiB");
         const int64_t cols = (p.N + 64 * C - 1) / (64 * C), grid = (p.max_rows / (16 * R) + (p.max_rows < p.E_local ? p.max_rows : p.E_local)) * cols;
-        auto kern = q4_stream_kernel<G, U, R, C, D, ZERO>;
+        auto kern = q4_stream_kernel<G, U, R, C, PAST, ZERO>;
         static std::atomic<uint64_t> allowed{0};
-        rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, fn);
+        rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, "moe_grouped_product_q4");
         if (rc == EXF_OK) hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid < (1 << 22) ? grid : 1 << 22)), dim3(256), lds, stream, p, static_cast<int>(cols));
     };
     const std::integral_constant<int, 1> one;
@@ -211,12 +216,13 @@ int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
     const std::integral_constant<int, 4> four;
     const std::integral_constant<int, 128> step;
     const std::integral_constant<int, 256> steps;
-    const int64_t mean = p.max_rows / p.E_local;
+    const int64_t mean = p.max_rows / p.E_local, bytes = static_cast<int64_t>(p.E_local) * p.N * p.K / 2;
     pick_q4_group(group, [&](auto size) {
         auto with = [&](auto zero) {
-            if (mean > 24) run(size, step, two, four, two, zero);
-            else if (p.K % 256 == 0) run(size, steps, one, two, two, zero);
-            else run(size, step, one, two, two, zero);
+            if (mean > 24) run(size, step, two, four, std::false_type(), zero);
+            else if (p.K % 256 != 0) run(size, step, one, two, std::false_type(), zero);
+            else if (bytes > (int64_t{256} << 20)) run(size, steps, one, two, std::true_type(), zero);
+            else run(size, steps, one, two, std::false_type(), zero);
         };
         if (p.zero != nullptr) with(std::true_type());
         else with(std::false_type());
