@@ -4,38 +4,49 @@
 // an access of its own to the L1, 64 a load, and the L1 is the bound.  Copied to LDS first, in units of 256 elements - 128 bytes of a column, 512 of a row -
 // neighbouring lanes fetch what lies together, and a load of a wavefront is 16 accesses.  Pieces of 16 bytes trade places inside a column's (row's) part of a
 // unit so that the 16 lanes that read one piece each of 16 columns (rows) meet all banks once.
-//   A workgroup has 16 R rows and 4 x 16 C columns of an expert, a wavefront all rows and 16 C of the columns, with two slots of codes, scales and
-// zero points of its own; the rows' two are shared, each wavefront copies a quarter of the rows there are (what a slot holds of others goes into sums that are not
-// stored).  One barrier a unit: behind it the unit is there for all, and the slot of the unit before is free.
+//   A workgroup has 16 R rows and 4 x 16 C columns of an expert, a wavefront all rows and 16 C of the columns, with two slots of codes, scales and zero points of
+// its own; the rows' two are shared by four wavefronts, each copies a quarter of the rows there are (what a slot holds of others goes into sums that are not
+// stored).  One barrier a unit: behind it the unit is there for all, and the slot of the unit before is free.  Where columns are too few to fill the chip, KS times
+// four wavefronts take every KS-th unit each, and their sums are added in order.
+//   ODD: K ends inside a unit.  Its groups past the end are left out; a column's scales and zero points begin anywhere in a word of four bytes.
 #include "q4.hpp"
 
 namespace exf {
 
-template <int GROUP, int U, int R, int C, bool ZERO>
+template <int GROUP, int U, int R, int C, int KS, bool ODD, bool ZERO>
 struct Q4Ring {
     static constexpr int kUnit = U, kSteps = U / 128, kGroups = kUnit / GROUP, kColumns = 16 * C;
-    // words of a column's unit, that hold its scales and its zero points
-    static constexpr int kScaleWords = (kGroups + 1) / 2, kZeroWords = (kGroups + 3) / 4;
+    // words of a column's unit, that hold its scales and its zero points; ODD: they begin anywhere in the first
+    static constexpr int kScaleWords = ODD ? kGroups / 2 + 1 : (kGroups + 1) / 2, kZeroWords = ODD ? (kGroups + 2) / 4 + 1 : (kGroups + 3) / 4;
+    static constexpr bool kWide = !ODD && kScaleWords == 4;  // 16 bytes at once
     static constexpr int kCodes = kColumns * kUnit / 2, kScales = kColumns * kScaleWords * 4, kZeros = ZERO ? kColumns * kZeroWords * 4 : 0, kRows = 16 * R * kUnit * 2;
     static constexpr int kWave64 = kCodes + kScales + kZeros;  // bytes of a unit of a wavefront
     static constexpr int kCodeLoads = kCodes / 1024, kRowLoads = kRows / 4096;
-    static constexpr int kScaleLanes = kScaleWords == 4 ? kColumns : kColumns * kScaleWords, kScaleLoads = (kScaleLanes + 63) / 64;
+    static constexpr int kScaleLanes = kWide ? kColumns : kColumns * kScaleWords, kScaleLoads = (kScaleLanes + 63) / 64;
     static constexpr int kZeroLanes = kColumns * kZeroWords, kZeroLoads = ZERO ? (kZeroLanes + 63) / 64 : 0;
-    static constexpr int kBytes = 2 * (kRows + 4 * kWave64);
+    static constexpr int kBytes = KS * 2 * (kRows + 4 * kWave64);
 };
 
-template <int GROUP, int U, int R, int C, bool PAST, bool ZERO>
-__global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, int col_tiles)
+// Words from byte `at` (0 to 3) of the first on.
+template <int N>
+__device__ __forceinline__ void from_byte(uint32_t (&w)[N], uint32_t at)
 {
-    using Ring = Q4Ring<GROUP, U, R, C, ZERO>;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_alignbyte(i + 1 < N ? w[i + 1] : 0u, w[i], at);
+}
+
+template <int GROUP, int U, int R, int C, int KS, bool PAST, bool ODD, bool ZERO>
+__global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(const Q4Product p, int col_tiles)
+{
+    using Ring = Q4Ring<GROUP, U, R, C, KS, ODD, ZERO>;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const uint32_t smem_addr = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
-    const int lane = lane_id(), in16 = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = lane_id(), in16 = lane & 15, quad = lane >> 4, nth = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wave = nth % 4, share = nth / 4;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
     const int tiles = (range.hi - range.lo + 16 * R - 1) / (16 * R), upto = wave_inclusive_scan(tiles);
     const int64_t N = p.N, groups = p.K / GROUP;
-    const int units = p.K / Ring::kUnit;
-    const uint32_t rows_at = smem_addr, mine_at = smem_addr + 2 * Ring::kRows + wave * (2 * Ring::kWave64);
+    const int units = (p.K + Ring::kUnit - 1) / Ring::kUnit, turns = (units + KS - 1) / KS, own = (units - share + KS - 1) / KS;
+    const uint32_t rows_at = smem_addr + share * (2 * Ring::kRows), mine_at = smem_addr + KS * 2 * Ring::kRows + nth * (2 * Ring::kWave64);
     const CodeBits bits = code_bits();
     for (int64_t tile = blockIdx.x;; tile += gridDim.x) {
         const int row_tile = static_cast<int>(tile / col_tiles);
@@ -62,24 +73,29 @@ __global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, in
             const int r = (i * 4 + wave) * (64 / kPieces) + lane / kPieces;
             row_at[i] = static_cast<uint32_t>(min(r, rows - 1)) * static_cast<uint32_t>(p.K * 2) + ((lane % kPieces) ^ (r & 15)) * 16;
         }
-        auto issue = [&](int u) {
-            const int slot = u % 2;
+        // What a unit has behind the end of a column or row is the next one's, and not used; of the last ones of all it is the last piece there is.
+        const int64_t cols_left = p.E_local * N - first_col, rows_left = p.max_rows - lo;
+        auto within = [&](uint32_t at, int64_t bytes) { return ODD ? min(at, static_cast<uint32_t>(bytes < 0x7fffffff ? bytes : 0x7fffffff)) : at; };
+        auto issue = [&](int t) {
+            const int u = t * KS + share, slot = t % 2;
             const uint32_t mine = mine_at + slot * Ring::kWave64;
 #pragma unroll
             for (int i = 0; i < Ring::kCodeLoads; ++i) {
-                if constexpr (PAST) lds_dma_16B_stream(codes + u * (Ring::kUnit / 2), code_at[i], mine + i * 1024);
-                else lds_dma_16B(codes + u * (Ring::kUnit / 2), code_at[i], mine + i * 1024);
+                const uint32_t at = within(code_at[i], cols_left * (p.K / 2) - u * (Ring::kUnit / 2) - 16);
+                if constexpr (PAST) lds_dma_16B_stream(codes + u * (Ring::kUnit / 2), at, mine + i * 1024);
+                else lds_dma_16B(codes + u * (Ring::kUnit / 2), at, mine + i * 1024);
             }
 #pragma unroll
             for (int i = 0; i < Ring::kRowLoads; ++i)
-                if ((i * 4 + wave) * (512 / U) < rows) lds_dma_16B(x + u * (Ring::kUnit * 2), row_at[i], rows_at + slot * Ring::kRows + (i * 4 + wave) * 1024);
+                if ((i * 4 + wave) * (512 / U) < rows)
+                    lds_dma_16B(x + u * (Ring::kUnit * 2), within(row_at[i], rows_left * (p.K * 2) - u * (Ring::kUnit * 2) - 16), rows_at + slot * Ring::kRows + (i * 4 + wave) * 1024);
 #pragma unroll
             for (int i = 0; i < Ring::kScaleLoads; ++i) {
                 const int l = i * 64 + lane;
                 if (l < Ring::kScaleLanes) {
-                    const uint32_t mine_of = static_cast<uint32_t>(max(min(Ring::kScaleWords == 4 ? l : l / Ring::kScaleWords, cols - 1), 0)) * static_cast<uint32_t>(groups * 2);
-                    if constexpr (Ring::kScaleWords == 4) lds_dma_16B(scales + u * 16, mine_of, mine + Ring::kCodes + i * 1024);
-                    else lds_dma_4B(scales, (mine_of + u * Ring::kGroups * 2 + l % Ring::kScaleWords * 4) & ~3u, mine + Ring::kCodes + i * 256);
+                    const uint32_t column = static_cast<uint32_t>(max(min(Ring::kWide ? l : l / Ring::kScaleWords, cols - 1), 0)) * static_cast<uint32_t>(groups * 2);
+                    if constexpr (Ring::kWide) lds_dma_16B(scales + u * 16, column, mine + Ring::kCodes + i * 1024);
+                    else lds_dma_4B(scales, within((column + u * Ring::kGroups * 2 + l % Ring::kScaleWords * 4) & ~3u, cols_left * groups * 2 - 4), mine + Ring::kCodes + i * 256);
                 }
             }
             if constexpr (ZERO)
@@ -88,7 +104,7 @@ __global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, in
                     const int l = i * 64 + lane;
                     if (l < Ring::kZeroLanes) {
                         const uint32_t at = static_cast<uint32_t>(max(min(l / Ring::kZeroWords, cols - 1), 0)) * static_cast<uint32_t>(groups) + u * Ring::kGroups + l % Ring::kZeroWords * 4;
-                        lds_dma_4B(zeros, at & ~3u, mine + Ring::kCodes + Ring::kScales + i * 256);
+                        lds_dma_4B(zeros, within(at & ~3u, cols_left * groups - 4), mine + Ring::kCodes + Ring::kScales + i * 256);
                     }
                 }
         };
@@ -97,19 +113,19 @@ __global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, in
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < C; ++c) total[r][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        auto multiply = [&](int u) {
-            const int slot = u % 2;
-            const unsigned char *mine = smem + 2 * Ring::kRows + wave * (2 * Ring::kWave64) + slot * Ring::kWave64, *shared = smem + slot * Ring::kRows;
+        auto multiply = [&](int t) {
+            const int u = t * KS + share, slot = t % 2;
+            const unsigned char *mine = smem + KS * 2 * Ring::kRows + nth * (2 * Ring::kWave64) + slot * Ring::kWave64, *shared = smem + (share * 2 + slot) * Ring::kRows;
             float scale[C][Ring::kGroups], zero[C][Ring::kGroups];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const uint32_t first = static_cast<uint32_t>(max(min(c * 16 + in16, cols - 1), 0)) * static_cast<uint32_t>(groups) + u * Ring::kGroups;
                 uint32_t s[Ring::kScaleWords], z[Ring::kZeroWords];
-                __builtin_memcpy(s, __builtin_assume_aligned(mine + Ring::kCodes + (c * 16 + in16) * Ring::kScaleWords * 4, Ring::kScaleWords * 4), sizeof(s));
-                if constexpr (Ring::kGroups == 1) s[0] >>= (first & 1u) * 16;  // (the one of the word's two)
+                __builtin_memcpy(s, __builtin_assume_aligned(mine + Ring::kCodes + (c * 16 + in16) * Ring::kScaleWords * 4, ODD ? 4 : Ring::kScaleWords * 4), sizeof(s));
+                if constexpr (ODD || Ring::kGroups == 1) from_byte(s, (first & 1u) * 2);
                 if constexpr (ZERO) {
-                    __builtin_memcpy(z, __builtin_assume_aligned(mine + Ring::kCodes + Ring::kScales + (c * 16 + in16) * Ring::kZeroWords * 4, Ring::kZeroWords * 4), sizeof(z));
-                    if constexpr (Ring::kGroups < 4) z[0] >>= (first & 3u) * 8;  // (those of the word's four)
+                    __builtin_memcpy(z, __builtin_assume_aligned(mine + Ring::kCodes + Ring::kScales + (c * 16 + in16) * Ring::kZeroWords * 4, ODD ? 4 : Ring::kZeroWords * 4), sizeof(z));
+                    if constexpr (ODD || Ring::kGroups < 4) from_byte(z, first & 3u);
                 }
 #pragma unroll
                 for (int g = 0; g < Ring::kGroups; ++g) {
@@ -129,6 +145,7 @@ __global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, in
                 }
 #pragma unroll
                 for (int g = 0; g < 128 / GROUP; ++g) {
+                    if (ODD && u * Ring::kGroups + h * (128 / GROUP) + g >= groups) continue;  // (the end of the columns)
                     f32x4_t sum[R][C], sum_x[R];
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
@@ -163,17 +180,31 @@ __global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, in
                 }
             }
         };
-        issue(0);
-        for (int u = 0; u < units; ++u) {
+        if (KS == 1 || own > 0) issue(0);
+        for (int t = 0; t < turns; ++t) {
             wait_vmcnt<0>();
             barrier_for_lds();
-            if (u + 1 < units) issue(u + 1);
-            multiply(u);
+            if (t + 1 < own) issue(t + 1);
+            if (KS == 1 || t < own) multiply(t);
+        }
+        if constexpr (KS > 1) {  // the shares' sums, in their order
+            static_assert(R == 1, "a tile of rows");
+            f32x4_t* const parts = reinterpret_cast<f32x4_t*>(smem) + wave * ((KS - 1) * C * kWave) + lane;
+            barrier_for_lds();
+            if (share > 0)
+#pragma unroll
+                for (int c = 0; c < C; ++c) parts[((share - 1) * C + c) * kWave] = total[0][c];
+            barrier_for_lds();
+            if (share == 0)
+#pragma unroll
+                for (int s = 1; s < KS; ++s)
+#pragma unroll
+                    for (int c = 0; c < C; ++c) total[0][c] += parts[((s - 1) * C + c) * kWave];
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = c * 16 + in16;
-            if (at >= cols) continue;
+            if (at >= cols || (KS > 1 && share > 0)) continue;
             const float b = p.bias != nullptr ? bf16_to_f32(static_cast<const bf16_t*>(p.bias)[first_col + at]) : 0.0f;
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -187,45 +218,72 @@ __global__ __launch_bounds__(256, 2) void q4_stream_kernel(const Q4Product p, in
     }
 }
 
-// Whole steps of 128 elements, and workgroups of 128 columns for half of the compute units at least.  Streamed and not, us: 512 rows over 64 experts of 16384 x
-// 4096 411 and 946, 64 rows 385 and 715; one row, 16384 x 4096 13.2 and 14; 8 over 8 of 4096 x 1024 6.4 and 9.5; one of 4096 x 1024 4.9 and 3.9; 16 over 2 of 2048 x
-// 8192 22 and 12.5.
-bool q4_streams(int64_t A, int n, int k, int E_local) { return k % 128 == 0 && (n + 127) / 128 * (A < E_local ? A : E_local) >= 128; }
+// What the choice goes by: tiles of 16 rows, were the rows spread evenly over the experts that can have any, and how many workgroups these are with 64 columns each.
+struct Q4Spread {
+    int64_t experts, mean, workgroups;
+};
+static Q4Spread spread_of(int64_t A, int n, int E_local)
+{
+    const int64_t experts = A < E_local ? A : E_local, mean = (A + experts - 1) / experts;
+    return {experts, mean, experts * ((mean + 15) / 16) * ((n + 63) / 64)};
+}
 
-// Tiles, us.  Few rows a tile read the weights once (1024 rows over 64 experts of 4096 x 1024: 31.6 with 16 x 128 a workgroup, 39.1 with 32 x 256), many share
-// what it costs to turn codes into numbers (2048 rows over the same 49.6 and 43.7; over 8 of 4096 x 4096 157.7 and 114.7).  Units of 256 elements are a whole line
-// of a column; those of 128 are for the columns that end inside one (512 rows over 64 of 16384 x 4096: 433 and 557).  A third slot in LDS costs a workgroup a
-// compute unit (488).  Weights that the 256 MB behind the L2 cannot hold until the next call go past the caches: 411 us for 512 rows over 64 of 16384 x 4096, 426
-// otherwise (64 rows: 385 and 402); weights that it can hold do not, 31.2 and 36.1 (1024 rows over 64 of 4096 x 1024, called again and again).
+// Workgroups for two thirds of the compute units; half of that where a tile has more than 8 rows, which the other kernel loads over and over.  Streamed and not, us (rows,
+// experts, columns x reduction): 512, 64, 16384 x 4096 411 and 946; 1024, 64, 4096 x 1056 57 and 96; 1, 1, 16384 x 4096 11.4 and 15.3; 43, 10, 1200 x 4096 10.9 and 13.5;
+// 100, 6, 512 x 8192 16.4 and 23.2; but 8, 8, 1024 x 4096 10.5 and 9.1; 16, 1, 4096 x 4096 10.2 and 8.5; 1, 1, 4096 x 1024 5.3 and 4.5; 66, 4, 352 x 10624 22 and 15.8.
+bool q4_streams(int64_t A, int n, int, int E_local)
+{
+    const Q4Spread s = spread_of(A, n, E_local);
+    return s.workgroups * (s.mean > 8 ? 2 : 1) >= 160;
+}
+
+// Tiles, us, as above.  32 x 256 a workgroup, in units of 128 so that three fit a compute unit, where many rows share what it costs to turn codes into numbers and a
+// workgroup a compute unit is left, otherwise 16 x 128: 2048, 8, 4096 x 4096 111 and 162; 2048, 64, 4096 x 1024 43.7 and 49.6; 512, 8, 4096 x 4096 43 and 49; but 1024,
+// 64, 4096 x 1024 41 and 31; 512, 2, 2048 x 2048 (128 workgroups) 21 and 15.  Of 64 columns and with two shares of the reduction while these are up to three a compute
+// unit: 5, 5, 8192 x 4096 22.9 and 23.8; 10, 10, 4096 x 4096 28.9 and 34.3; 509, 12, 696 x 11456 56 and 66; but 12, 12, 4096 x 2048 14.7 and 14.2; 115, 2, 7488 x 128 9.1 and
+// 6.2.  With four shares while they are one a compute unit and a share has some units: 1, 1, 16384 x 16384 29.6 and 34.3; 43, 10, 1200 x 4096 10.9 and 11.7; but 4, 4, 4096 x
+// 1024 6.0 and 5.5.  A third slot in LDS gained nothing, here or there (12.2 for 12.2 and 17.7 for 17.1; 488 for 433).
+//   Weights that the 256 MB behind the L2 cannot hold until the next call go past the caches: 411 us for 512, 64, 16384 x 4096, 426 otherwise (64 rows: 385 and
+// 402); weights that it can hold do not, 31.2 and 36.1 (1024, 64, 4096 x 1024, called again and again).
 int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
 {
     int rc = EXF_OK;
-    auto run = [&](auto size, auto unit, auto row_tiles, auto col_tiles, auto past, auto zero) {
-        constexpr int G = decltype(size)::value, U = decltype(unit)::value, R = decltype(row_tiles)::value, C = decltype(col_tiles)::value;
-        constexpr bool PAST = decltype(past)::value, ZERO = decltype(zero)::value;
-        constexpr size_t lds = Q4Ring<G, U, R, C, ZERO>::kBytes;
+    auto run = [&](auto size, auto unit, auto row_tiles, auto col_tiles, auto shares, auto past, auto odd, auto zero) {
+        constexpr int G = decltype(size)::value, U = decltype(unit)::value, R = decltype(row_tiles)::value, C = decltype(col_tiles)::value, KS = decltype(shares)::value;
+        constexpr bool PAST = decltype(past)::value, ODD = decltype(odd)::value, ZERO = decltype(zero)::value;
+        constexpr size_t lds = Q4Ring<G, U, R, C, KS, ODD, ZERO>::kBytes;
         static_assert(lds <= 160 * 1024, "a CU has 160 KiB");
         const int64_t cols = (p.N + 64 * C - 1) / (64 * C), grid = (p.max_rows / (16 * R) + (p.max_rows < p.E_local ? p.max_rows : p.E_local)) * cols;
-        auto kern = q4_stream_kernel<G, U, R, C, PAST, ZERO>;
+        auto kern = q4_stream_kernel<G, U, R, C, KS, PAST, ODD, ZERO>;
         static std::atomic<uint64_t> allowed{0};
         rc = allow_lds(reinterpret_cast<const void*>(kern), lds, allowed, "moe_grouped_product_q4");
-        if (rc == EXF_OK) hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid < (1 << 22) ? grid : 1 << 22)), dim3(256), lds, stream, p, static_cast<int>(cols));
+        if (rc == EXF_OK) hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid < (1 << 22) ? grid : 1 << 22)), dim3(256 * KS), lds, stream, p, static_cast<int>(cols));
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 2> two;
     const std::integral_constant<int, 4> four;
     const std::integral_constant<int, 128> step;
     const std::integral_constant<int, 256> steps;
-    const int64_t mean = p.max_rows / p.E_local, bytes = static_cast<int64_t>(p.E_local) * p.N * p.K / 2;
+    const std::true_type yes;
+    const std::false_type no;
+    const Q4Spread s = spread_of(p.max_rows, p.N, p.E_local);
+    const bool tall = s.mean > 24 && s.experts * ((s.mean + 31) / 32) * ((p.N + 255) / 256) >= 256, few = s.workgroups <= 768, fewest = s.workgroups <= 256 && p.K >= 2048;
+    const bool past = static_cast<int64_t>(p.E_local) * p.N * p.K / 2 > (int64_t{256} << 20);
     pick_q4_group(group, [&](auto size) {
         auto with = [&](auto zero) {
-            if (mean > 24) run(size, step, two, four, std::false_type(), zero);
-            else if (p.K % 256 != 0) run(size, step, one, two, std::false_type(), zero);
-            else if (bytes > (int64_t{256} << 20)) run(size, steps, one, two, std::true_type(), zero);
-            else run(size, steps, one, two, std::false_type(), zero);
+            auto ends = [&](auto unit, auto run_with) {
+                if constexpr (decltype(unit)::value > decltype(size)::value)
+                    if (p.K % decltype(unit)::value != 0) return run_with(yes);
+                run_with(no);  // (a unit that is a group always fits)
+            };
+            if (tall) ends(step, [&](auto odd) { run(size, step, two, four, one, no, odd, zero); });
+            else if (fewest) ends(steps, [&](auto odd) { run(size, steps, one, one, four, no, odd, zero); });
+            else if (few) ends(steps, [&](auto odd) { run(size, steps, one, one, two, no, odd, zero); });
+            else if (past) ends(steps, [&](auto odd) { run(size, steps, one, two, one, yes, odd, zero); });
+            else ends(steps, [&](auto odd) { run(size, steps, one, two, one, no, odd, zero); });
         };
-        if (p.zero != nullptr) with(std::true_type());
-        else with(std::false_type());
+        if (p.zero != nullptr) with(yes);
+        else with(no);
     });
     return rc;
 }

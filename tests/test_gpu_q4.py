@@ -128,6 +128,63 @@ def test_product_of_steps_that_are_not_full(k, group, dt):
     _check_product([3, 20, 0, 1], 44 if dt == F32 else 48, k, group, dt, bias=True)
 
 
+# (rows of the experts, n, k): many rows an expert; few columns for the chip, and still fewer with a long reduction; enough.  Of each, reductions that end with a line
+# of a column, inside one with whole and with odd numbers of groups, and inside the first.
+SPREADS = {"tall": ([64, 50, 0, 100, 64, 17, 130, 64], 4096, (128, 384, 32, 96, 160, 192)), "few": ([1, 0, 3, 1, 2, 1, 16, 1], 4104, (512, 384, 32, 288, 352, 320)),
+           "fewest": ([3, 2], 8192, (2048, 2176, 2080, 2112, 2272)), "wide": ([1, 4, 1, 0, 17, 1, 9, 1, 1, 1, 1, 1, 3], 4160, (256, 640, 64, 96, 288, 192))}
+
+
+@pytest.mark.parametrize("spread,k,group", [(name, k, group) for name, (_, _, ks) in SPREADS.items() for k in ks for group in (32, 64, 128) if k % group == 0])
+def test_product_of_many_columns(spread, k, group):
+    sizes, n, _ = SPREADS[spread]
+    _check_product(sizes, n, k, group, BF, zeros=True, bias=k % 3 == 0, first=2, behind=3)
+    _check_product(sizes, n, k, group, BF, zeros=False, bias=k % 3 != 0, seed=7)
+
+
+@pytest.mark.parametrize("k,group", [(k, group) for k in (512, 544, 576, 640) for group in (32, 64, 128) if k % group == 0])
+def test_product_of_weights_that_no_cache_holds(k, group):
+    """Six rows of four of 64 experts, the last among them."""
+    E, n, g = 64, 17000, torch.Generator(DEV).manual_seed(k + group)
+    q = torch.empty((E, n, k // 2), dtype=torch.uint8, device=DEV).random_(generator=g)
+    scale = torch.empty((E, n, k // group), dtype=BF, device=DEV).uniform_(0.01, 0.05, generator=g)
+    zero = torch.empty((E, n, k // group), dtype=torch.uint8, device=DEV).random_(0, 17, generator=g)
+    x = torch.randn((6, k), generator=torch.Generator().manual_seed(3)).to(BF).to(DEV)
+    sizes = [0] * E
+    sizes[0], sizes[5], sizes[40], sizes[63] = 1, 2, 1, 2
+    off = sizes_to_offsets(sizes)
+    for z in (zero, None):
+        y = exf.moe_grouped_product_q4(x, off.to(DEV), exf.Q4(q, scale, z))
+        for e in (0, 5, 40, 63):
+            lo, hi = int(off[e]), int(off[e + 1])
+            rows = x[lo:hi].double()
+            ref = rows @ R.q4_values(q[e], scale[e], None if z is None else z[e]).t()
+            mag = rows.abs() @ (scale[e].double().repeat_interleave(group, 1) * (16 + 15 + 16 + 17)).t()
+            R.assert_close(y[lo:hi].cpu(), ref.cpu(), mag.cpu(), 4 * (k / 16 + k / group + 8), f"expert {e}")
+
+
+@pytest.mark.parametrize("spread,k", [("tall", 160), ("few", 352), ("fewest", 2080), ("wide", 288), ("few", 512), ("tall", 128)])
+def test_what_is_no_number_stays_in_its_row_and_column(spread, k):
+    """... also where a step reads past the end of one into the next."""
+    sizes, n, _ = SPREADS[spread]
+    q, scale, zero = _weights(len(sizes), n, k, 32, BF, True, 3)
+    A, off = sum(sizes), sizes_to_offsets(sizes).to(DEV)
+    x = torch.randn(A, k, generator=torch.Generator().manual_seed(1)).to(BF)
+    rows = [1, A - 1]
+    x_bad, scale_bad = x.clone(), scale.clone()
+    x_bad[rows[0], :] = float("nan")
+    x_bad[rows[1], 0] = INF
+    bad = [e for e in range(len(sizes)) if sizes[e]][-1]
+    scale_bad[bad, 9, 0], scale_bad[bad, 70, -1] = float("nan"), INF
+    to = lambda t: t.to(DEV)  # noqa: E731
+    want = exf.moe_grouped_product_q4(to(x), off, exf.Q4(to(q), to(scale), to(zero)))
+    got = exf.moe_grouped_product_q4(to(x_bad), off, exf.Q4(to(q), to(scale_bad), to(zero)))
+    same = torch.ones((A, n), dtype=torch.bool, device=DEV)
+    same[rows] = False
+    lo, hi = int(off[bad]), int(off[bad + 1])
+    same[lo:hi, 9] = same[lo:hi, 70] = False
+    assert torch.equal(got[same], want[same]) and not torch.isfinite(got[rows]).any() and not torch.isfinite(got[lo:hi, [9, 70]]).any()
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_rows_outside_all_ranges_are_left_alone(dt):
     _check_product([4, 0, 30], 64, 256, 128, dt, first=3, behind=9)
