@@ -2,6 +2,11 @@
 //
 // A token belongs to L lanes of a wavefront, V consecutive experts to a lane, so that a lower lane and a lower register hold lower ids.
 // Slot j of the choice is kept by lane j of the token.
+//   What bounds it: reading takes 6 us of the 25.6 of 32768 tokens, 8 of 256 experts in 8 groups, sigmoid, bias, fp32; vector instructions the rest, 1270 a
+// wavefront of four tokens (470 of them for the groups, 280 for the scores and their classes, 330 to sort a lane's keys and take nine).  Without groups 19.5, softmax of
+// fp32 logits 14.8, bf16 11.2; keys of 64 bits throughout 98.  Registers for a fifth wavefront a SIMD (96 of 119, some spilled) gain nothing, 28.  One token 3.2, in groups
+// 6.4: loads that follow one another and nine turns of a maximum over lanes.
+//   The gradient, with that of the scores: 15.1 us for 69 MB, 4.6 TB/s.
 #include <math.h>
 
 #include <type_traits>
@@ -74,17 +79,17 @@ __device__ __forceinline__ uint32_t ordered(float l)
 template <bool BF16>
 __device__ __forceinline__ const void* row_at(const void* p, int64_t i) { return static_cast<const uint8_t*>(p) + i * (BF16 ? 2 : 4); }
 // A lane's experts are first + place(0), first + place(1), ..: pieces of four, P apart, with those of the other lanes between them, so that neighbouring lanes
-// load what lies together: 16 accesses to the L1 instead of 64 (gradient of 32768 x 256 fp32 logits with that of the scores: 22.9 us with V next to each other, now 16.4).
+// load what lies together: 16 accesses to the L1 instead of 64 (gradient of 32768 x 256 fp32 logits with that of the scores: 22.9 us with V next to each other, 16.4 when this was done).
 template <int P>
 __host__ __device__ constexpr int place(int v) { return v / 4 * P + v % 4; }
 
 // The lane's V values of a row, `none` past the last one; four at a time where rows are a multiple of that.
 template <int V, int P, bool BF16>
-__device__ __forceinline__ void load_row(const void* row, int first, int E, float none, float (&l)[V])
+__device__ __forceinline__ void load_row(const void* row, int first, int E, float none, float (&l)[V], bool aligned = true)
 {
 #pragma unroll
     for (int v = 0; v < V; ++v) l[v] = none;
-    if (E % 4 == 0) {
+    if (E % 4 == 0 && aligned) {
 #pragma unroll
         for (int v = 0; v < V; v += 4)
             if (first + place<P>(v) < E) {
@@ -133,7 +138,7 @@ __device__ __forceinline__ float exp_below(float x)
     const float t = x * 1.442695041f, rest = fmaf(x, 1.925963033e-8f, fmaf(x, 1.442695041f, -t)), whole = rintf(t);
     return ldexpf(__builtin_amdgcn_exp2f((t - whole) + rest), static_cast<int>(whole));
 }
-// a / b for b in [1, 2], to a unit.
+// a / b for b in [1/2, 16] and a in [0, b], to a unit.
 __device__ __forceinline__ float quotient(float a, float b)
 {
     const float r = __builtin_amdgcn_rcpf(b), q = a * r;
@@ -159,11 +164,11 @@ __device__ __forceinline__ float chosen_share(float l, bool live)
 {
     const float top = token_max<L>(live ? l : -INFINITY);
     float u;
-    if constexpr (SIGMOID) u = l > 0.0f ? 1.0f / (1.0f + expf(-l)) : expf(l - fminf(top, 0.0f)) / (1.0f + expf(l));
-    else u = expf(l - top);
+    if constexpr (SIGMOID) u = quotient(l > 0.0f ? 1.0f : exp_below(l - fminf(top, 0.0f)), 1.0f + exp_below(-fabsf(l)));
+    else u = exp_below(l - top);
     if (!live) u = 0.0f;
-    const float all = token_sum<L>(u);
-    return live ? u / all : 0.0f;
+    const float all = token_sum<L>(u);  // (from 1/2, that of the largest, to 16)
+    return live ? quotient(u, all) : 0.0f;
 }
 __device__ __forceinline__ double sigmoid64(double l)
 {
@@ -470,11 +475,10 @@ __device__ __forceinline__ uint32_t order_exactly(const float* bias, float* toke
 template <int V, int P>
 __device__ __forceinline__ void load_bias(const RouteCall& p, int first, float (&bias)[V])
 {
+    if (p.bias == nullptr) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) bias[v] = 0.0f;
-    if (p.bias == nullptr) return;
-#pragma unroll
-    for (int v = 0; v < V; ++v) bias[v] = p.bias[min(first + place<P>(v), p.E - 1)];
+        for (int v = 0; v < V; ++v) bias[v] = 0.0f;
+    } else load_row<V, P, false>(p.bias, first, p.E, 0.0f, bias, reinterpret_cast<uintptr_t>(p.bias) % 16 == 0);
 }
 
 // `token`: room for the token's logits in LDS.  sure: whether the lane's part of the choice is the definition's.
@@ -523,7 +527,7 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
 
     unsigned long long stay = ~0ull;  // lanes whose group stays, `parts` of them a group
     int parts = 1;
-    const int size = p.E / p.groups;
+    const int size = p.E / p.groups, inverse_size = ((1 << 20) + size - 1) / size;  // (e * inverse_size is less than e / size + 1 / 4 in 2^20s: floors agree up to 512)
     if constexpr (GROUPS) {
         const GroupParts<L> g(p.E, p.groups, in);
         uint32_t a = 0u, b = 0u;
@@ -572,7 +576,7 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         if constexpr (GROUPS) {
 #pragma unroll
             for (int v = 0; v < V; v += 4) {
-                int q = (first + place<P>(v)) / size, rest = first + place<P>(v) - q * size;
+                int q = (first + place<P>(v)) * inverse_size >> 20, rest = first + place<P>(v) - q * size;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (((stay >> min(q * parts, kWave - 1)) & 1ull) == 0ull) key[v + i] = 0u;

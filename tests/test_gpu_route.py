@@ -57,6 +57,18 @@ def test_sizes(T, E, k, dt, score):
     _check(l, k, bias, score=score, renormalize=True)
 
 
+@pytest.mark.parametrize("E", [64, 256, 512])
+def test_a_bias_that_begins_anywhere(E):
+    """A layer's part of all layers' biases."""
+    l = _logits(70, E, F32, E + 5)
+    every = (torch.randn(4 * E + 8, generator=torch.Generator().manual_seed(E)) * 0.1).to(DEV)
+    for at in (1, E + 2, 2 * E + 3, 3 * E + 4):
+        idx, w, _ = exf.moe_route(l.to(DEV), 8, every[at:at + E], score=R.SIGMOID, groups=4, top_groups=2, group_best=2)
+        same, same_w, _ = exf.moe_route(l.to(DEV), 8, every[at:at + E].clone(), score=R.SIGMOID, groups=4, top_groups=2, group_best=2)
+        assert torch.equal(idx, same) and torch.equal(w, same_w)
+    _check(l, 8, every[3:3 + E].cpu(), score=R.SIGMOID, groups=4, top_groups=2, group_best=2)
+
+
 @pytest.mark.parametrize("E,groups,top,k", [(256, 8, 4, 8), (64, 4, 1, 16), (60, 5, 2, 7), (6, 6, 2, 2), (512, 64, 20, 16), (500, 10, 3, 9), (128, 2, 1, 1), (512, 2, 2, 4), (48, 16, 7, 6), (130, 13, 4, 8)])
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("score", [R.SOFTMAX, R.SIGMOID])
