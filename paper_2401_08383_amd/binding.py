@@ -140,6 +140,14 @@ def _stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _stream_on(dev) -> int:
+    """The same for tensors on device number `dev`, which has to be the current one: a kernel launched elsewhere would not reach them."""
+    current = torch._C._cuda_getDevice()
+    if dev != current:
+        _bad(f"the arguments are on device {dev}, the current one is {current} (torch.cuda.device chooses it)")
+    return torch._C._cuda_getCurrentRawStream(current)
+
+
 def dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return EXF_F32
@@ -235,6 +243,7 @@ def _dispatch_topk_fits(x, topk_idx, expert_map, E, E_local, out, workspace):
     _expect("out.expert_offsets", out.expert_offsets, (E_local + 1,), _INT32, dev)
     if dev < 0:
         _on_host()
+    _stream_on(dev)
     _bytes_of(workspace, dev)
     return workspace.view(-1).view(_UINT8)
 
@@ -327,7 +336,7 @@ def _combine_rows(name, y_sorted, sorted_of_src, topk_w, k, out):
         topk_w = _expect("topk_w", topk_w, (T, k), _FLOAT, dev).data_ptr()
     if dev < 0:
         _on_host()
-    rc = lib().moe_combine_topk(y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w, T, d, k, code, out.data_ptr(), _stream())
+    rc = lib().moe_combine_topk(y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w, T, d, k, code, out.data_ptr(), _stream_on(dev))
     if rc:
         _check(rc)
     return out
@@ -374,7 +383,7 @@ def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, 
     if dev < 0:
         _on_host()
     rc = lib().moe_combine_backward(dout.data_ptr(), y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w.data_ptr(), T, d, k, code, _ptr(out), _ptr(out_weights),
-                                    _stream())
+                                    _stream_on(dev))
     if rc:
         _check(rc)
     return out, out_weights
@@ -410,7 +419,7 @@ def moe_route(logits, k, bias=None, score=EXF_SCORE_SOFTMAX, renormalize=False, 
         _expect("topk_w", w, (T, k), _FLOAT, dev)
     scores = _rows(T, E, _FLOAT, logits.device) if want_scores else None
     rc = lib().moe_route(logits.data_ptr(), bias, T, E, k, score, groups, groups if top_groups is None else top_groups, group_best, 1 if renormalize else 0, scale, code,
-                         idx.data_ptr(), w.data_ptr(), _ptr(scores), _stream())
+                         idx.data_ptr(), w.data_ptr(), _ptr(scores), _stream_on(dev))
     if rc:
         _check(rc)
     return idx, w, scores
@@ -439,7 +448,7 @@ def moe_route_backward(dtopk_w, logits, topk_idx, score=EXF_SCORE_SOFTMAX, renor
     if dev < 0:
         _on_host()
     rc = lib().moe_route_backward(dtopk_w.data_ptr(), logits.data_ptr(), topk_idx.data_ptr(), at, stride, T, E, k, score, 1 if renormalize else 0, scale, code,
-                                  out.data_ptr(), _stream())
+                                  out.data_ptr(), _stream_on(dev))
     if rc:
         _check(rc)
     return out
@@ -747,7 +756,7 @@ def q4_quantize(x, group=128, symmetric=False, out=None):
         _bad("q4_quantize: out holds other groups, or zero points where none are asked for")
     if dev < 0:
         _on_host()
-    rc = lib().q4_quantize(x.data_ptr(), x.numel() // k, k, group, code, out.q.data_ptr(), out.scale.data_ptr(), _ptr(out.zero), _stream())
+    rc = lib().q4_quantize(x.data_ptr(), x.numel() // k, k, group, code, out.q.data_ptr(), out.scale.data_ptr(), _ptr(out.zero), _stream_on(dev))
     if rc:
         _check(rc)
     return out
@@ -763,7 +772,7 @@ def q4_dequantize(m, out=None):
     out = torch.empty(shape, dtype=dt, device=m.q.device) if out is None else _expect("out", out, shape, dt, dev)
     if dev < 0:
         _on_host()
-    rc = lib().q4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), _ptr(m.zero), m.q.numel() * 2 // max(shape[-1], 1), shape[-1], group, code, out.data_ptr(), _stream())
+    rc = lib().q4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), _ptr(m.zero), m.q.numel() * 2 // max(shape[-1], 1), shape[-1], group, code, out.data_ptr(), _stream_on(dev))
     if rc:
         _check(rc)
     return out
@@ -791,7 +800,7 @@ def moe_grouped_product_q4(x_sorted, expert_offsets, w, bias=None, out=None):
             and x_sorted.is_contiguous() and out.is_contiguous() and expert_offsets.is_contiguous() and out.get_device() == expert_offsets.get_device() == dev >= 0):
         _misfit(x_sorted, (A, k), expert_offsets, E, scale, out, (A, n), dt, dev)
     rc = lib().moe_grouped_product_q4(x_sorted.data_ptr(), expert_offsets.data_ptr(), q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), bias, A, n, k, group, E, code,
-                                      out.data_ptr(), _stream())
+                                      out.data_ptr(), _stream_on(dev))
     if rc:
         _check(rc)
     return out

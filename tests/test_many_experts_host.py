@@ -141,8 +141,8 @@ class NothingIsLaunched:
     def __getattr__(self, name):
         if name.endswith("_bytes"):
             return getattr(B._lib, name)
-        if name == "moe_dispatch_topk":
-            return name
+        if name in ("moe_dispatch_topk", "moe_combine_topk", "moe_combine_backward", "moe_route", "moe_route_backward", "q4_quantize", "q4_dequantize", "moe_grouped_product_q4"):
+            return lambda *arguments: pytest.fail(f"{name} was called")
         pytest.fail(f"{name} was called")
 
 
@@ -158,6 +158,14 @@ def nothing_is_launched(monkeypatch):
 def test_host_tensors_are_refused(nothing_is_launched, call, dt):
     with pytest.raises(exf.ExflowError, match="on the host"):
         _fine(_arguments(dt=dt))[call]()
+
+
+@pytest.mark.parametrize("call", list(_fine(_arguments())))
+def test_tensors_of_a_device_that_is_not_the_current_one_are_refused(nothing_is_launched, monkeypatch, call):
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    with pytest.raises(exf.ExflowError, match="on device 1, the current one is 0"):
+        _fine(_arguments())[call]()
 
 
 @pytest.mark.parametrize("call,names", [("route", "logits"), ("route_backward", "w logits bias"), ("dispatch", "x"), ("dispatch_backward", "y"), ("combine", "y w"),
