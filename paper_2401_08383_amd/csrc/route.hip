@@ -2,10 +2,9 @@
 //
 // A token belongs to L lanes of a wavefront, V consecutive experts to a lane, so that a lower lane and a lower register hold lower ids.
 // Slot j of the choice is kept by lane j of the token.
-//   What bounds it: reading takes 6 us of the 25.6 of 32768 tokens, 8 of 256 experts in 8 groups, sigmoid, bias, fp32; vector instructions the rest, 1270 a
-// wavefront of four tokens (470 of them for the groups, 280 for the scores and their classes, 330 to sort a lane's keys and take nine).  Without groups 19.5, softmax of
-// fp32 logits 14.8, bf16 11.2; keys of 64 bits throughout 98.  Registers for a fifth wavefront a SIMD (96 of 119, some spilled) gain nothing, 28.  One token 3.2, in groups
-// 6.4: loads that follow one another and nine turns of a maximum over lanes.
+//   What bounds it: reading takes 6 us of the 25.0 of 32768 tokens, 8 of 256 experts in 8 groups, sigmoid, bias, fp32; vector instructions the rest, 1160 a
+// wavefront of four tokens (350 of them for the groups).  Without groups 18.4, softmax of fp32 logits 14.2, bf16 10.9; keys of 64 bits throughout 98.  Registers for a fifth wavefront a SIMD (96 of 119, some spilled) gain nothing, 28.  One token 3.1, in groups
+// 5.4: loads that follow one another and nine turns of a maximum over lanes.
 //   The gradient, with that of the scores: 15.1 us for 69 MB, 4.6 TB/s.
 #include <math.h>
 
@@ -350,11 +349,11 @@ __device__ __forceinline__ Classes classes_of(const float (&key)[V])
     const float range = most - least;
     return {most, range > 0.0f && range < 1e30f ? (kClasses - 2.0f) * __builtin_amdgcn_rcpf(range) : 0.0f};
 }
-// 0: out; 1: at the least, or below; otherwise in order, to within one.
-__device__ __forceinline__ uint32_t class_of(float key, Classes c)
+// 0: out; 1: at the least, or below; otherwise in order, to within one.  (What is out may have widened the range: classes are coarser then, and in order.)
+__device__ __forceinline__ uint32_t class_of(float key, Classes c, float logit)
 {
     const float at = fmaf(key - c.most, c.step, kClasses);
-    return key > -INFINITY ? static_cast<uint32_t>(fmaxf(at, 1.0f)) : 0u;
+    return logit > -INFINITY && key > -INFINITY ? static_cast<uint32_t>(fmaxf(at, 1.0f)) : 0u;
 }
 
 // LDS of a wavefront is written and read in order; this keeps the compiler from moving either.
@@ -502,13 +501,12 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         for (int v = 0; v < V; ++v) {
             f[v] = score(l[v]);
             if (SCORES && p.bias != nullptr) f[v] += bias[v];
-            f[v] = l[v] > -INFINITY && f[v] > -INFINITY ? f[v] : -INFINITY;
         }
         c = classes_of<V, L>(f);
         const float error = (SIGMOID ? 0x1p-21f : 0x1p-19f * inverse) + 0x1p-23f * fmaxf(fabsf(c.most), fabsf(c.most - kClasses * __builtin_amdgcn_rcpf(c.step)));
         apart = c.step > 0.0f ? 4.0f + 2.0f * error * c.step : 2.0f * kClasses;
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = class_of(f[v], c);
+        for (int v = 0; v < V; ++v) key[v] = class_of(f[v], c, l[v]);
     };
     auto classes_of_logits = [&]() {
         if constexpr (BF16) {
@@ -519,7 +517,7 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
             c = classes_of<V, L>(l);
             apart = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = class_of(l[v], c);
+            for (int v = 0; v < V; ++v) key[v] = class_of(l[v], c, l[v]);
         }
     };
     if constexpr (SCORES) classes_of_scores();
@@ -535,11 +533,21 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
 #pragma unroll
         for (int v = 0; v < V; v += 4) *reinterpret_cast<uint4*>(classes + first + place<P>(v)) = make_uint4(key[v], key[v + 1], key[v + 2], key[v + 3]);
         lds_in_order();
-#pragma unroll 4
-        for (int e = g.begin; e < g.end; ++e) {
+        auto meet = [&](int e) {
             const uint32_t k = classes[e];
             b = max(b, min(a, k));
             a = max(a, k);
+        };
+        const int share = size / g.parts;
+        if (share * g.parts == size && share >= 16 && (share & (share - 1)) == 0) {
+            // Lanes that begin a power of two apart would all be at the same banks (groups of 32, 32768 tokens: 3.9 M cycles of conflicts, now 0.3; one token 6.4 us, now 5.8):
+            // each begins elsewhere in its share, those of all tokens at different ones.
+            const int begin = g.mine < p.groups ? g.begin : 0, turn = (in & ~3) + lane_id() / L;
+#pragma unroll 4
+            for (int i = 0; i < share; ++i) meet(begin + ((i + turn) & (share - 1)));
+        } else {
+#pragma unroll 4
+            for (int e = g.begin; e < g.end; ++e) meet(e);
         }
         if (g.parts > 1) best_two<1>(a, b);
         if (g.parts > 2) best_two<2>(a, b);
@@ -601,13 +609,15 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         }
     };
     const std::integral_constant<int, V> all;
-    const std::integral_constant<int, (V > 9 ? 9 : V)> nine;
+    // With M places an element past the lane's first M + 1 is that one again, at once: neighbours that are equal, and not sure.  Four are enough for all but 1e-4 of tokens
+    // that choose eight of 256; where nothing else is unsure, nine.
+    const std::integral_constant<int, (V <= 9 ? V : BF16 && !SCORES ? 9 : 4)> some;
     number();
-    if (V > 9 && p.k <= 8) take(nine, p.k + 1);
+    if (V > 9 && p.k <= 8) take(some, p.k + 1);
     else take(all, p.k + 1);
     const uint32_t right = static_cast<uint32_t>(__shfl_down(static_cast<int>(mine), 1, kWave)), after = in == p.k - 1 ? next : right;
     const float gap = static_cast<float>(mine >> kIdBits) - static_cast<float>(after >> kIdBits);
-    const bool certain = in >= p.k || mine == 0u || (BF16 && p.bias == nullptr) || (gap > apart && mine >> kIdBits > 1u);
+    const bool certain = in >= p.k || mine == 0u || (mine != after && ((BF16 && p.bias == nullptr) || (gap > apart && mine >> kIdBits > 1u)));
     if (!(BF16 && !SCORES) && __ballot(!certain) != 0ull) {
         // Neighbours that classes do not tell apart: the L best by class, a lane each, put in order by their keys in 64 bits.  The k best are among them if the
         // last one is clearly behind the k-th, or there are no more.
@@ -650,14 +660,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteCall p)
     load_row<V, P, BF16>(at, first, p.E, -INFINITY, l);
     if constexpr (SCORES) load_bias<V, P>(p, first, bias);
     float most = -INFINITY;
-    uint32_t bits = 0u;
+    bool nan = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         most = fmaxf(most, l[v]);  // (ignores a NaN)
-        bits = max(bits, __float_as_uint(l[v]) & 0x7fffffffu);
+        nan |= l[v] != l[v];
     }
     most = token_max<L>(most);
-    const bool broken = token_max_u32<L>(bits) > 0x7f800000u || (!SIGMOID && most == INFINITY);
+    const bool broken = (__ballot(nan) >> (lane_id() & ~(L - 1)) & ((1ull << L) - 1ull)) != 0ull || (!SIGMOID && most == INFINITY);
     const float base = most == -INFINITY ? 0.0f : most;
     const bool share = p.renormalize && p.k > 1;
     float sum = 0.0f;

@@ -57,6 +57,26 @@ def test_sizes(T, E, k, dt, score):
     _check(l, k, bias, score=score, renormalize=True)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("score", [R.SOFTMAX, R.SIGMOID])
+@pytest.mark.parametrize("groups", [1, 4])
+def test_the_best_ones_far_apart_in_one_stride(dt, score, groups):
+    """Five to sixteen of the best experts at 4 i .. 4 i + 3 past multiples of 64: as a wavefront deals them out, one lane's."""
+    r = torch.Generator().manual_seed(3)
+    for E in (256, 512):
+        l = _logits(96, E, dt, E).clamp(-3, 3)
+        for t in range(96):
+            first = 4 * int(torch.randint(0, 16 if E == 256 else 32, (1,), generator=r))
+            at = (torch.arange(E) % (E // 4) >= first) & (torch.arange(E) % (E // 4) < first + 4)
+            ids = torch.nonzero(at).flatten()
+            ids = ids[torch.randperm(len(ids), generator=r)][:5 + t % 12]
+            l[t, ids] = (4 + torch.randperm(64, generator=r)[:len(ids)] / 16).to(dt)
+        bias = 0.01 * torch.randn(E, generator=r)
+        for b in (None, bias):
+            for best in (1, 2) if groups > 1 else (1,):
+                _check(l, 8, b, score=score, groups=groups, top_groups=min(groups, 3), group_best=best, renormalize=True)
+
+
 @pytest.mark.parametrize("E", [64, 256, 512])
 def test_a_bias_that_begins_anywhere(E):
     """A layer's part of all layers' biases."""
