@@ -1,5 +1,7 @@
 // moe_combine_topk, moe_combine_backward: the sorted rows of a token's assignments, summed by their weights, and the gradients of that.
-// Streams over rows: 16 bytes of a row a lane.
+// Streams over rows: 16 bytes of a row a lane.  HBM bounds them: 16384 tokens of 8 assignments, rows of 4 KiB, 605 MB in 105 us, 5.8 TB/s, the rate of a copy
+// (a token a group of 64 lanes in the first form: 139); gradients of 8192 x 8 571 MB in 107, 5.3 TB/s (141).  Short calls: 4.0 and 4.4 us for 333 x 6 rows of 4 KiB and
+// 129 x 3 of 2 KiB, a launch and two loads that follow one another.
 #include "product.hpp"
 
 namespace exf {
@@ -135,8 +137,9 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const CombineGrad
         }
 }
 
-// Rows of more than 32 pieces: a token a wavefront, or `waves` (1, 2, 4) of them a token, which share its columns: a row is read at one time.  Its positions and weights are fetched by a lane each and handed out on the scalar path, those of the
-// wavefront's next token while this one's rows travel, and U pieces a lane of every row are in flight.
+// Rows of more than 32 pieces: a token a wavefront, or `waves` (1, 2, 4) of them a token, which share its columns: a row is read at one time.  Its positions and
+// weights are fetched by a lane each and handed out on the scalar path, those of the wavefront's next token while this one's rows travel, and U pieces a lane of
+// every row are in flight.
 constexpr int kRowsPieces = 2;
 
 struct Assigned {  // what lane j has of slot j
