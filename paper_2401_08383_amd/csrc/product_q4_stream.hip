@@ -239,7 +239,8 @@ bool q4_streams(int64_t A, int n, int, int E_local)
 
 // Tiles, us, as above.  32 x 256 a workgroup, in units of 128 so that three fit a compute unit, where many rows share what it costs to turn codes into numbers and a
 // workgroup a compute unit is left, otherwise 16 x 128: 2048, 8, 4096 x 4096 111 and 162; 2048, 64, 4096 x 1024 43.7 and 49.6; 512, 8, 4096 x 4096 43 and 49; but 1024,
-// 64, 4096 x 1024 41 and 31; 512, 2, 2048 x 2048 (128 workgroups) 21 and 15.  Of 64 columns and with two shares of the reduction while these are up to three a compute
+// 64, 4096 x 1024 41 and 31; 512, 2, 2048 x 2048 (128 workgroups) 21 and 15.  64 x 256 from two workgroups a compute unit on: 8192, 8, 4096 x 4096 353 and 419 (32 x 256);
+// 2048, 8, 4096 x 4096 99 and 116; 2048, 4, 8192 x 2048 111 and 141; but 1500, 1, 4096 x 4096 (384 workgroups) 94 and 92; 512, 8, 4096 x 4096 63 and 42.  Of 64 columns and with two shares of the reduction while these are up to three a compute
 // unit: 5, 5, 8192 x 4096 22.9 and 23.8; 10, 10, 4096 x 4096 28.9 and 34.3; 509, 12, 696 x 11456 56 and 66; but 12, 12, 4096 x 2048 14.7 and 14.2; 115, 2, 7488 x 128 9.1 and
 // 6.2.  With four shares while they are one a compute unit and a share has some units: 1, 1, 16384 x 16384 29.6 and 34.3; 43, 10, 1200 x 4096 10.9 and 11.7; but 4, 4, 4096 x
 // 1024 6.0 and 5.5.  A third slot in LDS gained nothing, here or there (12.2 for 12.2 and 17.7 for 17.1; 488 for 433).
@@ -267,6 +268,7 @@ int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
     const std::true_type yes;
     const std::false_type no;
     const Q4Spread s = spread_of(p.max_rows, p.N, p.E_local);
+    const bool tallest = s.mean > 48 && s.experts * ((s.mean + 63) / 64) * ((p.N + 255) / 256) >= 512;
     const bool tall = s.mean > 24 && s.experts * ((s.mean + 31) / 32) * ((p.N + 255) / 256) >= 256, few = s.workgroups <= 768, fewest = s.workgroups <= 256 && p.K >= 2048;
     const bool past = static_cast<int64_t>(p.E_local) * p.N * p.K / 2 > (int64_t{256} << 20);
     pick_q4_group(group, [&](auto size) {
@@ -276,7 +278,8 @@ int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
                     if (p.K % decltype(unit)::value != 0) return run_with(yes);
                 run_with(no);  // (a unit that is a group always fits)
             };
-            if (tall) ends(step, [&](auto odd) { run(size, step, two, four, one, no, odd, zero); });
+            if (tallest) ends(step, [&](auto odd) { run(size, step, four, four, one, no, odd, zero); });
+            else if (tall) ends(step, [&](auto odd) { run(size, step, two, four, one, no, odd, zero); });
             else if (fewest) ends(steps, [&](auto odd) { run(size, steps, one, one, four, no, odd, zero); });
             else if (few) ends(steps, [&](auto odd) { run(size, steps, one, one, two, no, odd, zero); });
             else if (past) ends(steps, [&](auto odd) { run(size, steps, one, two, one, yes, odd, zero); });

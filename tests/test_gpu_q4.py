@@ -131,7 +131,7 @@ def test_product_of_steps_that_are_not_full(k, group, dt):
 # (rows of the experts, n, k): many rows an expert; few columns for the chip, and still fewer with a long reduction; enough.  Of each, reductions that end with a line
 # of a column, inside one with whole and with odd numbers of groups, and inside the first.
 SPREADS = {"tall": ([64, 50, 0, 100, 64, 17, 130, 64], 4096, (128, 384, 32, 96, 160, 192)), "few": ([1, 0, 3, 1, 2, 1, 16, 1], 4104, (512, 384, 32, 288, 352, 320)),
-           "fewest": ([3, 2], 8192, (2048, 2176, 2080, 2112, 2272)), "wide": ([1, 4, 1, 0, 17, 1, 9, 1, 1, 1, 1, 1, 3], 4160, (256, 640, 64, 96, 288, 192))}
+           "tallest": ([64, 70, 1, 130, 0, 64, 129, 64], 16392, (128, 384, 32, 96, 160, 192)), "fewest": ([3, 2], 8192, (2048, 2176, 2080, 2112, 2272)), "wide": ([1, 4, 1, 0, 17, 1, 9, 1, 1, 1, 1, 1, 3], 4160, (256, 640, 64, 96, 288, 192))}
 
 
 @pytest.mark.parametrize("spread,k,group", [(name, k, group) for name, (_, _, ks) in SPREADS.items() for k in ks for group in (32, 64, 128) if k % group == 0])
