@@ -134,8 +134,8 @@ __device__ __forceinline__ void store_row(void* row, int first, int E, const flo
 __device__ __forceinline__ float exp_below(float x)
 {
     x = x < -200.0f ? -200.0f : x;
-    const float t = x * 1.442695041f, rest = fmaf(x, 1.925963033e-8f, fmaf(x, 1.442695041f, -t)), whole = rintf(t);
-    return ldexpf(__builtin_amdgcn_exp2f((t - whole) + rest), static_cast<int>(whole));
+    const float whole = rintf(x * 1.442695041f);
+    return ldexpf(__builtin_amdgcn_exp2f(fmaf(x, 1.925963033e-8f, fmaf(x, 1.442695041f, -whole))), static_cast<int>(whole));
 }
 // a / b for b in [1/2, 16] and a in [0, b], to a unit.
 __device__ __forceinline__ float quotient(float a, float b)
