@@ -219,6 +219,17 @@ def test_quantised_and_multiplied():
         assert torch.equal(exf.moe_grouped_product_q4(x[10:49], torch.tensor([0, 39], dtype=torch.int32, device=DEV), few).double(), y[10:49])
 
 
+@pytest.mark.parametrize("symmetric", [False, True])
+def test_rows_past_32_bits_of_elements(symmetric):
+    """The last rows of 2.2 G values are held and given back as they are by themselves."""
+    x = torch.empty((270000, 8192), dtype=BF, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(1))
+    m = exf.q4_quantize(x, 128, symmetric=symmetric)
+    end = slice(270000 - 40, 270000)
+    few = exf.q4_quantize(x[end], 128, symmetric=symmetric)
+    assert torch.equal(m.q[end], few.q) and torch.equal(m.scale[end], few.scale) and (symmetric or torch.equal(m.zero[end], few.zero))
+    assert torch.equal(exf.q4_dequantize(m, out=x)[end], exf.q4_dequantize(few))
+
+
 def test_weights_past_32_bits_of_bytes():
     """4.6 GB of codes: the last expert's product is that of the expert by itself."""
     E, n, k = 3, 1 << 17, 24576
