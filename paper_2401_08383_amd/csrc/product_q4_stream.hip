@@ -108,6 +108,19 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
                     }
                 }
         };
+        // What this wavefront copied of the rows, in the order of the codes, once for the four that share it: 421 us for 428 (512 rows over 64 of 16384 x 4096), 387 for 397
+        // (64 rows).  Otherwise each puts what it multiplies in order: where it has 64 columns (512 rows over 8 of 4096 x 4096 39.5, once 44) or shares the reduction
+        // (7 over 3 of 13232 x 15488 97, once 120).
+        constexpr bool kOnce = R == 1 && KS == 1;
+        auto put_in_order = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < Ring::kRowLoads; ++i)
+                if ((i * 4 + wave) * (512 / U) < rows) {
+                    unsigned char* const at = smem + (share * 2 + t % 2) * Ring::kRows + (i * 4 + wave) * 1024 + lane * 16;
+                    const bf16x8_t v = in_code_order(*reinterpret_cast<const uint4*>(at));
+                    __builtin_memcpy(__builtin_assume_aligned(at, 16), &v, 16);
+                }
+        };
         f32x4_t total[R][C];
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -159,7 +172,8 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
                             const int piece = TURN ? m * 4 + quad : quad * 4 + m;
-                            a[r] = in_code_order(*reinterpret_cast<const uint4*>(shared + (r * 16 + in16) * (U * 2) + (h * 16 + (piece ^ in16)) * 16));
+                            const uint4 v = *reinterpret_cast<const uint4*>(shared + (r * 16 + in16) * (U * 2) + (h * 16 + (piece ^ in16)) * 16);
+                            a[r] = kOnce ? as_bf16x8(v.x, v.y, v.z, v.w) : in_code_order(v);
                             sum_x[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[r], ones_bf16(), sum_x[r], 0, 0, 0);
                         }
 #pragma unroll
@@ -183,6 +197,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
         if (KS == 1 || own > 0) issue(0);
         for (int t = 0; t < turns; ++t) {
             wait_vmcnt<0>();
+            if (kOnce) put_in_order(t);
             barrier_for_lds();
             if (t + 1 < own) issue(t + 1);
             if (KS == 1 || t < own) multiply(t);
