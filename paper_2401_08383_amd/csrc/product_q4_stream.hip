@@ -233,34 +233,37 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
     }
 }
 
-// What the choice goes by: tiles of 16 rows, were the rows spread evenly over the experts that can have any, and how many workgroups these are with 64 columns each.
+// What the choice goes by: tiles, were the rows spread evenly over the experts that can have any.
 struct Q4Spread {
-    int64_t experts, mean, workgroups;
+    int64_t experts, mean;
+    int N;
+    Q4Spread(int64_t A, int n, int E_local) : experts(A < E_local ? A : E_local), mean((A + experts - 1) / experts), N(n) {}
+    int64_t of_rows(int rows) const { return (mean + rows - 1) / rows; }  // of an expert
+    int64_t workgroups(int rows, int cols) const { return experts * of_rows(rows) * ((N + cols - 1) / cols); }
 };
-static Q4Spread spread_of(int64_t A, int n, int E_local)
-{
-    const int64_t experts = A < E_local ? A : E_local, mean = (A + experts - 1) / experts;
-    return {experts, mean, experts * ((mean + 15) / 16) * ((n + 63) / 64)};
-}
 
 // Workgroups for two thirds of the compute units; half of that where a tile has more than 8 rows, which the other kernel loads over and over.  Streamed and not, us (rows,
 // experts, columns x reduction): 512, 64, 16384 x 4096 411 and 946; 1024, 64, 4096 x 1056 57 and 96; 1, 1, 16384 x 4096 11.4 and 15.3; 43, 10, 1200 x 4096 10.9 and 13.5;
 // 100, 6, 512 x 8192 16.4 and 23.2; but 8, 8, 1024 x 4096 10.5 and 9.1; 16, 1, 4096 x 4096 10.2 and 8.5; 1, 1, 4096 x 1024 5.3 and 4.5; 66, 4, 352 x 10624 22 and 15.8.
 bool q4_streams(int64_t A, int n, int, int E_local)
 {
-    const Q4Spread s = spread_of(A, n, E_local);
-    return s.workgroups * (s.mean > 8 ? 2 : 1) >= 160;
+    const Q4Spread s(A, n, E_local);
+    return s.workgroups(16, 64) * (s.mean > 8 ? 2 : 1) >= 160;
 }
 
-// Tiles, us, as above.  32 x 256 a workgroup, in units of 128 so that three fit a compute unit, where many rows share what it costs to turn codes into numbers and a
-// workgroup a compute unit is left, otherwise 16 x 128: 2048, 8, 4096 x 4096 111 and 162; 2048, 64, 4096 x 1024 43.7 and 49.6; 512, 8, 4096 x 4096 43 and 49; but 1024,
-// 64, 4096 x 1024 41 and 31; 512, 2, 2048 x 2048 (128 workgroups) 21 and 15.  64 x 256 from two workgroups a compute unit on: 8192, 8, 4096 x 4096 353 and 419 (32 x 256);
-// 2048, 8, 4096 x 4096 99 and 116; 2048, 4, 8192 x 2048 111 and 141; but 1500, 1, 4096 x 4096 (384 workgroups) 94 and 92; 512, 8, 4096 x 4096 63 and 42.  Of 64 columns and with two shares of the reduction while these are up to three a compute
-// unit: 5, 5, 8192 x 4096 22.9 and 23.8; 10, 10, 4096 x 4096 28.9 and 34.3; 509, 12, 696 x 11456 56 and 66; but 12, 12, 4096 x 2048 14.7 and 14.2; 115, 2, 7488 x 128 9.1 and
-// 6.2.  With four shares while they are one a compute unit and a share has some units: 1, 1, 16384 x 16384 29.6 and 34.3; 43, 10, 1200 x 4096 10.9 and 11.7; but 4, 4, 4096 x
-// 1024 6.0 and 5.5.  A third slot in LDS gained nothing, here or there (12.2 for 12.2 and 17.7 for 17.1; 488 for 433).
-//   Weights that the 256 MB behind the L2 cannot hold until the next call go past the caches: 411 us for 512, 64, 16384 x 4096, 426 otherwise (64 rows: 385 and
-// 402); weights that it can hold do not, 31.2 and 36.1 (1024, 64, 4096 x 1024, called again and again).
+// Tiles, rows x columns, us, as above.
+//   64 x 256, units of 128, where the rows fill them and two workgroups a compute unit are left (what turns codes into numbers is shared by the rows), not 32 x 256: 8192, 8, 4096 x 4096
+// 353 and 419; 2048, 32, 4096 x 2048 70 and 76; but 1500, 1, 4096 x 4096 94 and 92; 2048, 40, 4096 x 2048 (51 rows of 64) 98 and 93.
+//   32 x 256, units of 128 so that three fit a compute unit, for nearly that many, not 32 x 128: 1500, 1, 4096 x 4096 86 and 98; 1500, 16, 4096 x 2048 48 and 55; but 600, 2, 8192 x 8192
+// 207 and 183; 1280, 64, 4096 x 4096 213 and 153.
+//   32 x 128 where an expert has more than 16 rows, not 16 x 128: 1280, 64, 16384 x 4096 608 and 717; 512, 16, 4096 x 4096 37 and 47; 256, 8, 4096 x 4096 24.6 and 27.1; but from 160
+// workgroups on, with fewer 16 x 64: 80, 3, 8192 x 4096 24.5 and 25.2; 200, 8, 2048 x 2048 17.5 and 13.0.
+//   16 x 64 with two shares of the reduction while 16 x 128 has less than one and a half workgroups a compute unit: 5, 5, 8192 x 4096 22.9 and 23.8; 10, 10, 4096 x 4096 28.9 and 34.3; but 12, 12,
+// 4096 x 2048 14.7 and 14.2; 115, 2, 7488 x 128 9.1 and 6.2.  With four shares while they are one a compute unit and a share has some units: 1, 1, 16384 x 16384 29.6 and 34.3;
+// 43, 10, 1200 x 4096 10.9 and 11.7; but 4, 4, 4096 x 1024 6.0 and 5.5.
+//   A third slot in LDS gained nothing (12.2 for 12.2, 17.7 for 17.1, 488 for 433).
+//   Weights that are read once and that the 256 MB behind the L2 cannot hold until the next call go past the caches: 411 us for 512, 64, 16384 x 4096, 426 otherwise (64 rows: 385 and 402; 1280
+// rows 588 and 608); weights that it can hold do not, 31.2 and 36.1 (1024, 64, 4096 x 1024, called again and again).
 int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
 {
     int rc = EXF_OK;
@@ -282,10 +285,10 @@ int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
     const std::integral_constant<int, 256> steps;
     const std::true_type yes;
     const std::false_type no;
-    const Q4Spread s = spread_of(p.max_rows, p.N, p.E_local);
-    const bool tallest = s.mean > 48 && s.experts * ((s.mean + 63) / 64) * ((p.N + 255) / 256) >= 512;
-    const bool tall = s.mean > 24 && s.experts * ((s.mean + 31) / 32) * ((p.N + 255) / 256) >= 256, few = s.workgroups <= 768, fewest = s.workgroups <= 256 && p.K >= 2048;
-    const bool past = static_cast<int64_t>(p.E_local) * p.N * p.K / 2 > (int64_t{256} << 20);
+    const Q4Spread s(p.max_rows, p.N, p.E_local);
+    const bool tallest = s.mean > 48 && s.workgroups(64, 256) >= 512 && 8 * s.mean >= 7 * 64 * s.of_rows(64), tall = s.mean > 48 && s.workgroups(32, 256) >= 700;
+    const bool two_tiles = s.mean > 16 && s.workgroups(32, 128) >= 160, few = s.workgroups(16, 64) <= 768, fewest = s.workgroups(16, 64) <= 256 && p.K >= 2048;
+    const bool past = s.mean <= 32 && static_cast<int64_t>(p.E_local) * p.N * p.K / 2 > (int64_t{256} << 20);
     pick_q4_group(group, [&](auto size) {
         auto with = [&](auto zero) {
             auto ends = [&](auto unit, auto run_with) {
@@ -295,6 +298,8 @@ int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream)
             };
             if (tallest) ends(step, [&](auto odd) { run(size, step, four, four, one, no, odd, zero); });
             else if (tall) ends(step, [&](auto odd) { run(size, step, two, four, one, no, odd, zero); });
+            else if (two_tiles && past) ends(steps, [&](auto odd) { run(size, steps, two, two, one, yes, odd, zero); });
+            else if (two_tiles) ends(steps, [&](auto odd) { run(size, steps, two, two, one, no, odd, zero); });
             else if (fewest) ends(steps, [&](auto odd) { run(size, steps, one, one, four, no, odd, zero); });
             else if (few) ends(steps, [&](auto odd) { run(size, steps, one, one, two, no, odd, zero); });
             else if (past) ends(steps, [&](auto odd) { run(size, steps, one, two, one, yes, odd, zero); });

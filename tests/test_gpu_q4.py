@@ -130,8 +130,8 @@ def test_product_of_steps_that_are_not_full(k, group, dt):
 
 # (rows of the experts, n, k): many rows an expert; few columns for the chip, and still fewer with a long reduction; enough.  Of each, reductions that end with a line
 # of a column, inside one with whole and with odd numbers of groups, and inside the first.
-SPREADS = {"tall": ([64, 50, 0, 100, 64, 17, 130, 64], 4096, (128, 384, 32, 96, 160, 192)), "few": ([1, 0, 3, 1, 2, 1, 16, 1], 4104, (512, 384, 32, 288, 352, 320)),
-           "tallest": ([64, 70, 1, 130, 0, 64, 129, 64], 16392, (128, 384, 32, 96, 160, 192)), "fewest": ([3, 2], 8192, (2048, 2176, 2080, 2112, 2272)), "wide": ([1, 4, 1, 0, 17, 1, 9, 1, 1, 1, 1, 1, 3], 4160, (256, 640, 64, 96, 288, 192))}
+SPREADS = {"two tiles": ([64, 50, 0, 100, 64, 17, 130, 64], 4096, (128, 384, 32, 96, 160, 192, 256, 512, 288, 320)), "tall": ([64, 50, 0, 100, 64, 17, 130, 64], 12288, (128, 384, 32, 96, 160, 192)), "few": ([1, 0, 3, 1, 2, 1, 16, 1], 4104, (512, 384, 32, 288, 352, 320)),
+           "tallest": ([64, 70, 1, 130, 0, 64, 100, 64], 16392, (128, 384, 32, 96, 160, 192)), "fewest": ([3, 2], 8192, (2048, 2176, 2080, 2112, 2272)), "wide": ([1, 4, 1, 0, 17, 1, 9, 1, 1, 1, 1, 1, 3], 4160, (256, 640, 64, 96, 288, 192))}
 
 
 @pytest.mark.parametrize("spread,k,group", [(name, k, group) for name, (_, _, ks) in SPREADS.items() for k in ks for group in (32, 64, 128) if k % group == 0])
@@ -142,15 +142,16 @@ def test_product_of_many_columns(spread, k, group):
 
 
 @pytest.mark.parametrize("k,group", [(k, group) for k in (512, 544, 576, 640) for group in (32, 64, 128) if k % group == 0])
-def test_product_of_weights_that_no_cache_holds(k, group):
-    """Six rows of four of 64 experts, the last among them."""
+@pytest.mark.parametrize("some", [(1, 2, 1, 2), (33, 1, 17, 25)])
+def test_product_of_weights_that_no_cache_holds(k, group, some):
+    """Rows of four of 64 experts, the last among them."""
     E, n, g = 64, 17000, torch.Generator(DEV).manual_seed(k + group)
     q = torch.empty((E, n, k // 2), dtype=torch.uint8, device=DEV).random_(generator=g)
     scale = torch.empty((E, n, k // group), dtype=BF, device=DEV).uniform_(0.01, 0.05, generator=g)
     zero = torch.empty((E, n, k // group), dtype=torch.uint8, device=DEV).random_(0, 17, generator=g)
-    x = torch.randn((6, k), generator=torch.Generator().manual_seed(3)).to(BF).to(DEV)
+    x = torch.randn((sum(some) if sum(some) < 64 else 1100, k), generator=torch.Generator().manual_seed(3)).to(BF).to(DEV)  # (rows behind the last expert's count as rows)
     sizes = [0] * E
-    sizes[0], sizes[5], sizes[40], sizes[63] = 1, 2, 1, 2
+    sizes[0], sizes[5], sizes[40], sizes[63] = some
     off = sizes_to_offsets(sizes)
     for z in (zero, None):
         y = exf.moe_grouped_product_q4(x, off.to(DEV), exf.Q4(q, scale, z))
@@ -162,7 +163,7 @@ def test_product_of_weights_that_no_cache_holds(k, group):
             R.assert_close(y[lo:hi].cpu(), ref.cpu(), mag.cpu(), 4 * (k / 16 + k / group + 8), f"expert {e}")
 
 
-@pytest.mark.parametrize("spread,k", [("tall", 160), ("few", 352), ("fewest", 2080), ("wide", 288), ("few", 512), ("tall", 128)])
+@pytest.mark.parametrize("spread,k", [("tall", 160), ("two tiles", 288), ("tallest", 96), ("few", 352), ("fewest", 2080), ("wide", 288), ("few", 512), ("tall", 128), ("two tiles", 512), ("tallest", 128)])
 def test_what_is_no_number_stays_in_its_row_and_column(spread, k):
     """... also where a step reads past the end of one into the next."""
     sizes, n, _ = SPREADS[spread]
