@@ -109,8 +109,8 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
                 }
         };
         // What this wavefront copied of the rows, in the order of the codes, once for the four that share it: 421 us for 428 (512 rows over 64 of 16384 x 4096), 387 for 397
-        // (64 rows).  Otherwise each puts what it multiplies in order: where it has 64 columns (512 rows over 8 of 4096 x 4096 39.5, once 44) or shares the reduction
-        // (7 over 3 of 13232 x 15488 97, once 120).
+        // (64 rows).  Otherwise each puts what it multiplies in order: where it has 64 columns (512 rows over 8 of 4096 x 4096 in such tiles 39.5, once 44) or shares the reduction
+        // (7 over 3 of 13232 x 15488 97, once 120), and where there are 32 rows (512 over 8 of 4096 x 4096 39.8, once 41.7).
         constexpr bool kOnce = R == 1 && KS == 1;
         auto put_in_order = [&](int t) {
 #pragma unroll
