@@ -44,7 +44,8 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
     const int lane = lane_id(), in16 = lane & 15, quad = lane >> 4, nth = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wave = nth % 4, share = nth / 4;
     const ExpertRows range = expert_rows(p.offsets, p.E_local, p.max_rows);
     const int tiles = (range.hi - range.lo + 16 * R - 1) / (16 * R), upto = wave_inclusive_scan(tiles);
-    const int64_t N = p.N, groups = p.K / GROUP;
+    const int64_t N = p.N;
+    const int groups = p.K / GROUP;
     const int units = (p.K + Ring::kUnit - 1) / Ring::kUnit, turns = (units + KS - 1) / KS, own = (units - share + KS - 1) / KS;
     const uint32_t rows_at = smem_addr + share * (2 * Ring::kRows), mine_at = smem_addr + KS * 2 * Ring::kRows + nth * (2 * Ring::kWave64);
     const CodeBits bits = code_bits();
@@ -60,18 +61,20 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
         const unsigned char* scales = uniform_ptr(static_cast<const unsigned char*>(p.scale) + first_col * groups * 2);
         const unsigned char* zeros = uniform_ptr(ZERO ? p.zero + first_col * groups : nullptr);
         const unsigned char* x = uniform_ptr(static_cast<const unsigned char*>(p.rows) + static_cast<int64_t>(lo) * p.K * 2);
+        // (Products of 24 bits: the wider form writes a scalar register pair too, which the loads that follow, in assembly, must not read at once.)
+        static_assert(EXF_MAX_PRODUCT_WIDTH <= 1 << 22, "twice a reduction has 24 bits");
         uint32_t code_at[Ring::kCodeLoads], row_at[Ring::kRowLoads];
 #pragma unroll
         for (int i = 0; i < Ring::kCodeLoads; ++i) {
             constexpr int kPieces = U / 32;  // of a column
             const int c = i * (64 / kPieces) + lane / kPieces;
-            code_at[i] = static_cast<uint32_t>(max(min(c, cols - 1), 0)) * static_cast<uint32_t>(p.K / 2) + ((lane ^ (c / (16 / kPieces))) % kPieces) * 16;
+            code_at[i] = __umul24(max(min(c, cols - 1), 0), p.K / 2) + ((lane ^ (c / (16 / kPieces))) % kPieces) * 16;
         }
 #pragma unroll
         for (int i = 0; i < Ring::kRowLoads; ++i) {
             constexpr int kPieces = U / 8;  // of a row
             const int r = (i * 4 + wave) * (64 / kPieces) + lane / kPieces;
-            row_at[i] = static_cast<uint32_t>(min(r, rows - 1)) * static_cast<uint32_t>(p.K * 2) + ((lane % kPieces) ^ (r & 15)) * 16;
+            row_at[i] = __umul24(min(r, rows - 1), p.K * 2) + ((lane % kPieces) ^ (r & 15)) * 16;
         }
         // What a unit has behind the end of a column or row is the next one's, and not used; of the last ones of all it is the last piece there is.
         const int64_t cols_left = p.E_local * N - first_col, rows_left = p.max_rows - lo;
@@ -93,7 +96,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
             for (int i = 0; i < Ring::kScaleLoads; ++i) {
                 const int l = i * 64 + lane;
                 if (l < Ring::kScaleLanes) {
-                    const uint32_t column = static_cast<uint32_t>(max(min(Ring::kWide ? l : l / Ring::kScaleWords, cols - 1), 0)) * static_cast<uint32_t>(groups * 2);
+                    const uint32_t column = __umul24(max(min(Ring::kWide ? l : l / Ring::kScaleWords, cols - 1), 0), groups * 2);
                     if constexpr (Ring::kWide) lds_dma_16B(scales + u * 16, column, mine + Ring::kCodes + i * 1024);
                     else lds_dma_4B(scales, within((column + u * Ring::kGroups * 2 + l % Ring::kScaleWords * 4) & ~3u, cols_left * groups * 2 - 4), mine + Ring::kCodes + i * 256);
                 }
@@ -103,7 +106,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
                 for (int i = 0; i < Ring::kZeroLoads; ++i) {
                     const int l = i * 64 + lane;
                     if (l < Ring::kZeroLanes) {
-                        const uint32_t at = static_cast<uint32_t>(max(min(l / Ring::kZeroWords, cols - 1), 0)) * static_cast<uint32_t>(groups) + u * Ring::kGroups + l % Ring::kZeroWords * 4;
+                        const uint32_t at = __umul24(max(min(l / Ring::kZeroWords, cols - 1), 0), groups) + u * Ring::kGroups + l % Ring::kZeroWords * 4;
                         lds_dma_4B(zeros, within(at & ~3u, cols_left * groups - 4), mine + Ring::kCodes + Ring::kScales + i * 256);
                     }
                 }
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
             float scale[C][Ring::kGroups], zero[C][Ring::kGroups];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const uint32_t first = static_cast<uint32_t>(max(min(c * 16 + in16, cols - 1), 0)) * static_cast<uint32_t>(groups) + u * Ring::kGroups;
+                const uint32_t first = __umul24(max(min(c * 16 + in16, cols - 1), 0), groups) + u * Ring::kGroups;
                 uint32_t s[Ring::kScaleWords], z[Ring::kZeroWords];
                 __builtin_memcpy(s, __builtin_assume_aligned(mine + Ring::kCodes + (c * 16 + in16) * Ring::kScaleWords * 4, ODD ? 4 : Ring::kScaleWords * 4), sizeof(s));
                 if constexpr (ODD || Ring::kGroups == 1) from_byte(s, (first & 1u) * 2);
