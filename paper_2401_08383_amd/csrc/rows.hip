@@ -1,4 +1,5 @@
-// moe_combine_topk, moe_combine_backward: the sorted rows of a token's assignments, summed by their weights, and the gradients of that.
+// moe_combine_topk, moe_combine_backward: the sorted rows of a token's assignments, summed by their weights, and the gradients of that; and the rows of
+// moe_dispatch_topk's long lists.
 // Streams over rows: 16 bytes of a row a lane.  HBM bounds them: 16384 tokens of 8 assignments, rows of 4 KiB, 605 MB in 105 us, 5.8 TB/s, the rate of a copy
 // (a token a group of 64 lanes in the first form: 139); gradients of 8192 x 8 571 MB in 107, 5.3 TB/s (141).  Short calls: 4.0 and 4.4 us for 333 x 6 rows of 4 KiB and
 // 129 x 3 of 2 KiB, a launch and two loads that follow one another.
@@ -279,6 +280,61 @@ __global__ __launch_bounds__(256) void combine_backward_wave_kernel(const Combin
     }
 }
 
+// Rows of moe_dispatch_topk: a token's row is read once and written to the places of its assignments.  HBM bounds it, and how writes of a row each fill its pages: 16384
+// tokens of 8, rows of 4 KiB, 604 MB 133 us with the list's positions (13), of which 119 for the rows, 5.1 TB/s; two wavefronts a token with streaming stores 138, four 131, a wavefront with
+// these 136; rows in the order of their places, each read for itself, 166 (of the dispatch of one or two assignments 188).  8192 tokens 58, 73, 71, 72, 86 and 90.
+struct SpreadCall {
+    const uint4* x;           // [T, vecs]
+    const int32_t* position;  // [T,k]
+    uint4* out;               // [A, vecs]
+    int64_t T;
+    int k, vecs, lanes;
+};
+__global__ __launch_bounds__(256) void spread_kernel(const SpreadCall p)
+{
+    const int64_t A = p.T * p.k, step = static_cast<int64_t>(gridDim.x) * (256 / p.lanes);
+    const int in = threadIdx.x & (p.lanes - 1);
+    for (int64_t t = static_cast<int64_t>(blockIdx.x) * (256 / p.lanes) + threadIdx.x / p.lanes; t < p.T; t += step)
+        for (int c = in; c < p.vecs; c += p.lanes) {
+            const uint4 v = p.x[t * p.vecs + c];
+            for (int j0 = 0; j0 < p.k; j0 += kRowsAhead) {
+                int64_t at[kRowsAhead];
+#pragma unroll
+                for (int j = 0; j < kRowsAhead; ++j) at[j] = j0 + j < p.k ? p.position[t * p.k + j0 + j] : -1;
+#pragma unroll
+                for (int j = 0; j < kRowsAhead; ++j)
+                    if (at[j] >= 0 && at[j] < A) store_stream16(p.out + at[j] * p.vecs + c, v);
+            }
+        }
+}
+// A token a wavefront, all of a row of up to 4 KiB in flight.
+__global__ __launch_bounds__(256) void spread_wave_kernel(const SpreadCall p)
+{
+    constexpr int U = 4;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t A = p.T * p.k, step = static_cast<int64_t>(gridDim.x) * 4;
+    int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    Assigned next = assigned(p.position, nullptr, t, p.T, p.k, A, lane);
+    for (; t < p.T; t += step) {
+        const Assigned mine = next;
+        next = assigned(p.position, nullptr, t + step, p.T, p.k, A, lane);
+        for (int c0 = lane; c0 < p.vecs; c0 += kWave * U) {
+            uint4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c0 + u * kWave < p.vecs) v[u] = load_stream16(p.x + t * p.vecs + c0 + u * kWave);
+            for (int j = 0; j < p.k; ++j) {
+                const int s = wave_read_lane(mine.at, j);
+                if (s < 0) continue;
+                uint4* row = p.out + static_cast<int64_t>(s) * p.vecs;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c0 + u * kWave < p.vecs) row[c0 + u * kWave] = v[u];
+            }
+        }
+    }
+}
+
 static int check_rows(const char* fn, int64_t T, int d, int k, int dt)
 {
     if (dt != EXF_F32 && dt != EXF_BF16) return fail(EXF_ERR_BAD_DTYPE, "%s: dt = %d", fn, dt);
@@ -301,6 +357,16 @@ static unsigned rows_grid(int64_t T, int lanes)
 {
     const int64_t blocks = (T * lanes + 255) / 256;
     return static_cast<unsigned>(blocks < 8 * kStreamWorkgroups ? blocks : 8 * kStreamWorkgroups);
+}
+
+void launch_spread(const void* x, const int32_t* position, int64_t T, int k, int vecs, void* out, hipStream_t stream)
+{
+    // Rows of 1 KiB and less, the list's positions included: 512 bytes of 32768 x 8 43 us with lanes a token, 50 with a wavefront; rows of 2 KiB of 32768 x 4 65 and 67, of 4 KiB of
+    // 8192 x 8 84 and 58.
+    const int lanes = lanes_for(vecs);
+    const SpreadCall p{static_cast<const uint4*>(x), position, static_cast<uint4*>(out), T, k, vecs, lanes};
+    if (vecs > kWave) hipLaunchKernelGGL(spread_wave_kernel, dim3(rows_grid(T, kWave)), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(spread_kernel, dim3(rows_grid(T, lanes)), dim3(256), 0, stream, p);
 }
 
 }  // namespace exf

@@ -75,7 +75,8 @@ def test_gradients(T, d, k, dt, kept):
 
 
 @pytest.mark.parametrize("T,d,k,E_local,E,gather", [(1, 64, 8, 64, 64, True), (50, 64, 16, 16, 512, True), (700, 1032, 8, 64, 64, True), (5000, 64, 10, 64, 64, True), (3000, 8, 5, 7, 30, False),
-                                                    (40000, 8, 16, 64, 64, False), (0, 64, 8, 8, 8, True)])
+                                                    (40000, 8, 16, 64, 64, False), (20000, 8, 16, 33, 64, True), (900, 2056, 5, 16, 300, True), (1400, 512, 3, 64, 64, True),
+                                                    (4099, 520, 16, 64, 64, True), (0, 64, 8, 8, 8, True)])
 def test_dispatch(T, d, k, E_local, E, gather):
     print(f"[case] dispatch T={T} d={d} k={k} E_local={E_local} E={E} gather={gather}", flush=True)
     g = torch.Generator().manual_seed(T + k)
