@@ -307,7 +307,8 @@ __global__ __launch_bounds__(256) void spread_kernel(const SpreadCall p)
             }
         }
 }
-// A token a wavefront, all of a row of up to 4 KiB in flight.
+// A token a wavefront, all of a row of up to 4 KiB in flight.  Not with streaming stores: who reads the rows next finds a part of them behind the L2 (8192 tokens, buffers that change from
+// call to call: 70 us with either, with moe_combine behind it 99 and 122 for both).
 __global__ __launch_bounds__(256) void spread_wave_kernel(const SpreadCall p)
 {
     constexpr int U = 4;
