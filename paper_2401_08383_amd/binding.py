@@ -782,21 +782,28 @@ def moe_grouped_product_q4(x_sorted, expert_offsets, w, bias=None, out=None):
     """moe_grouped_product with weights in 4-bit integers: w a Q4 [E_local,n,k] with scales of the rows' type."""
     if x_sorted.requires_grad or bias is not None and bias.requires_grad or w.scale.requires_grad:
         _untracked("moe_grouped_product_q4", "none: weights in 4 bits are not trained")
-    q, scale, zero, shape = w.q, w.scale, w.zero, w.q.shape
-    if len(shape) != 3 or len(x_sorted.shape) != 2:
-        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(x_sorted.shape)} and {w.shape}")
+    q, scale, zero = w.q, w.scale, w.zero
+    shape, groups, rows = q.shape, scale.shape, x_sorted.shape
+    if len(shape) != 3 or len(rows) != 2:
+        _bad(f"rows are [A,k] and weights [E_local,n,k], got {tuple(rows)} and {w.shape}")
     E, n, k = shape
     k *= 2
-    A, dt, dev = x_sorted.shape[0], x_sorted.dtype, x_sorted.get_device()
+    A, dt, dev = rows[0], x_sorted.dtype, x_sorted.get_device()
     code = _CODES.get(dt)
     if code is None:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
-    group = _expect_q4("w", w, (E, n, k), dt, dev)
+    # (what _expect_q4 finds of the usual case, number by number: a microsecond less)
+    if (len(groups) == 3 and groups[0] == E and groups[1] == n and groups[2] and not k % groups[2] and q.dtype is _UINT8 and scale.dtype is dt and q.is_contiguous()
+            and scale.is_contiguous() and q.get_device() == scale.get_device() == dev
+            and (zero is None or zero.shape == groups and zero.dtype is _UINT8 and zero.is_contiguous() and zero.get_device() == dev)):
+        group = k // groups[2]
+    else:
+        group = _expect_q4("w", w, (E, n, k), dt, dev)
     if out is None:
         out = _rows(A, n, dt, x_sorted.device)
     if bias is not None:
         bias = _expect("bias", bias, (E, n), dt, dev).data_ptr()
-    if not (x_sorted.shape[1] == k and expert_offsets.shape == (E + 1,) and out.shape == (A, n) and out.dtype is dt and expert_offsets.dtype is _INT32
+    if not (rows[1] == k and expert_offsets.shape == (E + 1,) and out.shape == (A, n) and out.dtype is dt and expert_offsets.dtype is _INT32
             and x_sorted.is_contiguous() and out.is_contiguous() and expert_offsets.is_contiguous() and out.get_device() == expert_offsets.get_device() == dev >= 0):
         _misfit(x_sorted, (A, k), expert_offsets, E, scale, out, (A, n), dt, dev)
     rc = lib().moe_grouped_product_q4(x_sorted.data_ptr(), expert_offsets.data_ptr(), q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), bias, A, n, k, group, E, code,
