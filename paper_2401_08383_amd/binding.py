@@ -329,9 +329,8 @@ def _combine_rows(name, y_sorted, sorted_of_src, topk_w, k, out):
     T, A, d, dt, code, dev = _assigned(y_sorted, sorted_of_src, k)
     if out is None:
         out = _rows(T, d, dt, y_sorted.device)
-    if not (y_sorted.shape[0] == A and out.shape == (T, d) and out.dtype is dt and y_sorted.is_contiguous() and out.is_contiguous() and out.get_device() == dev >= 0):
+    if not (out.shape == (T, d) and out.dtype is dt and out.is_contiguous() and out.get_device() == dev):
         _expect("out", out, (T, d), dt, dev)
-        _expect("the sorted rows", y_sorted, (A, d), dt, dev)
     if topk_w is not None:
         topk_w = _expect("topk_w", topk_w, (T, k), _FLOAT, dev).data_ptr()
     if dev < 0:
@@ -355,6 +354,8 @@ def _assigned(rows, sorted_of_src, k):
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
     if not (sorted_of_src.dtype is _INT32 and sorted_of_src.is_contiguous() and sorted_of_src.get_device() == dev):
         _expect("sorted_of_src", sorted_of_src, at, _INT32, dev)
+    if not (shape[0] == A and rows.is_contiguous()):
+        _expect("the sorted rows", rows, (A, shape[1]), dt, dev)
     return A // k, A, shape[1], dt, code, dev
 
 
@@ -363,14 +364,14 @@ def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, 
     (``out``), or zero."""
     if dout.requires_grad or y_sorted.requires_grad or topk_w.requires_grad:
         _untracked("moe_combine_backward", "none: there is no second derivative")
-    if len(topk_w.shape) != 2:
-        _bad(f"topk_w is [T,k], got {tuple(topk_w.shape)}")
-    k = topk_w.shape[1]
+    weights = topk_w.shape
+    if len(weights) != 2:
+        _bad(f"topk_w is [T,k], got {tuple(weights)}")
+    k = weights[1]
     T, A, d, dt, code, dev = _assigned(y_sorted, sorted_of_src, k)
-    if not (dout.shape == (T, d) and y_sorted.shape[0] == A and topk_w.shape[0] == T and dout.dtype is dt and topk_w.dtype is _FLOAT and dout.is_contiguous()
-            and y_sorted.is_contiguous() and topk_w.is_contiguous() and dout.get_device() == topk_w.get_device() == dev):
+    if not (dout.shape == (T, d) and weights[0] == T and dout.dtype is dt and topk_w.dtype is _FLOAT and dout.is_contiguous() and topk_w.is_contiguous()
+            and dout.get_device() == topk_w.get_device() == dev):
         _expect("dout", dout, (T, d), dt, dev)
-        _expect("y_sorted", y_sorted, (A, d), dt, dev)
         _expect("topk_w", topk_w, (T, k), _FLOAT, dev)
     if out is not None:
         _expect("out", out, (A, d), dt, dev)
@@ -379,7 +380,7 @@ def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, 
     if out_weights is not None:
         _expect("out_weights", out_weights, (T, k), _FLOAT, dev)
     elif want_weights:
-        out_weights = _rows(T, k, _FLOAT, dout.device)
+        out_weights = torch.empty_like(topk_w)
     if dev < 0:
         _on_host()
     rc = lib().moe_combine_backward(dout.data_ptr(), y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w.data_ptr(), T, d, k, code, _ptr(out), _ptr(out_weights),
@@ -433,18 +434,19 @@ def moe_route_backward(dtopk_w, logits, topk_idx, score=EXF_SCORE_SOFTMAX, renor
     code = _CODES.get(dt)
     if code is None:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
-    if len(shape) != 2 or len(topk_idx.shape) != 2 or not logits.is_contiguous():
-        _bad(f"logits: contiguous [T,E] expected, topk_idx [T,k], got {tuple(shape)} and {tuple(topk_idx.shape)}")
+    slots = topk_idx.shape
+    if len(shape) != 2 or len(slots) != 2 or not logits.is_contiguous():
+        _bad(f"logits: contiguous [T,E] expected, topk_idx [T,k], got {tuple(shape)} and {tuple(slots)}")
     T, E = shape
-    k, stride, at = topk_idx.shape[1], 0, None
-    if not (topk_idx.shape[0] == T and dtopk_w.shape == topk_idx.shape and topk_idx.dtype is _INT32 and dtopk_w.dtype is _FLOAT and topk_idx.is_contiguous()
+    k, stride, at = slots[1], 0, None
+    if not (slots[0] == T and dtopk_w.shape == slots and topk_idx.dtype is _INT32 and dtopk_w.dtype is _FLOAT and topk_idx.is_contiguous()
             and dtopk_w.is_contiguous() and topk_idx.get_device() == dtopk_w.get_device() == dev):
         _expect("topk_idx", topk_idx, (T, k), _INT32, dev)
         _expect("dtopk_w", dtopk_w, (T, k), _FLOAT, dev)
     if dscores is not None:
         stride = E if len(dscores.shape) == 2 else 0
         at = _expect("dscores", dscores, (T, E) if stride else (E,), _FLOAT, dev).data_ptr()
-    out = _rows(T, E, dt, logits.device) if out is None else _expect("out", out, shape, dt, dev)
+    out = torch.empty_like(logits) if out is None else _expect("out", out, shape, dt, dev)
     if dev < 0:
         _on_host()
     rc = lib().moe_route_backward(dtopk_w.data_ptr(), logits.data_ptr(), topk_idx.data_ptr(), at, stride, T, E, k, score, 1 if renormalize else 0, scale, code,
