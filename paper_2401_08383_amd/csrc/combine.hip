@@ -65,11 +65,11 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint4* __restrict__ 
         };
         const int total = rows * vec_per_row;
         constexpr int kPass = kWave * U;  // output chunks the wavefront produces per pass
-        if (total % kPass == 0) {
-            // Every lane has a chunk in every pass: no condition anywhere near the loads (a dropped
+        const int n_pass = total / kPass;
+        if (n_pass > 0) {
+            // Every lane has a chunk in every whole pass: no condition anywhere near the loads (a dropped
             // assignment reads row 0 and is zeroed afterwards), and the loads of the next pass are issued
             // before this pass is reduced and stored.
-            const int n_pass = total / kPass;
             auto load_pass = [&](int pass, uint4(&v)[U][K], float(&w)[U][K]) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -105,9 +105,9 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint4* __restrict__ 
                     }
             }
             store_pass(n_pass - 1, cur, wcur);
-            continue;
         }
-        for (int c0 = lane; c0 < total; c0 += kWave * U) {  // ragged batch: every chunk checked
+        if (n_pass * kPass < total) {  // The rest, every chunk checked.  All lanes take part: a position is read from the lane of its row, and from one that has left comes zero.
+            const int c0 = n_pass * kPass + lane;
             uint4 v[U][K];
             float w[U][K];
 #pragma unroll
