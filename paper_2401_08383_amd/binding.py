@@ -7,6 +7,7 @@ current HIP stream.  There is no CPU fallback: if the library is missing, loadin
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -206,7 +207,8 @@ def moe_dispatch(x, topk_idx, E, E_local=None, expert_map=None, out=None, worksp
     A = T * k
     dev = topk_idx.device
     assert topk_idx.dtype == torch.int32 and topk_idx.is_contiguous() and x.is_contiguous()
-    if out is None:
+    given = out is not None
+    if not given:
         out = DispatchResult(
             torch.empty((A, d), dtype=x.dtype, device=dev) if gather else None,
             torch.empty(A, dtype=torch.int32, device=dev),
@@ -216,36 +218,42 @@ def moe_dispatch(x, topk_idx, E, E_local=None, expert_map=None, out=None, worksp
         )
     if workspace is None:
         workspace = _workspace(lib().moe_dispatch_workspace_bytes(T, k, E_local), dev)
-    if k <= EXF_MAX_TOPK:
-        call = lib().moe_dispatch
-    else:
-        call = lib().moe_dispatch_topk
-        workspace = _dispatch_topk_fits(x, topk_idx, expert_map, E, E_local, out, workspace)
-    _check(call(_ptr(x), _ptr(topk_idx), _ptr(expert_map), T, d, k, E, E_local, dtype_code(x), _ptr(out.x_sorted), _ptr(out.src_of_sorted),
-                _ptr(out.sorted_of_src), _ptr(out.expert_counts), _ptr(out.expert_offsets), _ptr(workspace), workspace.numel(), _stream()))
+    stream = _dispatch_fits(x, topk_idx, T, k, expert_map, E, E_local, out, given)
+    workspace, size = _bytes_of(workspace, topk_idx.get_device())
+    call = lib().moe_dispatch if k <= EXF_MAX_TOPK else lib().moe_dispatch_topk
+    rc = call(x.data_ptr(), topk_idx.data_ptr(), _ptr(expert_map), T, d, k, E, E_local, dtype_code(x), _ptr(out.x_sorted), out.src_of_sorted.data_ptr(),
+              out.sorted_of_src.data_ptr(), out.expert_counts.data_ptr(), out.expert_offsets.data_ptr(), workspace, size, stream)
+    if rc:
+        _check(rc)
     return out
 
 
-def _dispatch_topk_fits(x, topk_idx, expert_map, E, E_local, out, workspace):
-    """Checks of what the library cannot see of a dispatch of more than two assignments a token; -> the workspace as bytes."""
-    T, k = topk_idx.shape
+def _dispatch_fits(x, topk_idx, T, k, expert_map, E, E_local, out, given):
+    """Checks of what the library cannot see of a dispatch (`given`: its results are the caller's); -> the stream."""
     dev = topk_idx.get_device()
-    if x.requires_grad:
+    if k > EXF_MAX_TOPK and x.requires_grad:
         _untracked("moe_dispatch", "moe_dispatch_backward")
-    _expect("x", x, (T, x.shape[1]), x.dtype, dev)
+    d, rows = x.shape[1], out.x_sorted
+    # (one and two assignments a token have always been taken with the buffers of a larger call)
+    fits = _expect if k > EXF_MAX_TOPK else _room
+    if rows is not None and not (x.numel() == T * d and x.get_device() == dev):
+        fits("x", x, (T, d), x.dtype, dev)
     if expert_map is not None:
-        _expect("expert_map", expert_map, (E,), _INT32, dev)
-    if out.x_sorted is not None:
-        _expect("out.x_sorted", out.x_sorted, (T * k, x.shape[1]), x.dtype, dev)
-    _expect("out.src_of_sorted", out.src_of_sorted, (T * k,), _INT32, dev)
-    _expect("out.sorted_of_src", out.sorted_of_src, (T * k,), _INT32, dev)
-    _expect("out.expert_counts", out.expert_counts, (E_local,), _INT32, dev)
-    _expect("out.expert_offsets", out.expert_offsets, (E_local + 1,), _INT32, dev)
+        fits("expert_map", expert_map, (E,), _INT32, dev)
+    if given:
+        A, src, at, counts, offsets = T * k, out.src_of_sorted, out.sorted_of_src, out.expert_counts, out.expert_offsets
+        if rows is not None and not (rows.numel() == A * d and rows.dtype is x.dtype and rows.is_contiguous() and rows.get_device() == dev):
+            fits("out.x_sorted", rows, (A, d), x.dtype, dev)
+        if not (src.numel() == at.numel() == A and counts.numel() == E_local and offsets.numel() == E_local + 1 and src.dtype is at.dtype is counts.dtype is offsets.dtype is _INT32
+                and src.is_contiguous() and at.is_contiguous() and counts.is_contiguous() and offsets.is_contiguous()
+                and src.get_device() == at.get_device() == counts.get_device() == offsets.get_device() == dev):
+            fits("out.src_of_sorted", src, (A,), _INT32, dev)
+            fits("out.sorted_of_src", at, (A,), _INT32, dev)
+            fits("out.expert_counts", counts, (E_local,), _INT32, dev)
+            fits("out.expert_offsets", offsets, (E_local + 1,), _INT32, dev)
     if dev < 0:
         _on_host()
-    _stream_on(dev)
-    _bytes_of(workspace, dev)
-    return workspace.view(-1).view(_UINT8)
+    return _stream_on(dev)
 
 
 def moe_dispatch_backward(dx_sorted, sorted_of_src, k, out=None):
@@ -309,12 +317,28 @@ def moe_combine(y_sorted, sorted_of_src, topk_w, out=None):
     T, k = topk_w.shape
     if k > EXF_MAX_TOPK:
         return _combine_rows("moe_combine", y_sorted, sorted_of_src, topk_w, k, out)
-    d = y_sorted.shape[1]
-    assert sorted_of_src.numel() == T * k and y_sorted.is_contiguous() and topk_w.dtype == torch.float32
+    if len(y_sorted.shape) != 2:
+        _bad(f"sorted rows are [T*k,d], got {tuple(y_sorted.shape)}")
+    d, dt, dev = y_sorted.shape[1], y_sorted.dtype, y_sorted.get_device()
+    code = _CODES.get(dt)
+    if code is None:
+        raise ExflowError(EXF_ERR_BAD_DTYPE, f"unsupported dtype {dt}")
+    if sorted_of_src.numel() != T * k:
+        _bad(f"positions of {T} x {k} assignments expected, got {tuple(sorted_of_src.shape)}")
     if out is None:
-        out = torch.empty((T, d), dtype=y_sorted.dtype, device=y_sorted.device)
-    _check(lib().moe_combine(_ptr(y_sorted), _ptr(sorted_of_src), _ptr(topk_w), T, d, k, dtype_code(y_sorted), _ptr(out),
-                             _stream()))
+        out = _rows(T, d, dt, y_sorted.device)
+    if not (y_sorted.shape[0] == T * k and out.shape == (T, d) and out.dtype is dt and sorted_of_src.dtype is _INT32 and topk_w.dtype is _FLOAT and y_sorted.is_contiguous()
+            and out.is_contiguous() and sorted_of_src.is_contiguous() and topk_w.is_contiguous()
+            and out.get_device() == sorted_of_src.get_device() == topk_w.get_device() == dev):
+        _room("the sorted rows", y_sorted, (T * k, d), dt, dev)
+        _room("sorted_of_src", sorted_of_src, (T * k,), _INT32, dev)
+        _room("topk_w", topk_w, (T, k), _FLOAT, dev)
+        _room("out", out, (T, d), dt, dev)
+    if dev < 0:
+        _on_host()
+    rc = lib().moe_combine(y_sorted.data_ptr(), sorted_of_src.data_ptr(), topk_w.data_ptr(), T, d, k, code, out.data_ptr(), _stream_on(dev))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -473,6 +497,13 @@ def _expect(name, t, shape, dtype, dev):
     if t.dtype is not dtype:
         raise ExflowError(EXF_ERR_BAD_DTYPE, f"{name} is {t.dtype}, expected {dtype}")
     _bad(f"{name} must be contiguous and on device {dev}")
+
+
+def _room(name, t, shape, dtype, dev):
+    """As _expect(), of a tensor that may be longer."""
+    if t.numel() < math.prod(shape):
+        _bad(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} needed")
+    return _expect(name, t, t.shape, dtype, dev)
 
 
 def _on_host():

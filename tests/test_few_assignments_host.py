@@ -1,0 +1,106 @@
+"""What the package refuses of a dispatch and a combine, whatever the number of assignments a token (one and two go to calls of their own)."""
+import pytest
+import torch
+
+import paper_2401_08383_amd as exf
+from paper_2401_08383_amd import binding as B
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+T, D = 4, 64
+
+
+class NothingIsLaunched:
+    def __getattr__(self, name):
+        if name.endswith("_bytes"):
+            return getattr(B._lib, name)
+        return lambda *arguments: pytest.fail(f"{name} was called")
+
+
+@pytest.fixture
+def nothing_is_launched(monkeypatch):
+    exf.lib()
+    monkeypatch.setattr(B, "lib", NothingIsLaunched)
+    monkeypatch.setattr(B, "_stream", lambda: None)
+
+
+def _arguments(k, dt=BF):
+    return dict(x=torch.zeros(T, D, dtype=dt), idx=torch.zeros(T, k, dtype=I32), y=torch.zeros(T * k, D, dtype=dt), pos=torch.zeros(T * k, dtype=I32), w=torch.zeros(T, k))
+
+
+def _result(k, **other):
+    a = dict(x_sorted=torch.zeros(T * k, D, dtype=BF), src_of_sorted=torch.zeros(T * k, dtype=I32), sorted_of_src=torch.zeros(T * k, dtype=I32), expert_counts=torch.zeros(8, dtype=I32),
+             expert_offsets=torch.zeros(9, dtype=I32))
+    a.update(other)
+    return exf.binding.DispatchResult(**a)
+
+
+@pytest.mark.parametrize("k", [1, 2, 3])
+def test_what_the_library_cannot_see(nothing_is_launched, k):
+    a = _arguments(k)
+    x, idx, y, pos, w = (a[n] for n in ("x", "idx", "y", "pos", "w"))
+    wide = torch.zeros(T, k + 1)
+    bad = {
+        "fewer sorted rows": lambda: exf.moe_combine(y[:-1], pos, w),
+        "rows without an axis": lambda: exf.moe_combine(y[0], pos, w),
+        "rows of fp16": lambda: exf.moe_combine(y.half(), pos, w),
+        "rows that are not dense": lambda: exf.moe_combine(torch.zeros(T * k, 2 * D, dtype=BF)[:, :D], pos, w),
+        "fewer positions": lambda: exf.moe_combine(y, pos[:-1], w),
+        "positions in 64 bits": lambda: exf.moe_combine(y, pos.long(), w),
+        "weights in bf16": lambda: exf.moe_combine(y, pos, w.to(BF)),
+        "weights that are not dense": lambda: exf.moe_combine(y, pos, wide[:, :k]),
+        "a short result": lambda: exf.moe_combine(y, pos, w, out=torch.zeros(T - 1, D, dtype=BF)),
+        "a result of another type": lambda: exf.moe_combine(y, pos, w, out=torch.zeros(T, D)),
+        "fewer tokens": lambda: exf.moe_dispatch(x[:-1], idx, 8),
+        "a short map": lambda: exf.moe_dispatch(x, idx, 8, expert_map=torch.zeros(7, dtype=I32)),
+        "a map in 64 bits": lambda: exf.moe_dispatch(x, idx, 8, expert_map=torch.zeros(8, dtype=torch.int64)),
+        "short sorted rows": lambda: exf.moe_dispatch(x, idx, 8, out=_result(k, x_sorted=torch.zeros(T * k - 1, D, dtype=BF))),
+        "sorted rows of another type": lambda: exf.moe_dispatch(x, idx, 8, out=_result(k, x_sorted=torch.zeros(T * k, D))),
+        "a short list of positions": lambda: exf.moe_dispatch(x, idx, 8, out=_result(k, sorted_of_src=torch.zeros(T * k - 1, dtype=I32))),
+        "a short list of assignments": lambda: exf.moe_dispatch(x, idx, 8, out=_result(k, src_of_sorted=torch.zeros(T * k - 1, dtype=I32))),
+        "counts in 64 bits": lambda: exf.moe_dispatch(x, idx, 8, out=_result(k, expert_counts=torch.zeros(8, dtype=torch.int64))),
+        "no last offset": lambda: exf.moe_dispatch(x, idx, 8, out=_result(k, expert_offsets=torch.zeros(8, dtype=I32))),
+    }
+    for name, call in bad.items():
+        with pytest.raises(exf.ExflowError) as caught:
+            call()
+        assert "on the host" not in str(caught.value), name
+
+
+@pytest.mark.parametrize("k", [1, 2, 3])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_host_tensors(nothing_is_launched, k, dt):
+    a = _arguments(k, dt)
+    for call in (lambda: exf.moe_combine(a["y"], a["pos"], a["w"]), lambda: exf.moe_dispatch(a["x"], a["idx"], 8), lambda: exf.moe_dispatch(a["x"], a["idx"], 8, gather=False)):
+        with pytest.raises(exf.ExflowError, match="on the host"):
+            call()
+
+
+@pytest.mark.parametrize("k", [1, 2, 3])
+def test_a_device_that_is_not_the_current_one(nothing_is_launched, monkeypatch, k):
+    a = _arguments(k)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    for call in (lambda: exf.moe_combine(a["y"], a["pos"], a["w"]), lambda: exf.moe_dispatch(a["x"], a["idx"], 8), lambda: exf.moe_dispatch(a["x"], a["idx"], 8, gather=False)):
+        with pytest.raises(exf.ExflowError, match="on device 1, the current one is 0"):
+            call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [1, 2])
+def test_buffers_of_a_larger_call(k):
+    """... and rows that are longer than the list are taken for one and two assignments, as ever."""
+    dev = "cuda:0"
+    g = torch.Generator(dev).manual_seed(k)
+    x, idx = torch.randn(300, D, device=dev, generator=g).to(BF), torch.randint(0, 8, (300, k), device=dev, generator=g).int()
+    w = torch.rand(300, k, device=dev, generator=g)
+    large = exf.moe_dispatch(x, idx, 8)
+    out = torch.zeros(300, D, dtype=BF, device=dev)
+    n = 41
+    want = exf.moe_dispatch(x[:n], idx[:n], 8)
+    got = exf.moe_dispatch(x, idx[:n], 8, out=large)
+    assert got is large and torch.equal(got.x_sorted[:n * k], want.x_sorted) and torch.equal(got.sorted_of_src[:n * k], want.sorted_of_src)
+    assert torch.equal(got.expert_offsets, want.expert_offsets)
+    want_rows = exf.moe_combine(want.x_sorted, want.sorted_of_src, w[:n])
+    assert exf.moe_combine(got.x_sorted, got.sorted_of_src[:n * k], w[:n], out=out) is out and torch.equal(out[:n], want_rows) and not out[n:].any()
+    maps = exf.moe_dispatch(x[:0], idx[:n], 8, gather=False)  # the rows themselves are not read
+    assert maps.x_sorted is None and torch.equal(maps.sorted_of_src, want.sorted_of_src)
