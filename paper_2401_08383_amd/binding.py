@@ -231,9 +231,9 @@ def moe_dispatch(x, topk_idx, E, E_local=None, expert_map=None, out=None, worksp
 def _dispatch_fits(x, topk_idx, T, k, expert_map, E, E_local, out, given):
     """Checks of what the library cannot see of a dispatch (`given`: its results are the caller's); -> the stream."""
     dev = topk_idx.get_device()
-    if k > EXF_MAX_TOPK and x.requires_grad:
-        _untracked("moe_dispatch", "moe_dispatch_backward")
     d, rows = x.shape[1], out.x_sorted
+    if rows is not None and x.requires_grad:
+        _untracked("moe_dispatch", "moe_dispatch_backward")
     # (one and two assignments a token have always been taken with the buffers of a larger call)
     fits = _expect if k > EXF_MAX_TOPK else _room
     if rows is not None and not (x.numel() == T * d and x.get_device() == dev):
@@ -317,6 +317,8 @@ def moe_combine(y_sorted, sorted_of_src, topk_w, out=None):
     T, k = topk_w.shape
     if k > EXF_MAX_TOPK:
         return _combine_rows("moe_combine", y_sorted, sorted_of_src, topk_w, k, out)
+    if y_sorted.requires_grad or topk_w.requires_grad:
+        _untracked("moe_combine", "moe_combine_backward")
     if len(y_sorted.shape) != 2:
         _bad(f"sorted rows are [T*k,d], got {tuple(y_sorted.shape)}")
     d, dt, dev = y_sorted.shape[1], y_sorted.dtype, y_sorted.get_device()

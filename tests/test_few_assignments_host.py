@@ -104,3 +104,24 @@ def test_buffers_of_a_larger_call(k):
     assert exf.moe_combine(got.x_sorted, got.sorted_of_src[:n * k], w[:n], out=out) is out and torch.equal(out[:n], want_rows) and not out[n:].any()
     maps = exf.moe_dispatch(x[:0], idx[:n], 8, gather=False)  # the rows themselves are not read
     assert maps.x_sorted is None and torch.equal(maps.sorted_of_src, want.sorted_of_src)
+
+
+@pytest.mark.parametrize("k", [1, 2, 3])
+@pytest.mark.parametrize("call,name", [("combine", "y"), ("combine", "w"), ("dispatch", "x")])
+def test_gradients_are_not_lost_without_a_word(nothing_is_launched, k, call, name):
+    a = _arguments(k)
+    a[name].requires_grad_()
+    run = {"combine": lambda: exf.moe_combine(a["y"], a["pos"], a["w"]), "dispatch": lambda: exf.moe_dispatch(a["x"], a["idx"], 8)}[call]
+    with pytest.raises(exf.ExflowError, match="autograd") as caught:
+        run()
+    assert caught.value.code == B.EXF_ERR_NOT_IMPLEMENTED and f"moe_{call}" in str(caught.value)
+    with torch.no_grad(), pytest.raises(exf.ExflowError, match="on the host"):
+        run()
+
+
+@pytest.mark.parametrize("k", [1, 2, 3])
+def test_maps_have_no_gradient(nothing_is_launched, k):
+    """... to lose: rows that require one are taken where only the maps are wanted."""
+    a = _arguments(k)
+    with pytest.raises(exf.ExflowError, match="on the host"):
+        exf.moe_dispatch(a["x"].requires_grad_(), a["idx"], 8, gather=False)
