@@ -776,6 +776,8 @@ def _expect_q4(name, m, shape, dtype, dev):
 
 def q4_quantize(x, group=128, symmetric=False, out=None):
     """Rows x [..., k] (k a multiple of the group: 32, 64 or 128) -> Q4, with zero points unless ``symmetric`` (``out`` says that by what it holds)."""
+    if x.requires_grad:
+        _untracked("q4_quantize", "none: codes have no gradient")
     shape, dt = x.shape, x.dtype
     code = _CODES.get(dt)
     if code is None:
@@ -799,6 +801,8 @@ def q4_quantize(x, group=128, symmetric=False, out=None):
 
 def q4_dequantize(m, out=None):
     """The values a Q4 stands for, in its scales' type."""
+    if m.scale.requires_grad:
+        _untracked("q4_dequantize", "none: weights in 4 bits are not trained")
     shape, dt, dev = m.shape, m.scale.dtype, m.q.get_device()
     code = _CODES.get(dt)
     if code is None:
