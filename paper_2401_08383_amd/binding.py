@@ -11,6 +11,7 @@ import math
 import os
 
 import torch
+from torch.autograd import forward_ad as _forward_ad
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libexflow_moe.so")
@@ -234,6 +235,8 @@ def _dispatch_fits(x, topk_idx, T, k, expert_map, E, E_local, out, given):
     d, rows = x.shape[1], out.x_sorted
     if rows is not None and x.requires_grad:
         _untracked("moe_dispatch", "moe_dispatch_backward")
+    if rows is not None and _forward_ad._current_level >= 0:
+        _no_tangents("moe_dispatch", x)
     # (one and two assignments a token have always been taken with the buffers of a larger call)
     fits = _expect if k > EXF_MAX_TOPK else _room
     if rows is not None and not (x.numel() == T * d and x.get_device() == dev):
@@ -319,6 +322,8 @@ def moe_combine(y_sorted, sorted_of_src, topk_w, out=None):
         return _combine_rows("moe_combine", y_sorted, sorted_of_src, topk_w, k, out)
     if y_sorted.requires_grad or topk_w.requires_grad:
         _untracked("moe_combine", "moe_combine_backward")
+    if _forward_ad._current_level >= 0:
+        _no_tangents("moe_combine", y_sorted, topk_w)
     if len(y_sorted.shape) != 2:
         _bad(f"sorted rows are [T*k,d], got {tuple(y_sorted.shape)}")
     d, dt, dev = y_sorted.shape[1], y_sorted.dtype, y_sorted.get_device()
@@ -352,6 +357,8 @@ def _rows(T, width, dtype, device):
 def _combine_rows(name, y_sorted, sorted_of_src, topk_w, k, out):
     if y_sorted.requires_grad or topk_w is not None and topk_w.requires_grad:
         _untracked(name, "moe_combine_backward" if name == "moe_combine" else "moe_dispatch")
+    if _forward_ad._current_level >= 0:
+        _no_tangents(name, y_sorted, topk_w)
     T, A, d, dt, code, dev = _assigned(y_sorted, sorted_of_src, k)
     if out is None:
         out = _rows(T, d, dt, y_sorted.device)
@@ -390,6 +397,8 @@ def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, 
     (``out``), or zero."""
     if dout.requires_grad or y_sorted.requires_grad or topk_w.requires_grad:
         _untracked("moe_combine_backward", "none: there is no second derivative")
+    if _forward_ad._current_level >= 0:
+        _no_tangents("moe_combine_backward", dout, y_sorted, topk_w)
     weights = topk_w.shape
     if len(weights) != 2:
         _bad(f"topk_w is [T,k], got {tuple(weights)}")
@@ -424,6 +433,8 @@ def moe_route(logits, k, bias=None, score=EXF_SCORE_SOFTMAX, renormalize=False, 
     ``out``: (topk_idx, topk_w) to write to."""
     if logits.requires_grad:
         _untracked("moe_route", "moe_route_backward")
+    if _forward_ad._current_level >= 0:
+        _no_tangents("moe_route", logits)
     shape, dt, dev = logits.shape, logits.dtype, logits.get_device()
     code = _CODES.get(dt)
     if code is None:
@@ -456,6 +467,8 @@ def moe_route_backward(dtopk_w, logits, topk_idx, score=EXF_SCORE_SOFTMAX, renor
     """Gradient of moe_route's logits, of their type, from that of the weights, fp32 [T,k], and of the scores, fp32 [T,E] or one row [E] for all tokens."""
     if dtopk_w.requires_grad or logits.requires_grad or dscores is not None and dscores.requires_grad:
         _untracked("moe_route_backward", "none: there is no second derivative")
+    if _forward_ad._current_level >= 0:
+        _no_tangents("moe_route_backward", dtopk_w, logits, dscores)
     shape, dt, dev = logits.shape, logits.dtype, logits.get_device()
     code = _CODES.get(dt)
     if code is None:
@@ -525,6 +538,13 @@ def _untracked(name, backward="moe_grouped_product_dx and moe_grouped_product_dw
     if torch.is_grad_enabled():
         raise ExflowError(EXF_ERR_NOT_IMPLEMENTED, f"{name} records no autograd history and an argument requires a gradient: call it under torch.no_grad(), or in the "
                                                    f"forward of a torch.autograd.Function whose backward calls {backward}")
+
+
+def _no_tangents(name, *tensors):
+    """Raises for a dual tensor of forward-mode differentiation, whose tangent a result would not have (in the forward of a torch.autograd.Function there are none)."""
+    for t in tensors:
+        if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+            raise ExflowError(EXF_ERR_NOT_IMPLEMENTED, f"{name} carries no tangents on and an argument is a dual tensor: call it in the forward of a torch.autograd.Function that has a jvp")
 
 
 _INT32, _UINT8 = torch.int32, torch.uint8
@@ -778,6 +798,8 @@ def q4_quantize(x, group=128, symmetric=False, out=None):
     """Rows x [..., k] (k a multiple of the group: 32, 64 or 128) -> Q4, with zero points unless ``symmetric`` (``out`` says that by what it holds)."""
     if x.requires_grad:
         _untracked("q4_quantize", "none: codes have no gradient")
+    if _forward_ad._current_level >= 0:
+        _no_tangents("q4_quantize", x)
     shape, dt = x.shape, x.dtype
     code = _CODES.get(dt)
     if code is None:
@@ -803,6 +825,8 @@ def q4_dequantize(m, out=None):
     """The values a Q4 stands for, in its scales' type."""
     if m.scale.requires_grad:
         _untracked("q4_dequantize", "none: weights in 4 bits are not trained")
+    if _forward_ad._current_level >= 0:
+        _no_tangents("q4_dequantize", m.scale)
     shape, dt, dev = m.shape, m.scale.dtype, m.q.get_device()
     code = _CODES.get(dt)
     if code is None:
@@ -821,6 +845,8 @@ def moe_grouped_product_q4(x_sorted, expert_offsets, w, bias=None, out=None):
     """moe_grouped_product with weights in 4-bit integers: w a Q4 [E_local,n,k] with scales of the rows' type."""
     if x_sorted.requires_grad or bias is not None and bias.requires_grad or w.scale.requires_grad:
         _untracked("moe_grouped_product_q4", "none: weights in 4 bits are not trained")
+    if _forward_ad._current_level >= 0:
+        _no_tangents("moe_grouped_product_q4", x_sorted, bias, w.scale)
     q, scale, zero = w.q, w.scale, w.zero
     shape, groups, rows = q.shape, scale.shape, x_sorted.shape
     if len(shape) != 3 or len(rows) != 2:
