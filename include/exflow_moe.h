@@ -345,7 +345,8 @@ int moe_combine_backward(const void* dout, const void* y_sorted, const int32_t* 
  *
  *   x, out [rows,k] dt;  q [rows,k/2]: elements 2i (low half) and 2i+1 of a row in byte i;  scale [rows,k/group] dt;  zero [rows,k/group]
  *   x_sorted [A,k] dt;  w [E_local,n,k/2], w_scale, w_zero (or NULL): E_local*n rows of k;  bias [E_local,n] dt or NULL;  y_sorted [A,n] dt
- * Shapes: rows >= 0, k >= group, k % group == 0; the product's as moe_grouped_product.  All arrays 16-byte aligned.
+ * Shapes: rows >= 0, k >= group, k % group == 0; the product's as moe_grouped_product.  All arrays 16-byte aligned, but zero points 8 (bf16) or 4 (fp32)
+ *         bytes: where those of an expert begin.
  * ------------------------------------------------------------------------------------- */
 int q4_quantize(const void* x, int64_t rows, int k, int group, int dt, uint8_t* q, void* scale, uint8_t* zero, void* stream);
 int q4_dequantize(const uint8_t* q, const void* scale, const uint8_t* zero, int64_t rows, int k, int group, int dt, void* out,

@@ -179,7 +179,7 @@ extern "C" int moe_grouped_product_q4(const void* x_sorted, const int32_t* exper
     EXF_CHECK_ALIGNED(fn, w);
     EXF_CHECK_ALIGNED(fn, w_scale);
     EXF_CHECK_ALIGNED(fn, y_sorted);
-    if (w_zero != nullptr) EXF_CHECK_ALIGNED(fn, w_zero);
+    if (int rc = check_q4_zero(fn, w_zero, dt)) return rc;
     if (bias != nullptr) EXF_CHECK_ALIGNED(fn, bias);
     const size_t el = dt == EXF_BF16 ? 2 : 4, weights = static_cast<size_t>(E_local) * n, rows = A, out_bytes = rows * n * el;
     const struct {

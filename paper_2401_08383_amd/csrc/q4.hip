@@ -212,7 +212,7 @@ static int check_q4(const char* fn, const void* x, int64_t rows, int k, int grou
     EXF_CHECK_ALIGNED(fn, x);
     EXF_CHECK_ALIGNED(fn, q);
     EXF_CHECK_ALIGNED(fn, scale);
-    if (zero != nullptr) EXF_CHECK_ALIGNED(fn, zero);
+    if (int rc = check_q4_zero(fn, zero, dt)) return rc;
     const size_t n = static_cast<size_t>(rows) * k, el = dt == EXF_BF16 ? 2 : 4, groups = n / group;
     const struct {
         const void* at;

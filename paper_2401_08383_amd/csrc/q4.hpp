@@ -26,6 +26,14 @@ inline int check_q4_group(const char* fn, int k, int group)
     return EXF_OK;
 }
 
+// Zero points begin where those of an expert may: rows come in eights (bf16) or fours (fp32), a byte a group.  (The kernels load bytes, or words of four.)
+inline int check_q4_zero(const char* fn, const uint8_t* zero, int dt)
+{
+    const unsigned by = dt == EXF_BF16 ? 8 : 4;
+    if (reinterpret_cast<uintptr_t>(zero) % by != 0) return fail(EXF_ERR_MISALIGNED, "%s: the zero points are not %u-byte aligned", fn, by);
+    return EXF_OK;
+}
+
 template <class F>
 void pick_q4_group(int group, F run)
 {
