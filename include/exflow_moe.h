@@ -341,7 +341,8 @@ int moe_combine_backward(const void* dout, const void* y_sorted, const int32_t* 
  *   moe_grouped_product_q4: y[s][v] = sum_u x[s][u] * value[e][v][u] + bias[e][v] for rows s of expert e, as moe_grouped_product; sums in
  *                fp32, rounded once, in an order that depends on the sizes and the offsets only.  For few rows an expert: weights are read once
  *                for every 16 rows or more.  In bf16 the codes are multiplied as 16 + code and 16 + zero times the row's sum is taken off again:
- *                a row that holds an infinity comes out NaN, or infinite.
+ *                a row that holds an infinity comes out NaN, or infinite.  A group's sums are formed in front of its scale: rows of magnitudes up to 2^113
+ *                do not overflow in them, larger ones may come out NaN or infinite.
  *
  *   x, out [rows,k] dt;  q [rows,k/2]: elements 2i (low half) and 2i+1 of a row in byte i;  scale [rows,k/group] dt;  zero [rows,k/group]
  *   x_sorted [A,k] dt;  w [E_local,n,k/2], w_scale, w_zero (or NULL): E_local*n rows of k;  bias [E_local,n] dt or NULL;  y_sorted [A,n] dt
