@@ -191,6 +191,6 @@ extern "C" int moe_grouped_product_q4(const void* x_sorted, const int32_t* exper
         if (overlap(y_sorted, out_bytes, i.at, i.bytes)) return fail(EXF_ERR_BAD_SHAPE, "%s: the result must not overlap an input", fn);
     const Q4Product p{x_sorted, expert_offsets, w, w_scale, w_zero, bias, y_sorted, static_cast<int>(A), k, n, E_local};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int rc = dt == EXF_BF16 && q4_streams(A, n, k, E_local) ? launch_q4_stream(p, group, s) : launch_q4_product(p, group, dt, s);
+    const int rc = dt == EXF_BF16 && q4_streams(A, n, E_local) ? launch_q4_stream(p, group, s) : launch_q4_product(p, group, dt, s);
     return rc == EXF_OK ? check_launch(fn) : rc;
 }

@@ -248,7 +248,7 @@ struct Q4Spread {
 // Workgroups for two thirds of the compute units; half of that where a tile has more than 8 rows, which the other kernel loads over and over.  Streamed and not, us (rows,
 // experts, columns x reduction): 512, 64, 16384 x 4096 411 and 946; 1024, 64, 4096 x 1056 57 and 96; 1, 1, 16384 x 4096 11.4 and 15.3; 43, 10, 1200 x 4096 10.9 and 13.5;
 // 100, 6, 512 x 8192 16.4 and 23.2; but 8, 8, 1024 x 4096 10.5 and 9.1; 16, 1, 4096 x 4096 10.2 and 8.5; 1, 1, 4096 x 1024 5.3 and 4.5; 66, 4, 352 x 10624 22 and 15.8.
-bool q4_streams(int64_t A, int n, int, int E_local)
+bool q4_streams(int64_t A, int n, int E_local)
 {
     const Q4Spread s(A, n, E_local);
     return s.workgroups(16, 64) * (s.mean > 8 ? 2 : 1) >= 160;

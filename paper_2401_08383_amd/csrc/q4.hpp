@@ -43,7 +43,7 @@ void pick_q4_group(int group, F run)
 }
 
 // bf16 products of many weights: operands staged through LDS (product_q4_stream.hip).
-bool q4_streams(int64_t A, int n, int k, int E_local);
+bool q4_streams(int64_t A, int n, int E_local);
 int launch_q4_stream(const Q4Product& p, int group, hipStream_t stream);
 
 // ---- device side -------------------------------------------------------------------------
@@ -96,11 +96,6 @@ __device__ __forceinline__ global_bytes shared_place(const void* p)
 __device__ __forceinline__ uint4 load_vector(global_bytes p)
 {
     const u32x4_v v = *reinterpret_cast<const __attribute__((address_space(1))) u32x4_v*>(p);
-    return uint4{v[0], v[1], v[2], v[3]};
-}
-__device__ __forceinline__ uint4 stream_vector(global_bytes p)
-{
-    const u32x4_v v = __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) u32x4_v*>(p));
     return uint4{v[0], v[1], v[2], v[3]};
 }
 
