@@ -282,6 +282,7 @@ int moe_grouped_product_mx4(const void* x_sorted, const uint8_t* x_scale, const 
  *   s[t][e]   = softmax(logits[t][:])[e]  or  1 / (1 + exp(-logits[t][e]))          (`score`)
  *   key[t][e] = s[t][e] + bias[e]; without a bias the logits themselves are compared.  Keys decide as if they were computed in
  *               64 bits.  A logit of -inf or NaN, or a bias that makes the key -inf or NaN, takes the expert out.
+ *               (-inf is the mask that costs nothing; fp32 logits without a bias masked by a number from -1e4 to -1e30 are slower to order.)
  *   groups > 1: the experts lie in groups of E / groups consecutive ones; the top_groups groups stay whose group_best (1 or 2) highest keys
  *               have the largest sum (with group_best == 2 and no bias: scores), ties to the lowest group.
  *   slot j    = the j-th largest key of the groups that stay, ties to the LOWEST expert id
@@ -340,7 +341,8 @@ int moe_combine_backward(const void* dout, const void* y_sorted, const int32_t* 
  *   q4_dequantize: the values, rounded to dt
  *   moe_grouped_product_q4: y[s][v] = sum_u x[s][u] * value[e][v][u] + bias[e][v] for rows s of expert e, as moe_grouped_product; sums in
  *                fp32, rounded once, in an order that depends on the sizes and the offsets only.  For few rows an expert: weights are read once
- *                for every 16 rows or more.  In bf16 the codes are multiplied as 16 + code and 16 + zero times the row's sum is taken off again:
+ *                for every 16 rows or more.  In bf16, from about 500 rows an expert on q4_dequantize and moe_grouped_product take less (4096 x 4096, 8 experts: 2048 rows 98 us
+ *                and 132, 4096 183 and 179, 8192 354 and 284).  In bf16 the codes are multiplied as 16 + code and 16 + zero times the row's sum is taken off again:
  *                a row that holds an infinity comes out NaN, or infinite.  A group's sums are formed in front of its scale: rows of magnitudes up to 2^113
  *                do not overflow in them, larger ones may come out NaN or infinite.
  *

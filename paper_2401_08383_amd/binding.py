@@ -394,7 +394,7 @@ def _assigned(rows, sorted_of_src, k):
 
 def moe_combine_backward(dout, y_sorted, sorted_of_src, topk_w, want_rows=True, want_weights=True, out=None, out_weights=None):
     """Gradients of moe_combine: (dy_sorted [T*k,d] or None, dtopk_w [T,k] or None).  Rows of dy_sorted that no assignment has are left as they were
-    (``out``), or zero."""
+    (``out``), or zero: without ``out`` all rows are cleared first (8192 x 8 of 4 KiB 152 us instead of 110)."""
     if dout.requires_grad or y_sorted.requires_grad or topk_w.requires_grad:
         _untracked("moe_combine_backward", "none: there is no second derivative")
     if _forward_ad._current_level >= 0:

@@ -236,7 +236,9 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? KS : 2) void q4_stream_kernel(co
     }
 }
 
-// What the choice goes by: tiles, were the rows spread evenly over the experts that can have any.
+// What the choice goes by: tiles, were the rows spread evenly over the experts that can have any.  The host knows how many rows there are, not whose, nor how many lie outside all
+// ranges.  us, even, nine tenths of them one expert's, and all of one expert in eight: 512, 64, 16384 x 4096 415, 499 and 215; 1280, 64, 4096 x 4096 155, 216 and 92; 2048, 32, 4096 x 2048 58, 90
+// and 50; 8192, 8, 4096 x 4096 355, 381 and 349.  Seven eighths of the rows outside, and a call with the others alone: 512, 64 396 and 392; 1280, 64 152 and 115; 2048, 32 65 and 46.
 struct Q4Spread {
     int64_t experts, mean;
     int N;
@@ -245,6 +247,7 @@ struct Q4Spread {
     int64_t workgroups(int rows, int cols) const { return experts * of_rows(rows) * ((N + cols - 1) / cols); }
 };
 
+// (Times of single calls are in a graph or back to back, which differ by less than boxes and moments do: 512, 64, 16384 x 4096 411 to 431.)
 // Workgroups for two thirds of the compute units; half of that where a tile has more than 8 rows, which the other kernel loads over and over.  Streamed and not, us (rows,
 // experts, columns x reduction): 512, 64, 16384 x 4096 411 and 946; 1024, 64, 4096 x 1056 57 and 96; 1, 1, 16384 x 4096 11.4 and 15.3; 43, 10, 1200 x 4096 10.9 and 13.5;
 // 100, 6, 512 x 8192 16.4 and 23.2; but 8, 8, 1024 x 4096 10.5 and 9.1; 16, 1, 4096 x 4096 10.2 and 8.5; 1, 1, 4096 x 1024 5.3 and 4.5; 66, 4, 352 x 10624 22 and 15.8.
@@ -256,7 +259,7 @@ bool q4_streams(int64_t A, int n, int E_local)
 
 // Tiles, rows x columns, us, as above.
 //   64 x 256, units of 128, where the rows fill them and two workgroups a compute unit are left (what turns codes into numbers is shared by the rows), not 32 x 256: 8192, 8, 4096 x 4096
-// 353 and 419; 2048, 32, 4096 x 2048 70 and 76; but 1500, 1, 4096 x 4096 94 and 92; 2048, 40, 4096 x 2048 (51 rows of 64) 98 and 93.
+// 353 and 419; 2048, 32, 4096 x 2048 70 and 76; but 1500, 1, 4096 x 4096 94 and 92 (82 to 92 since); 2048, 40, 4096 x 2048 (51 rows of 64) 98 and 93.
 //   32 x 256, units of 128 so that three fit a compute unit, for nearly that many, not 32 x 128: 1500, 1, 4096 x 4096 86 and 98; 1500, 16, 4096 x 2048 48 and 55; but 600, 2, 8192 x 8192
 // 207 and 183; 1280, 64, 4096 x 4096 213 and 153.
 //   32 x 128 where an expert has more than 16 rows, not 16 x 128: 1280, 64, 16384 x 4096 608 and 717; 512, 16, 4096 x 4096 37 and 47; 256, 8, 4096 x 4096 24.6 and 27.1; but from 160

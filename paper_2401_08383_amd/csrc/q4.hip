@@ -15,7 +15,7 @@ __device__ __forceinline__ uint32_t over_group(uint32_t v, F f)
     return v;
 }
 
-// x / 15 or x / 7 in 64 bits, correctly rounded: a reciprocal, and what it leaves.
+// x / 15 or x / 7 in 64 bits, correctly rounded: by a reciprocal, its remainder put back (as Markstein does).
 template <int BY>
 __device__ __forceinline__ double divided(double x)
 {

@@ -2,10 +2,12 @@
 //
 // A token belongs to L lanes of a wavefront, V consecutive experts to a lane, so that a lower lane and a lower register hold lower ids.
 // Slot j of the choice is kept by lane j of the token.
-//   What bounds it: reading takes 6 us of the 25.0 of 32768 tokens, 8 of 256 experts in 8 groups, sigmoid, bias, fp32; vector instructions the rest, 1160 a
-// wavefront of four tokens (350 of them for the groups).  Without groups 18.4, softmax of fp32 logits 14.2, bf16 10.9; keys of 64 bits throughout 98.  Registers for a fifth wavefront a SIMD (96 of 119, some spilled) gain nothing, 28.  One token 3.1, in groups
+//   What bounds it: reading takes 6 us of the 25.4 of 32768 tokens, 8 of 256 experts in 8 groups, sigmoid, bias, fp32 (calls in a graph); vector instructions the rest, 1160 a
+// wavefront of four tokens (350 of them for the groups).  Without groups 18.4; without a bias sigmoid 13.8, softmax of fp32 logits 15.7 and of bf16 ones 13.6, renormalised, which needs no
+// sum over all experts, 11.6; keys of 64 bits throughout 98.  Registers for a fifth wavefront a SIMD (96 of 119, some spilled) gain nothing, 28.  One token 3.2 (2.7 by itself), in groups
 // 5.4: loads that follow one another and nine turns of a maximum over lanes.
-//   The gradient, with that of the scores: 15.1 us for 69 MB, 4.6 TB/s.
+//   The gradient of 32768 x 256 fp32 logits: with that of the scores 16 to 18 us for 69 MB, 4.1 TB/s; without it 11.3 where only the chosen ones are read (33.5 MB are written), 16.8 of
+// softmax weights that are not renormalised; of bf16 logits 9.0 and 13.3.
 #include <math.h>
 
 #include <type_traits>
@@ -129,15 +131,15 @@ __device__ __forceinline__ void store_row(void* row, int first, int E, const flo
     }
 }
 
-// exp(x) for x <= 0 (0 below -200), to less than two units: what the argument loses on its way to base 2 is put back, and results below the normal range are
-// kept (the instruction flushes them).
+// exp(x) for x <= 0 (0 below -200), to less than two units: what the argument loses on its way to base 2 is put back by a second part of log2 e (the two-part reduction of
+// Cody and Waite), and results below the normal range are kept (the instruction flushes them).
 __device__ __forceinline__ float exp_below(float x)
 {
     x = x < -200.0f ? -200.0f : x;
     const float whole = rintf(x * 1.442695041f);
     return ldexpf(__builtin_amdgcn_exp2f(fmaf(x, 1.925963033e-8f, fmaf(x, 1.442695041f, -whole))), static_cast<int>(whole));
 }
-// a / b for b in [1/2, 16] and a in [0, b], to a unit.
+// a / b for b in [1/2, 16] and a in [0, b], to a unit: by a reciprocal, its remainder put back (as Markstein does).
 __device__ __forceinline__ float quotient(float a, float b)
 {
     const float r = __builtin_amdgcn_rcpf(b), q = a * r;
@@ -332,6 +334,8 @@ __device__ __forceinline__ void best_two(uint32_t& a, uint32_t& b)
 }
 
 // Largest of the finite values above the lowest that stand for masks, the least of them, and 2^22 steps between them.
+//   Masks are -inf and what is not above -1e30.  fp32 logits without a bias that are masked by a number nearer to zero leave few steps for the others: with -1e9 none, and rows
+// with more of them than the token has lanes are put in order by keys in 64 bits, 50 us where -inf takes 15.7 (32768 x 256, 30 % masked); with -1e4 21.  (Scores and bf16 logits do not mind.)
 struct Classes {
     float most, step;
 };
@@ -540,7 +544,7 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         };
         const int share = size / g.parts;
         if (share * g.parts == size && share >= 16 && (share & (share - 1)) == 0) {
-            // Lanes that begin a power of two apart would all be at the same banks (groups of 32, 32768 tokens: 3.9 M cycles of conflicts, now 0.3; one token 6.4 us, now 5.8):
+            // Lanes that begin a power of two apart would all be at the same banks (groups of 32, 32768 tokens: 3.9 M cycles of conflicts, now 0.3; one token 0.6 us less):
             // each begins elsewhere in its share, those of all tokens at different ones.
             const int begin = g.mine < p.groups ? g.begin : 0, turn = (in & ~3) + lane_id() / L;
 #pragma unroll 4
@@ -609,8 +613,8 @@ __device__ __forceinline__ int choose_by_classes(const RouteCall& p, const void*
         }
     };
     const std::integral_constant<int, V> all;
-    // With M places an element past the lane's first M + 1 is that one again, at once: neighbours that are equal, and not sure.  Four are enough for all but 1e-4 of tokens
-    // that choose eight of 256; where nothing else is unsure, nine.
+    // With M places an element past the lane's first M + 1 is that one again, at once: neighbours that are equal, and not sure.  Four are enough for all but 4e-4 of tokens
+    // that choose eight of 256 (7e-4 of half of eight groups), so for all but 3e-3 of wavefronts; where nothing else is unsure, nine.
     const std::integral_constant<int, (V <= 9 ? V : BF16 && !SCORES ? 9 : 4)> some;
     number();
     if (V > 9 && p.k <= 8) take(some, p.k + 1);
